@@ -70,7 +70,8 @@ enum {
   MCD_DEV_BAD_PARAM = 1u,   /* temperature < 0 or NaN, top_p <= 0 or NaN, non-finite w */
   MCD_DEV_GRID_RANGE = 2u,  /* grid_slot >= n_slots or frame >= F_max: cell not written */
   MCD_DEV_BAD_PLAN = 4u,    /* device plan does not match the counts of the call */
-  MCD_DEV_BAD_TOKEN = 8u    /* mcd_next_input: a token outside its table */
+  MCD_DEV_BAD_TOKEN = 8u,   /* mcd_next_input: a token outside its table */
+  MCD_DEV_BAD_PAGE = 16u    /* mcd_cache_*: a slot, length or page id out of range */
 };
 
 #define MCD_MAX_K 32         /* codebooks per head */
@@ -370,6 +371,144 @@ mcd_status mcd_sched_plan(mcd_sched *s, mcd_sched_batch *out);
 mcd_status mcd_sched_commit(mcd_sched *s, int32_t *finished, int32_t cap, int32_t *n_finished);
 /* Requests waiting and running. */
 mcd_status mcd_sched_counts(const mcd_sched *s, int32_t *waiting, int32_t *running);
+
+/* ---- 4-bit key/value cache ----------------------------------------------------
+ * The cache between mcd_next_input and the head: what the backbone's attention
+ * layers read for every row the scheduler plans (mcd_sched_batch: row_slot,
+ * row_context, row_tokens).  One mcd_cache is one layer's.
+ *
+ * A slot is a sequence of positions 0, 1, ... in pages of MCD_CACHE_PAGE tokens:
+ * position t lies in page table[slot][t / 64] at token t % 64.  Slots may share
+ * pages (a Companion that joins with a copy of its Main row's prefix) as long as
+ * no call appends to a shared page.  Keys are cached as attention multiplies
+ * them (after any rotary embedding), so positions may later be dropped.
+ *
+ * A page holds, for each K/V head, mcd_cache_page_bytes(D) bytes (66 D + 128):
+ * e2m1 codes of the keys and values (a sign and 0, 1/2, 1, 3/2, 2, 3, 4, 6) and
+ * their scales.
+ *   Keys: one power of two 2^(b - 127) for every token and 32 channels, the
+ *   smallest with max|k| <= 7 * 2^(b - 127), b in 1..254; b = 255 where a key of
+ *   the 32 is not finite: they read as NaN.
+ *   Values: one bfloat16 for every token, max|v| * (1/6) in fp32 rounded to
+ *   nearest even; NaN where a value of the token is not finite.
+ *   Codes: the nearest multiple of the scale, ties to the even code, at most 6.
+ * In bytes, with nb = D / 32:
+ *   [0, 32 D)        key codes [token][channel], the lower channel in the low bits
+ *   [32 D, 64 D)     value codes, 8 tokens of one channel to a 32-bit word: token
+ *                    32 h + 16 j + 4 g + i in bits 4 (4 j + i) of word
+ *                    [h][c / 4][16 g + m][c % 4], whose channel is
+ *                    (m / 4) (D / 4) + 4 c + m % 4
+ *   [64 D, 66 D)     key scales: token 16 t + m, block b at byte (m nb + b) 4 + t
+ *   [66 D, + 128)    value scales: token 16 t + 4 g + i at bfloat16 16 g + 4 t + i
+ *
+ * The device arrays (table, slot, context, start, length) are read when the
+ * kernels run, so a captured graph may be replayed with new contents.  A slot
+ * outside [0, n_slots), a page id outside [0, n_pages), a length beyond the
+ * table or beyond the call's max_* bounds sets MCD_DEV_BAD_PAGE in the workspace
+ * status word; the positions concerned are skipped (not written, not seen). */
+#define MCD_CACHE_PAGE 64
+
+typedef struct {
+  int32_t Hkv;               /* K/V heads, >= 1 */
+  int32_t D;                 /* channels of a head: 64, 128 or 256 */
+  int32_t n_slots, max_pages;/* rows and columns of table, >= 1 */
+  int32_t n_pages;           /* pages, >= 1 */
+  void *pages;               /* [n_pages][Hkv][mcd_cache_page_bytes(D)], 16-byte aligned */
+  const int32_t *table;      /* [n_slots][max_pages] page ids; read up to a slot's length only */
+  float *weight;             /* [n_slots][Hkv][max_pages * 64] attention weight every position
+                                has received, or NULL */
+} mcd_cache;
+
+/* The rows of a step and their new tokens; tokens of row r are start[r] ..
+ * start[r + 1] - 1 of the packed token arrays, at positions context[r],
+ * context[r] + 1, ... of its slot. */
+typedef struct {
+  int32_t R;                 /* rows, >= 0 */
+  int32_t n_tokens;          /* tokens of all rows (start[R]), >= 0 */
+  int32_t max_tokens;        /* no row has more tokens, >= 0 */
+  int32_t max_context;       /* no row has more positions (context + tokens), >= 0 */
+  const int32_t *slot;       /* [R] slot of each row (no two alike), or NULL: its index */
+  const int32_t *context;    /* [R] positions before the row's first token */
+  const int32_t *start;      /* [R + 1], ascending from 0; NULL: one token in every row
+                                (n_tokens == R, max_tokens == 1) */
+} mcd_cache_rows;
+
+size_t mcd_cache_page_bytes(int32_t D);   /* bytes of one page and head; 0 for another D */
+
+/* Workspace bytes that mcd_cache_attend needs for rows of these bounds (0 for
+ * invalid sizes); the other calls need the 256-byte status word only.  The
+ * workspace must be 256-byte aligned and zero-filled once before first use. */
+size_t mcd_cache_workspace_bytes(const mcd_cache *cache, const mcd_cache_rows *rows, int32_t Hq);
+
+/* Quantises the tokens' keys and values (k, v: [n_tokens][Hkv][D] of dtype, rows
+ * k_stride and v_stride elements apart) into their pages and, when the cache has
+ * weights, sets the new positions' weight to 0.  k, v and the strides in bytes
+ * must be multiples of 16.  The pages must be in the table already. */
+mcd_status mcd_cache_append(const mcd_cache *cache, const mcd_cache_rows *rows, mcd_dtype dtype,
+                            const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                            void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* What the rows' positions stand for, rounded once to dtype: positions
+ * context[r] + i into token start[r] + i of k and v (layout and alignment as in
+ * mcd_cache_append).  Skipped positions are left as they are. */
+mcd_status mcd_cache_read(const mcd_cache *cache, const mcd_cache_rows *rows, mcd_dtype dtype,
+                          void *k, int64_t k_stride, void *v, int64_t v_stride,
+                          void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+typedef struct {
+  int32_t Hq;                /* query heads, a multiple of Hkv; head n reads K/V head n / (Hq / Hkv) */
+  mcd_dtype dtype;           /* of q and out */
+  float scale;               /* > 0, finite: logits are scale * q . k */
+  const void *q;             /* [n_tokens][Hq][D], rows q_stride elements apart */
+  int64_t q_stride;
+  void *out;                 /* [n_tokens][Hq][D], rows out_stride elements apart */
+  int64_t out_stride;
+  float *lse;                /* [n_tokens][Hq] or NULL: log of the sum of exp(logits), natural;
+                                -infinity for a token that sees nothing */
+  float *weight_out;         /* NULL, or laid out as cache->weight (which it may be): receives
+                                cache->weight (0 where that is NULL) plus, at every position of
+                                the rows' slots, the softmax weight summed over the row's tokens
+                                and the query heads of the K/V head */
+  void *workspace;
+  size_t workspace_bytes;    /* mcd_cache_workspace_bytes() */
+} mcd_cache_attend_args;
+
+/* Attention of every new token over its row's cache, causal within the row:
+ * token i of row r sees positions 0 .. context[r] + i (append first; context[r]
+ * = length - 1 with one token attends over a cache that nothing was appended
+ * to).  A token that sees no position (context[r] + i < 0) gets zeros.  Logits,
+ * softmax and sums are in fp32; softmax weights enter the product with the
+ * values to 16 bits when dtype is MCD_BF16 and to 24 when it is MCD_F32.  The
+ * same inputs give the same bits.  q, out and the strides in bytes
+ * must be multiples of 16. */
+mcd_status mcd_cache_attend(const mcd_cache *cache, const mcd_cache_rows *rows,
+                            const mcd_cache_attend_args *args, hipStream_t stream);
+
+/* Eviction by received weight.  Row r's source slot holds length[r] positions.
+ * In every K/V head the `recent` newest stay and, of the others, the keep -
+ * recent that received the most weight (from->weight; equal weights: the lower
+ * position first; NaN below every number), in their order.  Their codes, scales
+ * and weights become positions 0, 1, ... of slot r of `to`, whose pages must be
+ * in its table and must not be pages of a source slot of the call (from and to
+ * may share the page array).  A row of at most keep positions is copied whole,
+ * so this also gives a Companion a copy of its own.
+ *   kept: [R][Hkv][keep] the positions kept, -1 past the row's new length
+ *   length_out: [R] min(length[r], keep)
+ * to->weight may be NULL; from->weight may be NULL when keep >= max_length. */
+typedef struct {
+  int32_t R;
+  int32_t max_length;        /* no row is longer, >= 0 */
+  int32_t keep, recent;      /* 0 <= recent <= keep, keep >= 1 */
+  const int32_t *slot;       /* [R] source slots, or NULL: the row's index */
+  const int32_t *length;     /* [R] */
+  int32_t *kept;
+  int32_t *length_out;
+  void *workspace;
+  size_t workspace_bytes;    /* the status word */
+} mcd_cache_evict_args;
+
+mcd_status mcd_cache_evict(const mcd_cache *from, const mcd_cache *to,
+                           const mcd_cache_evict_args *args, hipStream_t stream);
 
 /* ---- device status ----------------------------------------------------------
  * Synchronises `stream`, returns the status word of the workspace in *code

@@ -19,7 +19,8 @@ LIB = os.path.join(PKG, "libmcd.so")
 ARCH = "gfx950"
 
 SOURCES = ["mcd_api.cpp", "k_head_gemm.hip", "k_stream.hip", "k_mfma.hip", "k_fused.hip",
-           "k_mixed_32.hip", "k_mixed_64.hip", "k_mixed_128.hip", "k_sample.hip", "k_grid.hip", "k_embed.hip", "mcd_sched.cpp"]
+           "k_mixed_32.hip", "k_mixed_64.hip", "k_mixed_128.hip", "k_sample.hip", "k_grid.hip",
+           "k_embed.hip", "mcd_sched.cpp", "k_cache.hip", "k_cache_attend.hip", "mcd_cache.cpp"]
 
 COMMON = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wextra",

@@ -1,0 +1,574 @@
+// The 4-bit key/value cache's pages: quantising tokens into them, reading them
+// back, and eviction by received weight (mcd.h, mcd_cache).
+//
+// All of it moves bytes: the codes are found by comparing with exact products
+// of the scale, so every result is a function of the inputs alone, bit for bit.
+#include "cache_common.h"
+
+namespace mcd {
+namespace {
+
+constexpr int kHalf = 32;        // tokens of a workgroup: the words of a half page
+
+template <bool BF16>
+__device__ __forceinline__ void load8(const void *p, int64_t at, float x[8]) {
+  if constexpr (BF16) {
+    const u32x4 w = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(p) + at);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  } else {
+    const float4 *q = reinterpret_cast<const float4 *>(static_cast<const float *>(p) + at);
+    const float4 a = q[0], b = q[1];
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  }
+}
+
+template <bool BF16>
+__device__ __forceinline__ void store8(void *p, int64_t at, const float x[8]) {
+  if constexpr (BF16) {
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = bf16_bits(x[2 * i]) | bf16_bits(x[2 * i + 1]) << 16;
+    *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(p) + at) = w;
+  } else {
+    float4 *q = reinterpret_cast<float4 *>(static_cast<float *>(p) + at);
+    q[0] = make_float4(x[0], x[1], x[2], x[3]);
+    q[1] = make_float4(x[4], x[5], x[6], x[7]);
+  }
+}
+
+// Largest magnitude of x[8] and of the lanes whose index differs in the low
+// bits below W, as bits: larger than every finite number's where one is not
+// finite.
+template <int W>
+__device__ __forceinline__ uint32_t top_bits(const float x[8]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+#pragma unroll
+  for (int d = 1; d < W; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
+  return m;
+}
+
+__device__ __forceinline__ uint32_t codes8(const float x[8], float scale) {
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w |= e2m1_code(x[i], scale) << (4 * i);
+  return w;
+}
+
+// 8 channels' codes of a key block, its scale byte; all lanes of the block's
+// four take part
+__device__ __forceinline__ uint32_t key_codes(const float x[8], uint32_t &byte) {
+  const uint32_t top = top_bits<4>(x);
+  const bool finite = top < 0x7F800000u;
+  byte = finite ? key_scale(__uint_as_float(top)) : 255u;
+  return finite ? codes8(x, __uint_as_float(byte << 23)) : 0u;
+}
+
+template <int D>
+__device__ __forceinline__ uint32_t value_codes(const float x[8], uint32_t &scale) {
+  const uint32_t top = top_bits<D / 8>(x);
+  const bool finite = top < 0x7F800000u;
+  scale = finite ? bf16_bits(__uint_as_float(top) * (1.0f / 6.0f)) : 0x7FC0u;
+  return finite ? codes8(x, bf16_float(scale)) : 0u;
+}
+
+// ---- append ------------------------------------------------------------------
+
+// Rows of at most one token: D / 8 lanes for each (row, head), 8 channels each.
+// A value word is shared with seven other tokens of the slot, none of which the
+// call writes: read, changed and written by one thread.  A chain of two loads
+// (page id, word) and two stores; 512 rows x 8 heads are 4096 such chains.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void append_one_kernel(CacheView cv, RowsView rv, const void *k,
+                                                         int64_t ks, const void *v, int64_t vs,
+                                                         uint32_t *status) {
+  constexpr int L = D / 8;
+  const int item = (blockIdx.x * 256 + threadIdx.x) / L, chunk = threadIdx.x % L;
+  const int r = item / cv.Hkv, h = item % cv.Hkv;
+  if (r >= rv.R) return;
+  // the lanes of a wave may be of several rows: vector loads throughout
+  const int t0 = rv.start ? rv.start[r] : r, t1 = rv.start ? rv.start[r + 1] : r + 1;
+  const int slot = rv.slot ? rv.slot[r] : r, pos = rv.context[r];
+  if (t0 >= t1 && t0 >= 0 && t1 <= rv.N) return;             // no token
+  if (t0 < 0 || t1 > rv.N || t1 - t0 > 1 || slot < 0 || slot >= cv.n_slots || pos < 0 ||
+      pos >= rv.max_context || pos / kPage >= cv.max_pages) {
+    if (chunk == 0) set_bad(status);
+    return;
+  }
+  const int id = cv.table[(int64_t)slot * cv.max_pages + pos / kPage];
+  if (id < 0 || id >= cv.n_pages) {
+    if (chunk == 0) set_bad(status);
+    return;
+  }
+  uint8_t *page = cv.pages + ((int64_t)id * cv.Hkv + h) * cache_page_bytes(D);
+  const int t = pos % kPage;
+  float x[8], y[8];
+  load8<BF16>(k, t0 * ks + h * D + chunk * 8, x);
+  load8<BF16>(v, t0 * vs + h * D + chunk * 8, y);
+  uint32_t *word[8], old[8];
+  const int shift = 4 * value_nibble(t);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    word[i] = reinterpret_cast<uint32_t *>(
+        page + value_word<D>(t >> 5, (t >> 2) & 3, chunk * 8 + i));
+    old[i] = *word[i];
+  }
+  uint32_t byte, scale;
+  const uint32_t kc = key_codes(x, byte), vc = value_codes<D>(y, scale);
+  *reinterpret_cast<uint32_t *>(page + t * (D / 2) + chunk * 4) = kc;
+  if (chunk % 4 == 0) page[key_scale_at<D>(t, chunk / 4)] = (uint8_t)byte;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    *word[i] = (old[i] & ~(0xFu << shift)) | ((vc >> (4 * i)) & 0xFu) << shift;
+  if (chunk == 0) {
+    *reinterpret_cast<uint16_t *>(page + value_scale_at<D>(t)) = (uint16_t)scale;
+    if (cv.weight) cv.weight[((int64_t)slot * cv.Hkv + h) * cv.max_pages * kPage + pos] = 0.0f;
+  }
+}
+
+// The half pages that a row's tokens touch: at most tokens / 32 + 2, so the
+// items of row r begin at start[r] / 32 + 2 r.
+__host__ __device__ inline int64_t half_items(int32_t R, int32_t N) {
+  return (int64_t)N / kHalf + 2 * (int64_t)R;
+}
+
+struct HalfItem {
+  Span sp;
+  int pos0;                  // position of the half page's first token
+  int lo, hi;                // tokens of it that are the call's, lo < hi, else none
+  uint8_t *page;
+};
+
+template <int D>
+__device__ __forceinline__ HalfItem half_item(const CacheView &cv, const RowsView &rv, int h,
+                                              uint32_t *status) {
+  HalfItem it;
+  const int64_t x = blockIdx.x;
+  auto base = [&](int r) __attribute__((always_inline)) {
+    return (int64_t)row_start(rv, r) / kHalf + 2 * (int64_t)r;
+  };
+  const int r = find_row(rv.R, x, base);
+  it.sp = row_span(cv, rv, r);
+  const Span &s = it.sp;
+  const int first = max(s.ctx, 0);
+  const int64_t at = (int64_t)first / kHalf + (x - base(r));
+  const bool none = s.n == 0 || x < base(r) || at * kHalf >= s.len;
+  it.lo = it.hi = 0;
+  it.pos0 = 0;
+  it.page = nullptr;
+  if ((s.bad || s.ctx < 0) && threadIdx.x == 0) set_bad(status);
+  if (none) return it;
+  it.pos0 = (int)at * kHalf;
+  it.lo = max(first - it.pos0, 0);
+  it.hi = min(s.len - it.pos0, kHalf);
+  it.page = page_of<D>(cv, s.slot, it.pos0 / kPage, h);
+  if (!it.page) {
+    it.hi = it.lo;
+    if (threadIdx.x == 0) set_bad(status);
+  }
+  return it;
+}
+
+// Any number of tokens: a workgroup for each half page and head.  Key codes go
+// straight to the page (a lane's 8 channels are one word); value codes turn
+// through LDS, so that each word of 8 tokens is written once, whole.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void append_kernel(CacheView cv, RowsView rv, const void *k,
+                                                     int64_t ks, const void *v, int64_t vs,
+                                                     uint32_t *status) {
+  constexpr int L = D / 8;
+  __shared__ uint32_t codes[kHalf][L + 1];
+  const int h = blockIdx.y;
+  const HalfItem it = half_item<D>(cv, rv, h, status);
+  if (it.lo >= it.hi) return;
+  const int half = (it.pos0 / kHalf) & 1;
+#pragma unroll
+  for (int i = threadIdx.x; i < kHalf * L; i += 256) {
+    const int tt = i / L, chunk = i % L, t = half * kHalf + tt;
+    const bool mine = tt >= it.lo && tt < it.hi;
+    float x[8] = {}, y[8] = {};
+    if (mine) {
+      const int64_t tok = it.sp.t0 + (it.pos0 + tt - it.sp.ctx);
+      load8<BF16>(k, tok * ks + h * D + chunk * 8, x);
+      load8<BF16>(v, tok * vs + h * D + chunk * 8, y);
+    }
+    uint32_t byte, scale;
+    const uint32_t kc = key_codes(x, byte);
+    codes[tt][chunk] = value_codes<D>(y, scale);
+    if (mine) {
+      *reinterpret_cast<uint32_t *>(it.page + t * (D / 2) + chunk * 4) = kc;
+      if (chunk % 4 == 0) it.page[key_scale_at<D>(t, chunk / 4)] = (uint8_t)byte;
+      if (chunk == 0)
+        *reinterpret_cast<uint16_t *>(it.page + value_scale_at<D>(t)) = (uint16_t)scale;
+    }
+  }
+  if (cv.weight && (int)threadIdx.x >= it.lo && (int)threadIdx.x < it.hi)
+    cv.weight[((int64_t)it.sp.slot * cv.Hkv + h) * cv.max_pages * kPage + it.pos0 + threadIdx.x] =
+        0.0f;
+  __syncthreads();
+  uint32_t *words = reinterpret_cast<uint32_t *>(it.page + 32 * D) + half * 4 * D;
+#pragma unroll
+  for (int i = threadIdx.x; i < 4 * D; i += 256) {
+    const int lane = (i >> 2) & 63, ct = (i >> 8) * 4 + (i & 3), m = lane & 15, g = lane >> 4;
+    const int c = (m >> 2) * (D / 4) + 4 * ct + (m & 3);
+    uint32_t w = 0, mask = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int tt = (j >> 2) * 16 + 4 * g + (j & 3);
+      const bool mine = tt >= it.lo && tt < it.hi;
+      w |= ((codes[tt][c >> 3] >> (4 * (c & 7))) & 0xFu) << (4 * j);
+      mask |= (mine ? 0xFu : 0u) << (4 * j);
+    }
+    if (mask == 0xFFFFFFFFu) words[i] = w;
+    else if (mask) words[i] = (words[i] & ~mask) | (w & mask);
+  }
+}
+
+// ---- read --------------------------------------------------------------------
+
+// Rows of at most one token, as append_one_kernel.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void read_one_kernel(CacheView cv, RowsView rv, void *k,
+                                                       int64_t ks, void *v, int64_t vs,
+                                                       uint32_t *status) {
+  constexpr int L = D / 8;
+  const int item = (blockIdx.x * 256 + threadIdx.x) / L, chunk = threadIdx.x % L;
+  const int r = item / cv.Hkv, h = item % cv.Hkv;
+  if (r >= rv.R) return;
+  const int t0 = rv.start ? rv.start[r] : r, t1 = rv.start ? rv.start[r + 1] : r + 1;
+  const int slot = rv.slot ? rv.slot[r] : r, pos = rv.context[r];
+  if (t0 >= t1 && t0 >= 0 && t1 <= rv.N) return;
+  if (t0 < 0 || t1 > rv.N || t1 - t0 > 1 || slot < 0 || slot >= cv.n_slots || pos < 0 ||
+      pos >= rv.max_context || pos / kPage >= cv.max_pages) {
+    if (chunk == 0) set_bad(status);
+    return;
+  }
+  const int id = cv.table[(int64_t)slot * cv.max_pages + pos / kPage];
+  if (id < 0 || id >= cv.n_pages) {
+    if (chunk == 0) set_bad(status);
+    return;
+  }
+  const uint8_t *page = cv.pages + ((int64_t)id * cv.Hkv + h) * cache_page_bytes(D);
+  const int t = pos % kPage, shift = 4 * value_nibble(t);
+  const uint32_t kc = *reinterpret_cast<const uint32_t *>(page + t * (D / 2) + chunk * 4);
+  const float kscale = key_scale_float(page[key_scale_at<D>(t, chunk / 4)]);
+  const float vscale =
+      bf16_float(*reinterpret_cast<const uint16_t *>(page + value_scale_at<D>(t)));
+  float x[8], y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t w = *reinterpret_cast<const uint32_t *>(
+        page + value_word<D>(t >> 5, (t >> 2) & 3, chunk * 8 + i));
+    x[i] = e2m1_value((kc >> (4 * i)) & 0xFu) * kscale;
+    y[i] = e2m1_value((w >> shift) & 0xFu) * vscale;
+  }
+  store8<BF16>(k, t0 * ks + h * D + chunk * 8, x);
+  store8<BF16>(v, t0 * vs + h * D + chunk * 8, y);
+}
+
+// A workgroup for each half page and head; the value words go through LDS.
+// Writes 4 (bf16) or 8 times the bytes that it reads.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void read_kernel(CacheView cv, RowsView rv, void *k, int64_t ks,
+                                                   void *v, int64_t vs, uint32_t *status) {
+  constexpr int L = D / 8;
+  __shared__ uint32_t words[4 * D];
+  const int h = blockIdx.y;
+  const HalfItem it = half_item<D>(cv, rv, h, status);
+  if (it.lo >= it.hi) return;
+  const int half = (it.pos0 / kHalf) & 1;
+  const uint32_t *src = reinterpret_cast<const uint32_t *>(it.page + 32 * D) + half * 4 * D;
+  for (int i = threadIdx.x; i < D; i += 256)
+    reinterpret_cast<u32x4 *>(words)[i] = reinterpret_cast<const u32x4 *>(src)[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = threadIdx.x; i < kHalf * L; i += 256) {
+    const int tt = i / L, chunk = i % L, t = half * kHalf + tt;
+    if (tt < it.lo || tt >= it.hi) continue;
+    const int64_t tok = it.sp.t0 + (it.pos0 + tt - it.sp.ctx);
+    const int shift = 4 * value_nibble(t);
+    const uint32_t kc = *reinterpret_cast<const uint32_t *>(it.page + t * (D / 2) + chunk * 4);
+    const float kscale = key_scale_float(it.page[key_scale_at<D>(t, chunk / 4)]);
+    const float vscale =
+        bf16_float(*reinterpret_cast<const uint16_t *>(it.page + value_scale_at<D>(t)));
+    float x[8], y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t w = words[(value_word<D>(0, (t >> 2) & 3, chunk * 8 + e) - 32 * D) / 4];
+      x[e] = e2m1_value((kc >> (4 * e)) & 0xFu) * kscale;
+      y[e] = e2m1_value((w >> shift) & 0xFu) * vscale;
+    }
+    store8<BF16>(k, tok * ks + h * D + chunk * 8, x);
+    store8<BF16>(v, tok * vs + h * D + chunk * 8, y);
+  }
+}
+
+// ---- eviction ----------------------------------------------------------------
+
+constexpr int kSelect = 1024, kSelectWaves = kSelect / 64;
+
+// Ascending with the weight; NaN lowest, -0 as 0.
+__device__ __forceinline__ uint32_t weight_key(float w) {
+  if (w != w) return 0u;
+  const uint32_t u = __float_as_uint(w + 0.0f);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// One workgroup for each row and head.  The m-th largest key of the old
+// positions is found digit by digit (11, 11 and 10 bits, from the top): a
+// histogram of the digit among the keys that match so far, then the digit at
+// which the count from above reaches what is left of m.  Equal keys of a wave
+// are counted once by a vote before the LDS atomics: most positions of a cache
+// have received exactly nothing.  Then every wave walks a stretch of its own in
+// order, with the counts of the stretches before it: keys above the m-th, and
+// the first of its equals, are written in order.
+__global__ __launch_bounds__(kSelect) void evict_select_kernel(CacheView cv, EvictView ev) {
+  __shared__ uint32_t hist[2048];
+  __shared__ uint32_t wave_gt[kSelectWaves], wave_eq[kSelectWaves];
+  __shared__ uint32_t sh_digit, sh_left;
+  const int h = blockIdx.x, r = blockIdx.y, tid = threadIdx.x;
+  const int lane = tid & 63, wave = tid >> 6;
+  const int slot = ev.slot ? ld_const(ev.slot, r) : r;
+  int n = ld_const(ev.length, r);
+  const int cap = min((int64_t)ev.max_length, (int64_t)cv.max_pages * kPage);
+  const bool bad = slot < 0 || slot >= cv.n_slots || n < 0 || n > cap;
+  if (bad) {
+    n = slot < 0 || slot >= cv.n_slots ? 0 : min(max(n, 0), cap);
+    if (tid == 0) set_bad(ev.status);
+  }
+  const int len = min(n, ev.keep);
+  if (h == 0 && tid == 0) ev.length_out[r] = len;
+  int32_t *kept = ev.kept + ((int64_t)r * cv.Hkv + h) * ev.keep;
+  for (int i = len + tid; i < ev.keep; i += kSelect) kept[i] = -1;
+  if (n <= ev.keep) {
+    for (int i = tid; i < n; i += kSelect) kept[i] = i;
+    return;
+  }
+  const int old = n - ev.recent, m = ev.keep - ev.recent;
+  for (int i = tid; i < ev.recent; i += kSelect) kept[m + i] = old + i;
+  if (m == 0) return;
+  const float *w = cv.weight + ((int64_t)slot * cv.Hkv + h) * cv.max_pages * kPage;
+  uint32_t prefix = 0, left = (uint32_t)m;
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+    const int bits = pass == 2 ? 10 : 11;
+    for (int i = tid; i < 2048; i += kSelect) hist[i] = 0;
+    __syncthreads();
+    for (int i = tid; i - lane < old; i += kSelect) {
+      const uint32_t key = i < old ? weight_key(w[i]) : 0u;
+      const bool in = i < old && (pass == 0 || key >> (shift + bits) == prefix);
+      const uint32_t digit = (key >> shift) & ((1u << bits) - 1u);
+      const uint64_t live = __ballot(in);
+      if (live == 0) continue;
+      const int lead = __ffsll((unsigned long long)live) - 1;
+      const uint32_t dl = (uint32_t)__shfl((int)digit, lead);
+      const uint64_t same = __ballot(in && digit == dl);
+      if (lane == lead) atomicAdd(&hist[dl], (uint32_t)__popcll(same));
+      if (in && digit != dl) atomicAdd(&hist[digit], 1u);
+    }
+    __syncthreads();
+    // counts from the top: thread t holds digits 2047 - 2t and 2046 - 2t
+    const uint32_t a = hist[2047 - 2 * tid], b = hist[2046 - 2 * tid];
+    uint32_t sum = a + b;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint32_t o = (uint32_t)__shfl_up((int)sum, d);
+      if (lane >= d) sum += o;
+    }
+    if (lane == 63) wave_gt[wave] = sum;
+    __syncthreads();
+    for (int i = 0; i < wave; ++i) sum += wave_gt[i];
+    const uint32_t before = sum - a - b;       // keys of higher digits
+    if (before < left && sum >= left) {
+      const bool first = before + a >= left;
+      sh_digit = (uint32_t)(first ? 2047 - 2 * tid : 2046 - 2 * tid);
+      sh_left = left - before - (first ? 0u : a);
+    }
+    __syncthreads();
+    prefix = prefix << bits | sh_digit;
+    left = sh_left;
+  }
+  // `left` of the keys equal to prefix stay
+  const int per = ((old + kSelectWaves - 1) / kSelectWaves + 63) & ~63;
+  const int lo = min(wave * per, old), hi = min(lo + per, old);
+  uint32_t gt = 0, eq = 0;
+  for (int i = lo + lane; i - lane < hi; i += 64) {
+    const uint32_t key = i < hi ? weight_key(w[i]) : 0u;
+    gt += __popcll(__ballot(i < hi && key > prefix));
+    eq += __popcll(__ballot(i < hi && key == prefix));
+  }
+  __syncthreads();                             // wave_gt is free
+  if (lane == 0) {
+    wave_gt[wave] = gt;
+    wave_eq[wave] = eq;
+  }
+  __syncthreads();
+  gt = eq = 0;
+  for (int i = 0; i < wave; ++i) {
+    gt += wave_gt[i];
+    eq += wave_eq[i];
+  }
+  const uint64_t below = (1ull << lane) - 1;
+  for (int i = lo + lane; i - lane < hi; i += 64) {
+    const uint32_t key = i < hi ? weight_key(w[i]) : 0u;
+    const bool above = i < hi && key > prefix, equal = i < hi && key == prefix;
+    const uint64_t bg = __ballot(above), be = __ballot(equal);
+    const uint32_t my_eq = eq + __popcll(be & below), my_gt = gt + __popcll(bg & below);
+    if (above || (equal && my_eq < left)) kept[my_gt + min(my_eq, left)] = i;
+    gt += __popcll(bg);
+    eq += __popcll(be);
+  }
+}
+
+// A workgroup for each row, head and 32 positions of the new slot.  A lane
+// makes four value words (16 bytes) from the 16-byte chunks of their 8 tokens.
+template <int D>
+__global__ __launch_bounds__(256) void evict_move_kernel(CacheView from, CacheView to,
+                                                         EvictView ev) {
+  __shared__ const uint8_t *page[kHalf];
+  __shared__ int token[kHalf];
+  const int h = blockIdx.y, r = blockIdx.z, tid = threadIdx.x;
+  const int len = ld_const(ev.length_out, r);
+  const int pos0 = blockIdx.x * kHalf;
+  if (pos0 >= len) return;
+  const int count = min(len - pos0, kHalf);
+  const int slot = ev.slot ? ld_const(ev.slot, r) : r;
+  uint8_t *dst = nullptr;
+  if (r < to.n_slots && pos0 / kPage < to.max_pages) dst = page_of<D>(to, r, pos0 / kPage, h);
+  if (!dst) {
+    if (tid == 0) set_bad(ev.status);
+    return;
+  }
+  const int half = (pos0 / kHalf) & 1;
+  if (tid < kHalf) {
+    const uint8_t *p = nullptr;
+    int src = 0;
+    if (tid < count) {
+      src = ev.kept[((int64_t)r * from.Hkv + h) * ev.keep + pos0 + tid];
+      const int id = from.table[(int64_t)slot * from.max_pages + src / kPage];
+      if (id >= 0 && id < from.n_pages)
+        p = from.pages + ((int64_t)id * from.Hkv + h) * cache_page_bytes(D);
+      else
+        set_bad(ev.status);
+      if (to.weight) {
+        const int64_t f = ((int64_t)slot * from.Hkv + h) * from.max_pages * kPage + src;
+        to.weight[((int64_t)r * to.Hkv + h) * to.max_pages * kPage + pos0 + tid] =
+            from.weight ? from.weight[f] : 0.0f;
+      }
+    }
+    page[tid] = p;
+    token[tid] = src % kPage;
+  }
+  __syncthreads();
+  // keys: 16-byte chunks of 32 channels and their scale byte
+#pragma unroll
+  for (int i = tid; i < kHalf * (D / 32); i += 256) {
+    const int tt = i / (D / 32), b = i % (D / 32), t = half * kHalf + tt, s = token[tt];
+    const uint8_t *p = page[tt];
+    if (!p) continue;
+    *reinterpret_cast<u32x4 *>(dst + t * (D / 2) + b * 16) =
+        *reinterpret_cast<const u32x4 *>(p + s * (D / 2) + b * 16);
+    dst[key_scale_at<D>(t, b)] = p[key_scale_at<D>(s, b)];
+  }
+  if (tid < kHalf && page[tid])
+    *reinterpret_cast<uint16_t *>(dst + value_scale_at<D>(half * kHalf + tid)) =
+        *reinterpret_cast<const uint16_t *>(page[tid] + value_scale_at<D>(token[tid]));
+  // values: chunk i is words [half][i / 64][i % 64][0..3]
+#pragma unroll
+  for (int i = tid; i < D; i += 256) {
+    const int lane = i & 63, g = lane >> 4, m = lane & 15, q = i >> 6;
+    u32x4 w = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int tt = (j >> 2) * 16 + 4 * g + (j & 3), s = token[tt];
+      const uint8_t *p = page[tt];
+      if (!p) continue;
+      const int at = (((s >> 5) * (D / 64) + q) * 64 + ((s >> 2) & 3) * 16 + m) * 16;
+      const u32x4 x = *reinterpret_cast<const u32x4 *>(p + 32 * D + at);
+      const int shift = 4 * value_nibble(s);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] |= ((x[e] >> shift) & 0xFu) << (4 * j);
+    }
+    *reinterpret_cast<u32x4 *>(dst + 32 * D + ((half * (D / 64) + q) * 64 + lane) * 16) = w;
+  }
+}
+
+template <int D, bool BF16>
+void append_launch(const CacheView &cv, const RowsView &rv, const void *k, int64_t ks,
+                   const void *v, int64_t vs, uint32_t *status, hipStream_t st) {
+  if (rv.max_tokens <= 1) {
+    const int64_t lanes = (int64_t)rv.R * cv.Hkv * (D / 8);
+    hipLaunchKernelGGL((append_one_kernel<D, BF16>), dim3((unsigned)((lanes + 255) / 256)),
+                       dim3(256), 0, st, cv, rv, k, ks, v, vs, status);
+  } else {
+    const dim3 grid((unsigned)half_items(rv.R, rv.N), (unsigned)cv.Hkv);
+    hipLaunchKernelGGL((append_kernel<D, BF16>), grid, dim3(256), 0, st, cv, rv, k, ks, v, vs,
+                       status);
+  }
+}
+
+template <int D, bool BF16>
+void read_launch(const CacheView &cv, const RowsView &rv, void *k, int64_t ks, void *v, int64_t vs,
+                 uint32_t *status, hipStream_t st) {
+  if (rv.max_tokens <= 1) {
+    const int64_t lanes = (int64_t)rv.R * cv.Hkv * (D / 8);
+    hipLaunchKernelGGL((read_one_kernel<D, BF16>), dim3((unsigned)((lanes + 255) / 256)),
+                       dim3(256), 0, st, cv, rv, k, ks, v, vs, status);
+  } else {
+    const dim3 grid((unsigned)half_items(rv.R, rv.N), (unsigned)cv.Hkv);
+    hipLaunchKernelGGL((read_kernel<D, BF16>), grid, dim3(256), 0, st, cv, rv, k, ks, v, vs,
+                       status);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_cache_append(const CacheView &cv, const RowsView &rv, int D, bool bf16,
+                               const void *k, int64_t ks, const void *v, int64_t vs,
+                               uint32_t *status, hipStream_t st) {
+  auto go = [&](auto d) {
+    constexpr int W = decltype(d)::value;
+    if (bf16) append_launch<W, true>(cv, rv, k, ks, v, vs, status, st);
+    else append_launch<W, false>(cv, rv, k, ks, v, vs, status, st);
+  };
+  if (D == 64) go(std::integral_constant<int, 64>{});
+  else if (D == 128) go(std::integral_constant<int, 128>{});
+  else go(std::integral_constant<int, 256>{});
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_read(const CacheView &cv, const RowsView &rv, int D, bool bf16, void *k,
+                             int64_t ks, void *v, int64_t vs, uint32_t *status, hipStream_t st) {
+  auto go = [&](auto d) {
+    constexpr int W = decltype(d)::value;
+    if (bf16) read_launch<W, true>(cv, rv, k, ks, v, vs, status, st);
+    else read_launch<W, false>(cv, rv, k, ks, v, vs, status, st);
+  };
+  if (D == 64) go(std::integral_constant<int, 64>{});
+  else if (D == 128) go(std::integral_constant<int, 128>{});
+  else go(std::integral_constant<int, 256>{});
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_evict(const CacheView &from, const CacheView &to, const EvictView &ev,
+                              int D, hipStream_t st) {
+  hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)from.Hkv, (unsigned)ev.R), dim3(kSelect),
+                     0, st, from, ev);
+  const int longest = min(ev.keep, ev.max_length);
+  if (longest > 0) {
+    const dim3 grid((unsigned)((longest + kHalf - 1) / kHalf), (unsigned)from.Hkv, (unsigned)ev.R);
+    if (D == 64) hipLaunchKernelGGL(evict_move_kernel<64>, grid, dim3(256), 0, st, from, to, ev);
+    else if (D == 128)
+      hipLaunchKernelGGL(evict_move_kernel<128>, grid, dim3(256), 0, st, from, to, ev);
+    else hipLaunchKernelGGL(evict_move_kernel<256>, grid, dim3(256), 0, st, from, to, ev);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace mcd

@@ -25,6 +25,8 @@ MCD_OK, MCD_E_INVALID, MCD_E_UNSUPPORTED, MCD_E_WORKSPACE, MCD_E_HIP = range(5)
 MCD_F32, MCD_BF16 = 0, 1
 MCD_ROW_COND, MCD_ROW_UNCOND, MCD_ROW_SOLO, MCD_ROW_TEXT = 0, 1, 2, 3
 MCD_DEV_BAD_PARAM, MCD_DEV_GRID_RANGE, MCD_DEV_BAD_PLAN, MCD_DEV_BAD_TOKEN = 1, 2, 4, 8
+MCD_DEV_BAD_PAGE = 16
+MCD_CACHE_PAGE = 64
 MCD_MAX_K, MCD_MAX_V = 32, 4096
 
 _vp = ctypes.c_void_p
@@ -77,6 +79,29 @@ class mcd_sched_batch(ctypes.Structure):
                 ("n_frames", _vp), ("grid_slot", _vp)]
 
 
+class mcd_cache(ctypes.Structure):
+    _fields_ = [("Hkv", _i32), ("D", _i32), ("n_slots", _i32), ("max_pages", _i32),
+                ("n_pages", _i32), ("pages", _vp), ("table", _vp), ("weight", _vp)]
+
+
+class mcd_cache_rows(ctypes.Structure):
+    _fields_ = [("R", _i32), ("n_tokens", _i32), ("max_tokens", _i32), ("max_context", _i32),
+                ("slot", _vp), ("context", _vp), ("start", _vp)]
+
+
+class mcd_cache_attend_args(ctypes.Structure):
+    _fields_ = [("Hq", _i32), ("dtype", ctypes.c_int), ("scale", ctypes.c_float), ("q", _vp),
+                ("q_stride", ctypes.c_int64), ("out", _vp), ("out_stride", ctypes.c_int64),
+                ("lse", _vp), ("weight_out", _vp), ("workspace", _vp),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
+class mcd_cache_evict_args(ctypes.Structure):
+    _fields_ = [("R", _i32), ("max_length", _i32), ("keep", _i32), ("recent", _i32),
+                ("slot", _vp), ("length", _vp), ("kept", _vp), ("length_out", _vp),
+                ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
+
+
 def _sig(name, res, *args):
     f = getattr(_lib, name)
     f.restype = res
@@ -114,6 +139,18 @@ _mcd_phase_advance = _sig("mcd_phase_advance", ctypes.c_int, ctypes.POINTER(mcd_
                           _vp, _vp, _vp, _vp, _vp)
 _mcd_read_device_status = _sig("mcd_read_device_status", ctypes.c_int, _vp,
                                ctypes.POINTER(ctypes.c_uint32), _vp)
+_i64, _size = ctypes.c_int64, ctypes.c_size_t
+_cache_p, _rows_p = ctypes.POINTER(mcd_cache), ctypes.POINTER(mcd_cache_rows)
+_mcd_cache_page_bytes = _sig("mcd_cache_page_bytes", _size, _i32)
+_mcd_cache_workspace_bytes = _sig("mcd_cache_workspace_bytes", _size, _cache_p, _rows_p, _i32)
+_mcd_cache_append = _sig("mcd_cache_append", ctypes.c_int, _cache_p, _rows_p, ctypes.c_int, _vp,
+                         _i64, _vp, _i64, _vp, _size, _vp)
+_mcd_cache_read = _sig("mcd_cache_read", ctypes.c_int, _cache_p, _rows_p, ctypes.c_int, _vp,
+                       _i64, _vp, _i64, _vp, _size, _vp)
+_mcd_cache_attend = _sig("mcd_cache_attend", ctypes.c_int, _cache_p, _rows_p,
+                         ctypes.POINTER(mcd_cache_attend_args), _vp)
+_mcd_cache_evict = _sig("mcd_cache_evict", ctypes.c_int, _cache_p, _cache_p,
+                        ctypes.POINTER(mcd_cache_evict_args), _vp)
 _mcd_status_string = _sig("mcd_status_string", ctypes.c_char_p, ctypes.c_int)
 _mcd_last_error = _sig("mcd_last_error", ctypes.c_char_p)
 
@@ -125,6 +162,8 @@ EXPORTED = ["mcd_head_create", "mcd_head_destroy", "mcd_plan_words", "mcd_batch_
             "mcd_read_device_status",
             "mcd_sched_create", "mcd_sched_destroy", "mcd_sched_submit", "mcd_sched_plan",
             "mcd_sched_commit", "mcd_sched_counts",
+            "mcd_cache_page_bytes", "mcd_cache_workspace_bytes", "mcd_cache_append",
+            "mcd_cache_read", "mcd_cache_attend", "mcd_cache_evict",
             "mcd_status_string", "mcd_last_error"]
 
 
@@ -370,6 +409,165 @@ def mcd_read_device_status(workspace, stream=None):
     _check(_mcd_read_device_status(_ptr(workspace), ctypes.byref(code), _stream(stream)),
            "mcd_read_device_status")
     return code.value
+
+
+# ---------------------------------------------------------------------------
+# 4-bit key/value cache
+
+def mcd_cache_page_bytes(D):
+    return int(_mcd_cache_page_bytes(D))
+
+
+def mcd_cache_workspace_bytes(cache, rows, Hq):
+    n = int(_mcd_cache_workspace_bytes(cache.ref, rows.ref, Hq))
+    if n == 0:
+        raise McdError(MCD_E_INVALID, "mcd_cache_workspace_bytes")
+    return n
+
+
+_DTYPES = {torch.bfloat16: MCD_BF16, torch.float32: MCD_F32}
+
+
+def _tokens(name, t, rows, heads, D, like=None):
+    """dtype and row stride of a packed token tensor [n_tokens][heads][D], each head's channels
+    and a token's heads without gaps."""
+    shape, stride = t.shape, t.stride()
+    if shape[0] < rows.n_tokens or shape[1:] != (heads, D):
+        raise ValueError(f"{name}: shape {tuple(shape)}, expected [{rows.n_tokens}][{heads}][{D}]")
+    if stride[2] != 1 or (stride[1] != D and heads > 1):
+        raise ValueError(f"{name}: a token's heads must be contiguous (strides {stride})")
+    if t.dtype not in _DTYPES or (like is not None and t.dtype != like.dtype):
+        raise ValueError(f"{name}: dtype {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} is not on the GPU")
+    return _DTYPES[t.dtype], stride[0] if shape[0] > 1 else heads * D
+
+
+class Cache:
+    """A layer's 4-bit key/value cache and the device tensors it borrows.
+
+    pages: uint8 [n_pages][Hkv][mcd_cache_page_bytes(D)]; table: int32 [n_slots][max_pages];
+    weight: float32 [n_slots][Hkv][max_pages * 64] or None.  Cache.alloc makes the pages."""
+
+    def __init__(self, pages, table, D, weight=None):
+        self.pages, self.table, self.weight, self.D = pages, table, weight, int(D)
+        n_pages, self.Hkv, page_bytes = pages.shape
+        self.n_slots, self.max_pages = table.shape
+        if page_bytes != mcd_cache_page_bytes(D):
+            raise ValueError(f"pages of {page_bytes} bytes, heads of {D} take "
+                             f"{mcd_cache_page_bytes(D)}")
+        shape = (self.n_slots, self.Hkv, self.max_pages * MCD_CACHE_PAGE)
+        for name, t, dt in (("pages", pages, torch.uint8), ("table", table, torch.int32),
+                            ("weight", weight, torch.float32)):
+            if t is not None and (t.dtype != dt or not t.is_contiguous()):
+                raise ValueError(f"{name} must be contiguous {dt}")
+        if weight is not None and tuple(weight.shape) != shape:
+            raise ValueError(f"weight: shape {tuple(weight.shape)}, expected {shape}")
+        self.struct = mcd_cache(self.Hkv, self.D, self.n_slots, self.max_pages, n_pages,
+                                _ptr(pages), _ptr(table), _ptr(weight))
+        self.ref = ctypes.byref(self.struct)
+        self.on_gpu = all(t is None or t.is_cuda for t in (pages, table, weight))
+
+    @classmethod
+    def alloc(cls, n_pages, Hkv, D, n_slots, max_pages, weights=False, device="cuda"):
+        """Zeroed pages and weights and a table of -1 (no page)."""
+        pages = torch.zeros((n_pages, Hkv, mcd_cache_page_bytes(D)), dtype=torch.uint8,
+                            device=device)
+        table = torch.full((n_slots, max_pages), -1, dtype=torch.int32, device=device)
+        weight = torch.zeros((n_slots, Hkv, max_pages * MCD_CACHE_PAGE), device=device) \
+            if weights else None
+        return cls(pages, table, D, weight)
+
+    def workspace(self, rows, Hq):
+        """A zeroed workspace for these rows' bounds (a larger one serves smaller steps)."""
+        return torch.zeros(mcd_cache_workspace_bytes(self, rows, Hq), dtype=torch.uint8,
+                           device=self.pages.device)
+
+
+class CacheRows:
+    """The rows of a step (int32 device tensors, borrowed): context [R], slot [R] or None, start
+    [R + 1] or None for one token in every row.  max_tokens and max_context bound every row's
+    tokens and its positions after them."""
+
+    def __init__(self, context, start=None, slot=None, n_tokens=None, max_tokens=1,
+                 max_context=0):
+        self.context, self.start, self.slot = context, start, slot
+        self.R = context.shape[0]
+        self.n_tokens = self.R if n_tokens is None else int(n_tokens)
+        if start is not None and n_tokens is None:
+            raise ValueError("start needs n_tokens")
+        for name, t, n in (("context", context, self.R), ("start", start, self.R + 1),
+                           ("slot", slot, self.R)):
+            if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (n,)
+                                  or not t.is_contiguous()):
+                raise ValueError(f"{name} must be contiguous int32 [{n}]")
+        self.struct = mcd_cache_rows(self.R, self.n_tokens, int(max_tokens), int(max_context),
+                                     _ptr(slot), _ptr(context), _ptr(start))
+        self.ref = ctypes.byref(self.struct)
+        self.on_gpu = all(t is None or t.is_cuda for t in (context, start, slot))
+
+
+def _on_gpu(*parts):
+    if not all(p.on_gpu if hasattr(p, "on_gpu") else p is None or p.is_cuda for p in parts):
+        raise ValueError("a tensor of the call is not on the GPU")
+
+
+def mcd_cache_append(cache, rows, k, v, workspace, stream=None):
+    """k, v [n_tokens][Hkv][D] (bf16 or fp32) into the rows' pages."""
+    dt, ks = _tokens("k", k, rows, cache.Hkv, cache.D)
+    _, vs = _tokens("v", v, rows, cache.Hkv, cache.D, k)
+    _on_gpu(cache, rows, workspace)
+    _check(_mcd_cache_append(cache.ref, rows.ref, dt, k.data_ptr(), ks, v.data_ptr(), vs,
+                             workspace.data_ptr(), workspace.nbytes, _stream(stream)),
+           "mcd_cache_append")
+
+
+def mcd_cache_read(cache, rows, k, v, workspace, stream=None):
+    """The values at the rows' positions into k, v [n_tokens][Hkv][D] (bf16 or fp32)."""
+    dt, ks = _tokens("k", k, rows, cache.Hkv, cache.D)
+    _, vs = _tokens("v", v, rows, cache.Hkv, cache.D, k)
+    _on_gpu(cache, rows, workspace)
+    _check(_mcd_cache_read(cache.ref, rows.ref, dt, k.data_ptr(), ks, v.data_ptr(), vs,
+                           workspace.data_ptr(), workspace.nbytes, _stream(stream)),
+           "mcd_cache_read")
+
+
+def mcd_cache_attend(cache, rows, q, out, workspace, scale=None, lse=None, weight_out=None,
+                     stream=None):
+    """out = softmax(scale q k^T) v for q, out [n_tokens][Hq][D] (bf16 or fp32); scale: default
+    1 / sqrt(D).  weight_out: laid out as cache.weight (which it may be)."""
+    Hq = q.shape[1]
+    dt, qs = _tokens("q", q, rows, Hq, cache.D)
+    _, os_ = _tokens("out", out, rows, Hq, cache.D, q)
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous()
+                            or lse.numel() < rows.n_tokens * Hq):
+        raise ValueError("lse must be contiguous float32 [n_tokens][Hq]")
+    if weight_out is not None and (
+            weight_out.dtype != torch.float32 or not weight_out.is_contiguous()
+            or weight_out.numel() != cache.n_slots * cache.Hkv * cache.max_pages * MCD_CACHE_PAGE):
+        raise ValueError("weight_out must be laid out as the cache's weight")
+    _on_gpu(cache, rows, lse, weight_out, workspace)
+    a = mcd_cache_attend_args(Hq, dt, cache.D ** -0.5 if scale is None else scale, q.data_ptr(),
+                              qs, out.data_ptr(), os_, _ptr(lse), _ptr(weight_out),
+                              workspace.data_ptr(), workspace.nbytes)
+    _check(_mcd_cache_attend(cache.ref, rows.ref, ctypes.byref(a), _stream(stream)),
+           "mcd_cache_attend")
+
+
+def mcd_cache_evict(src, dst, length, keep, recent, kept, length_out, workspace, max_length,
+                    slot=None, stream=None):
+    """Row r: the positions kept of slot[r] (or r) of src, length[r] long, into slot r of dst.
+    kept: int32 [R][Hkv][keep]; length, length_out, slot: int32 [R]."""
+    R = length.shape[0]
+    for name, t, n in (("length", length, R), ("length_out", length_out, R), ("slot", slot, R),
+                       ("kept", kept, R * src.Hkv * keep)):
+        if t is not None and (t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous int32 with {n} elements")
+    _on_gpu(src, dst, length, slot, kept, length_out, workspace)
+    a = mcd_cache_evict_args(R, int(max_length), int(keep), int(recent), _ptr(slot), _ptr(length),
+                             _ptr(kept), _ptr(length_out), workspace.data_ptr(), workspace.nbytes)
+    _check(_mcd_cache_evict(src.ref, dst.ref, ctypes.byref(a), _stream(stream)),
+           "mcd_cache_evict")
 
 
 # ---------------------------------------------------------------------------
