@@ -8,6 +8,9 @@
 namespace mcd {
 namespace {
 
+// a * b, 0 when either is 0 whatever the other is (v_mul_legacy_f32)
+__device__ float mul_zero(float a, float b) __asm("llvm.amdgcn.fmul.legacy");
+
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // 8 e2m1 codes to bfloat16, times 2^(exponent of scale): exact.
@@ -50,57 +53,63 @@ struct PageRegs {
   uint32_t vs[8];                      // bfloat16 4 t + i
 };
 
+// A load at a wave-uniform address plus a 32-bit lane offset: the address stays
+// in scalar registers.
+template <class T>
+__device__ __forceinline__ T load_at(const uint8_t *base, uint32_t lane_at, uint32_t at) {
+  return *reinterpret_cast<const T *>(base + at + lane_at);
+}
+
 template <int D>
-__device__ __forceinline__ void load_keys(const uint8_t *page, int g, int m, PageRegs<D> &x) {
+__device__ __forceinline__ void load_keys(const uint8_t *page, uint32_t g, uint32_t m,
+                                          PageRegs<D> &x) {
+  const uint32_t lane_at = m * (D / 2) + g * (D / 8);
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const uint8_t *p = page + (16 * t + m) * (D / 2) + g * (D / 8);
+  for (uint32_t t = 0; t < 4; ++t) {
     if constexpr (D == 64) {
-      const uint2 w = *reinterpret_cast<const uint2 *>(p);
+      const uint2 w = load_at<uint2>(page, lane_at, 16 * t * (D / 2));
       x.k[t][0] = w.x;
       x.k[t][1] = w.y;
     } else {
 #pragma unroll
-      for (int i = 0; i < D / 128; ++i) {
-        const u32x4 w = reinterpret_cast<const u32x4 *>(p)[i];
+      for (uint32_t i = 0; i < D / 128; ++i) {
+        const u32x4 w = load_at<u32x4>(page, lane_at, 16 * t * (D / 2) + 16 * i);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x.k[t][4 * i + e] = w[e];
       }
     }
   }
-  const uint8_t *s = page + 64 * D + m * (D / 8);
-  if constexpr (D == 64) x.ks[0] = *reinterpret_cast<const uint32_t *>(s + (g >> 1) * 4);
-  else if constexpr (D == 128) x.ks[0] = *reinterpret_cast<const uint32_t *>(s + g * 4);
+  if constexpr (D == 64) x.ks[0] = load_at<uint32_t>(page, m * 8 + (g >> 1) * 4, 64 * D);
+  else if constexpr (D == 128) x.ks[0] = load_at<uint32_t>(page, m * 16 + g * 4, 64 * D);
   else {
-    const uint2 w = *reinterpret_cast<const uint2 *>(s + g * 8);
+    const uint2 w = load_at<uint2>(page, m * 32 + g * 8, 64 * D);
     x.ks[0] = w.x;
     x.ks[1] = w.y;
   }
 }
 
 template <int D>
-__device__ __forceinline__ void load_values(const uint8_t *page, int lane, PageRegs<D> &x) {
-  const u32x4 *p = reinterpret_cast<const u32x4 *>(page + 32 * D) + lane;
+__device__ __forceinline__ void load_values(const uint8_t *page, uint32_t lane, PageRegs<D> &x) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+  for (uint32_t h = 0; h < 2; ++h)
 #pragma unroll
-    for (int q = 0; q < D / 64; ++q) {
-      const u32x4 w = p[(h * (D / 64) + q) * 64];
+    for (uint32_t q = 0; q < D / 64; ++q) {
+      const u32x4 w = load_at<u32x4>(page, lane * 16, 32 * D + (h * (D / 64) + q) * 1024);
 #pragma unroll
       for (int e = 0; e < 4; ++e) x.v[h][4 * q + e] = w[e];
     }
-  const u32x4 *s = reinterpret_cast<const u32x4 *>(page + 66 * D) + (lane >> 4) * 2;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const u32x4 w = s[i];
+  for (uint32_t i = 0; i < 2; ++i) {
+    const u32x4 w = load_at<u32x4>(page, (lane >> 4) * 32, 66 * D + 16 * i);
 #pragma unroll
     for (int e = 0; e < 4; ++e) x.vs[4 * i + e] = w[e];
   }
 }
 
-// float whose exponent is key scale byte t of word w
+// float whose exponent is key scale byte t of word w; 255, infinity: dequant
+// then gives NaN for every code
 __device__ __forceinline__ float key_exp(uint32_t w, int t) {
-  return key_scale_float((w >> (8 * t)) & 0xFFu);
+  return __uint_as_float(t == 3 ? (w >> 24) << 23 : ((w >> (8 * t)) & 0xFFu) << 23);
 }
 
 // Scores of the page's tokens 16 t + 4 g + i (i: component) against query
@@ -114,6 +123,8 @@ __device__ __forceinline__ void scores(const PageRegs<D> &x, const bf16x8 (&q)[N
     for (int n = 0; n < NT; ++n) s[n][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int e = 0; e < D / 32; ++e) {
+      // (converted codes of two steps at a time, to keep the registers of three waves)
+      if (e % 2 == 0) __builtin_amdgcn_sched_barrier(0);
       const bf16x8 a = dequant(x.k[t][e], key_exp(x.ks[e / 4], t));
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -230,24 +241,103 @@ __device__ __forceinline__ void finish_row(const AttendView &av, int64_t row, fl
   if (av.stats) av.stats[row] = make_float2(top, l == 0.0f ? 0.0f : 1.0f / l);
 }
 
-// A workgroup of WQ x WK waves: WQ groups of 16 NT query rows, whose pages WK
-// waves share out.
-template <int D, int SPL, int NT, int WQ, int WK>
-__global__ __launch_bounds__(64 * WQ * WK) void attend_kernel(CacheView cv, RowsView rv,
-                                                             AttendView av) {
-  constexpr int TQ = 16 * NT * WQ, NCT = D / 16;
-  constexpr bool BF16 = SPL == 1;
+// A wave's running state: for each of NT tiles of 16 query rows (column m of the
+// lane) the largest q . k so far, the sum of its softmax weights at the lane's
+// positions, and the sums of weight x value code for the lane's channels.
+template <int D, int NT>
+struct Running {
+  float mx[NT], sum[NT];
+  floatx4 o[NT][D / 16];
+};
+
+// One page into the running state.  edge (uniform): some of its positions may be
+// hidden from some rows (limit: each row's last visible position less the page's
+// first).
+template <int D, int SPL, int NT>
+__device__ __forceinline__ void add_page(const PageRegs<D> &x,
+                                         const bf16x8 (&q)[NT][SPL][D / 32], int g, bool edge,
+                                         const int (&limit)[NT], float c, Running<D, NT> &st) {
   // terms of a softmax weight: 16 bits, so that a bf16 output is off by its own
   // rounding alone; 24 for fp32
-  constexpr int PTERMS = BF16 ? 2 : 3;
+  constexpr int PTERMS = SPL == 1 ? 2 : 3;
+  floatx4 s[NT][4];
+  scores<D, SPL, NT>(x, q, s);
+  if (edge) {
+    __builtin_amdgcn_sched_barrier(0);           // (kept a branch: few pages take it)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (16 * t + 4 * g + i > limit[n]) s[n][t][i] = -INFINITY;
+  }
+  float ref[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = fmaxf(top, s[n][t][i]);
+    top = across_groups_max(top);
+    if (__any(top > st.mx[n])) {
+      const float next = fmaxf(st.mx[n], top);
+      const float from = next == -INFINITY ? 0.0f : next;
+      const float f = __builtin_amdgcn_exp2f((st.mx[n] - from) * c);
+      st.mx[n] = next;
+      st.sum[n] *= f;
+#pragma unroll
+      for (int ct = 0; ct < D / 16; ++ct) st.o[n][ct] *= f;
+    }
+    ref[n] = st.mx[n] == -INFINITY ? 0.0f : st.mx[n];
+  }
+  // tokens 32 h onwards: weights, then their values
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    bf16x8 w[NT][PTERMS];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int t = 2 * h + (i >> 2);
+        const uint32_t two = x.vs[4 * h + (i >> 1)];
+        e[i] = __builtin_amdgcn_exp2f((s[n][t][i & 3] - ref[n]) * c);
+        st.sum[n] += e[i];
+        // (0 times anything is 0: a hidden position may hold a scale that is not finite)
+        e[i] = mul_zero(
+            e[i], __uint_as_float(i & 1 ? two & 0xFFFF0000u : two << 16));
+      }
+      split8<PTERMS>(e, w[n]);
+    }
+#pragma unroll
+    for (int ct = 0; ct < D / 16; ++ct) {
+      if (ct % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+      const bf16x8 a = dequant(x.v[h][ct], 1.0f);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = PTERMS - 1; e >= 0; --e) st.o[n][ct] = mfma(a, w[n][e], st.o[n][ct]);
+    }
+  }
+}
+
+// A workgroup of WQ x WK waves: WQ groups of 16 NT query rows, whose pages WK
+// waves share out.
+template <int D, int SPL, int NT, int WQ, int WK, int OCC>
+__global__ __launch_bounds__(64 * WQ * WK, OCC) void attend_kernel(CacheView cv, RowsView rv,
+                                                                  AttendView av) {
+  constexpr int TQ = 16 * NT * WQ, NCT = D / 16;
+  constexpr bool BF16 = SPL == 1;
   constexpr int PITCH = D + 4;
   __shared__ float sh_ml[WK > 1 ? 2 * WK * TQ : 1];
   __shared__ __align__(16) float sh_o[WK > 1 ? WK * TQ * PITCH : 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, m = lane & 15, wq = wave / WK, wk = wave % WK;
   const int h = blockIdx.y;
-  const int64_t item = blockIdx.x / av.splits;
-  const int split = blockIdx.x % av.splits;
+  const int item = blockIdx.x / av.splits;
+  const int split = blockIdx.x - item * av.splits;
   int tile;
   const int r = tile_row(rv, av.G, TQ, item, tile);
   const Span sp = row_span(cv, rv, r);
@@ -266,90 +356,53 @@ __global__ __launch_bounds__(64 * WQ * WK) void attend_kernel(CacheView cv, Rows
   for (int n = 0; n < NT; ++n) qr[n] = query_of(sp, av, h, rhow + 16 * n + m);
   // positions that every valid row of the wave sees
   const int all = min(sp.len - 1, sp.ctx + rhow / av.G);
-  bf16x8 q[NT][SPL][D / 32];
-  load_queries<D, SPL, NT>(av, sp, qr, g, q);
 
-  float mx[NT], sum[NT];
-  floatx4 o[NT][NCT];
+  Running<D, NT> st;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    mx[n] = -INFINITY;
-    sum[n] = 0.0f;
+    st.mx[n] = -INFINITY;
+    st.sum[n] = 0.0f;
 #pragma unroll
-    for (int c = 0; c < NCT; ++c) o[n][c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int c = 0; c < NCT; ++c) st.o[n][c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  for (int p = p0 + wk; p < p1; p += WK) {
-    const uint8_t *page = page_of<D>(cv, sp.slot, p, h);
-    if (!page) {
-      if (lane == 0) set_bad(av.status);
-      continue;
-    }
-    PageRegs<D> x;
+  PageRegs<D> xa;
+  const int32_t *table = cv.table + (int64_t)sp.slot * cv.max_pages;
+  // the wave's pages p, p + WK, ...; a page id out of range is replaced by page
+  // 0 with every position hidden
+  int p = p0 + wk;
+  int id = p < p1 ? ld_const(table, p) : 0, id_next = 0;
+  auto fetch = [&](int page_id, PageRegs<D> &x) __attribute__((always_inline)) {
+    const bool ok = page_id >= 0 && page_id < cv.n_pages;
+    const uint8_t *page =
+        cv.pages + ((int64_t)(ok ? page_id : 0) * cv.Hkv + h) * cache_page_bytes(D);
     load_keys<D>(page, g, m, x);
     load_values<D>(page, lane, x);
-    floatx4 s[NT][4];
-    scores<D, SPL, NT>(x, q, s);
-    float vs[16];
+  };
+  bf16x8 q[NT][SPL][D / 32];
+  auto work = [&](int at, int page_id, const PageRegs<D> &x) __attribute__((always_inline)) {
+    const bool ok = page_id >= 0 && page_id < cv.n_pages;
+    if (!ok && lane == 0) set_bad(av.status);
+    int limit[NT];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      vs[2 * i] = __uint_as_float(x.vs[i] << 16);
-      vs[2 * i + 1] = __uint_as_float(x.vs[i] & 0xFFFF0000u);
-    }
-    const bool edge = p * kPage + kPage - 1 > all;
-    if (edge) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int pos = p * kPage + 16 * t + 4 * g + i;
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-            if (pos > qr[n].limit) s[n][t][i] = -INFINITY;
-        }
-    }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      float top = -INFINITY;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[n][t][i]);
-      top = across_groups_max(top);
-      if (__any(top > mx[n])) {
-        const float next = fmaxf(mx[n], top);
-        const float ref = next == -INFINITY ? 0.0f : next;
-        const float f = __builtin_amdgcn_exp2f((mx[n] - ref) * av.c);
-        mx[n] = next;
-        sum[n] *= f;
-#pragma unroll
-        for (int c = 0; c < NCT; ++c) o[n][c] *= f;
-      }
-      const float ref = mx[n] == -INFINITY ? 0.0f : mx[n];
-      float w[16];
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float e = __builtin_amdgcn_exp2f((s[n][t][i] - ref) * av.c);
-          sum[n] += e;
-          // a hidden position may hold a value scale that is not finite
-          const bool hidden = edge && p * kPage + 16 * t + 4 * g + i > qr[n].limit;
-          w[4 * t + i] = hidden ? 0.0f : e * vs[4 * t + i];
-        }
-#pragma unroll
-      for (int hh = 0; hh < 2; ++hh) {
-        bf16x8 b[PTERMS];
-        split8<PTERMS>(w + 8 * hh, b);
-#pragma unroll
-        for (int c = 0; c < NCT; ++c) {
-          const bf16x8 a = dequant(x.v[hh][c], 1.0f);
-#pragma unroll
-          for (int e = PTERMS - 1; e >= 0; --e) o[n][c] = mfma(a, b[e], o[n][c]);
-        }
-      }
-    }
+    for (int n = 0; n < NT; ++n) limit[n] = ok ? qr[n].limit - at * kPage : -1;
+    add_page<D, SPL, NT>(x, q, g, !ok || at * kPage + kPage - 1 > all, limit, av.c, st);
+  };
+  if (p < p1) {
+    fetch(id, xa);
+    if (p + WK < p1) id_next = ld_const(table, p + WK);
   }
+  load_queries<D, SPL, NT>(av, sp, qr, g, q);
+  while (p < p1) {
+    work(p, id, xa);
+    p += WK;
+    id = id_next;
+    if (p < p1) fetch(id, xa);
+    id_next = p + WK < p1 ? ld_const(table, p + WK) : 0;
+  }
+  float (&mx)[NT] = st.mx;
+  float (&sum)[NT] = st.sum;
+  floatx4 (&o)[NT][NCT] = st.o;
 #pragma unroll
   for (int n = 0; n < NT; ++n) sum[n] = across_groups_sum(sum[n]);
 
@@ -559,11 +612,12 @@ template <int D, int SPL>
 void attend_launch(const CacheView &cv, const RowsView &rv, const AttendView &av,
                    const AttendPlan &plan, hipStream_t st) {
   const dim3 grid((unsigned)(plan.tiles * plan.splits), (unsigned)cv.Hkv);
+  constexpr int OCC = D * SPL > 384 ? 1 : D * SPL > 128 ? 2 : 3;
   if (plan.tile == 16)
-    hipLaunchKernelGGL((attend_kernel<D, SPL, 1, 1, 4>), grid, dim3(256), 0, st, cv, rv, av);
+    hipLaunchKernelGGL((attend_kernel<D, SPL, 1, 1, 4, OCC>), grid, dim3(256), 0, st, cv, rv, av);
   else
-    hipLaunchKernelGGL((attend_kernel<D, SPL, (D == 256 ? 1 : 2), 4, 1>), grid, dim3(256), 0, st,
-                       cv, rv, av);
+    hipLaunchKernelGGL((attend_kernel<D, SPL, (D == 256 ? 1 : 2), 4, 1, 1>), grid, dim3(256), 0,
+                       st, cv, rv, av);
   if (plan.splits > 1)
     hipLaunchKernelGGL((join_kernel<D, SPL == 1>), dim3((unsigned)plan.tiles, (unsigned)cv.Hkv),
                        dim3(256), 0, st, cv, rv, av, plan.tile);
