@@ -30,13 +30,14 @@ struct AttendView {
   int64_t q_stride, out_stride;
   float c;                     // scale * log2(e): softmax in powers of two
   float *lse;                  // the caller's, or null
-  float2 *stats;               // workspace [N][Hq] {max of q . k, 1 / sum}, or null: no weights
+  float2 *stats;               // workspace [N][Hq] {reference, 1 / sum}, or null: no weights
   float *weight_out;
   // Partial results of rows whose pages are split over workgroups: for each
   // query row of a tile and split {max, sum} and D sums.
   float2 *part_ml;
   float *part_o;
   int32_t splits, split_pages; // pages of a split: the workgroups of a tile
+  int32_t narrow;              // query rows of a narrow row at most, 0: no narrow rows
   uint32_t *status;
 };
 
@@ -45,12 +46,18 @@ hipError_t launch_cache_append(const CacheView &cv, const RowsView &rv, int D, b
                                uint32_t *status, hipStream_t st);
 hipError_t launch_cache_read(const CacheView &cv, const RowsView &rv, int D, bool bf16, void *k,
                              int64_t ks, void *v, int64_t vs, uint32_t *status, hipStream_t st);
-// Workspace of an attention call: the tiles' partials and the rows' statistics.
-struct AttendPlan {
-  int32_t tile;                // query rows of a tile (a workgroup)
-  int64_t tiles;               // tiles of one K/V head
+// How an attention call runs, and its workspace: the rows whose query rows of a
+// K/V head fit a narrow tile (of 16 rows and fewer), and the others.
+struct TilePlan {
+  int32_t tile;                // query rows of a tile
+  int64_t tiles;               // of one K/V head, 0: none
   int32_t splits, split_pages;
-  size_t ml_bytes, o_bytes, stat_bytes;
+  size_t ml_bytes, o_bytes;    // partial results
+};
+struct AttendPlan {
+  int32_t pack, narrow_rows;   // tiles of tokens side by side; AttendView::narrow
+  TilePlan narrow, wide;
+  size_t stat_bytes;
 };
 AttendPlan cache_attend_plan(const CacheView &cv, const RowsView &rv, int D, int32_t Hq);
 hipError_t launch_cache_attend(const CacheView &cv, const RowsView &rv, const AttendView &av,

@@ -5,11 +5,14 @@
 // in one pass over the pages with a running maximum and sum (base 2, fp32).
 #include "cache_common.h"
 
+#include <algorithm>
+
 namespace mcd {
-namespace {
 
 // a * b, 0 when either is 0 whatever the other is (v_mul_legacy_f32)
 __device__ float mul_zero(float a, float b) __asm("llvm.amdgcn.fmul.legacy");
+
+namespace {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
@@ -29,17 +32,55 @@ __device__ __forceinline__ floatx4 mfma(bf16x8 a, bf16x8 b, floatx4 c) {
 // x in SPL bfloat16 terms whose sum is x to 8 SPL bits
 template <int SPL>
 __device__ __forceinline__ void split8(const float x[8], bf16x8 (&out)[SPL]) {
+  typedef float float2v __attribute__((ext_vector_type(2)));
   float rest[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) rest[i] = x[i];
 #pragma unroll
   for (int n = 0; n < SPL; ++n) {
+    u32x4 w;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      out[n][i] = (__bf16)rest[i];
-      if (n + 1 < SPL) rest[i] -= (float)out[n][i];
+    for (int i = 0; i < 4; ++i) {
+      const bf16x2 two = __builtin_convertvector(float2v{rest[2 * i], rest[2 * i + 1]}, bf16x2);
+      w[i] = __builtin_bit_cast(uint32_t, two);
+      if (n + 1 < SPL) {
+        rest[2 * i] -= __uint_as_float(w[i] << 16);
+        rest[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
+      }
     }
+    out[n] = __builtin_bit_cast(bf16x8, w);
   }
+}
+
+// Lane moves on the vector units: x of lane i + n / i - n of the row of 16 lanes
+// (CTRL row_shl / row_shr / row_ror n), into the lanes of the banks of four of
+// BANKS; the other lanes keep old.
+template <int CTRL, int BANKS = 0xF>
+__device__ __forceinline__ uint32_t lane_move(uint32_t old, uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)x, CTRL, 0xF, BANKS, false);
+}
+template <int CTRL, int BANKS = 0xF>
+__device__ __forceinline__ float lane_move(float old, float x) {
+  return __uint_as_float(lane_move<CTRL, BANKS>(__float_as_uint(old), __float_as_uint(x)));
+}
+constexpr int kSame = 0xE4;                      // quad_perm 0 1 2 3
+constexpr int shl(int n) { return n == 0 ? kSame : n > 0 ? 0x100 + n : 0x110 - n; }
+constexpr int ror(int n) { return 0x120 + n; }
+
+// Over the four lanes 16 g + m of a column m.
+__device__ __forceinline__ float across_groups_max(float x) {
+  const uint32_t u = __float_as_uint(x);
+  auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const uint32_t v = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
+  auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float across_groups_sum(float x) {
+  const uint32_t u = __float_as_uint(x);
+  auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const uint32_t v = __float_as_uint(__uint_as_float(a[0]) + __uint_as_float(a[1]));
+  auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
 // A page's codes and scales as a wave's lanes hold them.  Lane 16 g + m has
@@ -88,7 +129,7 @@ __device__ __forceinline__ void load_keys(const uint8_t *page, uint32_t g, uint3
   }
 }
 
-template <int D>
+template <int D, bool SCALES = true>
 __device__ __forceinline__ void load_values(const uint8_t *page, uint32_t lane, PageRegs<D> &x) {
 #pragma unroll
   for (uint32_t h = 0; h < 2; ++h)
@@ -99,7 +140,7 @@ __device__ __forceinline__ void load_values(const uint8_t *page, uint32_t lane, 
       for (int e = 0; e < 4; ++e) x.v[h][4 * q + e] = w[e];
     }
 #pragma unroll
-  for (uint32_t i = 0; i < 2; ++i) {
+  for (uint32_t i = 0; i < (SCALES ? 2 : 0); ++i) {
     const u32x4 w = load_at<u32x4>(page, (lane >> 4) * 32, 66 * D + 16 * i);
 #pragma unroll
     for (int e = 0; e < 4; ++e) x.vs[4 * i + e] = w[e];
@@ -113,24 +154,32 @@ __device__ __forceinline__ float key_exp(uint32_t w, int t) {
 }
 
 // Scores of the page's tokens 16 t + 4 g + i (i: component) against query
-// column m of each of NT tiles.
-template <int D, int SPL, int NT>
-__device__ __forceinline__ void scores(const PageRegs<D> &x, const bf16x8 (&q)[NT][SPL][D / 32],
-                                       floatx4 (&s)[NT][4]) {
+// column m of each of NT tiles.  q(n, p, e): term p of the queries' operand for
+// channels' step e.  The four tiles of tokens are four independent chains of
+// matrix instructions.
+template <int D, int SPL, int NT, class Q>
+__device__ __forceinline__ void scores(const PageRegs<D> &x, Q &&q, floatx4 (&s)[NT][4]) {
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
+  for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int n = 0; n < NT; ++n) s[n][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int t = 0; t < 4; ++t) s[n][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e) {
-      // (converted codes of two steps at a time, to keep the registers of three waves)
-      if (e % 2 == 0) __builtin_amdgcn_sched_barrier(0);
-      const bf16x8 a = dequant(x.k[t][e], key_exp(x.ks[e / 4], t));
+  for (int e = 0; e < D / 32; ++e) {
+    __builtin_amdgcn_sched_barrier(0);       // (one step's converted codes in registers)
+    bf16x8 b[NT][SPL];
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int p = SPL - 1; p >= 0; --p) s[n][t] = mfma(a, q[n][p][e], s[n][t]);
-    }
+      for (int p = 0; p < SPL; ++p) b[n][p] = q(n, p, e);
+    bf16x8 a[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) a[t] = dequant(x.k[t][e], key_exp(x.ks[e / 4], t));
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int p = SPL - 1; p >= 0; --p)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) s[n][t] = mfma(a[t], b[n][p], s[n][t]);
   }
 }
 
@@ -151,16 +200,22 @@ __device__ __forceinline__ Query query_of(const Span &sp, const AttendView &av, 
   return q;
 }
 
+// A row whose query rows of a K/V head fit one narrow tile.
+__device__ __forceinline__ bool is_narrow(const Span &sp, const AttendView &av) {
+  return sp.n > 0 && (int64_t)sp.n * av.G <= av.narrow;
+}
+
 // Pages seen by the query rows below end.
 __device__ __forceinline__ int tile_pages(const Span &sp, int G, int end) {
   const int last = min(sp.len - 1, sp.ctx + (end - 1) / G);
   return last < 0 ? 0 : last / kPage + 1;
 }
 
+// (rows of which a lane's column has none: zeros)
 template <int D, int SPL, int NT>
 __device__ __forceinline__ void load_queries(const AttendView &av, const Span &sp,
                                              const Query (&qr)[NT], int g,
-                                             bf16x8 (&q)[NT][SPL][D / 32]) {
+                                             bf16x8 (&q)[NT][SPL][D / 32], bool has = true) {
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int64_t at = (int64_t)(sp.t0 + qr[n].tok) * av.q_stride + qr[n].head * D + g * (D / 4);
@@ -168,12 +223,12 @@ __device__ __forceinline__ void load_queries(const AttendView &av, const Span &s
     for (int e = 0; e < D / 32; ++e) {
       if constexpr (SPL == 1) {
         u32x4 w = {0u, 0u, 0u, 0u};
-        if (qr[n].valid)
+        if (qr[n].valid && has)
           w = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(av.q) + at + 8 * e);
         q[n][0][e] = __builtin_bit_cast(bf16x8, w);
       } else {
         float x[8] = {};
-        if (qr[n].valid) {
+        if (qr[n].valid && has) {
           const float4 *p =
               reinterpret_cast<const float4 *>(static_cast<const float *>(av.q) + at + 8 * e);
           const float4 a = p[0], b = p[1];
@@ -209,15 +264,6 @@ __device__ __forceinline__ int tile_row(const RowsView &rv, int G, int TQ, int64
   return r;
 }
 
-__device__ __forceinline__ float across_groups_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ __forceinline__ float across_groups_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
-}
-
 template <bool BF16>
 __device__ __forceinline__ void store4(void *p, int64_t at, const float x[4]) {
   if constexpr (BF16) {
@@ -231,31 +277,30 @@ __device__ __forceinline__ void store4(void *p, int64_t at, const float x[4]) {
   }
 }
 
-// A finished query row's largest q . k and sum: its lse, and what weight_kernel
-// needs of it.  Logits are compared before they are scaled, and the scale and
-// log2(e) applied to differences: no size of logits overflows a difference.
+// A finished query row's reference (in powers of two) and sum: its lse, and what
+// weight_kernel needs of them.
 __device__ __forceinline__ void finish_row(const AttendView &av, int64_t row, float top, float l) {
   if (av.lse)
     av.lse[row] = l == 0.0f ? -INFINITY
-                            : (top * av.c + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+                            : (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
   if (av.stats) av.stats[row] = make_float2(top, l == 0.0f ? 0.0f : 1.0f / l);
 }
 
 // A wave's running state: for each of NT tiles of 16 query rows (column m of the
-// lane) the largest q . k so far, the sum of its softmax weights at the lane's
+// lane) the reference of its softmax weights (about the largest logit so far, in
+// powers of two), the sum of its softmax weights at the lane's
 // positions, and the sums of weight x value code for the lane's channels.
 template <int D, int NT>
 struct Running {
-  float mx[NT], sum[NT];
+  float mx[NT], raw[NT], sum[NT];              // raw: the reference before its scaling
   floatx4 o[NT][D / 16];
 };
 
 // One page into the running state.  edge (uniform): some of its positions may be
 // hidden from some rows (limit: each row's last visible position less the page's
 // first).
-template <int D, int SPL, int NT>
-__device__ __forceinline__ void add_page(const PageRegs<D> &x,
-                                         const bf16x8 (&q)[NT][SPL][D / 32], int g, bool edge,
+template <int D, int SPL, int NT, class Q>
+__device__ __forceinline__ void add_page(const PageRegs<D> &x, Q &&q, int g, bool edge,
                                          const int (&limit)[NT], float c, Running<D, NT> &st) {
   // terms of a softmax weight: 16 bits, so that a bf16 output is off by its own
   // rounding alone; 24 for fp32
@@ -263,14 +308,15 @@ __device__ __forceinline__ void add_page(const PageRegs<D> &x,
   floatx4 s[NT][4];
   scores<D, SPL, NT>(x, q, s);
   if (edge) {
-    __builtin_amdgcn_sched_barrier(0);           // (kept a branch: few pages take it)
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+      for (int t = 0; t < 4; ++t) {
+        asm volatile("" : "+v"(s[n][t]));        // (kept a branch: few pages take it)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           if (16 * t + 4 * g + i > limit[n]) s[n][t][i] = -INFINITY;
+      }
   }
   float ref[NT];
 #pragma unroll
@@ -280,17 +326,34 @@ __device__ __forceinline__ void add_page(const PageRegs<D> &x,
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = fmaxf(top, s[n][t][i]);
-    top = across_groups_max(top);
-    if (__any(top > st.mx[n])) {
+    const float raw = across_groups_max(top);
+    top = raw * c;
+    // a new largest logit moves the reference once it is 2^8 above it: sums
+    // stay far below fp32's range, and most pages scale nothing
+    if (__any(top - st.mx[n] > 8.0f)) {
       const float next = fmaxf(st.mx[n], top);
-      const float from = next == -INFINITY ? 0.0f : next;
-      const float f = __builtin_amdgcn_exp2f((st.mx[n] - from) * c);
+      const float f = __builtin_amdgcn_exp2f(st.mx[n] - next);
+      // (nothing seen so far: -infinity less itself)
+      const float keep = st.mx[n] == -INFINITY ? 0.0f : f;
+      st.raw[n] = top > st.mx[n] ? raw : st.raw[n];
       st.mx[n] = next;
-      st.sum[n] *= f;
+      st.sum[n] *= keep;
 #pragma unroll
-      for (int ct = 0; ct < D / 16; ++ct) st.o[n][ct] *= f;
+      for (int ct = 0; ct < D / 16; ++ct) st.o[n][ct] *= keep;
     }
     ref[n] = st.mx[n] == -INFINITY ? 0.0f : st.mx[n];
+    // logits of 2^20 and more: the reference's own rounding would overflow a
+    // difference, so they are taken relative to the largest before they are scaled
+    if (__any(fabsf(ref[n]) >= 0x1p20f)) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        asm volatile("" : "+v"(s[n][t]));        // (kept a branch)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (st.mx[n] != -INFINITY) s[n][t][i] -= st.raw[n];
+      }
+      ref[n] = 0.0f;
+    }
   }
   // tokens 32 h onwards: weights, then their values
 #pragma unroll
@@ -303,7 +366,7 @@ __device__ __forceinline__ void add_page(const PageRegs<D> &x,
       for (int i = 0; i < 8; ++i) {
         const int t = 2 * h + (i >> 2);
         const uint32_t two = x.vs[4 * h + (i >> 1)];
-        e[i] = __builtin_amdgcn_exp2f((s[n][t][i & 3] - ref[n]) * c);
+        e[i] = __builtin_amdgcn_exp2f(fmaf(s[n][t][i & 3], c, -ref[n]));
         st.sum[n] += e[i];
         // (0 times anything is 0: a hidden position may hold a scale that is not finite)
         e[i] = mul_zero(
@@ -312,38 +375,221 @@ __device__ __forceinline__ void add_page(const PageRegs<D> &x,
       split8<PTERMS>(e, w[n]);
     }
 #pragma unroll
-    for (int ct = 0; ct < D / 16; ++ct) {
-      if (ct % 2 == 0) __builtin_amdgcn_sched_barrier(0);
-      const bf16x8 a = dequant(x.v[h][ct], 1.0f);
+    for (int c0 = 0; c0 < D / 16; c0 += 4) {
+      __builtin_amdgcn_sched_barrier(0);
+      bf16x8 a[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = dequant(x.v[h][c0 + i], 1.0f);
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int e = PTERMS - 1; e >= 0; --e) st.o[n][ct] = mfma(a, w[n][e], st.o[n][ct]);
+        for (int e = PTERMS - 1; e >= 0; --e)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) st.o[n][c0 + i] = mfma(a[i], w[n][e], st.o[n][c0 + i]);
     }
   }
 }
 
+// ---- few query rows: PACK tiles of tokens side by side ---------------------------
+//
+// With at most 16 / PACK query rows, most of a score tile's 16 columns are
+// empty.  The columns of PACK tiles of tokens are moved side by side (lane moves
+// within a row of 16 lanes), so that the softmax works on full registers, and
+// the terms of the weights go back to columns of their own: the first to the
+// query rows' columns, the second 16 / PACK columns further, so that one matrix
+// instruction multiplies the values with both; unpack_rows adds the sums up at
+// the end.  (Where the third term of fp32 finds no column it takes an
+// instruction of its own.)  About 200 vector and 32 matrix instructions for a
+// page of 64 tokens and 128 channels, where full tiles take 290 and 48.
+
+// Value scales of tokens 16 t + 4 g + i as bfloat16 i, t the lane's tile of each
+// of the 4 / PACK registers' worth.
+template <int D, int PACK>
+__device__ __forceinline__ void load_packed_scales(const uint8_t *page, uint32_t g, uint32_t m,
+                                                   PageRegs<D> &x) {
+#pragma unroll
+  for (uint32_t u = 0; u < 4 / PACK; ++u) {
+    const uint32_t lane_at = g * 32 + m / (16 / PACK) * 8;
+    const uint2 w = load_at<uint2>(page, lane_at, 66 * D + u * PACK * 8);
+    x.vs[2 * u] = w.x;
+    x.vs[2 * u + 1] = w.y;
+  }
+}
+
+template <int D, int SPL, int PACK, class Q>
+__device__ __forceinline__ void add_page_packed(const PageRegs<D> &x, Q &&q, int g, int m, bool edge,
+                                                int limit, float c, Running<D, 1> &st) {
+  constexpr int PTERMS = SPL == 1 ? 2 : 3;
+  constexpr int W = 16 / PACK, U = 4 / PACK;     // columns of a tile; registers of scores x 4
+  floatx4 s[1][4];
+  scores<D, SPL, 1>(x, q, s);
+  // p[u][i]: lane 16 g + m has token 16 (PACK u + m / W) + 4 g + i, query row m % W
+  float p[U][4];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (PACK == 4) {
+        float v = s[0][0][i];
+        v = lane_move<shl(-4), 0x2>(v, s[0][1][i]);
+        v = lane_move<shl(-8), 0x4>(v, s[0][2][i]);
+        p[u][i] = lane_move<shl(-12), 0x8>(v, s[0][3][i]);
+      } else {
+        p[u][i] = lane_move<shl(-8), 0xC>(s[0][2 * u][i], s[0][2 * u + 1][i]);
+      }
+    }
+  if (edge) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        asm volatile("" : "+v"(p[u][i]));        // (kept a branch: few pages take it)
+        if (16 * (PACK * u + m / W) + 4 * g + i > limit) p[u][i] = -INFINITY;
+      }
+  }
+  float top = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, p[u][i]);
+  if constexpr (PACK == 4) top = fmaxf(top, lane_move<ror(4)>(top, top));
+  top = fmaxf(top, lane_move<ror(8)>(top, top));
+  const float raw = across_groups_max(top);
+  top = raw * c;
+  // (reference and large logits as in add_page)
+  if (__any(top - st.mx[0] > 8.0f)) {
+    const float next = fmaxf(st.mx[0], top);
+    const float f = __builtin_amdgcn_exp2f(st.mx[0] - next);
+    const float keep = st.mx[0] == -INFINITY ? 0.0f : f;
+    st.raw[0] = top > st.mx[0] ? raw : st.raw[0];
+    st.mx[0] = next;
+    st.sum[0] *= keep;
+#pragma unroll
+    for (int ct = 0; ct < D / 16; ++ct) st.o[0][ct] *= keep;
+  }
+  float ref = st.mx[0] == -INFINITY ? 0.0f : st.mx[0];
+  if (__any(fabsf(ref) >= 0x1p20f)) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        asm volatile("" : "+v"(p[u][i]));
+        if (st.mx[0] != -INFINITY) p[u][i] -= st.raw[0];
+      }
+    ref = 0.0f;
+  }
+  // terms of the weights, two to a word
+  uint32_t w[U][PTERMS][2];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float e[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t two = x.vs[2 * u + (i >> 1)];
+      e[i] = __builtin_amdgcn_exp2f(fmaf(p[u][i], c, -ref));
+      st.sum[0] += e[i];
+      e[i] = mul_zero(e[i], __uint_as_float(i & 1 ? two & 0xFFFF0000u : two << 16));
+    }
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+      typedef float float2v __attribute__((ext_vector_type(2)));
+      float a = e[2 * d], b = e[2 * d + 1];
+#pragma unroll
+      for (int n = 0; n < PTERMS; ++n) {
+        w[u][n][d] = __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{a, b}, bf16x2));
+        a -= __uint_as_float(w[u][n][d] << 16);
+        b -= __uint_as_float(w[u][n][d] & 0xFFFF0000u);
+      }
+    }
+  }
+  // the operand of tokens 32 h onwards: tile t's first term from lanes W t' on to
+  // lanes 0 .., its second to lanes W .., its third to lanes 2 W ..
+  auto tile_words = [&](auto tc, int d) __attribute__((always_inline)) {
+    constexpr int t = decltype(tc)::value;
+    if constexpr (PACK == 4) {
+      uint32_t v = lane_move<shl(4 * t)>(0u, w[0][0][d]);
+      v = lane_move<shl(4 * t - 4), 0x2>(v, w[0][1][d]);
+      if constexpr (PTERMS == 3) v = lane_move<shl(4 * t - 8), 0x4>(v, w[0][2][d]);
+      return v;
+    } else if constexpr (t % 2 == 0) {
+      return lane_move<shl(-8), 0xC>(w[t / 2][0][d], w[t / 2][1][d]);
+    } else {
+      return lane_move<shl(8), 0x3>(w[t / 2][1][d], w[t / 2][0][d]);
+    }
+  };
+  static_for<0, 2>([&](auto hc) __attribute__((always_inline)) {
+    constexpr int h = decltype(hc)::value;
+    const std::integral_constant<int, 2 * h> t0{};
+    const std::integral_constant<int, 2 * h + 1> t1{};
+    const bf16x8 b = __builtin_bit_cast(
+        bf16x8, u32x4{tile_words(t0, 0), tile_words(t0, 1), tile_words(t1, 0), tile_words(t1, 1)});
+    bf16x8 third = b;
+    if constexpr (PACK == 2 && PTERMS == 3)
+      // (nothing in the second term's columns)
+      third = __builtin_bit_cast(
+          bf16x8, u32x4{lane_move<kSame, 0x3>(0u, w[h][2][0]), lane_move<kSame, 0x3>(0u, w[h][2][1]),
+                        lane_move<shl(8)>(0u, w[h][2][0]), lane_move<shl(8)>(0u, w[h][2][1])});
+#pragma unroll
+    for (int c0 = 0; c0 < D / 16; c0 += 4) {
+      __builtin_amdgcn_sched_barrier(0);
+      bf16x8 a[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = dequant(x.v[h][c0 + i], 1.0f);
+      if constexpr (PACK == 2 && PTERMS == 3) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          st.o[0][c0 + i] = mfma(a[i], third, st.o[0][c0 + i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) st.o[0][c0 + i] = mfma(a[i], b, st.o[0][c0 + i]);
+    }
+  });
+}
+
+// Sums of the terms' columns to the query rows' columns, and the softmax sum of
+// all lanes of a query row to each of them.
+template <int D, int SPL, int PACK>
+__device__ __forceinline__ void unpack_rows(Running<D, 1> &st) {
+  if constexpr (PACK > 1) {
+    constexpr int W = 16 / PACK;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = st.o[0][c][i];
+        float y = x + lane_move<shl(W)>(0.0f, x);
+        if constexpr (PACK == 4 && SPL == 3) y += lane_move<shl(2 * W)>(0.0f, x);
+        st.o[0][c][i] = y;
+      }
+    if constexpr (PACK == 4) st.sum[0] += lane_move<ror(4)>(st.sum[0], st.sum[0]);
+    st.sum[0] += lane_move<ror(8)>(st.sum[0], st.sum[0]);
+  }
+  st.sum[0] = across_groups_sum(st.sum[0]);
+}
+
 // A workgroup of WQ x WK waves: WQ groups of 16 NT query rows, whose pages WK
 // waves share out.
-template <int D, int SPL, int NT, int WQ, int WK, int OCC>
+template <int D, int SPL, int NT, int WQ, int WK, int PACK, int OCC>
 __global__ __launch_bounds__(64 * WQ * WK, OCC) void attend_kernel(CacheView cv, RowsView rv,
                                                                   AttendView av) {
-  constexpr int TQ = 16 * NT * WQ, NCT = D / 16;
+  constexpr int W = 16 / PACK, TQ = W * NT * WQ, NCT = D / 16;
   constexpr bool BF16 = SPL == 1;
   constexpr int PITCH = D + 4;
   __shared__ float sh_ml[WK > 1 ? 2 * WK * TQ : 1];
   __shared__ __align__(16) float sh_o[WK > 1 ? WK * TQ * PITCH : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, m = lane & 15, wq = wave / WK, wk = wave % WK;
-  const int h = blockIdx.y;
-  const int item = blockIdx.x / av.splits;
-  const int split = blockIdx.x - item * av.splits;
-  int tile;
-  const int r = tile_row(rv, av.G, TQ, item, tile);
+  // (heads fastest: a page's heads lie side by side)
+  constexpr bool NARROW = TQ <= 16;
+  const int h = blockIdx.x % cv.Hkv;
+  const int item = blockIdx.x / cv.Hkv / av.splits;
+  const int split = blockIdx.x / cv.Hkv - item * av.splits;
+  int tile = 0;
+  const int r = NARROW ? item : tile_row(rv, av.G, TQ, item, tile);
   const Span sp = row_span(cv, rv, r);
   if (sp.bad && h == 0 && threadIdx.x == 0) set_bad(av.status);
   const int rows = sp.n * av.G, rho0 = tile * TQ;
-  if (tile < 0 || rho0 >= rows) return;
+  if (rho0 >= rows || is_narrow(sp, av) != NARROW) return;
   // pages that any row of the tile sees
   const int pages = tile_pages(sp, av.G, min(rho0 + TQ, rows));
   const int used = (pages + av.split_pages - 1) / av.split_pages;
@@ -351,9 +597,9 @@ __global__ __launch_bounds__(64 * WQ * WK, OCC) void attend_kernel(CacheView cv,
   const int p0 = split * av.split_pages, p1 = min(pages, p0 + av.split_pages);
 
   Query qr[NT];
-  const int rhow = rho0 + wq * 16 * NT;
+  const int rhow = rho0 + wq * W * NT;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) qr[n] = query_of(sp, av, h, rhow + 16 * n + m);
+  for (int n = 0; n < NT; ++n) qr[n] = query_of(sp, av, h, rhow + W * n + m % W);
   // positions that every valid row of the wave sees
   const int all = min(sp.len - 1, sp.ctx + rhow / av.G);
 
@@ -361,6 +607,7 @@ __global__ __launch_bounds__(64 * WQ * WK, OCC) void attend_kernel(CacheView cv,
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     st.mx[n] = -INFINITY;
+    st.raw[n] = 0.0f;
     st.sum[n] = 0.0f;
 #pragma unroll
     for (int c = 0; c < NCT; ++c) st.o[n][c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -377,22 +624,45 @@ __global__ __launch_bounds__(64 * WQ * WK, OCC) void attend_kernel(CacheView cv,
     const uint8_t *page =
         cv.pages + ((int64_t)(ok ? page_id : 0) * cv.Hkv + h) * cache_page_bytes(D);
     load_keys<D>(page, g, m, x);
-    load_values<D>(page, lane, x);
+    load_values<D, PACK == 1>(page, lane, x);
+    if constexpr (PACK > 1) load_packed_scales<D, PACK>(page, g, m, x);
   };
-  bf16x8 q[NT][SPL][D / 32];
+  // one tile of 16 rows: its queries' operands in LDS, which leaves registers
+  // for a wave more on each SIMD; read once a page
+  constexpr bool QLDS = TQ <= 16;
+  __shared__ bf16x8 sh_q[QLDS ? SPL * (D / 32) * 64 : 1];
+  bf16x8 qreg[QLDS ? 1 : NT][SPL][D / 32];
+  auto q = [&](int n, int p, int e) __attribute__((always_inline)) {
+    if constexpr (QLDS) return sh_q[(p * (D / 32) + e) * 64 + lane];
+    else return qreg[n][p][e];
+  };
   auto work = [&](int at, int page_id, const PageRegs<D> &x) __attribute__((always_inline)) {
     const bool ok = page_id >= 0 && page_id < cv.n_pages;
     if (!ok && lane == 0) set_bad(av.status);
     int limit[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) limit[n] = ok ? qr[n].limit - at * kPage : -1;
-    add_page<D, SPL, NT>(x, q, g, !ok || at * kPage + kPage - 1 > all, limit, av.c, st);
+    const bool edge = !ok || at * kPage + kPage - 1 > all;
+    if constexpr (PACK == 1) add_page<D, SPL, NT>(x, q, g, edge, limit, av.c, st);
+    else add_page_packed<D, SPL, PACK>(x, q, g, m, edge, limit[0], av.c, st);
   };
   if (p < p1) {
     fetch(id, xa);
     if (p + WK < p1) id_next = ld_const(table, p + WK);
   }
-  load_queries<D, SPL, NT>(av, sp, qr, g, q);
+  if constexpr (QLDS) {
+    if (wave == 0) {
+      bf16x8 x[1][SPL][D / 32];
+      load_queries<D, SPL, 1>(av, sp, qr, g, x, m < W);
+#pragma unroll
+      for (int i = 0; i < SPL; ++i)
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) sh_q[(i * (D / 32) + e) * 64 + lane] = x[0][i][e];
+    }
+    __syncthreads();
+  } else {
+    load_queries<D, SPL, NT>(av, sp, qr, g, qreg);
+  }
   while (p < p1) {
     work(p, id, xa);
     p += WK;
@@ -403,28 +673,32 @@ __global__ __launch_bounds__(64 * WQ * WK, OCC) void attend_kernel(CacheView cv,
   float (&mx)[NT] = st.mx;
   float (&sum)[NT] = st.sum;
   floatx4 (&o)[NT][NCT] = st.o;
+  if constexpr (NT == 1) {
+    unpack_rows<D, SPL, PACK>(st);
+  } else {
 #pragma unroll
-  for (int n = 0; n < NT; ++n) sum[n] = across_groups_sum(sum[n]);
+    for (int n = 0; n < NT; ++n) sum[n] = across_groups_sum(sum[n]);
+  }
 
   if constexpr (WK > 1) {
     // join the waves of a query group: scale each to the common maximum
 #pragma unroll
     for (int n = 0; n < NT; ++n)
-      if (g == 0) {
-        sh_ml[wk * TQ + wq * 16 * NT + 16 * n + m] = mx[n];
-        sh_ml[(WK + wk) * TQ + wq * 16 * NT + 16 * n + m] = sum[n];
+      if (g == 0 && m < W) {
+        sh_ml[wk * TQ + (wq * NT + n) * W + m] = mx[n];
+        sh_ml[(WK + wk) * TQ + (wq * NT + n) * W + m] = sum[n];
       }
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const int row = wq * 16 * NT + 16 * n + m;
+      const int row = (wq * NT + n) * W + m % W;
       float top = -INFINITY;
 #pragma unroll
       for (int i = 0; i < WK; ++i) top = fmaxf(top, sh_ml[i * TQ + row]);
-      const float f = mx[n] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mx[n] - top) * av.c);
+      const float f = mx[n] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mx[n] - top);
 #pragma unroll
       for (int c = 0; c < NCT; ++c)
-        *reinterpret_cast<floatx4 *>(sh_o + (wk * TQ + row) * PITCH + g * (D / 4) + 4 * c) =
+        if (m < W) *reinterpret_cast<floatx4 *>(sh_o + (wk * TQ + row) * PITCH + g * (D / 4) + 4 * c) =
             o[n][c] * f;
     }
     __syncthreads();
@@ -439,7 +713,7 @@ __global__ __launch_bounds__(64 * WQ * WK, OCC) void attend_kernel(CacheView cv,
 #pragma unroll
       for (int k = 0; k < WK; ++k) {
         const float mk = sh_ml[k * TQ + row];
-        l += sh_ml[(WK + k) * TQ + row] * (mk == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mk - top) * av.c));
+        l += sh_ml[(WK + k) * TQ + row] * (mk == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mk - top));
         acc += *reinterpret_cast<const floatx4 *>(sh_o + (k * TQ + row) * PITCH + c4);
       }
       if (used > 1) {
@@ -490,14 +764,14 @@ __global__ __launch_bounds__(64 * WQ * WK, OCC) void attend_kernel(CacheView cv,
 // Joins the splits of a tile: a thread for four channels of a query row.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void join_kernel(CacheView cv, RowsView rv, AttendView av,
-                                                   int TQ) {
+                                                   int TQ, bool narrow) {
   const int h = blockIdx.y;
   const int64_t item = blockIdx.x;
-  int tile;
-  const int r = tile_row(rv, av.G, TQ, item, tile);
+  int tile = 0;
+  const int r = narrow ? (int)item : tile_row(rv, av.G, TQ, item, tile);
   const Span sp = row_span(cv, rv, r);
   const int rows = sp.n * av.G, rho0 = tile * TQ;
-  if (tile < 0 || rho0 >= rows) return;
+  if (rho0 >= rows || is_narrow(sp, av) != narrow) return;
   const int pages = tile_pages(sp, av.G, min(rho0 + TQ, rows));
   const int used = (pages + av.split_pages - 1) / av.split_pages;
   if (used <= 1) return;
@@ -511,7 +785,7 @@ __global__ __launch_bounds__(256) void join_kernel(CacheView cv, RowsView rv, At
     floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int k = 0; k < used; ++k) {
       const float2 ml = av.part_ml[part + (int64_t)k * TQ];
-      const float f = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((ml.x - top) * av.c);
+      const float f = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - top);
       l += ml.y * f;
       acc += *reinterpret_cast<const floatx4 *>(av.part_o + (part + (int64_t)k * TQ) * D + c4) * f;
     }
@@ -553,14 +827,15 @@ __global__ __launch_bounds__(256) void weight_kernel(CacheView cv, RowsView rv, 
                           ? av.stats[(int64_t)(sp.t0 + qr[0].tok) * av.Hq + qr[0].head]
                           : make_float2(0.0f, 0.0f);
     floatx4 s[1][4];
-    scores<D, SPL, 1>(x, q, s);
+    scores<D, SPL, 1>(
+        x, [&](int n, int p, int e) __attribute__((always_inline)) { return q[n][p][e]; }, s);
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (p * kPage + 16 * t + 4 * g + i <= qr[0].limit)
           total[4 * t + i] +=
-              __builtin_amdgcn_exp2f((s[0][t][i] - st.x) * av.c) * st.y;
+              __builtin_amdgcn_exp2f(fminf(fmaf(s[0][t][i], av.c, -st.x), 8.0f)) * st.y;
   }
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
@@ -581,46 +856,82 @@ __global__ __launch_bounds__(256) void weight_kernel(CacheView cv, RowsView rv, 
 
 }  // namespace
 
-AttendPlan cache_attend_plan(const CacheView &cv, const RowsView &rv, int D, int32_t Hq) {
-  AttendPlan p;
-  const int32_t G = Hq / cv.Hkv;
-  const bool wide = (int64_t)rv.max_tokens * G > 16;
-  p.tile = !wide ? 16 : D == 256 ? 64 : 128;
-  p.tiles = tile_items(rv.R, rv.N, G, p.tile, rv.start == nullptr);
-  const int64_t pages = ((int64_t)rv.max_context + kPage - 1) / kPage;
-  const int64_t groups = p.tiles * cv.Hkv;
-  const int64_t want = wide ? 512 : 1024;
-  int64_t splits = groups > 0 ? (want + groups - 1) / groups : 1;
-  splits = splits < 1 ? 1 : splits;
-  const int64_t most = (pages + 3) / 4 < 1 ? 1 : (pages + 3) / 4;
-  if (splits > most) splits = most;
-  int64_t per = (pages + splits - 1) / splits;
-  per = per < 4 ? 4 : (per + 3) / 4 * 4;
-  splits = (pages + per - 1) / per;
-  p.splits = (int32_t)(splits < 1 ? 1 : splits);
+namespace {
+
+// Tiles of `tile` query rows whose pages are split over workgroups until there
+// are `want` of them.
+TilePlan tile_plan(int32_t tile, int64_t tiles, int64_t pages, int Hkv, int D, int64_t want) {
+  TilePlan p = {};
+  if (tiles == 0) return p;
+  p.tile = tile;
+  p.tiles = tiles;
+  const int64_t groups = tiles * Hkv;
+  const int64_t most = std::max<int64_t>((pages + 3) / 4, 1);
+  int64_t splits = std::min(std::max<int64_t>((want + groups - 1) / groups, 1), most);
+  const int64_t per = std::max<int64_t>(((pages + splits - 1) / splits + 3) / 4 * 4, 4);
+  splits = std::max<int64_t>((pages + per - 1) / per, 1);
+  p.splits = (int32_t)splits;
   p.split_pages = (int32_t)per;
-  const size_t parts = p.splits > 1 ? (size_t)(groups * p.splits) * p.tile : 0;
+  const size_t parts = splits > 1 ? (size_t)(groups * splits) * tile : 0;
   p.ml_bytes = parts * sizeof(float2);
   p.o_bytes = parts * D * sizeof(float);
+  return p;
+}
+
+}  // namespace
+
+AttendPlan cache_attend_plan(const CacheView &cv, const RowsView &rv, int D, int32_t Hq) {
+  AttendPlan p = {};
+  const int32_t G = Hq / cv.Hkv;
+  const int64_t pages = ((int64_t)rv.max_context + kPage - 1) / kPage;
+  // rows of more than a tile of 16 query rows, and rows that may be of fewer: of
+  // one token where there are both
+  const bool wide = (int64_t)rv.max_tokens * G > 16;
+  const bool narrow = !wide || (G <= 16 && rv.start && rv.N < (int64_t)rv.R * rv.max_tokens);
+  const int64_t rows = wide ? G : (int64_t)rv.max_tokens * G;
+  p.pack = rows <= 4 ? 4 : rows <= 8 ? 2 : 1;
+  p.narrow_rows = narrow ? 16 / p.pack : 0;
+  if (narrow) p.narrow = tile_plan(16 / p.pack, rv.R, pages, cv.Hkv, D, 1024);
+  if (wide) {
+    const int tile = D == 256 ? 64 : 128;
+    p.wide = tile_plan(tile, tile_items(rv.R, rv.N, G, tile, rv.start == nullptr), pages, cv.Hkv, D,
+                       512);
+  }
   p.stat_bytes = (size_t)rv.N * Hq * sizeof(float2);
   return p;
 }
 
 namespace {
 
+template <int D, int SPL, int PACK>
+void narrow_launch(const CacheView &cv, const RowsView &rv, const AttendView &av, const dim3 &grid,
+                   hipStream_t st) {
+  constexpr int OCC = D * SPL > 384 ? 1 : D * SPL > 128 ? 2 : 4;
+  hipLaunchKernelGGL((attend_kernel<D, SPL, 1, 1, 4, PACK, OCC>), grid, dim3(256), 0, st, cv, rv,
+                     av);
+}
+
 template <int D, int SPL>
-void attend_launch(const CacheView &cv, const RowsView &rv, const AttendView &av,
-                   const AttendPlan &plan, hipStream_t st) {
-  const dim3 grid((unsigned)(plan.tiles * plan.splits), (unsigned)cv.Hkv);
-  constexpr int OCC = D * SPL > 384 ? 1 : D * SPL > 128 ? 2 : 3;
-  if (plan.tile == 16)
-    hipLaunchKernelGGL((attend_kernel<D, SPL, 1, 1, 4, OCC>), grid, dim3(256), 0, st, cv, rv, av);
-  else
-    hipLaunchKernelGGL((attend_kernel<D, SPL, (D == 256 ? 1 : 2), 4, 1, 1>), grid, dim3(256), 0,
-                       st, cv, rv, av);
-  if (plan.splits > 1)
-    hipLaunchKernelGGL((join_kernel<D, SPL == 1>), dim3((unsigned)plan.tiles, (unsigned)cv.Hkv),
-                       dim3(256), 0, st, cv, rv, av, plan.tile);
+void attend_launch(const CacheView &cv, const RowsView &rv, AttendView av, const AttendPlan &plan,
+                   hipStream_t st) {
+  for (const bool narrow : {true, false}) {
+    const TilePlan &t = narrow ? plan.narrow : plan.wide;
+    if (t.tiles == 0) continue;
+    av.splits = t.splits;
+    av.split_pages = t.split_pages;
+    const dim3 grid((unsigned)(t.tiles * t.splits * cv.Hkv));
+    if (!narrow)
+      hipLaunchKernelGGL((attend_kernel<D, SPL, (D == 256 ? 1 : 2), 4, 1, 1, 1>), grid, dim3(256),
+                         0, st, cv, rv, av);
+    else if (plan.pack == 4) narrow_launch<D, SPL, 4>(cv, rv, av, grid, st);
+    else if (plan.pack == 2) narrow_launch<D, SPL, 2>(cv, rv, av, grid, st);
+    else narrow_launch<D, SPL, 1>(cv, rv, av, grid, st);
+    if (t.splits > 1)
+      hipLaunchKernelGGL((join_kernel<D, SPL == 1>), dim3((unsigned)t.tiles, (unsigned)cv.Hkv),
+                         dim3(256), 0, st, cv, rv, av, t.tile, narrow);
+    av.part_ml += t.ml_bytes / sizeof(float2);
+    av.part_o += t.o_bytes / sizeof(float);
+  }
   if (av.weight_out) {
     const unsigned pages = (unsigned)((rv.max_context + kPage - 1) / kPage);
     hipLaunchKernelGGL((weight_kernel<D, SPL>),

@@ -100,8 +100,11 @@ mcd::RowsView view(const mcd_cache_rows *r) {
 
 bool heads_ok(int32_t Hq, int32_t Hkv) { return Hq >= 1 && Hq % Hkv == 0; }
 
+// Workspace: status, {max, sum} of partial results, their sums, row statistics.
+size_t ml_bytes(const mcd::AttendPlan &p) { return round_up(p.narrow.ml_bytes + p.wide.ml_bytes); }
+size_t o_bytes(const mcd::AttendPlan &p) { return round_up(p.narrow.o_bytes + p.wide.o_bytes); }
 size_t attend_bytes(const mcd::AttendPlan &p) {
-  return mcd::kStatusBytes + round_up(p.ml_bytes) + round_up(p.o_bytes) + round_up(p.stat_bytes);
+  return mcd::kStatusBytes + ml_bytes(p) + o_bytes(p) + round_up(p.stat_bytes);
 }
 
 #define CHECK(x)                        \
@@ -175,7 +178,8 @@ mcd_status mcd_cache_attend(const mcd_cache *c, const mcd_cache_rows *r,
   const mcd::CacheView cv = view(c);
   const mcd::RowsView rv = view(r);
   const mcd::AttendPlan p = mcd::cache_attend_plan(cv, rv, c->D, a->Hq);
-  if (p.tiles * p.splits > kMost) return bad("too many query rows");
+  if ((p.narrow.tiles * p.narrow.splits + p.wide.tiles * p.wide.splits) * c->Hkv > kMost)
+    return bad("too many query rows");
   CHECK(check_workspace(a->workspace, a->workspace_bytes, attend_bytes(p)));
   char *w = static_cast<char *>(a->workspace);
   mcd::AttendView av;
@@ -191,12 +195,12 @@ mcd_status mcd_cache_attend(const mcd_cache *c, const mcd_cache_rows *r,
   av.status = reinterpret_cast<uint32_t *>(w);
   w += mcd::kStatusBytes;
   av.part_ml = reinterpret_cast<float2 *>(w);
-  w += round_up(p.ml_bytes);
+  w += ml_bytes(p);
   av.part_o = reinterpret_cast<float *>(w);
-  w += round_up(p.o_bytes);
+  w += o_bytes(p);
   av.stats = a->weight_out ? reinterpret_cast<float2 *>(w) : nullptr;
-  av.splits = p.splits;
-  av.split_pages = p.split_pages;
+  av.narrow = p.narrow_rows;
+  av.splits = av.split_pages = 0;              // of each part's launch
   return launched(mcd::launch_cache_attend(cv, rv, av, p, c->D, a->dtype == MCD_BF16, stream),
                   "cache attention launch");
 }

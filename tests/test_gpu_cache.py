@@ -211,6 +211,15 @@ ATTENDS = [
     ("long_row_chunk", 2, 1, 64, BF16, [4000], [20]),
     ("long_beside_short", 4, 1, 64, BF16, [6000, 3, 0, 700], [1, 1, 1, 1]),
 ]
+# many rows: more pages than workgroups, rows of every length, empty rows among them
+_MANY = [(37 * i * i) % 1000 if i % 11 else -1 for i in range(70)]
+ATTENDS += [
+    ("many_rows", 10, 5, 64, BF16, _MANY, [1] * 70),
+    ("many_rows_fp32", 5, 5, 128, F32, _MANY, [1] * 70),
+    ("many_rows_of_wide_heads", 8, 4, 256, BF16, _MANY, [1] * 70),
+    ("many_drafts", 16, 4, 128, BF16, _MANY, [i % 4 for i in range(70)]),
+    ("many_rows_beside_prompts", 8, 4, 64, F32, _MANY[:40] + [0, 64], [1] * 40 + [70, 9]),
+]
 
 
 @pytest.mark.parametrize("weights", [False, True], ids=["plain", "weights"])
