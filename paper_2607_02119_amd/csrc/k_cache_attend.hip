@@ -153,12 +153,24 @@ __device__ __forceinline__ float key_exp(uint32_t w, int t) {
   return __uint_as_float(t == 3 ? (w >> 24) << 23 : ((w >> (8 * t)) & 0xFFu) << 23);
 }
 
+// A page's operands from its registers.
+template <int D>
+__device__ __forceinline__ auto keys_of(const PageRegs<D> &x) {
+  return [&x](int t, int e) __attribute__((always_inline)) {
+    return dequant(x.k[t][e], key_exp(x.ks[e / 4], t));
+  };
+}
+template <int D>
+__device__ __forceinline__ auto values_of(const PageRegs<D> &x) {
+  return [&x](int h, int ct) __attribute__((always_inline)) { return dequant(x.v[h][ct], 1.0f); };
+}
+
 // Scores of the page's tokens 16 t + 4 g + i (i: component) against query
-// column m of each of NT tiles.  q(n, p, e): term p of the queries' operand for
-// channels' step e.  The four tiles of tokens are four independent chains of
-// matrix instructions.
-template <int D, int SPL, int NT, class Q>
-__device__ __forceinline__ void scores(const PageRegs<D> &x, Q &&q, floatx4 (&s)[NT][4]) {
+// column m of each of NT tiles.  k(t, e): the keys' operand of tile t for
+// channels' step e; q(n, p, e): term p of the queries'.  The four tiles of tokens
+// are four independent chains of matrix instructions.
+template <int D, int SPL, int NT, class K, class Q>
+__device__ __forceinline__ void scores(K &&k, Q &&q, floatx4 (&s)[NT][4]) {
 #pragma unroll
   for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -173,7 +185,7 @@ __device__ __forceinline__ void scores(const PageRegs<D> &x, Q &&q, floatx4 (&s)
       for (int p = 0; p < SPL; ++p) b[n][p] = q(n, p, e);
     bf16x8 a[4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) a[t] = dequant(x.k[t][e], key_exp(x.ks[e / 4], t));
+    for (int t = 0; t < 4; ++t) a[t] = k(t, e);
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -299,14 +311,15 @@ struct Running {
 // One page into the running state.  edge (uniform): some of its positions may be
 // hidden from some rows (limit: each row's last visible position less the page's
 // first).
-template <int D, int SPL, int NT, class Q>
-__device__ __forceinline__ void add_page(const PageRegs<D> &x, Q &&q, int g, bool edge,
-                                         const int (&limit)[NT], float c, Running<D, NT> &st) {
+template <int D, int SPL, int NT, class K, class V, class Q>
+__device__ __forceinline__ void add_page(K &&k, V &&v, const uint32_t (&vs)[8], Q &&q, int g,
+                                         bool edge, const int (&limit)[NT], float c,
+                                         Running<D, NT> &st) {
   // terms of a softmax weight: 16 bits, so that a bf16 output is off by its own
   // rounding alone; 24 for fp32
   constexpr int PTERMS = SPL == 1 ? 2 : 3;
   floatx4 s[NT][4];
-  scores<D, SPL, NT>(x, q, s);
+  scores<D, SPL, NT>(k, q, s);
   if (edge) {
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -365,7 +378,7 @@ __device__ __forceinline__ void add_page(const PageRegs<D> &x, Q &&q, int g, boo
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int t = 2 * h + (i >> 2);
-        const uint32_t two = x.vs[4 * h + (i >> 1)];
+        const uint32_t two = vs[4 * h + (i >> 1)];
         e[i] = __builtin_amdgcn_exp2f(fmaf(s[n][t][i & 3], c, -ref[n]));
         st.sum[n] += e[i];
         // (0 times anything is 0: a hidden position may hold a scale that is not finite)
@@ -379,7 +392,7 @@ __device__ __forceinline__ void add_page(const PageRegs<D> &x, Q &&q, int g, boo
       __builtin_amdgcn_sched_barrier(0);
       bf16x8 a[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] = dequant(x.v[h][c0 + i], 1.0f);
+      for (int i = 0; i < 4; ++i) a[i] = v(h, c0 + i);
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -422,7 +435,7 @@ __device__ __forceinline__ void add_page_packed(const PageRegs<D> &x, Q &&q, int
   constexpr int PTERMS = SPL == 1 ? 2 : 3;
   constexpr int W = 16 / PACK, U = 4 / PACK;     // columns of a tile; registers of scores x 4
   floatx4 s[1][4];
-  scores<D, SPL, 1>(x, q, s);
+  scores<D, SPL, 1>(keys_of(x), q, s);
   // p[u][i]: lane 16 g + m has token 16 (PACK u + m / W) + 4 g + i, query row m % W
   float p[U][4];
 #pragma unroll
@@ -567,197 +580,303 @@ __device__ __forceinline__ void unpack_rows(Running<D, 1> &st) {
   st.sum[0] = across_groups_sum(st.sum[0]);
 }
 
-// A workgroup of WQ x WK waves: WQ groups of 16 NT query rows, whose pages WK
-// waves share out.
-template <int D, int SPL, int NT, int WQ, int WK, int PACK, int OCC>
-__global__ __launch_bounds__(64 * WQ * WK, OCC) void attend_kernel(CacheView cv, RowsView rv,
-                                                                  AttendView av) {
-  constexpr int W = 16 / PACK, TQ = W * NT * WQ, NCT = D / 16;
+// A query row's result, or its part of it where the row's pages are split over
+// workgroups: the lanes of a column hold its channels' sums o (from channel g D / 4).
+template <int D, bool BF16>
+__device__ __forceinline__ void write_row(const AttendView &av, const Span &sp, const Query &q,
+                                          int64_t part, bool partial, int g, float ref, float sum,
+                                          const floatx4 (&o)[D / 16]) {
+  if (partial) {
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c)
+      *reinterpret_cast<floatx4 *>(av.part_o + part * D + g * (D / 4) + 4 * c) = o[c];
+    if (g == 0) av.part_ml[part] = make_float2(ref, sum);
+    return;
+  }
+  const bool none = sum == 0.0f;                 // nothing seen
+  const float inv = none ? 0.0f : 1.0f / sum;
+  const int64_t tok = sp.t0 + q.tok;
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) {
+    const float y[4] = {none ? 0.0f : o[c][0] * inv, none ? 0.0f : o[c][1] * inv,
+                        none ? 0.0f : o[c][2] * inv, none ? 0.0f : o[c][3] * inv};
+    store4<BF16>(av.out, tok * av.out_stride + q.head * D + g * (D / 4) + 4 * c, y);
+  }
+  if (g == 0) finish_row(av, tok * av.Hq + q.head, ref, sum);
+}
+
+// Narrow rows: a workgroup of four waves for each (row, K/V head) and split, the
+// pages dealt out to the waves, whose sums meet in LDS.  HBM bounds it; four
+// waves on a SIMD, each waiting for a page of its own or working on one, keep
+// the loads going (three or two waves that load a page ahead were slower).
+template <int D, int SPL, int PACK, int OCC>
+__global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, RowsView rv,
+                                                         AttendView av) {
+  constexpr int W = 16 / PACK, WAVES = 4;
   constexpr bool BF16 = SPL == 1;
   constexpr int PITCH = D + 4;
-  __shared__ float sh_ml[WK > 1 ? 2 * WK * TQ : 1];
-  __shared__ __align__(16) float sh_o[WK > 1 ? WK * TQ * PITCH : 1];
+  __shared__ float sh_ml[2][WAVES][W];
+  __shared__ __align__(16) float sh_o[WAVES * W * PITCH];
+  // the queries' operands: in LDS they leave registers for the fourth wave
+  __shared__ bf16x8 sh_q[SPL * (D / 32) * 64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int g = lane >> 4, m = lane & 15, wq = wave / WK, wk = wave % WK;
+  const int g = lane >> 4, m = lane & 15;
   // (heads fastest: a page's heads lie side by side)
-  constexpr bool NARROW = TQ <= 16;
+  const int h = blockIdx.x % cv.Hkv;
+  const int r = blockIdx.x / cv.Hkv / av.splits;
+  const int split = blockIdx.x / cv.Hkv - r * av.splits;
+  const Span sp = row_span(cv, rv, r);
+  if (sp.bad && h == 0 && threadIdx.x == 0) set_bad(av.status);
+  if (!is_narrow(sp, av)) return;
+  const int rows = sp.n * av.G;
+  const int pages = tile_pages(sp, av.G, rows);
+  const int used = (pages + av.split_pages - 1) / av.split_pages;
+  if (split > 0 && split >= used) return;
+  const int p1 = min(pages, (split + 1) * av.split_pages);
+
+  const Query qr = query_of(sp, av, h, m % W);
+  const int all = min(sp.len - 1, sp.ctx);       // positions that every row sees
+  Running<D, 1> st;
+  st.mx[0] = -INFINITY;
+  st.raw[0] = st.sum[0] = 0.0f;
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) st.o[0][c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  PageRegs<D> x;
+  const int32_t *table = cv.table + (int64_t)sp.slot * cv.max_pages;
+  // a page id out of range is replaced by page 0 with every position hidden
+  auto fetch = [&](int id) __attribute__((always_inline)) {
+    const bool ok = id >= 0 && id < cv.n_pages;
+    const uint8_t *page = cv.pages + ((int64_t)(ok ? id : 0) * cv.Hkv + h) * cache_page_bytes(D);
+    load_keys<D>(page, g, m, x);
+    load_values<D, PACK == 1>(page, lane, x);
+    if constexpr (PACK > 1) load_packed_scales<D, PACK>(page, g, m, x);
+  };
+  auto q = [&](int, int p, int e) __attribute__((always_inline)) {
+    return sh_q[(p * (D / 32) + e) * 64 + lane];
+  };
+  int p = split * av.split_pages + wave;
+  int id = p < p1 ? ld_const(table, p) : 0, id_next = 0;
+  if (p < p1) {
+    fetch(id);
+    if (p + WAVES < p1) id_next = ld_const(table, p + WAVES);
+  }
+  if (wave == 0) {
+    const Query one[1] = {qr};
+    bf16x8 w[1][SPL][D / 32];
+    load_queries<D, SPL, 1>(av, sp, one, g, w, m < W);
+#pragma unroll
+    for (int i = 0; i < SPL; ++i)
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) sh_q[(i * (D / 32) + e) * 64 + lane] = w[0][i][e];
+  }
+  __syncthreads();
+  while (p < p1) {
+    const bool ok = id >= 0 && id < cv.n_pages;
+    if (!ok && lane == 0) set_bad(av.status);
+    const int limit[1] = {ok ? qr.limit - p * kPage : -1};
+    const bool edge = !ok || p * kPage + kPage - 1 > all;
+    if constexpr (PACK == 1)
+      add_page<D, SPL, 1>(keys_of(x), values_of(x), x.vs, q, g, edge, limit, av.c, st);
+    else
+      add_page_packed<D, SPL, PACK>(x, q, g, m, edge, limit[0], av.c, st);
+    p += WAVES;
+    id = id_next;
+    if (p < p1) fetch(id);
+    id_next = p + WAVES < p1 ? ld_const(table, p + WAVES) : 0;
+  }
+  unpack_rows<D, SPL, PACK>(st);
+
+  // the waves' sums, to their largest reference
+  if (g == 0 && m < W) {
+    sh_ml[0][wave][m] = st.mx[0];
+    sh_ml[1][wave][m] = st.sum[0];
+  }
+  __syncthreads();
+  if (m < W) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) top = fmaxf(top, sh_ml[0][i][m]);
+    const float f = st.mx[0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(st.mx[0] - top);
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c)
+      *reinterpret_cast<floatx4 *>(sh_o + (wave * W + m) * PITCH + g * (D / 4) + 4 * c) =
+          st.o[0][c] * f;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < W * (D / 4); i += 256) {
+    const int row = i / (D / 4), c4 = i % (D / 4) * 4;
+    const Query qy = query_of(sp, av, h, row);
+    if (!qy.valid) continue;
+    float top = -INFINITY, l = 0.0f;
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) top = fmaxf(top, sh_ml[0][k][row]);
+    floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) {
+      const float mk = sh_ml[0][k][row];
+      l += sh_ml[1][k][row] * (mk == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mk - top));
+      acc += *reinterpret_cast<const floatx4 *>(sh_o + (k * W + row) * PITCH + c4);
+    }
+    if (used > 1) {
+      const int64_t part = (((int64_t)r * cv.Hkv + h) * av.splits + split) * W + row;
+      *reinterpret_cast<floatx4 *>(av.part_o + part * D + c4) = acc;
+      if (c4 == 0) av.part_ml[part] = make_float2(top, l);
+      continue;
+    }
+    const bool none = l == 0.0f;                 // nothing seen
+    const float inv = none ? 0.0f : 1.0f / l;
+    const float y[4] = {none ? 0.0f : acc[0] * inv, none ? 0.0f : acc[1] * inv,
+                        none ? 0.0f : acc[2] * inv, none ? 0.0f : acc[3] * inv};
+    const int64_t tok = sp.t0 + qy.tok;
+    store4<BF16>(av.out, tok * av.out_stride + qy.head * D + c4, y);
+    if (c4 == 0) finish_row(av, tok * av.Hq + qy.head, top, l);
+  }
+}
+
+// Wide rows: a workgroup of four waves for 64 NT query rows of a K/V head and a
+// split of their pages.  The waves convert a quarter of the next page each, once
+// for all, into operands in LDS (two pages: the one at work and the next; one,
+// with another barrier, where two do not fit twice into a compute unit).  Matrix
+// instructions and the softmax's vector work take about as long as each other;
+// two workgroups on a compute unit overlap them.
+template <int D, int SPL, int NT, int OCC>
+__global__ __launch_bounds__(256, OCC) void wide_kernel(CacheView cv, RowsView rv, AttendView av) {
+  constexpr int TQ = 64 * NT, KF = D / 32, VF = D / 16;    // key operands of a tile, value of a half
+  constexpr int BUFS = D == 256 ? 1 : 2;
+  constexpr bool BF16 = SPL == 1;
+  __shared__ bf16x8 sh_k[BUFS][4 * KF * 64], sh_v[BUFS][2 * VF * 64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, m = lane & 15;
+  // (heads fastest: tiles that read the same pages are a multiple of Hkv apart)
   const int h = blockIdx.x % cv.Hkv;
   const int item = blockIdx.x / cv.Hkv / av.splits;
   const int split = blockIdx.x / cv.Hkv - item * av.splits;
-  int tile = 0;
-  const int r = NARROW ? item : tile_row(rv, av.G, TQ, item, tile);
+  int tile;
+  const int r = tile_row(rv, av.G, TQ, item, tile);
   const Span sp = row_span(cv, rv, r);
   if (sp.bad && h == 0 && threadIdx.x == 0) set_bad(av.status);
-  const int rows = sp.n * av.G, rho0 = tile * TQ;
-  if (rho0 >= rows || is_narrow(sp, av) != NARROW) return;
-  // pages that any row of the tile sees
+  const int rows = sp.n * av.G, tiles = (rows + TQ - 1) / TQ;
+  if (tile >= tiles || is_narrow(sp, av)) return;
+  const int rho0 = (tiles - 1 - tile) * TQ;      // the longest first
   const int pages = tile_pages(sp, av.G, min(rho0 + TQ, rows));
   const int used = (pages + av.split_pages - 1) / av.split_pages;
   if (split > 0 && split >= used) return;
   const int p0 = split * av.split_pages, p1 = min(pages, p0 + av.split_pages);
 
   Query qr[NT];
-  const int rhow = rho0 + wq * W * NT;
+  const int rhow = rho0 + wave * 16 * NT;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) qr[n] = query_of(sp, av, h, rhow + W * n + m % W);
-  // positions that every valid row of the wave sees
+  for (int n = 0; n < NT; ++n) qr[n] = query_of(sp, av, h, rhow + 16 * n + m);
+  // positions that every, and that any valid row of the wave sees
   const int all = min(sp.len - 1, sp.ctx + rhow / av.G);
-
+  const int any = rhow < rows ? min(sp.len - 1, sp.ctx + (min(rhow + 16 * NT, rows) - 1) / av.G)
+                              : -1;
   Running<D, NT> st;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     st.mx[n] = -INFINITY;
-    st.raw[n] = 0.0f;
-    st.sum[n] = 0.0f;
+    st.raw[n] = st.sum[n] = 0.0f;
 #pragma unroll
-    for (int c = 0; c < NCT; ++c) st.o[n][c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int c = 0; c < D / 16; ++c) st.o[n][c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  PageRegs<D> xa;
+  // the wave's quarter of a page: tokens 16 wave onwards of the keys, VF / 2
+  // operands of the values (one of two halves' worth of 64 channels each)
+  constexpr int VQ = D / 64 >= 2 ? D / 128 : 1;  // 16-byte chunks of a lane
+  constexpr bool VALL = D >= 128;                // (64 channels: two waves' work)
+  struct Quarter {
+    uint32_t k[KF], ks[D == 256 ? 2 : 1], vs[8];
+    u32x4 v[VQ];
+  } x;
   const int32_t *table = cv.table + (int64_t)sp.slot * cv.max_pages;
-  // the wave's pages p, p + WK, ...; a page id out of range is replaced by page
-  // 0 with every position hidden
-  int p = p0 + wk;
-  int id = p < p1 ? ld_const(table, p) : 0, id_next = 0;
-  auto fetch = [&](int page_id, PageRegs<D> &x) __attribute__((always_inline)) {
-    const bool ok = page_id >= 0 && page_id < cv.n_pages;
-    const uint8_t *page =
-        cv.pages + ((int64_t)(ok ? page_id : 0) * cv.Hkv + h) * cache_page_bytes(D);
-    load_keys<D>(page, g, m, x);
-    load_values<D, PACK == 1>(page, lane, x);
-    if constexpr (PACK > 1) load_packed_scales<D, PACK>(page, g, m, x);
+  auto fetch = [&](int id) __attribute__((always_inline)) {
+    const bool ok = id >= 0 && id < cv.n_pages;
+    const uint8_t *page = cv.pages + ((int64_t)(ok ? id : 0) * cv.Hkv + h) * cache_page_bytes(D);
+    const uint32_t at = m * (D / 2) + g * (D / 8), tile_at = wave * 8 * D;
+    if constexpr (D == 64) {
+      const uint2 w = load_at<uint2>(page, at, tile_at);
+      x.k[0] = w.x;
+      x.k[1] = w.y;
+    } else {
+#pragma unroll
+      for (uint32_t i = 0; i < D / 128; ++i) {
+        const u32x4 w = load_at<u32x4>(page, at, tile_at + 16 * i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x.k[4 * i + e] = w[e];
+      }
+    }
+    if constexpr (D == 64) x.ks[0] = load_at<uint32_t>(page, m * 8 + (g >> 1) * 4, 64 * D);
+    else if constexpr (D == 128) x.ks[0] = load_at<uint32_t>(page, m * 16 + g * 4, 64 * D);
+    else {
+      const uint2 w = load_at<uint2>(page, m * 32 + g * 8, 64 * D);
+      x.ks[0] = w.x;
+      x.ks[1] = w.y;
+    }
+    if (VALL || wave < 2) {
+#pragma unroll
+      for (uint32_t i = 0; i < VQ; ++i)
+        x.v[i] = load_at<u32x4>(page, lane * 16, 32 * D + (wave * VQ + i) * 1024);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) {
+      const u32x4 w = load_at<u32x4>(page, g * 32, 66 * D + 16 * i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x.vs[4 * i + e] = w[e];
+    }
   };
-  // one tile of 16 rows: its queries' operands in LDS, which leaves registers
-  // for a wave more on each SIMD; read once a page
-  constexpr bool QLDS = TQ <= 16;
-  __shared__ bf16x8 sh_q[QLDS ? SPL * (D / 32) * 64 : 1];
-  bf16x8 qreg[QLDS ? 1 : NT][SPL][D / 32];
-  auto q = [&](int n, int p, int e) __attribute__((always_inline)) {
-    if constexpr (QLDS) return sh_q[(p * (D / 32) + e) * 64 + lane];
-    else return qreg[n][p][e];
+  auto convert = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < KF; ++e) {
+      const float scale = __uint_as_float(((x.ks[e / 4] >> (8 * wave)) & 0xFFu) << 23);
+      sh_k[b][(wave * KF + e) * 64 + lane] = dequant(x.k[e], scale);
+    }
+    if (VALL || wave < 2) {
+#pragma unroll
+      for (int i = 0; i < VQ; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          sh_v[b][((wave * VQ + i) * 4 + e) * 64 + lane] = dequant(x.v[i][e], 1.0f);
+    }
   };
-  auto work = [&](int at, int page_id, const PageRegs<D> &x) __attribute__((always_inline)) {
-    const bool ok = page_id >= 0 && page_id < cv.n_pages;
+  int id = p0 < p1 ? ld_const(table, p0) : 0;
+  if (p0 < p1) fetch(id);
+  bf16x8 qreg[NT][SPL][D / 32];
+  load_queries<D, SPL, NT>(av, sp, qr, g, qreg);
+  auto q = [&](int n, int p, int e) __attribute__((always_inline)) { return qreg[n][p][e]; };
+  int b = 0;
+  uint32_t vs[8];
+  for (int p = p0; p < p1; ++p) {
+    convert(b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) vs[i] = x.vs[i];
+    const bool ok = id >= 0 && id < cv.n_pages;
     if (!ok && lane == 0) set_bad(av.status);
-    int limit[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) limit[n] = ok ? qr[n].limit - at * kPage : -1;
-    const bool edge = !ok || at * kPage + kPage - 1 > all;
-    if constexpr (PACK == 1) add_page<D, SPL, NT>(x, q, g, edge, limit, av.c, st);
-    else add_page_packed<D, SPL, PACK>(x, q, g, m, edge, limit[0], av.c, st);
-  };
-  if (p < p1) {
-    fetch(id, xa);
-    if (p + WK < p1) id_next = ld_const(table, p + WK);
-  }
-  if constexpr (QLDS) {
-    if (wave == 0) {
-      bf16x8 x[1][SPL][D / 32];
-      load_queries<D, SPL, 1>(av, sp, qr, g, x, m < W);
-#pragma unroll
-      for (int i = 0; i < SPL; ++i)
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e) sh_q[(i * (D / 32) + e) * 64 + lane] = x[0][i][e];
-    }
+    id = p + 1 < p1 ? ld_const(table, p + 1) : 0;
+    if (p + 1 < p1) fetch(id);
     __syncthreads();
-  } else {
-    load_queries<D, SPL, NT>(av, sp, qr, g, qreg);
-  }
-  while (p < p1) {
-    work(p, id, xa);
-    p += WK;
-    id = id_next;
-    if (p < p1) fetch(id, xa);
-    id_next = p + WK < p1 ? ld_const(table, p + WK) : 0;
-  }
-  float (&mx)[NT] = st.mx;
-  float (&sum)[NT] = st.sum;
-  floatx4 (&o)[NT][NCT] = st.o;
-  if constexpr (NT == 1) {
-    unpack_rows<D, SPL, PACK>(st);
-  } else {
+    if (p * kPage <= any) {
+      int limit[NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) sum[n] = across_groups_sum(sum[n]);
-  }
-
-  if constexpr (WK > 1) {
-    // join the waves of a query group: scale each to the common maximum
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-      if (g == 0 && m < W) {
-        sh_ml[wk * TQ + (wq * NT + n) * W + m] = mx[n];
-        sh_ml[(WK + wk) * TQ + (wq * NT + n) * W + m] = sum[n];
-      }
-    __syncthreads();
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int row = (wq * NT + n) * W + m % W;
-      float top = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < WK; ++i) top = fmaxf(top, sh_ml[i * TQ + row]);
-      const float f = mx[n] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mx[n] - top);
-#pragma unroll
-      for (int c = 0; c < NCT; ++c)
-        if (m < W) *reinterpret_cast<floatx4 *>(sh_o + (wk * TQ + row) * PITCH + g * (D / 4) + 4 * c) =
-            o[n][c] * f;
+      for (int n = 0; n < NT; ++n) limit[n] = ok ? qr[n].limit - p * kPage : -1;
+      auto k = [&](int t, int e) __attribute__((always_inline)) {
+        return sh_k[b][(t * KF + e) * 64 + lane];
+      };
+      auto v = [&](int hh, int ct) __attribute__((always_inline)) {
+        return sh_v[b][(hh * VF + ct) * 64 + lane];
+      };
+      add_page<D, SPL, NT>(k, v, vs, q, g, !ok || p * kPage + kPage - 1 > all, limit, av.c, st);
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < TQ * (D / 4); i += 64 * WQ * WK) {
-      const int row = i / (D / 4), c4 = i % (D / 4) * 4;
-      const Query qy = query_of(sp, av, h, rho0 + row);
-      if (!qy.valid) continue;
-      float top = -INFINITY, l = 0.0f;
+    if constexpr (BUFS == 1) __syncthreads();
+    else b ^= 1;
+  }
 #pragma unroll
-      for (int k = 0; k < WK; ++k) top = fmaxf(top, sh_ml[k * TQ + row]);
-      floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int k = 0; k < WK; ++k) {
-        const float mk = sh_ml[k * TQ + row];
-        l += sh_ml[(WK + k) * TQ + row] * (mk == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mk - top));
-        acc += *reinterpret_cast<const floatx4 *>(sh_o + (k * TQ + row) * PITCH + c4);
-      }
-      if (used > 1) {
-        const int64_t part = ((item * cv.Hkv + h) * av.splits + split) * TQ + row;
-        *reinterpret_cast<floatx4 *>(av.part_o + part * D + c4) = acc;
-        if (c4 == 0) av.part_ml[part] = make_float2(top, l);
-        continue;
-      }
-      const bool none = l == 0.0f;                // nothing seen
-      const float inv = none ? 0.0f : 1.0f / l;
-      const float y[4] = {none ? 0.0f : acc[0] * inv, none ? 0.0f : acc[1] * inv,
-                          none ? 0.0f : acc[2] * inv, none ? 0.0f : acc[3] * inv};
-      const int64_t tok = sp.t0 + qy.tok;
-      store4<BF16>(av.out, tok * av.out_stride + qy.head * D + c4, y);
-      if (c4 == 0) {
-        finish_row(av, tok * av.Hq + qy.head, top, l);
-      }
-    }
-  } else {
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      if (!qr[n].valid) continue;
-      if (used > 1) {
-        const int64_t part =
-            ((item * cv.Hkv + h) * av.splits + split) * TQ + wq * 16 * NT + 16 * n + m;
-#pragma unroll
-        for (int c = 0; c < NCT; ++c)
-          *reinterpret_cast<floatx4 *>(av.part_o + part * D + g * (D / 4) + 4 * c) = o[n][c];
-        if (g == 0) av.part_ml[part] = make_float2(mx[n], sum[n]);
-        continue;
-      }
-      const bool none = sum[n] == 0.0f;
-      const float inv = none ? 0.0f : 1.0f / sum[n];
-      const int64_t tok = sp.t0 + qr[n].tok;
-#pragma unroll
-      for (int c = 0; c < NCT; ++c) {
-        const float y[4] = {none ? 0.0f : o[n][c][0] * inv, none ? 0.0f : o[n][c][1] * inv,
-                            none ? 0.0f : o[n][c][2] * inv, none ? 0.0f : o[n][c][3] * inv};
-        store4<BF16>(av.out, tok * av.out_stride + qr[n].head * D + g * (D / 4) + 4 * c, y);
-      }
-      if (g == 0) {
-        finish_row(av, tok * av.Hq + qr[n].head, mx[n], sum[n]);
-      }
-    }
+  for (int n = 0; n < NT; ++n) {
+    const float sum = across_groups_sum(st.sum[n]);
+    const int64_t part = (((int64_t)item * cv.Hkv + h) * av.splits + split) * TQ +
+                         (rhow + 16 * n + m - rho0);
+    if (qr[n].valid)
+      write_row<D, BF16>(av, sp, qr[n], part, used > 1, g, st.mx[n], sum, st.o[n]);
   }
 }
 
@@ -770,8 +889,9 @@ __global__ __launch_bounds__(256) void join_kernel(CacheView cv, RowsView rv, At
   int tile = 0;
   const int r = narrow ? (int)item : tile_row(rv, av.G, TQ, item, tile);
   const Span sp = row_span(cv, rv, r);
-  const int rows = sp.n * av.G, rho0 = tile * TQ;
-  if (rho0 >= rows || is_narrow(sp, av) != narrow) return;
+  const int rows = sp.n * av.G, tiles = (rows + TQ - 1) / TQ;
+  if (tile >= tiles || is_narrow(sp, av) != narrow) return;
+  const int rho0 = (tiles - 1 - tile) * TQ;
   const int pages = tile_pages(sp, av.G, min(rho0 + TQ, rows));
   const int used = (pages + av.split_pages - 1) / av.split_pages;
   if (used <= 1) return;
@@ -828,7 +948,7 @@ __global__ __launch_bounds__(256) void weight_kernel(CacheView cv, RowsView rv, 
                           : make_float2(0.0f, 0.0f);
     floatx4 s[1][4];
     scores<D, SPL, 1>(
-        x, [&](int n, int p, int e) __attribute__((always_inline)) { return q[n][p][e]; }, s);
+        keys_of(x), [&](int n, int p, int e) __attribute__((always_inline)) { return q[n][p][e]; }, s);
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -907,8 +1027,7 @@ template <int D, int SPL, int PACK>
 void narrow_launch(const CacheView &cv, const RowsView &rv, const AttendView &av, const dim3 &grid,
                    hipStream_t st) {
   constexpr int OCC = D * SPL > 384 ? 1 : D * SPL > 128 ? 2 : 4;
-  hipLaunchKernelGGL((attend_kernel<D, SPL, 1, 1, 4, PACK, OCC>), grid, dim3(256), 0, st, cv, rv,
-                     av);
+  hipLaunchKernelGGL((narrow_kernel<D, SPL, PACK, OCC>), grid, dim3(256), 0, st, cv, rv, av);
 }
 
 template <int D, int SPL>
@@ -921,8 +1040,8 @@ void attend_launch(const CacheView &cv, const RowsView &rv, AttendView av, const
     av.split_pages = t.split_pages;
     const dim3 grid((unsigned)(t.tiles * t.splits * cv.Hkv));
     if (!narrow)
-      hipLaunchKernelGGL((attend_kernel<D, SPL, (D == 256 ? 1 : 2), 4, 1, 1, 1>), grid, dim3(256),
-                         0, st, cv, rv, av);
+      hipLaunchKernelGGL((wide_kernel<D, SPL, (D == 256 ? 1 : 2), (D * SPL > 256 ? 1 : 2)>), grid,
+                         dim3(256), 0, st, cv, rv, av);
     else if (plan.pack == 4) narrow_launch<D, SPL, 4>(cv, rv, av, grid, st);
     else if (plan.pack == 2) narrow_launch<D, SPL, 2>(cv, rv, av, grid, st);
     else narrow_launch<D, SPL, 1>(cv, rv, av, grid, st);
