@@ -32,6 +32,10 @@ struct AttendView {
   float *lse;                  // the caller's, or null
   float2 *stats;               // workspace [N][Hq] {reference, 1 / sum}, or null: no weights
   float *weight_out;
+  // workspace [R][Hkv][score_pages][64 16 / pack], or null: narrow rows' q . k as
+  // add_page_packed's lanes hold them, for the received weight
+  floatx4 *scores;
+  int32_t score_pages;
   // Partial results of rows whose pages are split over workgroups: for each
   // query row of a tile and split {max, sum} and D sums.
   float2 *part_ml;
@@ -57,7 +61,8 @@ struct TilePlan {
 struct AttendPlan {
   int32_t pack, narrow_rows;   // tiles of tokens side by side; AttendView::narrow
   TilePlan narrow, wide;
-  size_t stat_bytes;
+  size_t stat_bytes, score_bytes;
+  int32_t score_pages;
 };
 AttendPlan cache_attend_plan(const CacheView &cv, const RowsView &rv, int D, int32_t Hq);
 hipError_t launch_cache_attend(const CacheView &cv, const RowsView &rv, const AttendView &av,

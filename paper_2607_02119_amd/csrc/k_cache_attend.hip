@@ -431,7 +431,8 @@ __device__ __forceinline__ void load_packed_scales(const uint8_t *page, uint32_t
 
 template <int D, int SPL, int PACK, class Q>
 __device__ __forceinline__ void add_page_packed(const PageRegs<D> &x, Q &&q, int g, int m, bool edge,
-                                                int limit, float c, Running<D, 1> &st) {
+                                                int limit, float c, floatx4 *keep_scores,
+                                                Running<D, 1> &st) {
   constexpr int PTERMS = SPL == 1 ? 2 : 3;
   constexpr int W = 16 / PACK, U = 4 / PACK;     // columns of a tile; registers of scores x 4
   floatx4 s[1][4];
@@ -451,6 +452,11 @@ __device__ __forceinline__ void add_page_packed(const PageRegs<D> &x, Q &&q, int
         p[u][i] = lane_move<shl(-8), 0xC>(s[0][2 * u][i], s[0][2 * u + 1][i]);
       }
     }
+  if (keep_scores) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      keep_scores[u * 64 + 16 * g + m] = floatx4{p[u][0], p[u][1], p[u][2], p[u][3]};
+  }
   if (edge) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -679,7 +685,11 @@ __global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, RowsView
     if constexpr (PACK == 1)
       add_page<D, SPL, 1>(keys_of(x), values_of(x), x.vs, q, g, edge, limit, av.c, st);
     else
-      add_page_packed<D, SPL, PACK>(x, q, g, m, edge, limit[0], av.c, st);
+      add_page_packed<D, SPL, PACK>(
+          x, q, g, m, edge, limit[0], av.c,
+          av.scores ? av.scores + (((int64_t)r * cv.Hkv + h) * av.score_pages + p) * (256 / PACK)
+                    : nullptr,
+          st);
     p += WAVES;
     id = id_next;
     if (p < p1) fetch(id);
@@ -921,16 +931,84 @@ __global__ __launch_bounds__(256) void join_kernel(CacheView cv, RowsView rv, At
   }
 }
 
-// Weight that every position received: the scores again, against the finished
-// sums.  A wave for each page; its query tiles in order, so the sum's order is
-// fixed.
+// ---- received weight ------------------------------------------------------------
+
+// The same lane moves within four lanes.
+template <int PERM>
+__device__ __forceinline__ float quad_move(float x) {
+  return __uint_as_float(
+      (uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), PERM, 0xF, 0xF, false));
+}
+
+// Narrow rows, from the scores that narrow_kernel left: 1 KiB of a page of 64
+// tokens and 4 query rows (a quarter of its key codes, or a half for 8 rows).  A
+// wave for four pages, their loads in flight together; bound by HBM.
+template <int PACK>
+__global__ __launch_bounds__(256) void weight_scores_kernel(CacheView cv, RowsView rv,
+                                                           AttendView av) {
+  constexpr int W = 16 / PACK, U = 4 / PACK, PAGES = 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int g = lane >> 4, m = lane & 15, h = blockIdx.y, r = blockIdx.z;
+  const int first = (blockIdx.x * 4 + wave) * PAGES;
+  const Span sp = row_span(cv, rv, r);
+  if (!is_narrow(sp, av) || first * kPage >= sp.len) return;
+  const Query qr = query_of(sp, av, h, m % W);
+  const int last = min(first + PAGES - 1, (sp.len - 1) / kPage);
+  const floatx4 *from =
+      av.scores + (((int64_t)r * cv.Hkv + h) * av.score_pages) * (256 / PACK) + lane;
+  const int64_t row = ((int64_t)sp.slot * cv.Hkv + h) * cv.max_pages * kPage;
+  floatx4 s[PAGES][U], w[PAGES][U];
+#pragma unroll
+  for (int k = 0; k < PAGES; ++k)
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int p = min(first + k, last);
+      s[k][u] = from[(int64_t)p * (256 / PACK) + u * 64];
+      const int64_t at = row + p * kPage + 16 * (PACK * u + m / W) + 4 * g;
+      w[k][u] = cv.weight ? *reinterpret_cast<const floatx4 *>(cv.weight + at)
+                          : floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+  const float2 st = qr.valid ? av.stats[(int64_t)(sp.t0 + qr.tok) * av.Hq + qr.head]
+                             : make_float2(0.0f, 0.0f);
+#pragma unroll
+  for (int k = 0; k < PAGES; ++k) {
+    const int p = first + k;
+    if (p > last) break;
+    const int id = ld_const(cv.table + (int64_t)sp.slot * cv.max_pages, p);
+    if (id < 0 || id >= cv.n_pages) continue;  // reported by narrow_kernel
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int pos = p * kPage + 16 * (PACK * u + m / W) + 4 * g;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float e = __builtin_amdgcn_exp2f(fminf(fmaf(s[k][u][i], av.c, -st.x), 8.0f)) * st.y;
+        e = pos + i <= qr.limit ? e : 0.0f;
+        e += quad_move<0xB1>(e);               // lanes 1 0 3 2
+        e += quad_move<0x4E>(e);               // lanes 2 3 0 1
+        if constexpr (W == 8) e += lane_move<shl(4)>(0.0f, e);   // (for the lane that writes)
+        w[k][u][i] += e;
+      }
+      if (m % W != 0) continue;
+      if (pos + 4 <= sp.len) {
+        *reinterpret_cast<floatx4 *>(av.weight_out + row + pos) = w[k][u];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (pos + i < sp.len) av.weight_out[row + pos + i] = w[k][u][i];
+      }
+    }
+  }
+}
+
+// The other rows: the scores again, against the finished sums.  A wave for each
+// page; its query tiles in order, so the sum's order is fixed.
 template <int D, int SPL>
 __global__ __launch_bounds__(256) void weight_kernel(CacheView cv, RowsView rv, AttendView av) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int g = lane >> 4, m = lane & 15, h = blockIdx.y, r = blockIdx.z;
   const int p = blockIdx.x * 4 + wave;
   const Span sp = row_span(cv, rv, r);
-  if (sp.n == 0 || p * kPage >= sp.len) return;
+  if (sp.n == 0 || p * kPage >= sp.len || (av.scores && is_narrow(sp, av))) return;
   const uint8_t *page = page_of<D>(cv, sp.slot, p, h);
   if (!page) return;                           // reported by attend_kernel
   PageRegs<D> x;
@@ -978,6 +1056,9 @@ __global__ __launch_bounds__(256) void weight_kernel(CacheView cv, RowsView rv, 
 
 namespace {
 
+// Kept scores at most; larger steps compute them again.
+constexpr size_t kMostScores = (size_t)1 << 30;
+
 // Tiles of `tile` query rows whose pages are split over workgroups until there
 // are `want` of them.
 TilePlan tile_plan(int32_t tile, int64_t tiles, int64_t pages, int Hkv, int D, int64_t want) {
@@ -1003,7 +1084,8 @@ TilePlan tile_plan(int32_t tile, int64_t tiles, int64_t pages, int Hkv, int D, i
 AttendPlan cache_attend_plan(const CacheView &cv, const RowsView &rv, int D, int32_t Hq) {
   AttendPlan p = {};
   const int32_t G = Hq / cv.Hkv;
-  const int64_t pages = ((int64_t)rv.max_context + kPage - 1) / kPage;
+  const int64_t pages =
+      std::min<int64_t>(((int64_t)rv.max_context + kPage - 1) / kPage, cv.max_pages);
   // rows of more than a tile of 16 query rows, and rows that may be of fewer: of
   // one token where there are both
   const bool wide = (int64_t)rv.max_tokens * G > 16;
@@ -1018,6 +1100,13 @@ AttendPlan cache_attend_plan(const CacheView &cv, const RowsView &rv, int D, int
                        512);
   }
   p.stat_bytes = (size_t)rv.N * Hq * sizeof(float2);
+  // kept scores, of a cache that has weights: worth it where they are fewer bytes
+  // than the key codes
+  p.score_pages = (int32_t)pages;
+  if (narrow && p.pack > 1 && cv.weight) {
+    const size_t bytes = (size_t)rv.R * cv.Hkv * pages * (64 * 16 / p.pack) * sizeof(float);
+    p.score_bytes = bytes <= kMostScores ? bytes : 0;
+  }
   return p;
 }
 
@@ -1052,7 +1141,15 @@ void attend_launch(const CacheView &cv, const RowsView &rv, AttendView av, const
     av.part_o += t.o_bytes / sizeof(float);
   }
   if (av.weight_out) {
-    const unsigned pages = (unsigned)((rv.max_context + kPage - 1) / kPage);
+    const unsigned pages = (unsigned)plan.score_pages;
+    if (av.scores) {
+      const dim3 grid((pages + 15) / 16, (unsigned)cv.Hkv, (unsigned)rv.R);
+      if (plan.pack == 4)
+        hipLaunchKernelGGL(weight_scores_kernel<4>, grid, dim3(256), 0, st, cv, rv, av);
+      else
+        hipLaunchKernelGGL(weight_scores_kernel<2>, grid, dim3(256), 0, st, cv, rv, av);
+      if (plan.wide.tiles == 0) return;
+    }
     hipLaunchKernelGGL((weight_kernel<D, SPL>),
                        dim3((pages + 3) / 4, (unsigned)cv.Hkv, (unsigned)rv.R), dim3(256), 0, st,
                        cv, rv, av);

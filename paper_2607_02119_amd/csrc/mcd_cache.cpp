@@ -100,11 +100,13 @@ mcd::RowsView view(const mcd_cache_rows *r) {
 
 bool heads_ok(int32_t Hq, int32_t Hkv) { return Hq >= 1 && Hq % Hkv == 0; }
 
-// Workspace: status, {max, sum} of partial results, their sums, row statistics.
+// Workspace: status, {max, sum} of partial results, their sums, row statistics,
+// kept scores.
 size_t ml_bytes(const mcd::AttendPlan &p) { return round_up(p.narrow.ml_bytes + p.wide.ml_bytes); }
 size_t o_bytes(const mcd::AttendPlan &p) { return round_up(p.narrow.o_bytes + p.wide.o_bytes); }
 size_t attend_bytes(const mcd::AttendPlan &p) {
-  return mcd::kStatusBytes + ml_bytes(p) + o_bytes(p) + round_up(p.stat_bytes);
+  return mcd::kStatusBytes + ml_bytes(p) + o_bytes(p) + round_up(p.stat_bytes) +
+         round_up(p.score_bytes);
 }
 
 #define CHECK(x)                        \
@@ -199,6 +201,9 @@ mcd_status mcd_cache_attend(const mcd_cache *c, const mcd_cache_rows *r,
   av.part_o = reinterpret_cast<float *>(w);
   w += o_bytes(p);
   av.stats = a->weight_out ? reinterpret_cast<float2 *>(w) : nullptr;
+  w += round_up(p.stat_bytes);
+  av.scores = a->weight_out && p.score_bytes ? reinterpret_cast<mcd::floatx4 *>(w) : nullptr;
+  av.score_pages = p.score_pages;
   av.narrow = p.narrow_rows;
   av.splits = av.split_pages = 0;              // of each part's launch
   return launched(mcd::launch_cache_attend(cv, rv, av, p, c->D, a->dtype == MCD_BF16, stream),
