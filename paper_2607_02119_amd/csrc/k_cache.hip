@@ -5,10 +5,12 @@
 // of the scale, so every result is a function of the inputs alone, bit for bit.
 #include "cache_common.h"
 
+#include <algorithm>
+
 namespace mcd {
 namespace {
 
-constexpr int kHalf = 32;        // tokens of a workgroup: the words of a half page
+constexpr int kHalf = 32;        // tokens whose value words lie together
 
 template <bool BF16>
 __device__ __forceinline__ void load8(const void *p, int64_t at, float x[8]) {
@@ -132,42 +134,42 @@ __global__ __launch_bounds__(256) void append_one_kernel(CacheView cv, RowsView 
   }
 }
 
-// The half pages that a row's tokens touch: at most tokens / 32 + 2, so the
-// items of row r begin at start[r] / 32 + 2 r.
-__host__ __device__ inline int64_t half_items(int32_t R, int32_t N) {
-  return (int64_t)N / kHalf + 2 * (int64_t)R;
+// The pages that a row's tokens touch: at most tokens / 64 + 2, so the items of
+// row r begin at start[r] / 64 + 2 r.
+__host__ __device__ inline int64_t page_items(int32_t R, int32_t N) {
+  return (int64_t)N / kPage + 2 * (int64_t)R;
 }
 
-struct HalfItem {
+struct PageItem {
   Span sp;
-  int pos0;                  // position of the half page's first token
+  int pos0;                  // position of the page's first token
   int lo, hi;                // tokens of it that are the call's, lo < hi, else none
-  uint8_t *page;
+  uint8_t *page;             // of head 0
 };
 
 template <int D>
-__device__ __forceinline__ HalfItem half_item(const CacheView &cv, const RowsView &rv, int h,
+__device__ __forceinline__ PageItem page_item(const CacheView &cv, const RowsView &rv,
                                               uint32_t *status) {
-  HalfItem it;
+  PageItem it;
   const int64_t x = blockIdx.x;
   auto base = [&](int r) __attribute__((always_inline)) {
-    return (int64_t)row_start(rv, r) / kHalf + 2 * (int64_t)r;
+    return (int64_t)row_start(rv, r) / kPage + 2 * (int64_t)r;
   };
   const int r = find_row(rv.R, x, base);
   it.sp = row_span(cv, rv, r);
   const Span &s = it.sp;
   const int first = max(s.ctx, 0);
-  const int64_t at = (int64_t)first / kHalf + (x - base(r));
-  const bool none = s.n == 0 || x < base(r) || at * kHalf >= s.len;
+  const int64_t at = (int64_t)first / kPage + (x - base(r));
+  const bool none = s.n == 0 || x < base(r) || at * kPage >= s.len;
   it.lo = it.hi = 0;
   it.pos0 = 0;
   it.page = nullptr;
   if ((s.bad || s.ctx < 0) && threadIdx.x == 0) set_bad(status);
   if (none) return it;
-  it.pos0 = (int)at * kHalf;
+  it.pos0 = (int)at * kPage;
   it.lo = max(first - it.pos0, 0);
-  it.hi = min(s.len - it.pos0, kHalf);
-  it.page = page_of<D>(cv, s.slot, it.pos0 / kPage, h);
+  it.hi = min(s.len - it.pos0, kPage);
+  it.page = page_of<D>(cv, s.slot, (int)at, 0);
   if (!it.page) {
     it.hi = it.lo;
     if (threadIdx.x == 0) set_bad(status);
@@ -175,58 +177,71 @@ __device__ __forceinline__ HalfItem half_item(const CacheView &cv, const RowsVie
   return it;
 }
 
-// Any number of tokens: a workgroup for each half page and head.  Key codes go
-// straight to the page (a lane's 8 channels are one word); value codes turn
-// through LDS, so that each word of 8 tokens is written once, whole.
+// Workgroups that share out the heads of a page: all heads in one where there
+// are pages enough for eight workgroups on each compute unit (the chain of loads
+// to a page's address then counts once for all), fewer otherwise.
+inline unsigned head_groups(int64_t items, int Hkv) {
+  const int64_t want = (2048 + items - 1) / std::max<int64_t>(items, 1);
+  return (unsigned)std::min<int64_t>(std::max<int64_t>(want, 1), Hkv);
+}
+
+// Any number of tokens: a workgroup for each page and its share of the heads.
+// Key codes go straight to the page (a lane's 8 channels are one word); value
+// codes turn through LDS, so that each word of 8 tokens is written once, whole.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void append_kernel(CacheView cv, RowsView rv, const void *k,
                                                      int64_t ks, const void *v, int64_t vs,
                                                      uint32_t *status) {
   constexpr int L = D / 8;
-  __shared__ uint32_t codes[kHalf][L + 1];
-  const int h = blockIdx.y;
-  const HalfItem it = half_item<D>(cv, rv, h, status);
+  __shared__ uint32_t codes[2][kPage][L + 1];
+  const PageItem it = page_item<D>(cv, rv, status);
   if (it.lo >= it.hi) return;
-  const int half = (it.pos0 / kHalf) & 1;
-#pragma unroll
-  for (int i = threadIdx.x; i < kHalf * L; i += 256) {
-    const int tt = i / L, chunk = i % L, t = half * kHalf + tt;
-    const bool mine = tt >= it.lo && tt < it.hi;
-    float x[8] = {}, y[8] = {};
-    if (mine) {
-      const int64_t tok = it.sp.t0 + (it.pos0 + tt - it.sp.ctx);
-      load8<BF16>(k, tok * ks + h * D + chunk * 8, x);
-      load8<BF16>(v, tok * vs + h * D + chunk * 8, y);
+  int b = 0;
+  for (int h = blockIdx.y; h < cv.Hkv; h += gridDim.y, b ^= 1) {
+    uint8_t *page = it.page + (int64_t)h * cache_page_bytes(D);
+    for (int i = threadIdx.x + it.lo / (256 / L) * 256; i < kPage * L; i += 256) {
+      const int t = i / L, chunk = i % L;
+      if (i - (int)threadIdx.x >= it.hi * L) break;          // (uniform)
+      const bool mine = t >= it.lo && t < it.hi;
+      float x[8] = {}, y[8] = {};
+      if (mine) {
+        const int64_t tok = it.sp.t0 + (it.pos0 + t - it.sp.ctx);
+        load8<BF16>(k, tok * ks + h * D + chunk * 8, x);
+        load8<BF16>(v, tok * vs + h * D + chunk * 8, y);
+      }
+      uint32_t byte, scale;
+      const uint32_t kc = key_codes(x, byte);
+      codes[b][t][chunk] = value_codes<D>(y, scale);
+      if (mine) {
+        *reinterpret_cast<uint32_t *>(page + t * (D / 2) + chunk * 4) = kc;
+        if (chunk % 4 == 0) page[key_scale_at<D>(t, chunk / 4)] = (uint8_t)byte;
+        if (chunk == 0)
+          *reinterpret_cast<uint16_t *>(page + value_scale_at<D>(t)) = (uint16_t)scale;
+      }
     }
-    uint32_t byte, scale;
-    const uint32_t kc = key_codes(x, byte);
-    codes[tt][chunk] = value_codes<D>(y, scale);
-    if (mine) {
-      *reinterpret_cast<uint32_t *>(it.page + t * (D / 2) + chunk * 4) = kc;
-      if (chunk % 4 == 0) it.page[key_scale_at<D>(t, chunk / 4)] = (uint8_t)byte;
-      if (chunk == 0)
-        *reinterpret_cast<uint16_t *>(it.page + value_scale_at<D>(t)) = (uint16_t)scale;
-    }
-  }
-  if (cv.weight && (int)threadIdx.x >= it.lo && (int)threadIdx.x < it.hi)
-    cv.weight[((int64_t)it.sp.slot * cv.Hkv + h) * cv.max_pages * kPage + it.pos0 + threadIdx.x] =
-        0.0f;
-  __syncthreads();
-  uint32_t *words = reinterpret_cast<uint32_t *>(it.page + 32 * D) + half * 4 * D;
+    if (cv.weight && (int)threadIdx.x >= it.lo && (int)threadIdx.x < it.hi)
+      cv.weight[((int64_t)it.sp.slot * cv.Hkv + h) * cv.max_pages * kPage + it.pos0 +
+                threadIdx.x] = 0.0f;
+    __syncthreads();
+    uint32_t *words = reinterpret_cast<uint32_t *>(page + 32 * D);
 #pragma unroll
-  for (int i = threadIdx.x; i < 4 * D; i += 256) {
-    const int lane = (i >> 2) & 63, ct = (i >> 8) * 4 + (i & 3), m = lane & 15, g = lane >> 4;
-    const int c = (m >> 2) * (D / 4) + 4 * ct + (m & 3);
-    uint32_t w = 0, mask = 0;
+    for (int i = threadIdx.x; i < 8 * D; i += 256) {
+      const int half = i / (4 * D), j0 = i % (4 * D);
+      const int lane = (j0 >> 2) & 63, ct = (j0 >> 8) * 4 + (j0 & 3), m = lane & 15, g = lane >> 4;
+      const int c = (m >> 2) * (D / 4) + 4 * ct + (m & 3);
+      uint32_t w = 0, mask = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int tt = (j >> 2) * 16 + 4 * g + (j & 3);
-      const bool mine = tt >= it.lo && tt < it.hi;
-      w |= ((codes[tt][c >> 3] >> (4 * (c & 7))) & 0xFu) << (4 * j);
-      mask |= (mine ? 0xFu : 0u) << (4 * j);
+      for (int j = 0; j < 8; ++j) {
+        const int t = half * kHalf + (j >> 2) * 16 + 4 * g + (j & 3);
+        const bool mine = t >= it.lo && t < it.hi;
+        if (mine) {
+          w |= ((codes[b][t][c >> 3] >> (4 * (c & 7))) & 0xFu) << (4 * j);
+          mask |= 0xFu << (4 * j);
+        }
+      }
+      if (mask == 0xFFFFFFFFu) words[i] = w;
+      else if (mask) words[i] = (words[i] & ~mask) | w;
     }
-    if (mask == 0xFFFFFFFFu) words[i] = w;
-    else if (mask) words[i] = (words[i] & ~mask) | (w & mask);
   }
 }
 
@@ -272,40 +287,70 @@ __global__ __launch_bounds__(256) void read_one_kernel(CacheView cv, RowsView rv
   store8<BF16>(v, t0 * vs + h * D + chunk * 8, y);
 }
 
-// A workgroup for each half page and head; the value words go through LDS.
+// A workgroup for each page and its share of the heads; the value words go
+// through LDS, the next head's on their way while this one's are written.
 // Writes 4 (bf16) or 8 times the bytes that it reads.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void read_kernel(CacheView cv, RowsView rv, void *k, int64_t ks,
                                                    void *v, int64_t vs, uint32_t *status) {
-  constexpr int L = D / 8;
-  __shared__ uint32_t words[4 * D];
-  const int h = blockIdx.y;
-  const HalfItem it = half_item<D>(cv, rv, h, status);
+  constexpr int L = D / 8, E = kPage * L / 256, V = (2 * D + 255) / 256;
+  __shared__ u32x4 words[2][2 * D];
+  const PageItem it = page_item<D>(cv, rv, status);
   if (it.lo >= it.hi) return;
-  const int half = (it.pos0 / kHalf) & 1;
-  const uint32_t *src = reinterpret_cast<const uint32_t *>(it.page + 32 * D) + half * 4 * D;
-  for (int i = threadIdx.x; i < D; i += 256)
-    reinterpret_cast<u32x4 *>(words)[i] = reinterpret_cast<const u32x4 *>(src)[i];
-  __syncthreads();
+  u32x4 vw[V];
+  uint32_t kc[E];
+  uint8_t kb[E];
+  uint16_t vb[E];
+  auto fetch = [&](int h) __attribute__((always_inline)) {
+    const uint8_t *page = it.page + (int64_t)h * cache_page_bytes(D);
 #pragma unroll
-  for (int i = threadIdx.x; i < kHalf * L; i += 256) {
-    const int tt = i / L, chunk = i % L, t = half * kHalf + tt;
-    if (tt < it.lo || tt >= it.hi) continue;
-    const int64_t tok = it.sp.t0 + (it.pos0 + tt - it.sp.ctx);
-    const int shift = 4 * value_nibble(t);
-    const uint32_t kc = *reinterpret_cast<const uint32_t *>(it.page + t * (D / 2) + chunk * 4);
-    const float kscale = key_scale_float(it.page[key_scale_at<D>(t, chunk / 4)]);
-    const float vscale =
-        bf16_float(*reinterpret_cast<const uint16_t *>(it.page + value_scale_at<D>(t)));
-    float x[8], y[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t w = words[(value_word<D>(0, (t >> 2) & 3, chunk * 8 + e) - 32 * D) / 4];
-      x[e] = e2m1_value((kc >> (4 * e)) & 0xFu) * kscale;
-      y[e] = e2m1_value((w >> shift) & 0xFu) * vscale;
+    for (int i = 0; i < V; ++i) {
+      const int at = threadIdx.x + 256 * i;
+      if (at < 2 * D) vw[i] = reinterpret_cast<const u32x4 *>(page + 32 * D)[at];
     }
-    store8<BF16>(k, tok * ks + h * D + chunk * 8, x);
-    store8<BF16>(v, tok * vs + h * D + chunk * 8, y);
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int at = threadIdx.x + 256 * i, t = at / L, chunk = at % L;
+      kc[i] = *reinterpret_cast<const uint32_t *>(page + t * (D / 2) + chunk * 4);
+      kb[i] = page[key_scale_at<D>(t, chunk / 4)];
+      vb[i] = *reinterpret_cast<const uint16_t *>(page + value_scale_at<D>(t));
+    }
+  };
+  int b = 0;
+  fetch(blockIdx.y);
+  for (int h = blockIdx.y; h < cv.Hkv; h += gridDim.y, b ^= 1) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int at = threadIdx.x + 256 * i;
+      if (at < 2 * D) words[b][at] = vw[i];
+    }
+    uint32_t kc0[E];
+    float ksc[E], vsc[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      kc0[i] = kc[i];
+      ksc[i] = key_scale_float(kb[i]);
+      vsc[i] = bf16_float(vb[i]);
+    }
+    if (h + (int)gridDim.y < cv.Hkv) fetch(h + gridDim.y);
+    __syncthreads();
+    const uint32_t *w32 = reinterpret_cast<const uint32_t *>(words[b]);
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int at = threadIdx.x + 256 * i, t = at / L, chunk = at % L;
+      if (t < it.lo || t >= it.hi) continue;
+      const int64_t tok = it.sp.t0 + (it.pos0 + t - it.sp.ctx);
+      const int shift = 4 * value_nibble(t);
+      float x[8], y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t w = w32[(value_word<D>(t >> 5, (t >> 2) & 3, chunk * 8 + e) - 32 * D) / 4];
+        x[e] = e2m1_value((kc0[i] >> (4 * e)) & 0xFu) * ksc[i];
+        y[e] = e2m1_value((w >> shift) & 0xFu) * vsc[i];
+      }
+      store8<BF16>(k, tok * ks + h * D + chunk * 8, x);
+      store8<BF16>(v, tok * vs + h * D + chunk * 8, y);
+    }
   }
 }
 
@@ -325,12 +370,13 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 // histogram of the digit among the keys that match so far, then the digit at
 // which the count from above reaches what is left of m.  Equal keys of a wave
 // are counted once by a vote before the LDS atomics: most positions of a cache
-// have received exactly nothing.  Then every wave walks a stretch of its own in
-// order, with the counts of the stretches before it: keys above the m-th, and
-// the first of its equals, are written in order.
+// have received exactly nothing.  Then keys above the m-th, and the first of its
+// equals, are written in order.  Blocks of 16 keys a thread, loaded together: of
+// up to 16384 positions they stay in registers for all four passes.
 __global__ __launch_bounds__(kSelect) void evict_select_kernel(CacheView cv, EvictView ev) {
+  constexpr int KEYS = 16, BLOCK = KEYS * kSelect;
   __shared__ uint32_t hist[2048];
-  __shared__ uint32_t wave_gt[kSelectWaves], wave_eq[kSelectWaves];
+  __shared__ uint32_t counts[KEYS * kSelectWaves], wave_sum[kSelectWaves];
   __shared__ uint32_t sh_digit, sh_left;
   const int h = blockIdx.x, r = blockIdx.y, tid = threadIdx.x;
   const int lane = tid & 63, wave = tid >> 6;
@@ -354,23 +400,37 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(CacheView cv, Evi
   for (int i = tid; i < ev.recent; i += kSelect) kept[m + i] = old + i;
   if (m == 0) return;
   const float *w = cv.weight + ((int64_t)slot * cv.Hkv + h) * cv.max_pages * kPage;
+  // key j of a block: position block + j kSelect + tid
+  uint32_t key[KEYS];
+  auto load = [&](int block) __attribute__((always_inline)) {
+    float x[KEYS];
+#pragma unroll
+    for (int j = 0; j < KEYS; ++j) x[j] = w[min(block + j * kSelect + tid, old - 1)];
+#pragma unroll
+    for (int j = 0; j < KEYS; ++j) key[j] = weight_key(x[j]);
+  };
+  load(0);
   uint32_t prefix = 0, left = (uint32_t)m;
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
     const int bits = pass == 2 ? 10 : 11;
     for (int i = tid; i < 2048; i += kSelect) hist[i] = 0;
     __syncthreads();
-    for (int i = tid; i - lane < old; i += kSelect) {
-      const uint32_t key = i < old ? weight_key(w[i]) : 0u;
-      const bool in = i < old && (pass == 0 || key >> (shift + bits) == prefix);
-      const uint32_t digit = (key >> shift) & ((1u << bits) - 1u);
-      const uint64_t live = __ballot(in);
-      if (live == 0) continue;
-      const int lead = __ffsll((unsigned long long)live) - 1;
-      const uint32_t dl = (uint32_t)__shfl((int)digit, lead);
-      const uint64_t same = __ballot(in && digit == dl);
-      if (lane == lead) atomicAdd(&hist[dl], (uint32_t)__popcll(same));
-      if (in && digit != dl) atomicAdd(&hist[digit], 1u);
+    for (int block = 0; block < old; block += BLOCK) {
+      if (old > BLOCK) load(block);
+#pragma unroll
+      for (int j = 0; j < KEYS; ++j) {
+        const bool in = block + j * kSelect + tid < old &&
+                        (pass == 0 || key[j] >> (shift + bits) == prefix);
+        const uint32_t digit = (key[j] >> shift) & ((1u << bits) - 1u);
+        const uint64_t live = __ballot(in);
+        if (live == 0) continue;
+        const int lead = __ffsll((unsigned long long)live) - 1;
+        const uint32_t dl = (uint32_t)__shfl((int)digit, lead);
+        const uint64_t same = __ballot(in && digit == dl);
+        if (lane == lead) atomicAdd(&hist[dl], (uint32_t)__popcll(same));
+        if (in && digit != dl) atomicAdd(&hist[digit], 1u);
+      }
     }
     __syncthreads();
     // counts from the top: thread t holds digits 2047 - 2t and 2046 - 2t
@@ -381,9 +441,9 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(CacheView cv, Evi
       const uint32_t o = (uint32_t)__shfl_up((int)sum, d);
       if (lane >= d) sum += o;
     }
-    if (lane == 63) wave_gt[wave] = sum;
+    if (lane == 63) wave_sum[wave] = sum;
     __syncthreads();
-    for (int i = 0; i < wave; ++i) sum += wave_gt[i];
+    for (int i = 0; i < wave; ++i) sum += wave_sum[i];
     const uint32_t before = sum - a - b;       // keys of higher digits
     if (before < left && sum >= left) {
       const bool first = before + a >= left;
@@ -394,59 +454,74 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(CacheView cv, Evi
     prefix = prefix << bits | sh_digit;
     left = sh_left;
   }
-  // `left` of the keys equal to prefix stay
-  const int per = ((old + kSelectWaves - 1) / kSelectWaves + 63) & ~63;
-  const int lo = min(wave * per, old), hi = min(lo + per, old);
-  uint32_t gt = 0, eq = 0;
-  for (int i = lo + lane; i - lane < hi; i += 64) {
-    const uint32_t key = i < hi ? weight_key(w[i]) : 0u;
-    gt += __popcll(__ballot(i < hi && key > prefix));
-    eq += __popcll(__ballot(i < hi && key == prefix));
-  }
-  __syncthreads();                             // wave_gt is free
-  if (lane == 0) {
-    wave_gt[wave] = gt;
-    wave_eq[wave] = eq;
-  }
-  __syncthreads();
-  gt = eq = 0;
-  for (int i = 0; i < wave; ++i) {
-    gt += wave_gt[i];
-    eq += wave_eq[i];
-  }
+  // `left` of the keys equal to prefix stay.  counts: of each key index and wave
+  // of a block, in position order, keys above (low half) and equal (high half)
+  uint32_t gt = 0, eq = 0;                     // before the block
   const uint64_t below = (1ull << lane) - 1;
-  for (int i = lo + lane; i - lane < hi; i += 64) {
-    const uint32_t key = i < hi ? weight_key(w[i]) : 0u;
-    const bool above = i < hi && key > prefix, equal = i < hi && key == prefix;
-    const uint64_t bg = __ballot(above), be = __ballot(equal);
-    const uint32_t my_eq = eq + __popcll(be & below), my_gt = gt + __popcll(bg & below);
-    if (above || (equal && my_eq < left)) kept[my_gt + min(my_eq, left)] = i;
-    gt += __popcll(bg);
-    eq += __popcll(be);
+  for (int block = 0; block < old; block += BLOCK) {
+    if (old > BLOCK) load(block);
+#pragma unroll
+    for (int j = 0; j < KEYS; ++j) {
+      const bool in = block + j * kSelect + tid < old;
+      const uint64_t bg = __ballot(in && key[j] > prefix), be = __ballot(in && key[j] == prefix);
+      if (lane == 0) counts[j * kSelectWaves + wave] = __popcll(bg) | __popcll(be) << 16;
+    }
+    __syncthreads();
+    uint32_t mine = 0, sum = 0;
+    if (tid < KEYS * kSelectWaves) {
+      mine = sum = counts[tid];
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = (uint32_t)__shfl_up((int)sum, d);
+        if (lane >= d) sum += o;
+      }
+      if (lane == 63) wave_sum[wave] = sum;
+    }
+    __syncthreads();
+    uint32_t all = 0;
+#pragma unroll
+    for (int i = 0; i < KEYS * kSelectWaves / 64; ++i) {
+      if (i < wave) sum += wave_sum[i];
+      all += wave_sum[i];
+    }
+    if (tid < KEYS * kSelectWaves) counts[tid] = sum - mine;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < KEYS; ++j) {
+      const int i = block + j * kSelect + tid;
+      const bool above = i < old && key[j] > prefix, equal = i < old && key[j] == prefix;
+      const uint64_t bg = __ballot(above), be = __ballot(equal);
+      const uint32_t c = counts[j * kSelectWaves + wave];
+      const uint32_t my_gt = gt + (c & 0xFFFFu) + __popcll(bg & below);
+      const uint32_t my_eq = eq + (c >> 16) + __popcll(be & below);
+      if (above || (equal && my_eq < left)) kept[my_gt + min(my_eq, left)] = i;
+    }
+    gt += all & 0xFFFFu;
+    eq += all >> 16;
+    __syncthreads();                           // counts and wave_sum are read
   }
 }
 
-// A workgroup for each row, head and 32 positions of the new slot.  A lane
-// makes four value words (16 bytes) from the 16-byte chunks of their 8 tokens.
+// A workgroup for each row, head and page of the new slot.  A lane makes four
+// value words (16 bytes) from the 16-byte chunks of their 8 tokens.
 template <int D>
 __global__ __launch_bounds__(256) void evict_move_kernel(CacheView from, CacheView to,
                                                          EvictView ev) {
-  __shared__ const uint8_t *page[kHalf];
-  __shared__ int token[kHalf];
-  const int h = blockIdx.y, r = blockIdx.z, tid = threadIdx.x;
-  const int len = ld_const(ev.length_out, r);
-  const int pos0 = blockIdx.x * kHalf;
-  if (pos0 >= len) return;
-  const int count = min(len - pos0, kHalf);
+  __shared__ const uint8_t *page[kPage];
+  __shared__ int token[kPage];
+  const int h = blockIdx.x % from.Hkv, r = blockIdx.y, tid = threadIdx.x;
+  const int at = blockIdx.x / from.Hkv, pos0 = at * kPage;
   const int slot = ev.slot ? ld_const(ev.slot, r) : r;
+  const int len = ld_const(ev.length_out, r);
+  if (pos0 >= len) return;
+  const int count = min(len - pos0, kPage);
   uint8_t *dst = nullptr;
-  if (r < to.n_slots && pos0 / kPage < to.max_pages) dst = page_of<D>(to, r, pos0 / kPage, h);
+  if (r < to.n_slots && at < to.max_pages) dst = page_of<D>(to, r, at, h);
   if (!dst) {
     if (tid == 0) set_bad(ev.status);
     return;
   }
-  const int half = (pos0 / kHalf) & 1;
-  if (tid < kHalf) {
+  if (tid < kPage) {
     const uint8_t *p = nullptr;
     int src = 0;
     if (tid < count) {
@@ -468,34 +543,39 @@ __global__ __launch_bounds__(256) void evict_move_kernel(CacheView from, CacheVi
   __syncthreads();
   // keys: 16-byte chunks of 32 channels and their scale byte
 #pragma unroll
-  for (int i = tid; i < kHalf * (D / 32); i += 256) {
-    const int tt = i / (D / 32), b = i % (D / 32), t = half * kHalf + tt, s = token[tt];
-    const uint8_t *p = page[tt];
+  for (int i = tid; i < kPage * (D / 32); i += 256) {
+    const int t = i / (D / 32), b = i % (D / 32), s = token[t];
+    const uint8_t *p = page[t];
     if (!p) continue;
     *reinterpret_cast<u32x4 *>(dst + t * (D / 2) + b * 16) =
         *reinterpret_cast<const u32x4 *>(p + s * (D / 2) + b * 16);
     dst[key_scale_at<D>(t, b)] = p[key_scale_at<D>(s, b)];
   }
-  if (tid < kHalf && page[tid])
-    *reinterpret_cast<uint16_t *>(dst + value_scale_at<D>(half * kHalf + tid)) =
+  if (tid < kPage && page[tid])
+    *reinterpret_cast<uint16_t *>(dst + value_scale_at<D>(tid)) =
         *reinterpret_cast<const uint16_t *>(page[tid] + value_scale_at<D>(token[tid]));
-  // values: chunk i is words [half][i / 64][i % 64][0..3]
+  // values: chunk i is words [half][q][lane][0..3]
 #pragma unroll
-  for (int i = tid; i < D; i += 256) {
-    const int lane = i & 63, g = lane >> 4, m = lane & 15, q = i >> 6;
-    u32x4 w = {0u, 0u, 0u, 0u};
+  for (int i = tid; i < 2 * D; i += 256) {
+    const int lane = i & 63, g = lane >> 4, m = lane & 15, hq = i >> 6;
+    const int half = hq / (D / 64), q = hq % (D / 64);
+    u32x4 x[8];
+    int shift[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int tt = (j >> 2) * 16 + 4 * g + (j & 3), s = token[tt];
-      const uint8_t *p = page[tt];
-      if (!p) continue;
-      const int at = (((s >> 5) * (D / 64) + q) * 64 + ((s >> 2) & 3) * 16 + m) * 16;
-      const u32x4 x = *reinterpret_cast<const u32x4 *>(p + 32 * D + at);
-      const int shift = 4 * value_nibble(s);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] |= ((x[e] >> shift) & 0xFu) << (4 * j);
+      const int t = half * kHalf + (j >> 2) * 16 + 4 * g + (j & 3), s = token[t];
+      const uint8_t *p = page[t];
+      const int from_at = (((s >> 5) * (D / 64) + q) * 64 + ((s >> 2) & 3) * 16 + m) * 16;
+      x[j] = u32x4{0u, 0u, 0u, 0u};
+      if (p) x[j] = *reinterpret_cast<const u32x4 *>(p + 32 * D + from_at);
+      shift[j] = 4 * value_nibble(s);
     }
-    *reinterpret_cast<u32x4 *>(dst + 32 * D + ((half * (D / 64) + q) * 64 + lane) * 16) = w;
+    u32x4 w = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] |= ((x[j][e] >> shift[j]) & 0xFu) << (4 * j);
+    *reinterpret_cast<u32x4 *>(dst + 32 * D + i * 16) = w;
   }
 }
 
@@ -507,7 +587,8 @@ void append_launch(const CacheView &cv, const RowsView &rv, const void *k, int64
     hipLaunchKernelGGL((append_one_kernel<D, BF16>), dim3((unsigned)((lanes + 255) / 256)),
                        dim3(256), 0, st, cv, rv, k, ks, v, vs, status);
   } else {
-    const dim3 grid((unsigned)half_items(rv.R, rv.N), (unsigned)cv.Hkv);
+    const int64_t items = page_items(rv.R, rv.N);
+    const dim3 grid((unsigned)items, head_groups(items, cv.Hkv));
     hipLaunchKernelGGL((append_kernel<D, BF16>), grid, dim3(256), 0, st, cv, rv, k, ks, v, vs,
                        status);
   }
@@ -521,7 +602,8 @@ void read_launch(const CacheView &cv, const RowsView &rv, void *k, int64_t ks, v
     hipLaunchKernelGGL((read_one_kernel<D, BF16>), dim3((unsigned)((lanes + 255) / 256)),
                        dim3(256), 0, st, cv, rv, k, ks, v, vs, status);
   } else {
-    const dim3 grid((unsigned)half_items(rv.R, rv.N), (unsigned)cv.Hkv);
+    const int64_t items = page_items(rv.R, rv.N);
+    const dim3 grid((unsigned)items, head_groups(items, cv.Hkv));
     hipLaunchKernelGGL((read_kernel<D, BF16>), grid, dim3(256), 0, st, cv, rv, k, ks, v, vs,
                        status);
   }
@@ -562,7 +644,7 @@ hipError_t launch_cache_evict(const CacheView &from, const CacheView &to, const 
                      0, st, from, ev);
   const int longest = min(ev.keep, ev.max_length);
   if (longest > 0) {
-    const dim3 grid((unsigned)((longest + kHalf - 1) / kHalf), (unsigned)from.Hkv, (unsigned)ev.R);
+    const dim3 grid((unsigned)((longest + kPage - 1) / kPage * from.Hkv), (unsigned)ev.R);
     if (D == 64) hipLaunchKernelGGL(evict_move_kernel<64>, grid, dim3(256), 0, st, from, to, ev);
     else if (D == 128)
       hipLaunchKernelGGL(evict_move_kernel<128>, grid, dim3(256), 0, st, from, to, ev);

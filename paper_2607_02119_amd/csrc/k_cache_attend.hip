@@ -96,12 +96,15 @@ struct PageRegs {
 
 // A load at a wave-uniform address plus a 32-bit lane offset: the address stays
 // in scalar registers.
-template <class T>
+// ONCE: read by no other workgroup, so not kept in the caches.
+template <class T, bool ONCE = false>
 __device__ __forceinline__ T load_at(const uint8_t *base, uint32_t lane_at, uint32_t at) {
-  return *reinterpret_cast<const T *>(base + at + lane_at);
+  const T *p = reinterpret_cast<const T *>(base + at + lane_at);
+  if constexpr (ONCE) return __builtin_nontemporal_load(p);
+  else return *p;
 }
 
-template <int D>
+template <int D, bool ONCE = false>
 __device__ __forceinline__ void load_keys(const uint8_t *page, uint32_t g, uint32_t m,
                                           PageRegs<D> &x) {
   const uint32_t lane_at = m * (D / 2) + g * (D / 8);
@@ -114,7 +117,7 @@ __device__ __forceinline__ void load_keys(const uint8_t *page, uint32_t g, uint3
     } else {
 #pragma unroll
       for (uint32_t i = 0; i < D / 128; ++i) {
-        const u32x4 w = load_at<u32x4>(page, lane_at, 16 * t * (D / 2) + 16 * i);
+        const u32x4 w = load_at<u32x4, ONCE>(page, lane_at, 16 * t * (D / 2) + 16 * i);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x.k[t][4 * i + e] = w[e];
       }
@@ -129,13 +132,14 @@ __device__ __forceinline__ void load_keys(const uint8_t *page, uint32_t g, uint3
   }
 }
 
-template <int D, bool SCALES = true>
+template <int D, bool SCALES = true, bool ONCE = false>
 __device__ __forceinline__ void load_values(const uint8_t *page, uint32_t lane, PageRegs<D> &x) {
 #pragma unroll
   for (uint32_t h = 0; h < 2; ++h)
 #pragma unroll
     for (uint32_t q = 0; q < D / 64; ++q) {
-      const u32x4 w = load_at<u32x4>(page, lane * 16, 32 * D + (h * (D / 64) + q) * 1024);
+      const u32x4 w =
+          load_at<u32x4, ONCE>(page, lane * 16, 32 * D + (h * (D / 64) + q) * 1024);
 #pragma unroll
       for (int e = 0; e < 4; ++e) x.v[h][4 * q + e] = w[e];
     }
@@ -654,8 +658,8 @@ __global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, RowsView
   auto fetch = [&](int id) __attribute__((always_inline)) {
     const bool ok = id >= 0 && id < cv.n_pages;
     const uint8_t *page = cv.pages + ((int64_t)(ok ? id : 0) * cv.Hkv + h) * cache_page_bytes(D);
-    load_keys<D>(page, g, m, x);
-    load_values<D, PACK == 1>(page, lane, x);
+    load_keys<D, true>(page, g, m, x);
+    load_values<D, PACK == 1, true>(page, lane, x);
     if constexpr (PACK > 1) load_packed_scales<D, PACK>(page, g, m, x);
   };
   auto q = [&](int, int p, int e) __attribute__((always_inline)) {
