@@ -185,21 +185,10 @@ __device__ __forceinline__ uint32_t e2m1_code(float x, float scale) {
                (a > 5.0f * scale);
   return (a > 0.0f ? c : 0u) | (__float_as_uint(x) >> 31) << 3;   // (all multiples of 0 are 0)
 }
-// the value of a code: halves 0, 1, 2, 3, 4, 6, 8, 12
-__device__ __forceinline__ float e2m1_value(uint32_t code) {
-  const uint32_t m = code & 7u;
-  const float a = 0.5f * (float)(m < 4 ? m : (m & 1u ? 6u : 4u) << ((m - 4) >> 1));
-  return code & 8u ? -a : a;
-}
-
 // Exponent byte of a key block whose largest magnitude is top (finite).
 __device__ __forceinline__ uint32_t key_scale(float top) {
   const int e = (int)((__float_as_uint(top) + 0x1FFFFFu) >> 23) - 2;
   return (uint32_t)min(max(e, 1), 254);
 }
-__device__ __forceinline__ float key_scale_float(uint32_t byte) {
-  return byte == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float(byte << 23);
-}
-
 }  // namespace
 }  // namespace mcd

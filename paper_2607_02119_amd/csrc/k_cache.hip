@@ -10,6 +10,9 @@
 namespace mcd {
 namespace {
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float float2v __attribute__((ext_vector_type(2)));
+
 constexpr int kHalf = 32;        // tokens whose value words lie together
 
 template <bool BF16>
@@ -26,20 +29,6 @@ __device__ __forceinline__ void load8(const void *p, int64_t at, float x[8]) {
     const float4 a = q[0], b = q[1];
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
     x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-  }
-}
-
-template <bool BF16>
-__device__ __forceinline__ void store8(void *p, int64_t at, const float x[8]) {
-  if constexpr (BF16) {
-    u32x4 w;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = bf16_bits(x[2 * i]) | bf16_bits(x[2 * i + 1]) << 16;
-    *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(p) + at) = w;
-  } else {
-    float4 *q = reinterpret_cast<float4 *>(static_cast<float *>(p) + at);
-    q[0] = make_float4(x[0], x[1], x[2], x[3]);
-    q[1] = make_float4(x[4], x[5], x[6], x[7]);
   }
 }
 
@@ -64,12 +53,62 @@ __device__ __forceinline__ uint32_t codes8(const float x[8], float scale) {
 }
 
 // 8 channels' codes of a key block, its scale byte; all lanes of the block's
-// four take part
+// four take part.  A power of two is the conversion's own scale.
 __device__ __forceinline__ uint32_t key_codes(const float x[8], uint32_t &byte) {
   const uint32_t top = top_bits<4>(x);
   const bool finite = top < 0x7F800000u;
   byte = finite ? key_scale(__uint_as_float(top)) : 255u;
-  return finite ? codes8(x, __uint_as_float(byte << 23)) : 0u;
+  const float scale = __uint_as_float(byte << 23);
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
+  return finite ? w : 0u;
+}
+
+// 8 channels in dtype from their codes: keys with the exponent byte as the
+// conversion's scale (255: infinity, which converts to NaN), values times theirs.
+template <bool BF16>
+__device__ __forceinline__ void store_keys(void *p, int64_t at, uint32_t codes, uint32_t byte) {
+  const float scale = __uint_as_float(byte << 23);
+  if constexpr (BF16) {
+    u32x4 w;
+    w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
+    w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
+    w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
+    w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+    *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(p) + at) = w;
+  } else {
+    const float2v a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0);
+    const float2v b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1);
+    const float2v c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 2);
+    const float2v d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 3);
+    float4 *q = reinterpret_cast<float4 *>(static_cast<float *>(p) + at);
+    q[0] = make_float4(a[0], a[1], b[0], b[1]);
+    q[1] = make_float4(c[0], c[1], d[0], d[1]);
+  }
+}
+
+template <bool BF16>
+__device__ __forceinline__ void store_values(void *p, int64_t at, uint32_t codes, float scale) {
+  float2v x[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 0),
+                  __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 1),
+                  __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 2),
+                  __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 3)};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = float2v{x[i][0] * scale, x[i][1] * scale};
+  if constexpr (BF16) {
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x[i], bf16x2));
+    *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(p) + at) = w;
+  } else {
+    float4 *q = reinterpret_cast<float4 *>(static_cast<float *>(p) + at);
+    q[0] = make_float4(x[0][0], x[0][1], x[1][0], x[1][1]);
+    q[1] = make_float4(x[2][0], x[2][1], x[3][0], x[3][1]);
+  }
 }
 
 template <int D>
@@ -192,26 +231,33 @@ template <int D, bool BF16>
 __global__ __launch_bounds__(256) void append_kernel(CacheView cv, RowsView rv, const void *k,
                                                      int64_t ks, const void *v, int64_t vs,
                                                      uint32_t *status) {
-  constexpr int L = D / 8;
+  constexpr int L = D / 8, E = kPage * L / 256;
   __shared__ uint32_t codes[2][kPage][L + 1];
   const PageItem it = page_item<D>(cv, rv, status);
   if (it.lo >= it.hi) return;
   int b = 0;
   for (int h = blockIdx.y; h < cv.Hkv; h += gridDim.y, b ^= 1) {
     uint8_t *page = it.page + (int64_t)h * cache_page_bytes(D);
-    for (int i = threadIdx.x + it.lo / (256 / L) * 256; i < kPage * L; i += 256) {
-      const int t = i / L, chunk = i % L;
-      if (i - (int)threadIdx.x >= it.hi * L) break;          // (uniform)
-      const bool mine = t >= it.lo && t < it.hi;
-      float x[8] = {}, y[8] = {};
-      if (mine) {
+    float x[E][8], y[E][8];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int at = threadIdx.x + 256 * i, t = at / L, chunk = at % L;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[i][e] = y[i][e] = 0.0f;
+      if (t >= it.lo && t < it.hi) {
         const int64_t tok = it.sp.t0 + (it.pos0 + t - it.sp.ctx);
-        load8<BF16>(k, tok * ks + h * D + chunk * 8, x);
-        load8<BF16>(v, tok * vs + h * D + chunk * 8, y);
+        load8<BF16>(k, tok * ks + h * D + chunk * 8, x[i]);
+        load8<BF16>(v, tok * vs + h * D + chunk * 8, y[i]);
       }
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int at = threadIdx.x + 256 * i, t = at / L, chunk = at % L;
+      const bool mine = t >= it.lo && t < it.hi;
+      if (!__any(mine)) continue;
       uint32_t byte, scale;
-      const uint32_t kc = key_codes(x, byte);
-      codes[b][t][chunk] = value_codes<D>(y, scale);
+      const uint32_t kc = key_codes(x[i], byte);
+      codes[b][t][chunk] = value_codes<D>(y[i], scale);
       if (mine) {
         *reinterpret_cast<uint32_t *>(page + t * (D / 2) + chunk * 4) = kc;
         if (chunk % 4 == 0) page[key_scale_at<D>(t, chunk / 4)] = (uint8_t)byte;
@@ -272,19 +318,18 @@ __global__ __launch_bounds__(256) void read_one_kernel(CacheView cv, RowsView rv
   const uint8_t *page = cv.pages + ((int64_t)id * cv.Hkv + h) * cache_page_bytes(D);
   const int t = pos % kPage, shift = 4 * value_nibble(t);
   const uint32_t kc = *reinterpret_cast<const uint32_t *>(page + t * (D / 2) + chunk * 4);
-  const float kscale = key_scale_float(page[key_scale_at<D>(t, chunk / 4)]);
+  const uint32_t byte = page[key_scale_at<D>(t, chunk / 4)];
   const float vscale =
       bf16_float(*reinterpret_cast<const uint16_t *>(page + value_scale_at<D>(t)));
-  float x[8], y[8];
+  uint32_t vc = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const uint32_t w = *reinterpret_cast<const uint32_t *>(
         page + value_word<D>(t >> 5, (t >> 2) & 3, chunk * 8 + i));
-    x[i] = e2m1_value((kc >> (4 * i)) & 0xFu) * kscale;
-    y[i] = e2m1_value((w >> shift) & 0xFu) * vscale;
+    vc |= ((w >> shift) & 0xFu) << (4 * i);
   }
-  store8<BF16>(k, t0 * ks + h * D + chunk * 8, x);
-  store8<BF16>(v, t0 * vs + h * D + chunk * 8, y);
+  store_keys<BF16>(k, t0 * ks + h * D + chunk * 8, kc, byte);
+  store_values<BF16>(v, t0 * vs + h * D + chunk * 8, vc, vscale);
 }
 
 // A workgroup for each page and its share of the heads; the value words go
@@ -324,13 +369,13 @@ __global__ __launch_bounds__(256) void read_kernel(CacheView cv, RowsView rv, vo
       const int at = threadIdx.x + 256 * i;
       if (at < 2 * D) words[b][at] = vw[i];
     }
-    uint32_t kc0[E];
-    float ksc[E], vsc[E];
+    uint32_t kc0[E], kb0[E];
+    float vb0[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) {
       kc0[i] = kc[i];
-      ksc[i] = key_scale_float(kb[i]);
-      vsc[i] = bf16_float(vb[i]);
+      kb0[i] = kb[i];
+      vb0[i] = bf16_float(vb[i]);
     }
     if (h + (int)gridDim.y < cv.Hkv) fetch(h + gridDim.y);
     __syncthreads();
@@ -341,15 +386,14 @@ __global__ __launch_bounds__(256) void read_kernel(CacheView cv, RowsView rv, vo
       if (t < it.lo || t >= it.hi) continue;
       const int64_t tok = it.sp.t0 + (it.pos0 + t - it.sp.ctx);
       const int shift = 4 * value_nibble(t);
-      float x[8], y[8];
+      uint32_t vc = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const uint32_t w = w32[(value_word<D>(t >> 5, (t >> 2) & 3, chunk * 8 + e) - 32 * D) / 4];
-        x[e] = e2m1_value((kc0[i] >> (4 * e)) & 0xFu) * ksc[i];
-        y[e] = e2m1_value((w >> shift) & 0xFu) * vsc[i];
+        vc |= ((w >> shift) & 0xFu) << (4 * e);
       }
-      store8<BF16>(k, tok * ks + h * D + chunk * 8, x);
-      store8<BF16>(v, tok * vs + h * D + chunk * 8, y);
+      store_keys<BF16>(k, tok * ks + h * D + chunk * 8, kc0[i], kb0[i]);
+      store_values<BF16>(v, tok * vs + h * D + chunk * 8, vc, vb0[i]);
     }
   }
 }
