@@ -173,42 +173,43 @@ __global__ __launch_bounds__(256) void append_one_kernel(CacheView cv, RowsView 
   }
 }
 
-// The pages that a row's tokens touch: at most tokens / 64 + 2, so the items of
-// row r begin at start[r] / 64 + 2 r.
-__host__ __device__ inline int64_t page_items(int32_t R, int32_t N) {
-  return (int64_t)N / kPage + 2 * (int64_t)R;
+// The stretches of TOK positions (a page, or half of one) that a row's tokens
+// touch: at most tokens / TOK + 2, so the items of row r begin at
+// start[r] / TOK + 2 r.
+inline int64_t stretch_items(int32_t R, int32_t N, int tok) {
+  return (int64_t)N / tok + 2 * (int64_t)R;
 }
 
-struct PageItem {
+struct StretchItem {
   Span sp;
-  int pos0;                  // position of the page's first token
-  int lo, hi;                // tokens of it that are the call's, lo < hi, else none
+  int pos0;                  // its first position
+  int lo, hi;                // positions of it that are the call's, lo < hi, else none
   uint8_t *page;             // of head 0
 };
 
-template <int D>
-__device__ __forceinline__ PageItem page_item(const CacheView &cv, const RowsView &rv,
-                                              uint32_t *status) {
-  PageItem it;
+template <int D, int TOK>
+__device__ __forceinline__ StretchItem stretch_item(const CacheView &cv, const RowsView &rv,
+                                                    uint32_t *status) {
+  StretchItem it;
   const int64_t x = blockIdx.x;
   auto base = [&](int r) __attribute__((always_inline)) {
-    return (int64_t)row_start(rv, r) / kPage + 2 * (int64_t)r;
+    return (int64_t)row_start(rv, r) / TOK + 2 * (int64_t)r;
   };
   const int r = find_row(rv.R, x, base);
   it.sp = row_span(cv, rv, r);
   const Span &s = it.sp;
   const int first = max(s.ctx, 0);
-  const int64_t at = (int64_t)first / kPage + (x - base(r));
-  const bool none = s.n == 0 || x < base(r) || at * kPage >= s.len;
+  const int64_t at = (int64_t)first / TOK + (x - base(r));
+  const bool none = s.n == 0 || x < base(r) || at * TOK >= s.len;
   it.lo = it.hi = 0;
   it.pos0 = 0;
   it.page = nullptr;
   if ((s.bad || s.ctx < 0) && threadIdx.x == 0) set_bad(status);
   if (none) return it;
-  it.pos0 = (int)at * kPage;
+  it.pos0 = (int)at * TOK;
   it.lo = max(first - it.pos0, 0);
-  it.hi = min(s.len - it.pos0, kPage);
-  it.page = page_of<D>(cv, s.slot, (int)at, 0);
+  it.hi = min(s.len - it.pos0, TOK);
+  it.page = page_of<D>(cv, s.slot, it.pos0 / kPage, 0);
   if (!it.page) {
     it.hi = it.lo;
     if (threadIdx.x == 0) set_bad(status);
@@ -216,25 +217,26 @@ __device__ __forceinline__ PageItem page_item(const CacheView &cv, const RowsVie
   return it;
 }
 
-// Workgroups that share out the heads of a page: all heads in one where there
-// are pages enough for eight workgroups on each compute unit (the chain of loads
+// Workgroups that share out the heads of a stretch: all heads in one where there
+// are enough for eight workgroups on each compute unit (the chain of loads
 // to a page's address then counts once for all), fewer otherwise.
 inline unsigned head_groups(int64_t items, int Hkv) {
   const int64_t want = (2048 + items - 1) / std::max<int64_t>(items, 1);
   return (unsigned)std::min<int64_t>(std::max<int64_t>(want, 1), Hkv);
 }
 
-// Any number of tokens: a workgroup for each page and its share of the heads.
+// Any number of tokens: a workgroup for each half page and its share of the heads.
 // Key codes go straight to the page (a lane's 8 channels are one word); value
 // codes turn through LDS, so that each word of 8 tokens is written once, whole.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void append_kernel(CacheView cv, RowsView rv, const void *k,
                                                      int64_t ks, const void *v, int64_t vs,
                                                      uint32_t *status) {
-  constexpr int L = D / 8, E = kPage * L / 256;
-  __shared__ uint32_t codes[2][kPage][L + 1];
-  const PageItem it = page_item<D>(cv, rv, status);
+  constexpr int L = D / 8, E = kHalf * L / 256;
+  __shared__ uint32_t codes[2][kHalf][L + 1];
+  const StretchItem it = stretch_item<D, kHalf>(cv, rv, status);
   if (it.lo >= it.hi) return;
+  const int t0 = it.pos0 % kPage;                // the half's first token in the page
   int b = 0;
   for (int h = blockIdx.y; h < cv.Hkv; h += gridDim.y, b ^= 1) {
     uint8_t *page = it.page + (int64_t)h * cache_page_bytes(D);
@@ -259,26 +261,25 @@ __global__ __launch_bounds__(256) void append_kernel(CacheView cv, RowsView rv, 
       const uint32_t kc = key_codes(x[i], byte);
       codes[b][t][chunk] = value_codes<D>(y[i], scale);
       if (mine) {
-        *reinterpret_cast<uint32_t *>(page + t * (D / 2) + chunk * 4) = kc;
-        if (chunk % 4 == 0) page[key_scale_at<D>(t, chunk / 4)] = (uint8_t)byte;
+        *reinterpret_cast<uint32_t *>(page + (t0 + t) * (D / 2) + chunk * 4) = kc;
+        if (chunk % 4 == 0) page[key_scale_at<D>(t0 + t, chunk / 4)] = (uint8_t)byte;
         if (chunk == 0)
-          *reinterpret_cast<uint16_t *>(page + value_scale_at<D>(t)) = (uint16_t)scale;
+          *reinterpret_cast<uint16_t *>(page + value_scale_at<D>(t0 + t)) = (uint16_t)scale;
       }
     }
     if (cv.weight && (int)threadIdx.x >= it.lo && (int)threadIdx.x < it.hi)
       cv.weight[((int64_t)it.sp.slot * cv.Hkv + h) * cv.max_pages * kPage + it.pos0 +
                 threadIdx.x] = 0.0f;
     __syncthreads();
-    uint32_t *words = reinterpret_cast<uint32_t *>(page + 32 * D);
+    uint32_t *words = reinterpret_cast<uint32_t *>(page + 32 * D) + t0 / kHalf * 4 * D;
 #pragma unroll
-    for (int i = threadIdx.x; i < 8 * D; i += 256) {
-      const int half = i / (4 * D), j0 = i % (4 * D);
-      const int lane = (j0 >> 2) & 63, ct = (j0 >> 8) * 4 + (j0 & 3), m = lane & 15, g = lane >> 4;
+    for (int i = threadIdx.x; i < 4 * D; i += 256) {
+      const int lane = (i >> 2) & 63, ct = (i >> 8) * 4 + (i & 3), m = lane & 15, g = lane >> 4;
       const int c = (m >> 2) * (D / 4) + 4 * ct + (m & 3);
       uint32_t w = 0, mask = 0;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int t = half * kHalf + (j >> 2) * 16 + 4 * g + (j & 3);
+        const int t = (j >> 2) * 16 + 4 * g + (j & 3);
         const bool mine = t >= it.lo && t < it.hi;
         if (mine) {
           w |= ((codes[b][t][c >> 3] >> (4 * (c & 7))) & 0xFu) << (4 * j);
@@ -340,7 +341,7 @@ __global__ __launch_bounds__(256) void read_kernel(CacheView cv, RowsView rv, vo
                                                    void *v, int64_t vs, uint32_t *status) {
   constexpr int L = D / 8, E = kPage * L / 256, V = (2 * D + 255) / 256;
   __shared__ u32x4 words[2][2 * D];
-  const PageItem it = page_item<D>(cv, rv, status);
+  const StretchItem it = stretch_item<D, kPage>(cv, rv, status);
   if (it.lo >= it.hi) return;
   u32x4 vw[V];
   uint32_t kc[E];
@@ -631,7 +632,7 @@ void append_launch(const CacheView &cv, const RowsView &rv, const void *k, int64
     hipLaunchKernelGGL((append_one_kernel<D, BF16>), dim3((unsigned)((lanes + 255) / 256)),
                        dim3(256), 0, st, cv, rv, k, ks, v, vs, status);
   } else {
-    const int64_t items = page_items(rv.R, rv.N);
+    const int64_t items = stretch_items(rv.R, rv.N, kHalf);
     const dim3 grid((unsigned)items, head_groups(items, cv.Hkv));
     hipLaunchKernelGGL((append_kernel<D, BF16>), grid, dim3(256), 0, st, cv, rv, k, ks, v, vs,
                        status);
@@ -646,7 +647,7 @@ void read_launch(const CacheView &cv, const RowsView &rv, void *k, int64_t ks, v
     hipLaunchKernelGGL((read_one_kernel<D, BF16>), dim3((unsigned)((lanes + 255) / 256)),
                        dim3(256), 0, st, cv, rv, k, ks, v, vs, status);
   } else {
-    const int64_t items = page_items(rv.R, rv.N);
+    const int64_t items = stretch_items(rv.R, rv.N, kPage);
     const dim3 grid((unsigned)items, head_groups(items, cv.Hkv));
     hipLaunchKernelGGL((read_kernel<D, BF16>), grid, dim3(256), 0, st, cv, rv, k, ks, v, vs,
                        status);
