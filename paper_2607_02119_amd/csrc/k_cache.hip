@@ -554,6 +554,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(CacheView from, CacheVi
                                                          EvictView ev) {
   __shared__ const uint8_t *page[kPage];
   __shared__ int token[kPage];
+  __shared__ uint32_t valid[kPage];
   const int h = blockIdx.x % from.Hkv, r = blockIdx.y, tid = threadIdx.x;
   const int at = blockIdx.x / from.Hkv, pos0 = at * kPage;
   const int slot = ev.slot ? ld_const(ev.slot, r) : r;
@@ -582,46 +583,47 @@ __global__ __launch_bounds__(256) void evict_move_kernel(CacheView from, CacheVi
             from.weight ? from.weight[f] : 0.0f;
       }
     }
-    page[tid] = p;
+    // (a position without a page is read from the destination and left out)
+    page[tid] = p ? p : dst;
     token[tid] = src % kPage;
+    valid[tid] = p ? 0xFu : 0u;
   }
   __syncthreads();
-  // keys: 16-byte chunks of 32 channels and their scale byte
-#pragma unroll
-  for (int i = tid; i < kPage * (D / 32); i += 256) {
-    const int t = i / (D / 32), b = i % (D / 32), s = token[t];
-    const uint8_t *p = page[t];
-    if (!p) continue;
-    *reinterpret_cast<u32x4 *>(dst + t * (D / 2) + b * 16) =
-        *reinterpret_cast<const u32x4 *>(p + s * (D / 2) + b * 16);
-    dst[key_scale_at<D>(t, b)] = p[key_scale_at<D>(s, b)];
-  }
-  if (tid < kPage && page[tid])
-    *reinterpret_cast<uint16_t *>(dst + value_scale_at<D>(tid)) =
-        *reinterpret_cast<const uint16_t *>(page[tid] + value_scale_at<D>(token[tid]));
-  // values: chunk i is words [half][q][lane][0..3]
+  // the loads of a thread's pieces go out together.  Keys: 16-byte chunks of 32
+  // channels and their scale byte; values: chunk i is words [half][q][lane][0..3]
 #pragma unroll
   for (int i = tid; i < 2 * D; i += 256) {
+    const int kt = i / (D / 32), kb = i % (D / 32), ks = token[kt];
+    const uint8_t *kp = page[kt];
+    const u32x4 kx = *reinterpret_cast<const u32x4 *>(kp + ks * (D / 2) + kb * 16);
+    const uint8_t kscale = kp[key_scale_at<D>(ks, kb)];
     const int lane = i & 63, g = lane >> 4, m = lane & 15, hq = i >> 6;
     const int half = hq / (D / 64), q = hq % (D / 64);
     u32x4 x[8];
     int shift[8];
+    uint32_t mask[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int t = half * kHalf + (j >> 2) * 16 + 4 * g + (j & 3), s = token[t];
-      const uint8_t *p = page[t];
       const int from_at = (((s >> 5) * (D / 64) + q) * 64 + ((s >> 2) & 3) * 16 + m) * 16;
-      x[j] = u32x4{0u, 0u, 0u, 0u};
-      if (p) x[j] = *reinterpret_cast<const u32x4 *>(p + 32 * D + from_at);
+      x[j] = *reinterpret_cast<const u32x4 *>(page[t] + 32 * D + from_at);
       shift[j] = 4 * value_nibble(s);
+      mask[j] = valid[t];
+    }
+    if (valid[kt]) {
+      *reinterpret_cast<u32x4 *>(dst + kt * (D / 2) + kb * 16) = kx;
+      dst[key_scale_at<D>(kt, kb)] = kscale;
     }
     u32x4 w = {0u, 0u, 0u, 0u};
 #pragma unroll
     for (int j = 0; j < 8; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] |= ((x[j][e] >> shift[j]) & 0xFu) << (4 * j);
+      for (int e = 0; e < 4; ++e) w[e] |= ((x[j][e] >> shift[j]) & mask[j]) << (4 * j);
     *reinterpret_cast<u32x4 *>(dst + 32 * D + i * 16) = w;
   }
+  if (tid < kPage && valid[tid])
+    *reinterpret_cast<uint16_t *>(dst + value_scale_at<D>(tid)) =
+        *reinterpret_cast<const uint16_t *>(page[tid] + value_scale_at<D>(token[tid]));
 }
 
 template <int D, bool BF16>

@@ -139,7 +139,7 @@ __device__ __forceinline__ void load_values(const uint8_t *page, uint32_t lane, 
 #pragma unroll
     for (uint32_t q = 0; q < D / 64; ++q) {
       const u32x4 w =
-          load_at<u32x4, ONCE>(page, lane * 16, 32 * D + (h * (D / 64) + q) * 1024);
+          load_at<u32x4, ONCE>(page, lane * 16, 32 * D + (h * (D / 64) + q) * 1016);
 #pragma unroll
       for (int e = 0; e < 4; ++e) x.v[h][4 * q + e] = w[e];
     }
@@ -154,7 +154,7 @@ __device__ __forceinline__ void load_values(const uint8_t *page, uint32_t lane, 
 // float whose exponent is key scale byte t of word w; 255, infinity: dequant
 // then gives NaN for every code
 __device__ __forceinline__ float key_exp(uint32_t w, int t) {
-  return __uint_as_float(t == 3 ? (w >> 24) << 23 : ((w >> (8 * t)) & 0xFFu) << 23);
+  return __uint_as_float(t == 3 ? (w >> 16) << 23 : ((w >> (8 * t)) & 0xFFu) << 23);
 }
 
 // A page's operands from its registers.
@@ -181,7 +181,8 @@ __device__ __forceinline__ void scores(K &&k, Q &&q, floatx4 (&s)[NT][4]) {
     for (int t = 0; t < 4; ++t) s[n][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) {
-    __builtin_amdgcn_sched_barrier(0);       // (one step's converted codes in registers)
+    // (one step's operands in registers, where registers make waves)
+    if constexpr (NT == 1) __builtin_amdgcn_sched_barrier(0);
     bf16x8 b[NT][SPL];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -393,7 +394,7 @@ __device__ __forceinline__ void add_page(K &&k, V &&v, const uint32_t (&vs)[8], 
     }
 #pragma unroll
     for (int c0 = 0; c0 < D / 16; c0 += 4) {
-      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (NT == 1) __builtin_amdgcn_sched_barrier(0);
       bf16x8 a[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) a[i] = v(h, c0 + i);
@@ -830,7 +831,7 @@ __global__ __launch_bounds__(256, OCC) void wide_kernel(CacheView cv, RowsView r
     if (VALL || wave < 2) {
 #pragma unroll
       for (uint32_t i = 0; i < VQ; ++i)
-        x.v[i] = load_at<u32x4>(page, lane * 16, 32 * D + (wave * VQ + i) * 1024);
+        x.v[i] = load_at<u32x4>(page, lane * 16, 32 * D + (wave * VQ + i) * 1016);
     }
 #pragma unroll
     for (uint32_t i = 0; i < 2; ++i) {
@@ -1065,15 +1066,16 @@ constexpr size_t kMostScores = (size_t)1 << 30;
 
 // Tiles of `tile` query rows whose pages are split over workgroups until there
 // are `want` of them.
-TilePlan tile_plan(int32_t tile, int64_t tiles, int64_t pages, int Hkv, int D, int64_t want) {
+TilePlan tile_plan(int32_t tile, int64_t tiles, int64_t pages, int Hkv, int D, int64_t want,
+                   int64_t least) {
   TilePlan p = {};
   if (tiles == 0) return p;
   p.tile = tile;
   p.tiles = tiles;
   const int64_t groups = tiles * Hkv;
-  const int64_t most = std::max<int64_t>((pages + 3) / 4, 1);
+  const int64_t most = std::max<int64_t>((pages + least - 1) / least, 1);
   int64_t splits = std::min(std::max<int64_t>((want + groups - 1) / groups, 1), most);
-  const int64_t per = std::max<int64_t>(((pages + splits - 1) / splits + 3) / 4 * 4, 4);
+  const int64_t per = std::max<int64_t>(((pages + splits - 1) / splits + 3) / 4 * 4, least);
   splits = std::max<int64_t>((pages + per - 1) / per, 1);
   p.splits = (int32_t)splits;
   p.split_pages = (int32_t)per;
@@ -1097,11 +1099,11 @@ AttendPlan cache_attend_plan(const CacheView &cv, const RowsView &rv, int D, int
   const int64_t rows = wide ? G : (int64_t)rv.max_tokens * G;
   p.pack = rows <= 4 ? 4 : rows <= 8 ? 2 : 1;
   p.narrow_rows = narrow ? 16 / p.pack : 0;
-  if (narrow) p.narrow = tile_plan(16 / p.pack, rv.R, pages, cv.Hkv, D, 1024);
+  if (narrow) p.narrow = tile_plan(16 / p.pack, rv.R, pages, cv.Hkv, D, 1024, 16);
   if (wide) {
     const int tile = D == 256 ? 64 : 128;
     p.wide = tile_plan(tile, tile_items(rv.R, rv.N, G, tile, rv.start == nullptr), pages, cv.Hkv, D,
-                       512);
+                       512, 4);
   }
   p.stat_bytes = (size_t)rv.N * Hq * sizeof(float2);
   // kept scores, of a cache that has weights: worth it where they are fewer bytes
