@@ -139,7 +139,7 @@ __device__ __forceinline__ void load_values(const uint8_t *page, uint32_t lane, 
 #pragma unroll
     for (uint32_t q = 0; q < D / 64; ++q) {
       const u32x4 w =
-          load_at<u32x4, ONCE>(page, lane * 16, 32 * D + (h * (D / 64) + q) * 1016);
+          load_at<u32x4, ONCE>(page, lane * 16, 32 * D + (h * (D / 64) + q) * 1024);
 #pragma unroll
       for (int e = 0; e < 4; ++e) x.v[h][4 * q + e] = w[e];
     }
@@ -154,7 +154,7 @@ __device__ __forceinline__ void load_values(const uint8_t *page, uint32_t lane, 
 // float whose exponent is key scale byte t of word w; 255, infinity: dequant
 // then gives NaN for every code
 __device__ __forceinline__ float key_exp(uint32_t w, int t) {
-  return __uint_as_float(t == 3 ? (w >> 16) << 23 : ((w >> (8 * t)) & 0xFFu) << 23);
+  return __uint_as_float(t == 3 ? (w >> 24) << 23 : ((w >> (8 * t)) & 0xFFu) << 23);
 }
 
 // A page's operands from its registers.
@@ -831,7 +831,7 @@ __global__ __launch_bounds__(256, OCC) void wide_kernel(CacheView cv, RowsView r
     if (VALL || wave < 2) {
 #pragma unroll
       for (uint32_t i = 0; i < VQ; ++i)
-        x.v[i] = load_at<u32x4>(page, lane * 16, 32 * D + (wave * VQ + i) * 1016);
+        x.v[i] = load_at<u32x4>(page, lane * 16, 32 * D + (wave * VQ + i) * 1024);
     }
 #pragma unroll
     for (uint32_t i = 0; i < 2; ++i) {
