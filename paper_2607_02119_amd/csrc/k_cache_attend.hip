@@ -1005,24 +1005,33 @@ __global__ __launch_bounds__(256) void weight_scores_kernel(CacheView cv, RowsVi
   }
 }
 
-// The other rows: the scores again, against the finished sums.  A wave for each
-// page; its query tiles in order, so the sum's order is fixed.
+// The other rows: the scores again, against the finished sums.  SHARED (where
+// there are wide rows): the waves of a workgroup take a page's query tiles in
+// turn and their sums meet in LDS, in the same order always; otherwise a wave for
+// each page.  Bound by the chain of its query loads: 21 rows of up to 820
+// positions and 5 prompts with 8 query heads a K/V head of 64 channels took 201 us
+// (the whole call) with a wave for each page, 69 with eight.  (Of the widest rows'
+// operands eight waves spill: four.)
 template <int D, int SPL>
-__global__ __launch_bounds__(256) void weight_kernel(CacheView cv, RowsView rv, AttendView av) {
+constexpr int kWeightWaves = D * SPL > 384 ? 4 : 8;
+template <int D, int SPL, bool SHARED>
+__global__ __launch_bounds__(SHARED ? 64 * kWeightWaves<D, SPL> : 256) void weight_kernel(CacheView cv, RowsView rv,
+                                                                    AttendView av) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int g = lane >> 4, m = lane & 15, h = blockIdx.y, r = blockIdx.z;
-  const int p = blockIdx.x * 4 + wave;
+  constexpr int W = SHARED ? kWeightWaves<D, SPL> : 1;
+  const int p = SHARED ? blockIdx.x : blockIdx.x * 4 + wave;
   const Span sp = row_span(cv, rv, r);
   if (sp.n == 0 || p * kPage >= sp.len || (av.scores && is_narrow(sp, av))) return;
   const uint8_t *page = page_of<D>(cv, sp.slot, p, h);
-  if (!page) return;                           // reported by attend_kernel
+  if (!page) return;                           // reported by the kernels above
   PageRegs<D> x;
   load_keys<D>(page, g, m, x);
   float total[16] = {};
   const int rows = sp.n * av.G;
   // the first token that sees the page
   const int first = max(0, p * kPage - sp.ctx) * av.G / 16 * 16;
-  for (int rho = first; rho < rows; rho += 16) {
+  for (int rho = first + (SHARED ? 16 * wave : 0); rho < rows; rho += 16 * W) {
     Query qr[1] = {query_of(sp, av, h, rho + m)};
     bf16x8 q[1][SPL][D / 32];
     load_queries<D, SPL, 1>(av, sp, qr, g, q);
@@ -1050,6 +1059,14 @@ __global__ __launch_bounds__(256) void weight_kernel(CacheView cv, RowsView rv, 
 #pragma unroll
   for (int i = 0; i < 16; ++i)
     if (m == i) mine = total[i];
+  if constexpr (SHARED) {
+    __shared__ float part[W][64];
+    part[wave][lane] = mine;
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int w = 1; w < W; ++w) mine += part[w][lane];
+  }
   const int pos = p * kPage + 16 * (m >> 2) + 4 * g + (m & 3);
   if (pos < sp.len) {
     const int64_t at = ((int64_t)sp.slot * cv.Hkv + h) * cv.max_pages * kPage + pos;
@@ -1101,7 +1118,10 @@ AttendPlan cache_attend_plan(const CacheView &cv, const RowsView &rv, int D, int
   p.narrow_rows = narrow ? 16 / p.pack : 0;
   if (narrow) p.narrow = tile_plan(16 / p.pack, rv.R, pages, cv.Hkv, D, 1024, 16);
   if (wide) {
-    const int tile = D == 256 ? 64 : 128;
+    // steps of short chunks in tiles of 64 rows: 52 rows of 2 to 12 tokens of four
+    // heads (fp32, up to 2221 positions) 208 -> 85 us, 49 of 2 to 5 (bf16, 270)
+    // 38 -> 31
+    const int tile = D == 256 || (int64_t)rv.max_tokens * G <= 64 ? 64 : 128;
     p.wide = tile_plan(tile, tile_items(rv.R, rv.N, G, tile, rv.start == nullptr), pages, cv.Hkv, D,
                        512, 4);
   }
@@ -1134,9 +1154,14 @@ void attend_launch(const CacheView &cv, const RowsView &rv, AttendView av, const
     av.splits = t.splits;
     av.split_pages = t.split_pages;
     const dim3 grid((unsigned)(t.tiles * t.splits * cv.Hkv));
-    if (!narrow)
-      hipLaunchKernelGGL((wide_kernel<D, SPL, (D == 256 ? 1 : 2), (D * SPL > 256 ? 1 : 2)>), grid,
-                         dim3(256), 0, st, cv, rv, av);
+    if (!narrow && t.tile == 64)
+      hipLaunchKernelGGL((wide_kernel<D, SPL, 1, (D * SPL > 384 ? 1 : 2)>), grid, dim3(256), 0, st,
+                         cv, rv, av);
+    else if (!narrow) {
+      if constexpr (D < 256)
+        hipLaunchKernelGGL((wide_kernel<D, SPL, 2, (D * SPL > 256 ? 1 : 2)>), grid, dim3(256), 0,
+                           st, cv, rv, av);
+    }
     else if (plan.pack == 4) narrow_launch<D, SPL, 4>(cv, rv, av, grid, st);
     else if (plan.pack == 2) narrow_launch<D, SPL, 2>(cv, rv, av, grid, st);
     else narrow_launch<D, SPL, 1>(cv, rv, av, grid, st);
@@ -1156,9 +1181,14 @@ void attend_launch(const CacheView &cv, const RowsView &rv, AttendView av, const
         hipLaunchKernelGGL(weight_scores_kernel<2>, grid, dim3(256), 0, st, cv, rv, av);
       if (plan.wide.tiles == 0) return;
     }
-    hipLaunchKernelGGL((weight_kernel<D, SPL>),
-                       dim3((pages + 3) / 4, (unsigned)cv.Hkv, (unsigned)rv.R), dim3(256), 0, st,
-                       cv, rv, av);
+    if (plan.wide.tiles)
+      hipLaunchKernelGGL((weight_kernel<D, SPL, true>),
+                         dim3(pages, (unsigned)cv.Hkv, (unsigned)rv.R),
+                         dim3(64 * kWeightWaves<D, SPL>), 0, st, cv, rv, av);
+    else
+      hipLaunchKernelGGL((weight_kernel<D, SPL, false>),
+                         dim3((pages + 3) / 4, (unsigned)cv.Hkv, (unsigned)rv.R), dim3(256), 0, st,
+                         cv, rv, av);
   }
 }
 
