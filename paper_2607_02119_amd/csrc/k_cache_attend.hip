@@ -1012,14 +1012,14 @@ __global__ __launch_bounds__(256) void weight_scores_kernel(CacheView cv, RowsVi
 // positions and 5 prompts with 8 query heads a K/V head of 64 channels took 201 us
 // (the whole call) with a wave for each page, 69 with eight.  (Of the widest rows'
 // operands eight waves spill: four.)
-template <int D, int SPL>
-constexpr int kWeightWaves = D * SPL > 384 ? 4 : 8;
+constexpr int weight_waves(int D, int SPL) { return D * SPL > 384 ? 4 : 8; }
+
 template <int D, int SPL, bool SHARED>
-__global__ __launch_bounds__(SHARED ? 64 * kWeightWaves<D, SPL> : 256) void weight_kernel(CacheView cv, RowsView rv,
-                                                                    AttendView av) {
+__global__ __launch_bounds__(SHARED ? 64 * weight_waves(D, SPL) : 256)
+void weight_kernel(CacheView cv, RowsView rv, AttendView av) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int g = lane >> 4, m = lane & 15, h = blockIdx.y, r = blockIdx.z;
-  constexpr int W = SHARED ? kWeightWaves<D, SPL> : 1;
+  constexpr int W = SHARED ? weight_waves(D, SPL) : 1;
   const int p = SHARED ? blockIdx.x : blockIdx.x * 4 + wave;
   const Span sp = row_span(cv, rv, r);
   if (sp.n == 0 || p * kPage >= sp.len || (av.scores && is_narrow(sp, av))) return;
@@ -1184,7 +1184,7 @@ void attend_launch(const CacheView &cv, const RowsView &rv, AttendView av, const
     if (plan.wide.tiles)
       hipLaunchKernelGGL((weight_kernel<D, SPL, true>),
                          dim3(pages, (unsigned)cv.Hkv, (unsigned)rv.R),
-                         dim3(64 * kWeightWaves<D, SPL>), 0, st, cv, rv, av);
+                         dim3(64 * weight_waves(D, SPL)), 0, st, cv, rv, av);
     else
       hipLaunchKernelGGL((weight_kernel<D, SPL, false>),
                          dim3((pages + 3) / 4, (unsigned)cv.Hkv, (unsigned)rv.R), dim3(256), 0, st,
