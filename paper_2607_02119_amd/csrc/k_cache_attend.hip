@@ -895,7 +895,10 @@ __global__ __launch_bounds__(256, OCC) void wide_kernel(CacheView cv, RowsView r
   }
 }
 
-// Joins the splits of a tile: a thread for four channels of a query row.
+// Joins the splits of a tile: a thread for four channels of a query row, a
+// workgroup for 256 of them.  A chain of loads over the splits, so four splits'
+// loads go out together, and spread over the chip: one workgroup for a tile of 128
+// rows of 14 splits took 100 us.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void join_kernel(CacheView cv, RowsView rv, AttendView av,
                                                    int TQ, bool narrow) {
@@ -910,30 +913,29 @@ __global__ __launch_bounds__(256) void join_kernel(CacheView cv, RowsView rv, At
   const int pages = tile_pages(sp, av.G, min(rho0 + TQ, rows));
   const int used = (pages + av.split_pages - 1) / av.split_pages;
   if (used <= 1) return;
-  for (int i = threadIdx.x; i < TQ * (D / 4); i += 256) {
-    const int row = i / (D / 4), c4 = i % (D / 4) * 4;
-    const Query qy = query_of(sp, av, h, rho0 + row);
-    if (!qy.valid) continue;
-    const int64_t part = (item * cv.Hkv + h) * av.splits * TQ + row;
-    float top = -INFINITY, l = 0.0f;
-    for (int k = 0; k < used; ++k) top = fmaxf(top, av.part_ml[part + (int64_t)k * TQ].x);
-    floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k = 0; k < used; ++k) {
-      const float2 ml = av.part_ml[part + (int64_t)k * TQ];
-      const float f = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - top);
-      l += ml.y * f;
-      acc += *reinterpret_cast<const floatx4 *>(av.part_o + (part + (int64_t)k * TQ) * D + c4) * f;
-    }
-    const bool none = l == 0.0f;
-    const float inv = none ? 0.0f : 1.0f / l;
-    const float y[4] = {none ? 0.0f : acc[0] * inv, none ? 0.0f : acc[1] * inv,
-                        none ? 0.0f : acc[2] * inv, none ? 0.0f : acc[3] * inv};
-    const int64_t tok = sp.t0 + qy.tok;
-    store4<BF16>(av.out, tok * av.out_stride + qy.head * D + c4, y);
-    if (c4 == 0) {
-      finish_row(av, tok * av.Hq + qy.head, top, l);
-    }
+  const int i = blockIdx.z * 256 + threadIdx.x, row = i / (D / 4), c4 = i % (D / 4) * 4;
+  if (row >= TQ) return;
+  const Query qy = query_of(sp, av, h, rho0 + row);
+  if (!qy.valid) return;
+  const int64_t part = (item * cv.Hkv + h) * av.splits * TQ + row;
+  float top = -INFINITY, l = 0.0f;
+#pragma unroll 4
+  for (int k = 0; k < used; ++k) top = fmaxf(top, av.part_ml[part + (int64_t)k * TQ].x);
+  floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int k = 0; k < used; ++k) {
+    const float2 ml = av.part_ml[part + (int64_t)k * TQ];
+    const float f = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - top);
+    l += ml.y * f;
+    acc += *reinterpret_cast<const floatx4 *>(av.part_o + (part + (int64_t)k * TQ) * D + c4) * f;
   }
+  const bool none = l == 0.0f;
+  const float inv = none ? 0.0f : 1.0f / l;
+  const float y[4] = {none ? 0.0f : acc[0] * inv, none ? 0.0f : acc[1] * inv,
+                      none ? 0.0f : acc[2] * inv, none ? 0.0f : acc[3] * inv};
+  const int64_t tok = sp.t0 + qy.tok;
+  store4<BF16>(av.out, tok * av.out_stride + qy.head * D + c4, y);
+  if (c4 == 0) finish_row(av, tok * av.Hq + qy.head, top, l);
 }
 
 // ---- received weight ------------------------------------------------------------
@@ -1166,7 +1168,9 @@ void attend_launch(const CacheView &cv, const RowsView &rv, AttendView av, const
     else if (plan.pack == 2) narrow_launch<D, SPL, 2>(cv, rv, av, grid, st);
     else narrow_launch<D, SPL, 1>(cv, rv, av, grid, st);
     if (t.splits > 1)
-      hipLaunchKernelGGL((join_kernel<D, SPL == 1>), dim3((unsigned)t.tiles, (unsigned)cv.Hkv),
+      hipLaunchKernelGGL((join_kernel<D, SPL == 1>),
+                         dim3((unsigned)t.tiles, (unsigned)cv.Hkv,
+                              (unsigned)((t.tile * (D / 4) + 255) / 256)),
                          dim3(256), 0, st, cv, rv, av, t.tile, narrow);
     av.part_ml += t.ml_bytes / sizeof(float2);
     av.part_o += t.o_bytes / sizeof(float);
