@@ -417,8 +417,11 @@ __device__ __forceinline__ void add_page(K &&k, V &&v, const uint32_t (&vs)[8], 
 // query rows' columns, the second 16 / PACK columns further, so that one matrix
 // instruction multiplies the values with both; unpack_rows adds the sums up at
 // the end.  (Where the third term of fp32 finds no column it takes an
-// instruction of its own.)  About 200 vector and 32 matrix instructions for a
-// page of 64 tokens and 128 channels, where full tiles take 290 and 48.
+// instruction of its own.)  32 matrix instructions for a page of 64 tokens and 128
+// channels, where full tiles take 48, and fewer vector ones.  512 rows of 100 to
+// 1100 positions, 32 query and 8 K/V heads of 128: 65 us for four tiles side by
+// side, 67 for two, 87 for one; 256 rows of 8 query heads a K/V head: 36 for two,
+// 49 for one.
 
 // Value scales of tokens 16 t + 4 g + i as bfloat16 i, t the lane's tile of each
 // of the 4 / PACK registers' worth.
@@ -619,7 +622,9 @@ __device__ __forceinline__ void write_row(const AttendView &av, const Span &sp, 
 // Narrow rows: a workgroup of four waves for each (row, K/V head) and split, the
 // pages dealt out to the waves, whose sums meet in LDS.  HBM bounds it; four
 // waves on a SIMD, each waiting for a page of its own or working on one, keep
-// the loads going (three or two waves that load a page ahead were slower).
+// the loads going (three or two waves that load a page ahead were slower).  512
+// rows of 100 to 1100 positions (8 K/V heads of 128, 341 MB): 61 us, 5.6 TB/s,
+// where a plain read reaches 6.4.
 template <int D, int SPL, int PACK, int OCC>
 __global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, RowsView rv,
                                                          AttendView av) {
@@ -754,7 +759,10 @@ __global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, RowsView
 // for all, into operands in LDS (two pages: the one at work and the next; one,
 // with another barrier, where two do not fit twice into a compute unit).  Matrix
 // instructions and the softmax's vector work take about as long as each other;
-// two workgroups on a compute unit overlap them.
+// two workgroups on a compute unit overlap them (one of eight waves was slower,
+// 785 against 753 us).  Four rows of 2048 new tokens over up to 4096 positions (32
+// query and 8 K/V heads of 128): 715 us, 0.78 PFLOP/s, the matrix units busy half
+// of the time; the values' second term is a third of their work.
 template <int D, int SPL, int NT, int OCC>
 __global__ __launch_bounds__(256, OCC) void wide_kernel(CacheView cv, RowsView rv, AttendView av) {
   constexpr int TQ = 64 * NT, KF = D / 32, VF = D / 16;    // key operands of a tile, value of a half
@@ -949,7 +957,8 @@ __device__ __forceinline__ float quad_move(float x) {
 
 // Narrow rows, from the scores that narrow_kernel left: 1 KiB of a page of 64
 // tokens and 4 query rows (a quarter of its key codes, or a half for 8 rows).  A
-// wave for four pages, their loads in flight together; bound by HBM.
+// wave for four pages, their loads in flight together; bound by HBM: 14 us for 128
+// rows of 900 to 4500 positions.
 template <int PACK>
 __global__ __launch_bounds__(256) void weight_scores_kernel(CacheView cv, RowsView rv,
                                                            AttendView av) {
@@ -1080,11 +1089,17 @@ void weight_kernel(CacheView cv, RowsView rv, AttendView av) {
 
 namespace {
 
-// Kept scores at most; larger steps compute them again.
+// Kept scores at most; larger steps compute them again (128 rows of 900 to 4500
+// positions: 104 us with the scores kept, 152 without).
 constexpr size_t kMostScores = (size_t)1 << 30;
 
 // Tiles of `tile` query rows whose pages are split over workgroups until there
-// are `want` of them.
+// are `want` of them, in splits of at least `least` pages.  512 workgroups, two on
+// a compute unit, are the best of 256 / 512 / 1024 both for narrow rows (8 of up to
+// 16 k positions: 32.7 / 26.5 / 29.7 us; 64 of up to 3000: 31.5 / 31.7 / 36.7) and
+// for wide ones (2 of 512 tokens over 4 k: 178 / 124 / 143; 9 of 150 to 357 over up
+// to 3 k: 97 / 78 / 77).  Least splits: of narrow rows 8 pages (one row of 4000
+// positions 11.1 us, 16 pages 12.9, 4 pages 11.2), of wide ones 4 (8: no change).
 TilePlan tile_plan(int32_t tile, int64_t tiles, int64_t pages, int Hkv, int D, int64_t want,
                    int64_t least) {
   TilePlan p = {};
@@ -1118,7 +1133,7 @@ AttendPlan cache_attend_plan(const CacheView &cv, const RowsView &rv, int D, int
   const int64_t rows = wide ? G : (int64_t)rv.max_tokens * G;
   p.pack = rows <= 4 ? 4 : rows <= 8 ? 2 : 1;
   p.narrow_rows = narrow ? 16 / p.pack : 0;
-  if (narrow) p.narrow = tile_plan(16 / p.pack, rv.R, pages, cv.Hkv, D, 1024, 16);
+  if (narrow) p.narrow = tile_plan(16 / p.pack, rv.R, pages, cv.Hkv, D, 512, 8);
   if (wide) {
     // steps of short chunks in tiles of 64 rows: 52 rows of 2 to 12 tokens of four
     // heads (fp32, up to 2221 positions) 208 -> 85 us, 49 of 2 to 5 (bf16, 270)
@@ -1143,7 +1158,9 @@ namespace {
 template <int D, int SPL, int PACK>
 void narrow_launch(const CacheView &cv, const RowsView &rv, const AttendView &av, const dim3 &grid,
                    hipStream_t st) {
-  constexpr int OCC = D * SPL > 384 ? 1 : D * SPL > 128 ? 2 : 4;
+  // registers for four waves on a SIMD; a single tile of 128 channels spilled there
+  // (256 rows, 16 query heads a K/V head: 50 us, with three 44)
+  constexpr int OCC = D * SPL > 384 ? 1 : D * SPL > 128 ? 2 : PACK == 1 ? 3 : 4;
   hipLaunchKernelGGL((narrow_kernel<D, SPL, PACK, OCC>), grid, dim3(256), 0, st, cv, rv, av);
 }
 
