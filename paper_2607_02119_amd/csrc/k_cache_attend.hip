@@ -1133,7 +1133,10 @@ AttendPlan cache_attend_plan(const CacheView &cv, const RowsView &rv, int D, int
   const int64_t rows = wide ? G : (int64_t)rv.max_tokens * G;
   p.pack = rows <= 4 ? 4 : rows <= 8 ? 2 : 1;
   p.narrow_rows = narrow ? 16 / p.pack : 0;
-  if (narrow) p.narrow = tile_plan(16 / p.pack, rv.R, pages, cv.Hkv, D, 512, 8);
+  // (of up to 16 pages not split: the join's launch costs more, 37 rows of up to
+  // 1003 positions 9.2 us, in two splits 11.2)
+  if (narrow)
+    p.narrow = tile_plan(16 / p.pack, rv.R, pages, cv.Hkv, D, 512, pages <= 16 ? 16 : 8);
   if (wide) {
     // steps of short chunks in tiles of 64 rows: 52 rows of 2 to 12 tokens of four
     // heads (fp32, up to 2221 positions) 208 -> 85 us, 49 of 2 to 5 (bf16, 270)
