@@ -761,7 +761,7 @@ __global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, RowsView
 // instructions and the softmax's vector work take about as long as each other;
 // two workgroups on a compute unit overlap them (one of eight waves was slower,
 // 785 against 753 us).  Four rows of 2048 new tokens over up to 4096 positions (32
-// query and 8 K/V heads of 128): 715 us, 0.78 PFLOP/s, the matrix units busy half
+// query and 8 K/V heads of 128): 719 us, 0.77 PFLOP/s, the matrix units busy half
 // of the time; the values' second term is a third of their work.
 template <int D, int SPL, int NT, int OCC>
 __global__ __launch_bounds__(256, OCC) void wide_kernel(CacheView cv, RowsView rv, AttendView av) {
