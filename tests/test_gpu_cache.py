@@ -221,6 +221,20 @@ ATTENDS += [
     ("many_rows_beside_prompts", 8, 4, 64, F32, _MANY[:40] + [0, 64], [1] * 40 + [70, 9]),
 ]
 
+# tiles of 64 and 128 query rows on both sides of the choice, chunks whose pages are
+# split and joined, received weight of more tiles than a page's waves
+ATTENDS += [
+    ("tiles_of_64_full", 8, 2, 128, BF16, [0, 200, 61], [16, 16, 5]),
+    ("tiles_of_64_one_more", 8, 2, 128, BF16, [0, 200, 61], [17, 16, 5]),
+    ("tiles_of_64_fp32", 8, 2, 128, F32, [900, 0, -3], [12, 2, 7]),
+    ("tiles_of_64_narrow_heads_fp32", 5, 1, 64, F32, [70, 1], [12, 9]),
+    ("split_chunk_fp32", 4, 1, 128, F32, [2500], [40]),
+    ("split_short_chunk", 8, 1, 128, BF16, [3900, 63], [8, 3]),
+    ("many_tiles_of_weights", 8, 1, 128, BF16, [130], [300]),
+    ("many_tiles_of_weights_wide_heads_fp32", 4, 1, 256, F32, [100, 3], [70, 1]),
+    ("rows_just_split", 4, 1, 128, BF16, [1023, 1024, 511], [1, 1, 1]),
+]
+
 
 @pytest.mark.parametrize("weights", [False, True], ids=["plain", "weights"])
 @pytest.mark.parametrize("name,Hq,Hkv,D,dtype,ctx,new", ATTENDS, ids=[a[0] for a in ATTENDS])
