@@ -37,7 +37,7 @@ struct AttendView {
   floatx4 *scores;
   int32_t score_pages;
   // Partial results of rows whose pages are split over workgroups: for each
-  // query row of a tile and split {max, sum} and D sums.
+  // query row of a tile and split {reference, sum} and D sums.
   float2 *part_ml;
   float *part_o;
   int32_t splits, split_pages; // pages of a split: the workgroups of a tile

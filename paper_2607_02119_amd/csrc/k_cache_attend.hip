@@ -294,24 +294,87 @@ __device__ __forceinline__ void store4(void *p, int64_t at, const float x[4]) {
   }
 }
 
-// A finished query row's reference (in powers of two) and sum: its lse, and what
-// weight_kernel needs of them.
-__device__ __forceinline__ void finish_row(const AttendView &av, int64_t row, float top, float l) {
+// The reference of a query row's softmax weights is a score, about its largest so
+// far; -infinity: none seen.  The weight of score s is 2^((s - reference) c), and
+// every sum is a multiple of the reference's: partial sums, the row's statistics and
+// the received weight all carry the reference itself.  Below 2^20 (in powers of
+// two) the product of reference and c is rounded once and stands for the
+// reference everywhere, so one fused multiply-add gives an exponent; beyond,
+// that rounding would be a part of the exponent that counts, or overflow it, and
+// differences are taken before they are scaled.
+constexpr float kLargeLogit = 0x1p20f;
+
+// (the product as fp32 rounds it, in no fused operation)
+__device__ __forceinline__ float scaled(float score, float c) {
+#pragma clang fp contract(off)
+  return score * c;
+}
+
+struct Origin {
+  float shift, top;            // exponent of score s: fma(s - shift, c, -top)
+};
+__device__ __forceinline__ Origin origin_of(float ref, float c) {
+  const float x = scaled(ref, c);
+  const bool none = ref == -INFINITY, large = fabsf(x) >= kLargeLogit;
+  return Origin{large && !none ? ref : 0.0f, large ? 0.0f : x};
+}
+
+// Exponent of what sums of reference a are multiplied with to become b's (a may
+// be -infinity).  LARGE: one of the two may be large.
+__device__ __forceinline__ bool is_large(float ref, float c) {
+  return fabsf(scaled(ref, c)) >= kLargeLogit && ref != -INFINITY;
+}
+template <bool LARGE>
+__device__ __forceinline__ float origin_gap_of(float a, float b, float c) {
+#pragma clang fp contract(off)
+  const float x = a * c, y = b * c;
+  if constexpr (!LARGE) return x - y;
+  const bool ax = is_large(a, c), by = is_large(b, c);
+  // beside a reference below 2^20: what the large one's product was rounded by
+  // (nothing that counts from 2^30 on)
+  const float ra = ax && fabsf(x) < 0x1p30f ? fmaf(a, c, -x) : 0.0f;
+  const float rb = by && fabsf(y) < 0x1p30f ? fmaf(b, c, -y) : 0.0f;
+  return ax && by ? (a - b) * c : (x - y) + (ra - rb);
+}
+__device__ __forceinline__ float origin_gap(float a, float b, float c) {
+  if (__any(is_large(a, c) || is_large(b, c))) return origin_gap_of<true>(a, b, c);
+  return origin_gap_of<false>(a, b, c);
+}
+
+// A finished query row's reference and sum: its lse, and what weight_kernel needs
+// of them.
+__device__ __forceinline__ void finish_row(const AttendView &av, int64_t row, float ref, float l) {
   if (av.lse)
     av.lse[row] = l == 0.0f ? -INFINITY
-                            : (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-  if (av.stats) av.stats[row] = make_float2(top, l == 0.0f ? 0.0f : 1.0f / l);
+                            : (scaled(ref, av.c) + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  if (av.stats) av.stats[row] = make_float2(ref, l == 0.0f ? 0.0f : 1.0f / l);
 }
 
 // A wave's running state: for each of NT tiles of 16 query rows (column m of the
-// lane) the reference of its softmax weights (about the largest logit so far, in
-// powers of two), the sum of its softmax weights at the lane's
-// positions, and the sums of weight x value code for the lane's channels.
+// lane) the reference of its softmax weights, the sum of its softmax weights at
+// the lane's positions, and the sums of weight x value code for the lane's channels.
 template <int D, int NT>
 struct Running {
-  float mx[NT], raw[NT], sum[NT];              // raw: the reference before its scaling
+  float ref[NT], top[NT], sum[NT];             // top: the reference times c
   floatx4 o[NT][D / 16];
 };
+
+// Takes tile n's reference up to its largest score once that is 2^8 above it: sums
+// stay far below fp32's range, and most pages scale nothing.
+template <int D, int NT>
+__device__ __forceinline__ void move_reference(Running<D, NT> &st, int n, float top, float c) {
+  if (__any((top - st.ref[n]) * c > 8.0f)) {
+    const float next = fmaxf(st.ref[n], top);
+    const float f = __builtin_amdgcn_exp2f(origin_gap(st.ref[n], next, c));
+    // (nothing seen so far: -infinity less itself)
+    const float keep = st.ref[n] == -INFINITY ? 0.0f : f;
+    st.ref[n] = next;
+    st.top[n] = scaled(next, c);
+    st.sum[n] *= keep;
+#pragma unroll
+    for (int ct = 0; ct < D / 16; ++ct) st.o[n][ct] *= keep;
+  }
+}
 
 // One page into the running state.  edge (uniform): some of its positions may be
 // hidden from some rows (limit: each row's last visible position less the page's
@@ -344,33 +407,17 @@ __device__ __forceinline__ void add_page(K &&k, V &&v, const uint32_t (&vs)[8], 
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = fmaxf(top, s[n][t][i]);
-    const float raw = across_groups_max(top);
-    top = raw * c;
-    // a new largest logit moves the reference once it is 2^8 above it: sums
-    // stay far below fp32's range, and most pages scale nothing
-    if (__any(top - st.mx[n] > 8.0f)) {
-      const float next = fmaxf(st.mx[n], top);
-      const float f = __builtin_amdgcn_exp2f(st.mx[n] - next);
-      // (nothing seen so far: -infinity less itself)
-      const float keep = st.mx[n] == -INFINITY ? 0.0f : f;
-      st.raw[n] = top > st.mx[n] ? raw : st.raw[n];
-      st.mx[n] = next;
-      st.sum[n] *= keep;
-#pragma unroll
-      for (int ct = 0; ct < D / 16; ++ct) st.o[n][ct] *= keep;
-    }
-    ref[n] = st.mx[n] == -INFINITY ? 0.0f : st.mx[n];
-    // logits of 2^20 and more: the reference's own rounding would overflow a
-    // difference, so they are taken relative to the largest before they are scaled
-    if (__any(fabsf(ref[n]) >= 0x1p20f)) {
+    move_reference(st, n, across_groups_max(top), c);
+    ref[n] = st.top[n] == -INFINITY ? 0.0f : st.top[n];
+    if (__any(fabsf(ref[n]) >= kLargeLogit)) {
+      const Origin at = origin_of(st.ref[n], c);
+      ref[n] = at.top;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         asm volatile("" : "+v"(s[n][t]));        // (kept a branch)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (st.mx[n] != -INFINITY) s[n][t][i] -= st.raw[n];
+        for (int i = 0; i < 4; ++i) s[n][t][i] -= at.shift;
       }
-      ref[n] = 0.0f;
     }
   }
   // tokens 32 h onwards: weights, then their values
@@ -481,29 +528,18 @@ __device__ __forceinline__ void add_page_packed(const PageRegs<D> &x, Q &&q, int
     for (int i = 0; i < 4; ++i) top = fmaxf(top, p[u][i]);
   if constexpr (PACK == 4) top = fmaxf(top, lane_move<ror(4)>(top, top));
   top = fmaxf(top, lane_move<ror(8)>(top, top));
-  const float raw = across_groups_max(top);
-  top = raw * c;
-  // (reference and large logits as in add_page)
-  if (__any(top - st.mx[0] > 8.0f)) {
-    const float next = fmaxf(st.mx[0], top);
-    const float f = __builtin_amdgcn_exp2f(st.mx[0] - next);
-    const float keep = st.mx[0] == -INFINITY ? 0.0f : f;
-    st.raw[0] = top > st.mx[0] ? raw : st.raw[0];
-    st.mx[0] = next;
-    st.sum[0] *= keep;
-#pragma unroll
-    for (int ct = 0; ct < D / 16; ++ct) st.o[0][ct] *= keep;
-  }
-  float ref = st.mx[0] == -INFINITY ? 0.0f : st.mx[0];
-  if (__any(fabsf(ref) >= 0x1p20f)) {
+  move_reference(st, 0, across_groups_max(top), c);
+  float ref = st.top[0] == -INFINITY ? 0.0f : st.top[0];
+  if (__any(fabsf(ref) >= kLargeLogit)) {
+    const Origin at = origin_of(st.ref[0], c);
+    ref = at.top;
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        asm volatile("" : "+v"(p[u][i]));
-        if (st.mx[0] != -INFINITY) p[u][i] -= st.raw[0];
+        asm volatile("" : "+v"(p[u][i]));        // (kept a branch)
+        p[u][i] -= at.shift;
       }
-    ref = 0.0f;
   }
   // terms of the weights, two to a word
   uint32_t w[U][PTERMS][2];
@@ -653,8 +689,8 @@ __global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, RowsView
   const Query qr = query_of(sp, av, h, m % W);
   const int all = min(sp.len - 1, sp.ctx);       // positions that every row sees
   Running<D, 1> st;
-  st.mx[0] = -INFINITY;
-  st.raw[0] = st.sum[0] = 0.0f;
+  st.ref[0] = st.top[0] = -INFINITY;
+  st.sum[0] = 0.0f;
 #pragma unroll
   for (int c = 0; c < D / 16; ++c) st.o[0][c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 
@@ -709,7 +745,7 @@ __global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, RowsView
 
   // the waves' sums, to their largest reference
   if (g == 0 && m < W) {
-    sh_ml[0][wave][m] = st.mx[0];
+    sh_ml[0][wave][m] = st.ref[0];
     sh_ml[1][wave][m] = st.sum[0];
   }
   __syncthreads();
@@ -717,7 +753,9 @@ __global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, RowsView
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) top = fmaxf(top, sh_ml[0][i][m]);
-    const float f = st.mx[0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(st.mx[0] - top);
+    const float f = st.ref[0] == -INFINITY
+                        ? 0.0f
+                        : __builtin_amdgcn_exp2f(origin_gap(st.ref[0], top, av.c));
 #pragma unroll
     for (int c = 0; c < D / 16; ++c)
       *reinterpret_cast<floatx4 *>(sh_o + (wave * W + m) * PITCH + g * (D / 4) + 4 * c) =
@@ -735,7 +773,8 @@ __global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, RowsView
 #pragma unroll
     for (int k = 0; k < WAVES; ++k) {
       const float mk = sh_ml[0][k][row];
-      l += sh_ml[1][k][row] * (mk == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mk - top));
+      l += sh_ml[1][k][row] *
+           (mk == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(origin_gap(mk, top, av.c)));
       acc += *reinterpret_cast<const floatx4 *>(sh_o + (k * W + row) * PITCH + c4);
     }
     if (used > 1) {
@@ -798,8 +837,8 @@ __global__ __launch_bounds__(256, OCC) void wide_kernel(CacheView cv, RowsView r
   Running<D, NT> st;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    st.mx[n] = -INFINITY;
-    st.raw[n] = st.sum[n] = 0.0f;
+    st.ref[n] = st.top[n] = -INFINITY;
+    st.sum[n] = 0.0f;
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) st.o[n][c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
   }
@@ -899,7 +938,7 @@ __global__ __launch_bounds__(256, OCC) void wide_kernel(CacheView cv, RowsView r
     const int64_t part = (((int64_t)item * cv.Hkv + h) * av.splits + split) * TQ +
                          (rhow + 16 * n + m - rho0);
     if (qr[n].valid)
-      write_row<D, BF16>(av, sp, qr[n], part, used > 1, g, st.mx[n], sum, st.o[n]);
+      write_row<D, BF16>(av, sp, qr[n], part, used > 1, g, st.ref[n], sum, st.o[n]);
   }
 }
 
@@ -927,16 +966,26 @@ __global__ __launch_bounds__(256) void join_kernel(CacheView cv, RowsView rv, At
   if (!qy.valid) return;
   const int64_t part = (item * cv.Hkv + h) * av.splits * TQ + row;
   float top = -INFINITY, l = 0.0f;
-#pragma unroll 4
-  for (int k = 0; k < used; ++k) top = fmaxf(top, av.part_ml[part + (int64_t)k * TQ].x);
-  floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  bool large = false;
 #pragma unroll 4
   for (int k = 0; k < used; ++k) {
-    const float2 ml = av.part_ml[part + (int64_t)k * TQ];
-    const float f = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - top);
-    l += ml.y * f;
-    acc += *reinterpret_cast<const floatx4 *>(av.part_o + (part + (int64_t)k * TQ) * D + c4) * f;
+    const float ref = av.part_ml[part + (int64_t)k * TQ].x;
+    top = fmaxf(top, ref);
+    large |= is_large(ref, av.c);
   }
+  floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  auto add = [&](auto any_large) __attribute__((always_inline)) {
+#pragma unroll 4
+    for (int k = 0; k < used; ++k) {
+      const float2 ml = av.part_ml[part + (int64_t)k * TQ];
+      const float gap = origin_gap_of<decltype(any_large)::value>(ml.x, top, av.c);
+      const float f = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(gap);
+      l += ml.y * f;
+      acc += *reinterpret_cast<const floatx4 *>(av.part_o + (part + (int64_t)k * TQ) * D + c4) * f;
+    }
+  };
+  if (__any(large)) add(std::integral_constant<bool, true>{});
+  else add(std::integral_constant<bool, false>{});
   const bool none = l == 0.0f;
   const float inv = none ? 0.0f : 1.0f / l;
   const float y[4] = {none ? 0.0f : acc[0] * inv, none ? 0.0f : acc[1] * inv,
@@ -986,6 +1035,7 @@ __global__ __launch_bounds__(256) void weight_scores_kernel(CacheView cv, RowsVi
     }
   const float2 st = qr.valid ? av.stats[(int64_t)(sp.t0 + qr.tok) * av.Hq + qr.head]
                              : make_float2(0.0f, 0.0f);
+  const Origin at = origin_of(st.x, av.c);
 #pragma unroll
   for (int k = 0; k < PAGES; ++k) {
     const int p = first + k;
@@ -997,7 +1047,7 @@ __global__ __launch_bounds__(256) void weight_scores_kernel(CacheView cv, RowsVi
       const int pos = p * kPage + 16 * (PACK * u + m / W) + 4 * g;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float e = __builtin_amdgcn_exp2f(fminf(fmaf(s[k][u][i], av.c, -st.x), 8.0f)) * st.y;
+        float e = __builtin_amdgcn_exp2f(fmaf(s[k][u][i] - at.shift, av.c, -at.top)) * st.y;
         e = pos + i <= qr.limit ? e : 0.0f;
         e += quad_move<0xB1>(e);               // lanes 1 0 3 2
         e += quad_move<0x4E>(e);               // lanes 2 3 0 1
@@ -1052,13 +1102,14 @@ void weight_kernel(CacheView cv, RowsView rv, AttendView av) {
     floatx4 s[1][4];
     scores<D, SPL, 1>(
         keys_of(x), [&](int n, int p, int e) __attribute__((always_inline)) { return q[n][p][e]; }, s);
+    const Origin at = origin_of(st.x, av.c);
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (p * kPage + 16 * t + 4 * g + i <= qr[0].limit)
           total[4 * t + i] +=
-              __builtin_amdgcn_exp2f(fminf(fmaf(s[0][t][i], av.c, -st.x), 8.0f)) * st.y;
+              __builtin_amdgcn_exp2f(fmaf(s[0][t][i] - at.shift, av.c, -at.top)) * st.y;
   }
 #pragma unroll
   for (int i = 0; i < 16; ++i) {

@@ -100,7 +100,7 @@ mcd::RowsView view(const mcd_cache_rows *r) {
 
 bool heads_ok(int32_t Hq, int32_t Hkv) { return Hq >= 1 && Hq % Hkv == 0; }
 
-// Workspace: status, {max, sum} of partial results, their sums, row statistics,
+// Workspace: status, {reference, sum} of partial results, their sums, row statistics,
 // kept scores.
 size_t ml_bytes(const mcd::AttendPlan &p) { return round_up(p.narrow.ml_bytes + p.wide.ml_bytes); }
 size_t o_bytes(const mcd::AttendPlan &p) { return round_up(p.narrow.o_bytes + p.wide.o_bytes); }

@@ -1,0 +1,93 @@
+"""The 4-bit key/value cache on the GPU where its inputs or its use go to the limits: logits and
+values of any size, rows that have no token, replays with other rows, workspaces and buffers that
+are shared.  Against tests/_cache_ref.py in 64 bits."""
+import numpy as np
+import pytest
+
+import _cache_ref as ref
+import test_gpu_cache as base
+from test_gpu_cache import BF16, F32, dev, i32, make_cache, make_rows, rounded, slot_kv, starts
+
+torch = pytest.importorskip("torch")
+mcd = pytest.importorskip("paper_2607_02119_amd.mcd", reason="libmcd.so not built")
+
+pytestmark = [pytest.mark.gpu,
+              pytest.mark.skipif(not torch.cuda.is_available(), reason="no GPU")]
+
+
+def fill(cache, k, v):
+    """Keys and values [slot][Hkv][L][D] (numpy) into a cache's pages, in order; the host copy of
+    the pages and of the table."""
+    R, H, L, D = k.shape
+    n = -(-L // 64)
+    table = np.full(tuple(cache.table.shape), -1, np.int32)
+    table[:, :n] = np.arange(R * n)[::-1].reshape(R, n)
+    cache.table.copy_(i32(table))
+    kt, vt = (dev(x.astype(np.float32)).permute(0, 2, 1, 3).reshape(R * L, H, D).contiguous()
+              for x in (k, v))
+    ws = torch.zeros(256, dtype=torch.uint8, device="cuda")
+    mcd.mcd_cache_append(cache, make_rows([0] * R, [L] * R), kt, vt, ws)
+    assert mcd.mcd_read_device_status(ws) == 0
+    return cache.pages.cpu().numpy(), table
+
+
+# ---- logits of any size ------------------------------------------------------
+
+LARGE = [
+    # name, Hq, Hkv, D, dtype, context, new tokens
+    ("kept_scores", 8, 2, 64, BF16, [300, 64, 20, 0], [1, 1, 1, 1]),
+    ("kept_scores_fp32", 16, 2, 128, F32, [300, 64, 20, 0], [1, 1, 1, 1]),
+    ("single_tile", 32, 2, 64, BF16, [300, 64, 20, 0], [1, 1, 1, 1]),
+    ("chunks", 8, 2, 64, BF16, [300, 0, 64], [40, 70, 3]),
+    ("chunks_fp32", 4, 2, 64, F32, [300, 0], [40, 70]),
+    ("decode_beside_a_prompt", 8, 2, 128, BF16, [300, 0, 64], [1, 70, 1]),
+    ("split_row", 4, 1, 64, BF16, [2600], [1]),
+    ("split_row_fp32", 4, 1, 64, F32, [2600], [1]),
+    ("split_chunk", 4, 1, 64, BF16, [2600], [20]),
+]
+
+
+@pytest.mark.parametrize("name,Hq,Hkv,D,dtype,ctx,new", LARGE, ids=[a[0] for a in LARGE])
+def test_large_logits(name, Hq, Hkv, D, dtype, ctx, new):
+    """Logits of up to 1.5e31 and of both signs, apart by whole numbers from 0 upwards, so that
+    many positions share the weight: outputs, lse and received weight.  Keys of channels 0 and 2
+    are 6, of channel 1 a whole number of [-6, 6]; the queries' entries make every score a whole
+    number below 2^24 (or a multiple of a power of two, of few bits), which fp32 holds exactly.
+    What is left are the exponent (a difference of at most 60 that matters, times log2(e): 3
+    roundings), the exponential and the sums: below 128 of 2^-23."""
+    rng = np.random.default_rng(sum(map(ord, name)))
+    R, N, L = len(ctx), sum(new), max(c + n for c, n in zip(ctx, new))
+    k, v = np.zeros((R, Hkv, L, D)), rng.standard_normal((R, Hkv, L, D))
+    k[..., 0] = k[..., 2] = 6.0
+    k[..., 1] = rng.choice([-6, -4, -3, -2, -1, 0, 1, 2, 3, 4, 6], (R, Hkv, L))
+    k[:, :, :L // 2, 1] = np.minimum(k[:, :, :L // 2, 1], -1.0)     # the largest come late
+    n_pages = R * -(-L // 64) + 1
+    cache = mcd.Cache.alloc(n_pages, Hkv, D, R, -(-L // 64) + 1, weights=True)
+    pages, table = fill(cache, k, v)
+    # (channel 0, channel 1, channel 2): 2^20 / log2(e) is 726817.2, between the third's logits
+    kinds = np.array([(0, 1, 0), (1000, 1, 0), (120832, 1, 304), (121344, 1, 0), (2 ** 17, 1, 0),
+                      (2 ** 20, 1, 0), (-2 ** 20, 1, 0), (-120832, -1, -304), (786432, -1, 0),
+                      (2490368, 1, 0), (2.0 ** 100, 2.0 ** 100, 0), (-2.0 ** 40, 2.0 ** 40, 0)])
+    q = np.zeros((N, Hq, D))
+    q[..., :3] = kinds[rng.integers(0, len(kinds), (N, Hq))]
+    rows = make_rows(ctx, new)
+    qt = dev(q.astype(np.float32)).to(dtype)
+    out, wout = torch.full_like(qt, 9.0), torch.full_like(cache.weight, 9.0)
+    lse = torch.zeros((N, Hq), device="cuda")
+    ws = cache.workspace(rows, Hq)
+    print(f"case large logits {name}", flush=True)
+    mcd.mcd_cache_attend(cache, rows, qt, out, ws, scale=1.0, lse=lse, weight_out=wout)
+    assert mcd.mcd_read_device_status(ws) == 0
+    rel = 128 * 2.0 ** -23
+    got, got_lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    for r in range(R):
+        a, n = starts(new)[r], new[r]
+        kd, vd = slot_kv(pages, table, r, ctx[r] + n, D)
+        assert np.array_equal(kd[..., :3], k[r, :, :ctx[r] + n, :3])
+        o, l, wt, size = ref.attend(kd, vd, q[a:a + n], ctx[r], 1.0)
+        to = (rel + (2.0 ** -8 if dtype == BF16 else 2.0 ** -22)) * size
+        w = wout[r, :, :ctx[r] + n].double().cpu().numpy()
+        assert (np.abs(w - wt) <= rel * wt + 1e-12).all(), (r, np.abs(w - wt).max())
+        assert (np.abs(got[a:a + n] - o) <= to).all(), (r, np.abs(got[a:a + n] - o).max())
+        # the reference, log2(e) and the sum: six roundings of 2^-24
+        assert (np.abs(got_lse[a:a + n] - l) <= rel + 2.0 ** -21 * np.abs(l)).all()
