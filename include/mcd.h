@@ -421,10 +421,12 @@ typedef struct {
 
 /* The rows of a step and their new tokens; tokens of row r are start[r] ..
  * start[r + 1] - 1 of the packed token arrays, at positions context[r],
- * context[r] + 1, ... of its slot. */
+ * context[r] + 1, ... of its slot.  n_tokens, max_tokens and max_context are
+ * bounds: the device arrays may hold fewer (a replayed step in which some rows
+ * are idle, start[r] == start[r + 1]). */
 typedef struct {
   int32_t R;                 /* rows, >= 0 */
-  int32_t n_tokens;          /* tokens of all rows (start[R]), >= 0 */
+  int32_t n_tokens;          /* tokens of all rows at most (start[R] <= n_tokens), >= 0 */
   int32_t max_tokens;        /* no row has more tokens, >= 0 */
   int32_t max_context;       /* no row has more positions (context + tokens), >= 0 */
   const int32_t *slot;       /* [R] slot of each row (no two alike), or NULL: its index */

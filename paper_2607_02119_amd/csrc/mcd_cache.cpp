@@ -92,10 +92,8 @@ mcd::CacheView view(const mcd_cache *c) {
 }
 
 mcd::RowsView view(const mcd_cache_rows *r) {
-  // as many tokens as rows and none with more than one: every row has one
-  const bool each = r->max_tokens == 1 && r->n_tokens == r->R;
   return mcd::RowsView{r->R, r->n_tokens, r->max_tokens, r->max_context, r->slot, r->context,
-                       each ? nullptr : r->start};
+                       r->start};
 }
 
 bool heads_ok(int32_t Hq, int32_t Hkv) { return Hq >= 1 && Hq % Hkv == 0; }

@@ -91,3 +91,71 @@ def test_large_logits(name, Hq, Hkv, D, dtype, ctx, new):
         assert (np.abs(got[a:a + n] - o) <= to).all(), (r, np.abs(got[a:a + n] - o).max())
         # the reference, log2(e) and the sum: six roundings of 2^-24
         assert (np.abs(got_lse[a:a + n] - l) <= rel + 2.0 ** -21 * np.abs(l)).all()
+
+
+# ---- start is read when the kernels run --------------------------------------
+
+def test_replay_with_idle_rows():
+    """A decode step (append, read, attention with weights) captured with a token in every row and
+    replayed while some rows are idle: equal starts, fewer tokens than the call's bound."""
+    D, Hq, H, R = 64, 8, 2, 4
+    rng = np.random.default_rng(31)
+    ctx0 = [130, 62, 63, 300]
+    cache, pages, table, w, _ = make_cache(rng, [c + 3 for c in ctx0], H, D, weights=True)
+    context, start = i32(ctx0), i32(np.arange(R + 1))
+    rows = mcd.CacheRows(context, start=start, n_tokens=R, max_context=400)
+    ws = cache.workspace(rows, Hq)
+    qkv = torch.zeros((R, Hq + 2 * H, D), dtype=F32, device="cuda")
+    k, v = qkv[:, Hq:Hq + H], qkv[:, Hq + H:]
+    kr, vr = torch.zeros((R, H, D), device="cuda"), torch.zeros((R, H, D), device="cuda")
+    out = torch.zeros((R, Hq, D), device="cuda")
+
+    def step():
+        mcd.mcd_cache_append(cache, rows, k, v, ws)
+        mcd.mcd_cache_read(cache, rows, kr, vr, ws)
+        mcd.mcd_cache_attend(cache, rows, qkv[:, :Hq], out, ws, weight_out=cache.weight)
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    length = np.array(ctx0)
+    want = w.astype(np.float64)
+    for new in ([1, 1, 1, 1], [1, 0, 1, 1], [0, 0, 0, 1], [0, 0, 0, 0]):
+        x = rng.standard_normal((R, Hq + 2 * H, D)).astype(np.float32)
+        qkv.copy_(dev(x))
+        context.copy_(i32(length))
+        start.copy_(i32(starts(new)))
+        for t in (kr, vr, out):
+            t.fill_(9.0)
+        print(f"case replay {new}", flush=True)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert mcd.mcd_read_device_status(ws) == 0
+        a = starts(new)
+        tol_w = np.full(want.shape, 2.0 ** -22) * want
+        for r in range(R):
+            if new[r]:
+                for h in range(H):
+                    ref.put(pages[table[r, length[r] // 64], h], D, length[r] % 64,
+                            x[a[r], Hq + h], x[a[r], Hq + H + h])
+                want[r, :, length[r]] = tol_w[r, :, length[r]] = 0.0
+        assert np.array_equal(cache.pages.cpu().numpy(), pages)
+        for r in range(R):
+            if not new[r]:
+                continue
+            L = length[r] + 1
+            kd, vd = slot_kv(pages, table, r, L, D)
+            assert np.array_equal(kr[a[r]].cpu().numpy(), kd[:, -1])
+            assert np.array_equal(vr[a[r]].cpu().numpy(), rounded(vd[:, -1], F32))
+            q = x[a[r]:a[r] + 1, :Hq].astype(np.float64)
+            o, _, wt, size = ref.attend(kd, vd, q, L - 1, 0.125)
+            to, tw, _ = base.bounds(kd, q, 0.125, F32, wt, size)
+            assert (np.abs(out[a[r]].double().cpu().numpy() - o[0]) <= to).all()
+            want[r, :, :L] += wt
+            tol_w[r, :, :L] += tw
+        got = cache.weight.double().cpu().numpy()
+        assert (np.abs(got - want) <= tol_w).all()
+        want = got
+        assert bool((out[a[-1]:] == 9.0).all()) and bool((kr[a[-1]:] == 9.0).all())
+        length = length + new
