@@ -471,8 +471,8 @@ typedef struct {
                                 -infinity for a token that sees nothing */
   float *weight_out;         /* NULL, or laid out as cache->weight (which it may be): receives
                                 cache->weight (0 where that is NULL) plus, at every position of
-                                the rows' slots, the softmax weight summed over the row's tokens
-                                and the query heads of the K/V head */
+                                the rows' slots (of rows without a token too), the softmax weight
+                                summed over the row's tokens and the query heads of the K/V head */
   void *workspace;
   size_t workspace_bytes;    /* mcd_cache_workspace_bytes() */
 } mcd_cache_attend_args;

@@ -67,6 +67,9 @@ struct AttendPlan {
 AttendPlan cache_attend_plan(const CacheView &cv, const RowsView &rv, int D, int32_t Hq);
 hipError_t launch_cache_attend(const CacheView &cv, const RowsView &rv, const AttendView &av,
                                const AttendPlan &plan, int D, bool bf16, hipStream_t st);
+// weight_out of a call without a token: what the rows' positions had received.
+hipError_t launch_cache_keep_weight(const CacheView &cv, const RowsView &rv, float *weight_out,
+                                    hipStream_t st);
 struct EvictView {
   int32_t R, max_length, keep, recent;
   const int32_t *slot, *length;

@@ -1004,6 +1004,17 @@ __device__ __forceinline__ float quad_move(float x) {
       (uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), PERM, 0xF, 0xF, false));
 }
 
+// A row without a token receives nothing: where weight_out is another array, what
+// its positions [pos0, pos0 + n) had received before, by the lanes of a wave.
+__device__ __forceinline__ void keep_weight(const CacheView &cv, const AttendView &av,
+                                            const Span &sp, int h, int pos0, int n) {
+  if (av.weight_out == cv.weight) return;
+  const int64_t row = ((int64_t)sp.slot * cv.Hkv + h) * cv.max_pages * kPage;
+  const int end = min(sp.len, pos0 + n);
+  for (int pos = pos0 + (threadIdx.x & 63); pos < end; pos += 64)
+    av.weight_out[row + pos] = cv.weight ? cv.weight[row + pos] : 0.0f;
+}
+
 // Narrow rows, from the scores that narrow_kernel left: 1 KiB of a page of 64
 // tokens and 4 query rows (a quarter of its key codes, or a half for 8 rows).  A
 // wave for four pages, their loads in flight together; bound by HBM: 14 us for 128
@@ -1016,7 +1027,9 @@ __global__ __launch_bounds__(256) void weight_scores_kernel(CacheView cv, RowsVi
   const int g = lane >> 4, m = lane & 15, h = blockIdx.y, r = blockIdx.z;
   const int first = (blockIdx.x * 4 + wave) * PAGES;
   const Span sp = row_span(cv, rv, r);
-  if (!is_narrow(sp, av) || first * kPage >= sp.len) return;
+  if (first * kPage >= sp.len) return;
+  if (sp.n == 0) keep_weight(cv, av, sp, h, first * kPage, PAGES * kPage);
+  if (!is_narrow(sp, av)) return;
   const Query qr = query_of(sp, av, h, m % W);
   const int last = min(first + PAGES - 1, (sp.len - 1) / kPage);
   const floatx4 *from =
@@ -1083,7 +1096,12 @@ void weight_kernel(CacheView cv, RowsView rv, AttendView av) {
   constexpr int W = SHARED ? weight_waves(D, SPL) : 1;
   const int p = SHARED ? blockIdx.x : blockIdx.x * 4 + wave;
   const Span sp = row_span(cv, rv, r);
-  if (sp.n == 0 || p * kPage >= sp.len || (av.scores && is_narrow(sp, av))) return;
+  if (p * kPage >= sp.len) return;
+  if (av.scores && (sp.n == 0 || is_narrow(sp, av))) return;   // (weight_scores_kernel's)
+  if (sp.n == 0) {
+    if (!SHARED || wave == 0) keep_weight(cv, av, sp, h, p * kPage, kPage);
+    return;
+  }
   const uint8_t *page = page_of<D>(cv, sp.slot, p, h);
   if (!page) return;                           // reported by the kernels above
   PageRegs<D> x;
@@ -1268,6 +1286,20 @@ void attend_launch(const CacheView &cv, const RowsView &rv, AttendView av, const
 }
 
 }  // namespace
+
+hipError_t launch_cache_keep_weight(const CacheView &cv, const RowsView &rv, float *weight_out,
+                                    hipStream_t st) {
+  AttendView av = {};
+  av.weight_out = weight_out;
+  const int64_t pages =
+      std::min<int64_t>(((int64_t)rv.max_context + kPage - 1) / kPage, cv.max_pages);
+  if (pages == 0) return hipSuccess;
+  // (no row has a token, so channels and type do not matter)
+  hipLaunchKernelGGL((weight_kernel<64, 1, false>),
+                     dim3((unsigned)((pages + 3) / 4), (unsigned)cv.Hkv, (unsigned)rv.R), dim3(256),
+                     0, st, cv, rv, av);
+  return hipGetLastError();
+}
 
 hipError_t launch_cache_attend(const CacheView &cv, const RowsView &rv, const AttendView &av,
                                const AttendPlan &plan, int D, bool bf16, hipStream_t st) {

@@ -170,7 +170,11 @@ mcd_status mcd_cache_attend(const mcd_cache *c, const mcd_cache_rows *r,
   CHECK(check_dtype(a->dtype));
   if (!heads_ok(a->Hq, c->Hkv)) return bad("Hq=%d is no multiple of Hkv=%d", a->Hq, c->Hkv);
   if (!(a->scale > 0.0f) || !std::isfinite(a->scale)) return bad("scale must be > 0 and finite");
-  if (r->n_tokens == 0) return MCD_OK;
+  if (r->n_tokens == 0) {
+    if (r->R == 0 || !a->weight_out || a->weight_out == c->weight) return MCD_OK;
+    return launched(mcd::launch_cache_keep_weight(view(c), view(r), a->weight_out, stream),
+                    "cache weight launch");
+  }
   const int64_t width = (int64_t)a->Hq * c->D;
   if (r->n_tokens * (int64_t)a->Hq > kMost || width > kMost) return bad("too many query rows");
   CHECK(check_tokens("q", a->q, a->q_stride, width, a->dtype));

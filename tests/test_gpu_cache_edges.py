@@ -159,3 +159,44 @@ def test_replay_with_idle_rows():
         want = got
         assert bool((out[a[-1]:] == 9.0).all()) and bool((kr[a[-1]:] == 9.0).all())
         length = length + new
+
+
+# ---- rows without a token ----------------------------------------------------
+
+@pytest.mark.parametrize("name,Hq,ctx,new", [
+    ("kept_scores", 4, [70, 200, 0, 5], [1, 0, 0, 2]),
+    ("single_tile", 32, [70, 200, 0, 5], [1, 0, 0, 1]),
+    ("beside_a_prompt", 8, [70, 200, 0, 5], [1, 0, 0, 40]),
+    ("wide", 40, [70, 200, 0, 5], [1, 0, 0, 40]),
+    ("no_token_at_all", 8, [70, 200, 0, 5], [0, 0, 0, 0]),
+])
+@pytest.mark.parametrize("cached", [True, False], ids=["weights", "no_weights"])
+def test_weight_of_rows_without_a_token(name, Hq, ctx, new, cached):
+    """weight_out holds what they had received before, or 0 of a cache without weights; in place
+    they keep it."""
+    rng = np.random.default_rng(len(name))
+    D, H, R, N = 64, 2, 4, sum(new)
+    slot = [2, 0, 3, 1]
+    lengths = np.zeros(R, int)
+    lengths[slot] = np.array(ctx) + new
+    cache, pages, table, w, _ = make_cache(rng, lengths, H, D, weights=cached)
+    rows = make_rows(ctx, new, slot)
+    q = dev(rng.standard_normal((max(N, 1), Hq, D)).astype(np.float32)).to(BF16)
+    shape = (R, H, table.shape[1] * 64)
+    wout = torch.full(shape, 9.0, device="cuda")
+    ws = cache.workspace(rows, Hq)
+    print(f"case no token {name} {cached}", flush=True)
+    mcd.mcd_cache_attend(cache, rows, q, torch.zeros_like(q), ws, weight_out=wout)
+    assert mcd.mcd_read_device_status(ws) == 0
+    for r in range(R):
+        if new[r] == 0:
+            got = wout[slot[r]].cpu().numpy()
+            want = w[slot[r]] if cached else np.zeros(shape[1:])
+            assert np.array_equal(got[:, :ctx[r]], want[:, :ctx[r]])
+            assert (got[:, ctx[r]:] == 9.0).all()
+    if cached:
+        mcd.mcd_cache_attend(cache, rows, q, torch.zeros_like(q), ws, weight_out=cache.weight)
+        got = cache.weight.cpu().numpy()
+        for r in range(R):
+            if new[r] == 0:
+                assert np.array_equal(got[slot[r]], w[slot[r]])
