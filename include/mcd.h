@@ -439,7 +439,10 @@ size_t mcd_cache_page_bytes(int32_t D);   /* bytes of one page and head; 0 for a
 
 /* Workspace bytes of mcd_cache_attend for rows of these bounds (0 for invalid
  * sizes); with a cache that has weights that is also room for the scores of
- * rows of few query heads, from which their received weight is added up.  The
+ * rows of few query heads, from which their received weight is added up (1 GiB
+ * at most).  Enough for every step of no more rows, tokens, tokens of a row and
+ * positions as well, with weight_out or without.  Attention that adds up no
+ * weight may be given the cache with weight NULL, and needs no such room.  The
  * other calls need the 256-byte status word only.  The
  * workspace must be 256-byte aligned and zero-filled once before first use. */
 size_t mcd_cache_workspace_bytes(const mcd_cache *cache, const mcd_cache_rows *rows, int32_t Hq);

@@ -65,6 +65,8 @@ struct AttendPlan {
   int32_t score_pages;
 };
 AttendPlan cache_attend_plan(const CacheView &cv, const RowsView &rv, int D, int32_t Hq);
+// Only the bytes: no plan of rows within rv's bounds has more of any of them.
+AttendPlan cache_attend_room(const CacheView &cv, const RowsView &rv, int D, int32_t Hq);
 hipError_t launch_cache_attend(const CacheView &cv, const RowsView &rv, const AttendView &av,
                                const AttendPlan &plan, int D, bool bf16, hipStream_t st);
 // weight_out of a call without a token: what the rows' positions had received.

@@ -1162,6 +1162,10 @@ namespace {
 // positions: 104 us with the scores kept, 152 without).
 constexpr size_t kMostScores = (size_t)1 << 30;
 
+size_t score_bytes(int64_t R, int64_t Hkv, int64_t pages, int pack) {
+  return (size_t)(R * Hkv * pages) * (64 * 16 / pack) * sizeof(float);
+}
+
 // Tiles of `tile` query rows whose pages are split over workgroups until there
 // are `want` of them, in splits of at least `least` pages.  512 workgroups, two on
 // a compute unit, are the best of 256 / 512 / 1024 both for narrow rows (8 of up to
@@ -1169,8 +1173,10 @@ constexpr size_t kMostScores = (size_t)1 << 30;
 // for wide ones (2 of 512 tokens over 4 k: 178 / 124 / 143; 9 of 150 to 357 over up
 // to 3 k: 97 / 78 / 77).  Least splits: of narrow rows 8 pages (one row of 4000
 // positions 11.1 us, 16 pages 12.9, 4 pages 11.2), of wide ones 4 (8: no change).
-TilePlan tile_plan(int32_t tile, int64_t tiles, int64_t pages, int Hkv, int D, int64_t want,
-                   int64_t least) {
+constexpr int64_t kWantGroups = 512, kLeastNarrow = 8, kWholeNarrow = 16, kLeastWide = 4;
+
+TilePlan tile_plan(int32_t tile, int64_t tiles, int64_t pages, int Hkv, int D, int64_t least) {
+  constexpr int64_t want = kWantGroups;
   TilePlan p = {};
   if (tiles == 0) return p;
   p.tile = tile;
@@ -1205,23 +1211,56 @@ AttendPlan cache_attend_plan(const CacheView &cv, const RowsView &rv, int D, int
   // (of up to 16 pages not split: the join's launch costs more, 37 rows of up to
   // 1003 positions 9.2 us, in two splits 11.2)
   if (narrow)
-    p.narrow = tile_plan(16 / p.pack, rv.R, pages, cv.Hkv, D, 512, pages <= 16 ? 16 : 8);
+    p.narrow = tile_plan(16 / p.pack, rv.R, pages, cv.Hkv, D,
+                         pages <= kWholeNarrow ? kWholeNarrow : kLeastNarrow);
   if (wide) {
     // steps of short chunks in tiles of 64 rows: 52 rows of 2 to 12 tokens of four
     // heads (fp32, up to 2221 positions) 208 -> 85 us, 49 of 2 to 5 (bf16, 270)
     // 38 -> 31
     const int tile = D == 256 || (int64_t)rv.max_tokens * G <= 64 ? 64 : 128;
     p.wide = tile_plan(tile, tile_items(rv.R, rv.N, G, tile, rv.start == nullptr), pages, cv.Hkv, D,
-                       512, 4);
+                       kLeastWide);
   }
   p.stat_bytes = (size_t)rv.N * Hq * sizeof(float2);
   // kept scores, of a cache that has weights: worth it where they are fewer bytes
   // than the key codes
   p.score_pages = (int32_t)pages;
   if (narrow && p.pack > 1 && cv.weight) {
-    const size_t bytes = (size_t)rv.R * cv.Hkv * pages * (64 * 16 / p.pack) * sizeof(float);
+    const size_t bytes = score_bytes(rv.R, cv.Hkv, pages, p.pack);
     p.score_bytes = bytes <= kMostScores ? bytes : 0;
   }
+  return p;
+}
+
+// The most that the plan of any rows within these bounds asks for: fewer rows
+// are split into more parts, and keep scores where more rows do not.
+AttendPlan cache_attend_room(const CacheView &cv, const RowsView &rv, int D, int32_t Hq) {
+  AttendPlan p = {};
+  const int32_t G = Hq / cv.Hkv;
+  const int64_t pages =
+      std::min<int64_t>(((int64_t)rv.max_context + kPage - 1) / kPage, cv.max_pages);
+  auto part_rows = [&](int64_t tiles, int64_t tile, int64_t least) {
+    const int64_t most = (pages + least - 1) / least;
+    // (from kWantGroups workgroups on nothing is split)
+    const int64_t groups = std::min(tiles * cv.Hkv, kWantGroups - 1);
+    return most <= 1 ? 0 : std::min(kWantGroups + groups - 1, groups * most) * tile;
+  };
+  const int64_t narrow = std::min<int64_t>(rv.max_tokens, 16 / G) * G;   // query rows, 0: none
+  int64_t rows = 0;
+  if (narrow > 0 && pages > kWholeNarrow)
+    rows += part_rows(rv.R, narrow <= 4 ? 4 : narrow <= 8 ? 8 : 16, kLeastNarrow);
+  if ((int64_t)rv.max_tokens * G > 16) {
+    auto wide = [&](int64_t tile) {
+      return part_rows(tile_items(rv.R, rv.N, G, (int)tile, false), tile, kLeastWide);
+    };
+    rows += D < 256 && (int64_t)rv.max_tokens * G > 64 ? std::max(wide(64), wide(128)) : wide(64);
+  }
+  p.wide.ml_bytes = (size_t)rows * sizeof(float2);
+  p.wide.o_bytes = (size_t)rows * D * sizeof(float);
+  p.stat_bytes = (size_t)rv.N * Hq * sizeof(float2);
+  const int64_t kept = std::min<int64_t>(rv.max_tokens, 8 / G) * G;
+  if (kept > 0 && cv.weight)
+    p.score_bytes = std::min(score_bytes(rv.R, cv.Hkv, pages, kept <= 4 ? 4 : 2), kMostScores);
   return p;
 }
 

@@ -2,6 +2,7 @@
 // Nothing here allocates device memory, synchronises or throws.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -107,6 +108,12 @@ size_t attend_bytes(const mcd::AttendPlan &p) {
          round_up(p.score_bytes);
 }
 
+// What a call asks for: enough for every step within the rows' bounds.
+size_t workspace_need(const mcd::AttendPlan &p, const mcd::CacheView &cv, const mcd::RowsView &rv,
+                      int D, int32_t Hq) {
+  return std::max(attend_bytes(p), attend_bytes(mcd::cache_attend_room(cv, rv, D, Hq)));
+}
+
 #define CHECK(x)                        \
   do {                                  \
     const mcd_status s_ = (x);          \
@@ -139,7 +146,9 @@ size_t mcd_cache_workspace_bytes(const mcd_cache *c, const mcd_cache_rows *r, in
     bad("Hq=%d is no multiple of Hkv=%d", Hq, c->Hkv);
     return 0;
   }
-  return attend_bytes(mcd::cache_attend_plan(view(c), view(r), c->D, Hq));
+  const mcd::CacheView cv = view(c);
+  const mcd::RowsView rv = view(r);
+  return workspace_need(mcd::cache_attend_plan(cv, rv, c->D, Hq), cv, rv, c->D, Hq);
 }
 
 mcd_status mcd_cache_append(const mcd_cache *c, const mcd_cache_rows *r, mcd_dtype d,
@@ -184,7 +193,8 @@ mcd_status mcd_cache_attend(const mcd_cache *c, const mcd_cache_rows *r,
   const mcd::AttendPlan p = mcd::cache_attend_plan(cv, rv, c->D, a->Hq);
   if ((p.narrow.tiles * p.narrow.splits + p.wide.tiles * p.wide.splits) * c->Hkv > kMost)
     return bad("too many query rows");
-  CHECK(check_workspace(a->workspace, a->workspace_bytes, attend_bytes(p)));
+  CHECK(check_workspace(a->workspace, a->workspace_bytes,
+                        workspace_need(p, cv, rv, c->D, a->Hq)));
   char *w = static_cast<char *>(a->workspace);
   mcd::AttendView av;
   av.Hq = a->Hq;

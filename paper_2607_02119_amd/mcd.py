@@ -479,7 +479,7 @@ class Cache:
         return cls(pages, table, D, weight)
 
     def workspace(self, rows, Hq):
-        """A zeroed workspace for these rows' bounds (a larger one serves smaller steps)."""
+        """A zeroed workspace for these rows' bounds and every smaller step."""
         return torch.zeros(mcd_cache_workspace_bytes(self, rows, Hq), dtype=torch.uint8,
                            device=self.pages.device)
 

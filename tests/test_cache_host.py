@@ -200,3 +200,40 @@ def test_binding_refuses_what_the_library_cannot_see():
         mcd.CacheRows(torch.zeros(2, dtype=torch.int32), start=torch.zeros(3, dtype=torch.int32))
     with pytest.raises(ValueError, match="kept"):
         mcd.mcd_cache_evict(cache, cache, i32(2), 8, 2, i32(2, 2, 7), i32(2), ws, 10)
+
+
+def test_workspace_of_a_larger_step_serves_smaller_ones():
+    """No fewer rows, tokens or positions need more: 8 rows are split where 512 are not, and keep
+    scores where more than 1 GiB of them are computed again."""
+    rng = np.random.default_rng(6)
+
+    def size(cache, b, Hq, start):
+        r = _rows(R=b[0], n_tokens=b[1], max_tokens=b[2], max_context=b[3],
+                  start=FAKE if start else None)
+        return mcd._mcd_cache_workspace_bytes(ctypes.byref(cache), ctypes.byref(r), Hq)
+
+    def log(lo, hi):
+        return int(round(np.exp(rng.uniform(np.log(lo), np.log(hi)))))
+
+    for _ in range(4000):
+        Hkv, G = int(rng.choice([1, 2, 8])), int(rng.choice([1, 2, 3, 4, 5, 8, 9, 16, 17, 64, 100]))
+        cache = _cache(Hkv=Hkv, D=int(rng.choice([64, 128, 256])), n_slots=512, max_pages=256,
+                       weight=FAKE if rng.random() < 0.5 else None)
+        R = log(1, 512)
+        mt = log(1, 600) if rng.random() < 0.7 else 1
+        N = int(rng.integers(mt, R * mt + 1))
+        large = (R, N, mt, log(1, 20000))
+        whole = size(cache, large, Hkv * G, True)
+        assert whole > 0
+        for _ in range(3):
+            mt2 = int(rng.integers(1, mt + 1))
+            R2 = int(rng.integers(1, R + 1))
+            N2 = int(rng.integers(mt2, max(mt2, min(N, R2 * mt2)) + 1))
+            small = (R2, N2, mt2, int(rng.integers(1, large[3] + 1)))
+            assert size(cache, small, Hkv * G, True) <= whole, (Hkv, G, cache.D, large, small)
+            if R2 <= N:
+                one = (R2, R2, 1, small[3])
+                assert size(cache, one, Hkv * G, False) <= whole, (Hkv, G, cache.D, large, one)
+    # without weights there is no room for scores
+    need = size(_cache(weight=None, n_slots=512, max_pages=256), (512, 512, 1, 16384), 8, True)
+    assert need < 1 << 24 < size(_cache(n_slots=512, max_pages=256), (512, 512, 1, 16384), 8, True)

@@ -200,3 +200,32 @@ def test_weight_of_rows_without_a_token(name, Hq, ctx, new, cached):
         for r in range(R):
             if new[r] == 0:
                 assert np.array_equal(got[slot[r]], w[slot[r]])
+
+
+# ---- one workspace -----------------------------------------------------------
+
+def test_one_workspace_for_every_smaller_step():
+    """A workspace sized once, for the largest step: fewer and longer rows (split and joined), kept
+    scores, chunks.  The same bits as with a workspace of their own, and nothing written past the
+    size that the largest step asked for."""
+    rng = np.random.default_rng(17)
+    H, D, Hq = 2, 64, 8
+    cache, *_ = make_cache(rng, [3000] * 4 + [200] * 60, H, D, weights=True)
+    most = mcd.CacheRows(i32([0] * 64), start=i32(np.arange(65)), n_tokens=300, max_tokens=40,
+                         max_context=3000)
+    size = mcd.mcd_cache_workspace_bytes(cache, most, Hq)
+    buf = torch.full((size + 4096,), 171, dtype=torch.uint8, device="cuda")
+    buf[:256] = 0
+    for ctx, new in (([2999], [1]), ([2900, 100], [40, 1]), ([150] * 60, [1] * 60), ([2000], [3]),
+                     ([2500, 0, 1000], [2, 2, 2]), ([100, 50, 0], [0, 7, 1])):
+        rows, N = make_rows(ctx, new), sum(new)
+        q = dev(rng.standard_normal((N, Hq, D)).astype(np.float32)).to(BF16)
+        got = []
+        print(f"case one workspace {ctx[:3]} {new[:3]}", flush=True)
+        for ws in (buf[:size], cache.workspace(rows, Hq)):
+            out, wout = torch.zeros_like(q), torch.zeros_like(cache.weight)
+            mcd.mcd_cache_attend(cache, rows, q, out, ws, weight_out=wout)
+            assert mcd.mcd_read_device_status(ws) == 0
+            got.append((out, wout))
+        assert all(torch.equal(a, b) for a, b in zip(*got))
+        assert bool((buf[size:] == 171).all())
