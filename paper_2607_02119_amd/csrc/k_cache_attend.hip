@@ -359,6 +359,25 @@ struct Running {
   floatx4 o[NT][D / 16];
 };
 
+typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+constexpr uint32_t kSpecialScale = 0x7F80u;      // bfloat16 infinity; NaN above
+
+// Whether one of a page's value scales (bfloat16, two to a word, no negative one
+// that is visible) is at least kSpecialScale.  Uniform.
+template <int N, int M>
+__device__ __forceinline__ bool special_scales(const uint32_t (&vs)[M]) {
+  ushort2v top = __builtin_bit_cast(ushort2v, vs[0]);
+#pragma unroll
+  for (int i = 1; i < N; ++i)
+    top = __builtin_elementwise_max(top, __builtin_bit_cast(ushort2v, vs[i]));
+  constexpr unsigned short below = kSpecialScale - 1;
+  return __any(__builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(
+                   top, ushort2v{below, below})) != 0u);
+}
+__device__ __forceinline__ uint32_t scale_bits(uint32_t two, int i) {
+  return (i & 1 ? two >> 16 : two) & 0x7FFFu;
+}
+
 // Takes tile n's reference up to its largest score once that is 2^8 above it: sums
 // stay far below fp32's range, and most pages scale nothing.
 template <int D, int NT>
@@ -376,10 +395,35 @@ __device__ __forceinline__ void move_reference(Running<D, NT> &st, int n, float 
   }
 }
 
+// sees: the lane's query row sees a value that is not finite.  Where its softmax
+// weight is a number of fp32 the product is NaN by itself; where it is not, the
+// product is 0 and the sums become NaN here.
+template <int D, int NT>
+__device__ __forceinline__ void add_nan(Running<D, NT> &st, int n, bool sees) {
+  if (!__any(sees)) return;
+#pragma unroll
+  for (int ct = 0; ct < D / 16; ++ct)
+    st.o[n][ct] += sees ? __builtin_nanf("") : 0.0f;
+}
+
+// The same for a page's scales vs (PageRegs::vs) and all tiles; limit as in add_page.
+template <int D, int NT>
+__device__ __forceinline__ void add_nans(const uint32_t (&vs)[8], int g, const int (&limit)[NT],
+                                         Running<D, NT> &st) {
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    bool sees = false;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      sees |= scale_bits(vs[i >> 1], i) >= 0x7F80u && 16 * (i >> 2) + 4 * g + (i & 3) <= limit[n];
+    add_nan(st, n, across_groups_max(sees ? 1.0f : 0.0f) > 0.0f);
+  }
+}
+
 // One page into the running state.  edge (uniform): some of its positions may be
 // hidden from some rows (limit: each row's last visible position less the page's
-// first).
-template <int D, int SPL, int NT, class K, class V, class Q>
+// first).  CHECK: looks for scales that are not finite (otherwise the caller has).
+template <int D, int SPL, int NT, bool CHECK, class K, class V, class Q>
 __device__ __forceinline__ void add_page(K &&k, V &&v, const uint32_t (&vs)[8], Q &&q, int g,
                                          bool edge, const int (&limit)[NT], float c,
                                          Running<D, NT> &st) {
@@ -399,6 +443,8 @@ __device__ __forceinline__ void add_page(K &&k, V &&v, const uint32_t (&vs)[8], 
           if (16 * t + 4 * g + i > limit[n]) s[n][t][i] = -INFINITY;
       }
   }
+  if constexpr (CHECK)
+    if (special_scales<8>(vs)) add_nans<D, NT>(vs, g, limit, st);
   float ref[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
@@ -520,6 +566,17 @@ __device__ __forceinline__ void add_page_packed(const PageRegs<D> &x, Q &&q, int
         asm volatile("" : "+v"(p[u][i]));        // (kept a branch: few pages take it)
         if (16 * (PACK * u + m / W) + 4 * g + i > limit) p[u][i] = -INFINITY;
       }
+  }
+  if (special_scales<2 * U>(x.vs)) {
+    bool sees = false;
+#pragma unroll
+    for (int i = 0; i < 4 * U; ++i)
+      sees |= scale_bits(x.vs[i >> 1], i) >= 0x7F80u &&
+              16 * (PACK * (i >> 2) + m / W) + 4 * g + (i & 3) <= limit;
+    float any = sees ? 1.0f : 0.0f;
+    if constexpr (PACK == 4) any = fmaxf(any, lane_move<ror(4)>(any, any));
+    any = fmaxf(any, lane_move<ror(8)>(any, any));
+    add_nan(st, 0, across_groups_max(any) > 0.0f);
   }
   float top = -INFINITY;
 #pragma unroll
@@ -729,7 +786,7 @@ __global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, RowsView
     const int limit[1] = {ok ? qr.limit - p * kPage : -1};
     const bool edge = !ok || p * kPage + kPage - 1 > all;
     if constexpr (PACK == 1)
-      add_page<D, SPL, 1>(keys_of(x), values_of(x), x.vs, q, g, edge, limit, av.c, st);
+      add_page<D, SPL, 1, true>(keys_of(x), values_of(x), x.vs, q, g, edge, limit, av.c, st);
     else
       add_page_packed<D, SPL, PACK>(
           x, q, g, m, edge, limit[0], av.c,
@@ -916,18 +973,20 @@ __global__ __launch_bounds__(256, OCC) void wide_kernel(CacheView cv, RowsView r
     if (!ok && lane == 0) set_bad(av.status);
     id = p + 1 < p1 ? ld_const(table, p + 1) : 0;
     if (p + 1 < p1) fetch(id);
+    int limit[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) limit[n] = ok ? qr[n].limit - p * kPage : -1;
+    if (special_scales<8>(vs)) add_nans<D, NT>(vs, g, limit, st);
     __syncthreads();
     if (p * kPage <= any) {
-      int limit[NT];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) limit[n] = ok ? qr[n].limit - p * kPage : -1;
       auto k = [&](int t, int e) __attribute__((always_inline)) {
         return sh_k[b][(t * KF + e) * 64 + lane];
       };
       auto v = [&](int hh, int ct) __attribute__((always_inline)) {
         return sh_v[b][(hh * VF + ct) * 64 + lane];
       };
-      add_page<D, SPL, NT>(k, v, vs, q, g, !ok || p * kPage + kPage - 1 > all, limit, av.c, st);
+      add_page<D, SPL, NT, false>(k, v, vs, q, g, !ok || p * kPage + kPage - 1 > all, limit, av.c,
+                                  st);
     }
     if constexpr (BUFS == 1) __syncthreads();
     else b ^= 1;

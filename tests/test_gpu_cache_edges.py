@@ -229,3 +229,34 @@ def test_one_workspace_for_every_smaller_step():
             got.append((out, wout))
         assert all(torch.equal(a, b) for a, b in zip(*got))
         assert bool((buf[size:] == 171).all())
+
+
+# ---- values that are not finite, and the largest -----------------------------
+
+@pytest.mark.parametrize("n", [1, 40], ids=["decode", "chunk"])
+@pytest.mark.parametrize("Hq", [4, 8, 16, 32])
+def test_value_that_is_not_finite_at_a_weight_of_nearly_nothing(Hq, n):
+    """A softmax weight below what fp32 holds is still a weight: what sees the position is NaN, in
+    a full page as in the last one, and what does not see it is not."""
+    D, H, ctx = 64, 2, 200
+    for at in (30, 195, ctx + n // 2):
+        k, v = np.full((1, H, ctx + n, D), -6.0), np.ones((1, H, ctx + n, D))
+        k[:, :, 3] = 6.0                                      # the only one that has any weight
+        v[0, 1, at, 5] = np.nan
+        cache = mcd.Cache.alloc(6, H, D, 1, 5, weights=True)
+        fill(cache, k, v)
+        q = torch.full((n, Hq, D), 2.0, dtype=BF16, device="cuda")
+        rows = make_rows([ctx], [n])
+        out, lse = torch.zeros_like(q), torch.zeros((n, Hq), device="cuda")
+        wout = torch.zeros_like(cache.weight)
+        ws = cache.workspace(rows, Hq)
+        print(f"case nearly no weight Hq={Hq} n={n} at={at}", flush=True)
+        mcd.mcd_cache_attend(cache, rows, q, out, ws, scale=1.0, lse=lse, weight_out=wout)
+        nan = torch.isnan(out).cpu().numpy()
+        sees = ctx + np.arange(n) >= at
+        assert not nan[:, :Hq // 2].any()
+        assert nan[sees][:, Hq // 2:].all() and not nan[~sees].any()
+        assert bool(torch.isfinite(lse).all())
+        w = wout[0, :, :ctx + n].cpu().numpy()
+        want = np.where(np.arange(ctx + n) == 3, n * Hq // H, 0.0)
+        assert (np.abs(w - want) <= 2.0 ** -20 * want).all()
