@@ -483,7 +483,9 @@ typedef struct {
 /* Attention of every new token over its row's cache, causal within the row:
  * token i of row r sees positions 0 .. context[r] + i (append first; context[r]
  * = length - 1 with one token attends over a cache that nothing was appended
- * to).  A token that sees no position (context[r] + i < 0) gets zeros.  Logits,
+ * to).  A token that sees no position (context[r] + i < 0) gets zeros, one that
+ * sees a key or value that is not finite gets NaN.  Values may be as large as
+ * fp32 holds (with logits below 2^29).  Logits,
  * softmax and sums are in fp32; softmax weights enter the product with the
  * values to 16 bits when dtype is MCD_BF16 and to 24 when it is MCD_F32.  The
  * same inputs give the same bits.  q, out and the strides in bytes

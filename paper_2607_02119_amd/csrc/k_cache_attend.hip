@@ -360,17 +360,23 @@ struct Running {
 };
 
 typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
-constexpr uint32_t kSpecialScale = 0x7F80u;      // bfloat16 infinity; NaN above
+// Value scales from 2^64 on are looked at: sums of weights of up to 2^8 might
+// overflow with them though the result does not, so the reference goes kLift
+// (powers of two) above the largest score where a row sees one: weights are then
+// below 2^-56 and sums of 2^30 of them below 2^105.  (A reference of 2^30 and more
+// does not hold the difference.)
+constexpr uint32_t kLargeScale = 0x5F80u, kNanScale = 0x7F80u;   // bfloat16
+constexpr float kLift = 64.0f;
 
 // Whether one of a page's value scales (bfloat16, two to a word, no negative one
-// that is visible) is at least kSpecialScale.  Uniform.
+// that is visible) is at least kLargeScale.  Uniform.
 template <int N, int M>
 __device__ __forceinline__ bool special_scales(const uint32_t (&vs)[M]) {
   ushort2v top = __builtin_bit_cast(ushort2v, vs[0]);
 #pragma unroll
   for (int i = 1; i < N; ++i)
     top = __builtin_elementwise_max(top, __builtin_bit_cast(ushort2v, vs[i]));
-  constexpr unsigned short below = kSpecialScale - 1;
+  constexpr unsigned short below = kLargeScale - 1;
   return __any(__builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(
                    top, ushort2v{below, below})) != 0u);
 }
@@ -395,37 +401,50 @@ __device__ __forceinline__ void move_reference(Running<D, NT> &st, int n, float 
   }
 }
 
-// sees: the lane's query row sees a value that is not finite.  Where its softmax
-// weight is a number of fp32 the product is NaN by itself; where it is not, the
-// product is 0 and the sums become NaN here.
+// A page's scales of kLargeScale and more that the lane's query row of tile n sees
+// (seen: the largest, as bits) where its softmax weight is a number of fp32 a value
+// that is not finite gives NaN by itself; where it is not, the product is 0, and the
+// sums become NaN here.  Returns what to add to the largest score for the
+// reference: uniform.
 template <int D, int NT>
-__device__ __forceinline__ void add_nan(Running<D, NT> &st, int n, bool sees) {
-  if (!__any(sees)) return;
+__device__ __forceinline__ float special_row(Running<D, NT> &st, int n, uint32_t seen, float c) {
+  const bool nan = seen >= kNanScale;
+  if (__any(nan)) {
 #pragma unroll
-  for (int ct = 0; ct < D / 16; ++ct)
-    st.o[n][ct] += sees ? __builtin_nanf("") : 0.0f;
+    for (int ct = 0; ct < D / 16; ++ct) st.o[n][ct] += nan ? __builtin_nanf("") : 0.0f;
+  }
+  return __any(seen >= kLargeScale && !nan) ? fminf(kLift / c, 0x1p126f) : 0.0f;
+}
+__device__ __forceinline__ uint32_t across_groups_max(uint32_t bits) {
+  auto a = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
+  const uint32_t v = max(a[0], a[1]);
+  auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return max(b[0], b[1]);
 }
 
 // The same for a page's scales vs (PageRegs::vs) and all tiles; limit as in add_page.
 template <int D, int NT>
-__device__ __forceinline__ void add_nans(const uint32_t (&vs)[8], int g, const int (&limit)[NT],
-                                         Running<D, NT> &st) {
+__device__ __forceinline__ float special_page(const uint32_t (&vs)[8], int g,
+                                              const int (&limit)[NT], float c,
+                                              Running<D, NT> &st) {
+  float lift = 0.0f;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    bool sees = false;
+    uint32_t seen = 0;
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-      sees |= scale_bits(vs[i >> 1], i) >= 0x7F80u && 16 * (i >> 2) + 4 * g + (i & 3) <= limit[n];
-    add_nan(st, n, across_groups_max(sees ? 1.0f : 0.0f) > 0.0f);
+      if (16 * (i >> 2) + 4 * g + (i & 3) <= limit[n]) seen = max(seen, scale_bits(vs[i >> 1], i));
+    lift = fmaxf(lift, special_row(st, n, across_groups_max(seen), c));
   }
+  return lift;
 }
 
 // One page into the running state.  edge (uniform): some of its positions may be
 // hidden from some rows (limit: each row's last visible position less the page's
-// first).  CHECK: looks for scales that are not finite (otherwise the caller has).
+// first).  lift: special_page's; CHECK: looked for here.
 template <int D, int SPL, int NT, bool CHECK, class K, class V, class Q>
 __device__ __forceinline__ void add_page(K &&k, V &&v, const uint32_t (&vs)[8], Q &&q, int g,
-                                         bool edge, const int (&limit)[NT], float c,
+                                         bool edge, const int (&limit)[NT], float c, float lift,
                                          Running<D, NT> &st) {
   // terms of a softmax weight: 16 bits, so that a bf16 output is off by its own
   // rounding alone; 24 for fp32
@@ -444,7 +463,7 @@ __device__ __forceinline__ void add_page(K &&k, V &&v, const uint32_t (&vs)[8], 
       }
   }
   if constexpr (CHECK)
-    if (special_scales<8>(vs)) add_nans<D, NT>(vs, g, limit, st);
+    if (special_scales<8>(vs)) lift = special_page<D, NT>(vs, g, limit, c, st);
   float ref[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
@@ -453,7 +472,7 @@ __device__ __forceinline__ void add_page(K &&k, V &&v, const uint32_t (&vs)[8], 
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = fmaxf(top, s[n][t][i]);
-    move_reference(st, n, across_groups_max(top), c);
+    move_reference(st, n, across_groups_max(top) + lift, c);
     ref[n] = st.top[n] == -INFINITY ? 0.0f : st.top[n];
     if (__any(fabsf(ref[n]) >= kLargeLogit)) {
       const Origin at = origin_of(st.ref[n], c);
@@ -567,16 +586,16 @@ __device__ __forceinline__ void add_page_packed(const PageRegs<D> &x, Q &&q, int
         if (16 * (PACK * u + m / W) + 4 * g + i > limit) p[u][i] = -INFINITY;
       }
   }
+  float lift = 0.0f;
   if (special_scales<2 * U>(x.vs)) {
-    bool sees = false;
+    uint32_t seen = 0;
 #pragma unroll
     for (int i = 0; i < 4 * U; ++i)
-      sees |= scale_bits(x.vs[i >> 1], i) >= 0x7F80u &&
-              16 * (PACK * (i >> 2) + m / W) + 4 * g + (i & 3) <= limit;
-    float any = sees ? 1.0f : 0.0f;
-    if constexpr (PACK == 4) any = fmaxf(any, lane_move<ror(4)>(any, any));
-    any = fmaxf(any, lane_move<ror(8)>(any, any));
-    add_nan(st, 0, across_groups_max(any) > 0.0f);
+      if (16 * (PACK * (i >> 2) + m / W) + 4 * g + (i & 3) <= limit)
+        seen = max(seen, scale_bits(x.vs[i >> 1], i));
+    if constexpr (PACK == 4) seen = max(seen, lane_move<ror(4)>(seen, seen));
+    seen = max(seen, lane_move<ror(8)>(seen, seen));
+    lift = special_row(st, 0, across_groups_max(seen), c);
   }
   float top = -INFINITY;
 #pragma unroll
@@ -585,7 +604,7 @@ __device__ __forceinline__ void add_page_packed(const PageRegs<D> &x, Q &&q, int
     for (int i = 0; i < 4; ++i) top = fmaxf(top, p[u][i]);
   if constexpr (PACK == 4) top = fmaxf(top, lane_move<ror(4)>(top, top));
   top = fmaxf(top, lane_move<ror(8)>(top, top));
-  move_reference(st, 0, across_groups_max(top), c);
+  move_reference(st, 0, across_groups_max(top) + lift, c);
   float ref = st.top[0] == -INFINITY ? 0.0f : st.top[0];
   if (__any(fabsf(ref) >= kLargeLogit)) {
     const Origin at = origin_of(st.ref[0], c);
@@ -786,7 +805,7 @@ __global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, RowsView
     const int limit[1] = {ok ? qr.limit - p * kPage : -1};
     const bool edge = !ok || p * kPage + kPage - 1 > all;
     if constexpr (PACK == 1)
-      add_page<D, SPL, 1, true>(keys_of(x), values_of(x), x.vs, q, g, edge, limit, av.c, st);
+      add_page<D, SPL, 1, true>(keys_of(x), values_of(x), x.vs, q, g, edge, limit, av.c, 0.0f, st);
     else
       add_page_packed<D, SPL, PACK>(
           x, q, g, m, edge, limit[0], av.c,
@@ -976,7 +995,8 @@ __global__ __launch_bounds__(256, OCC) void wide_kernel(CacheView cv, RowsView r
     int limit[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) limit[n] = ok ? qr[n].limit - p * kPage : -1;
-    if (special_scales<8>(vs)) add_nans<D, NT>(vs, g, limit, st);
+    float lift = 0.0f;
+    if (special_scales<8>(vs)) lift = special_page<D, NT>(vs, g, limit, av.c, st);
     __syncthreads();
     if (p * kPage <= any) {
       auto k = [&](int t, int e) __attribute__((always_inline)) {
@@ -986,7 +1006,7 @@ __global__ __launch_bounds__(256, OCC) void wide_kernel(CacheView cv, RowsView r
         return sh_v[b][(hh * VF + ct) * 64 + lane];
       };
       add_page<D, SPL, NT, false>(k, v, vs, q, g, !ok || p * kPage + kPage - 1 > all, limit, av.c,
-                                  st);
+                                  lift, st);
     }
     if constexpr (BUFS == 1) __syncthreads();
     else b ^= 1;

@@ -260,3 +260,55 @@ def test_value_that_is_not_finite_at_a_weight_of_nearly_nothing(Hq, n):
         w = wout[0, :, :ctx + n].cpu().numpy()
         want = np.where(np.arange(ctx + n) == 3, n * Hq // H, 0.0)
         assert (np.abs(w - want) <= 2.0 ** -20 * want).all()
+
+
+HUGE = [
+    # name, Hq, Hkv, D, dtype, context, new tokens
+    ("decode", 8, 2, 64, BF16, [700, 64, 20, 0], [1, 1, 1, 1]),
+    ("decode_fp32", 4, 2, 128, F32, [700, 64, 20, 0], [1, 1, 1, 1]),
+    ("groups_of_eight", 16, 2, 64, BF16, [700, 64, 20, 0], [1, 1, 1, 1]),
+    ("groups_of_sixteen", 32, 2, 64, BF16, [700, 64, 20, 0], [1, 1, 1, 1]),
+    ("groups_of_sixteen_fp32", 32, 2, 64, F32, [700, 64, 20, 0], [1, 1, 1, 1]),
+    ("wide_heads", 4, 2, 256, BF16, [100, 3], [1, 30]),
+    ("chunks", 8, 2, 128, BF16, [300, 0], [40, 70]),
+    ("chunks_fp32", 4, 2, 64, F32, [300, 0], [40, 70]),
+    ("split_row", 4, 1, 64, BF16, [2600], [1]),
+    ("split_chunk_fp32", 4, 1, 64, F32, [2600], [20]),
+]
+
+
+@pytest.mark.parametrize("where", ["all", "some", "late"])
+@pytest.mark.parametrize("name,Hq,Hkv,D,dtype,ctx,new", HUGE, ids=[a[0] for a in HUGE])
+def test_largest_values(name, Hq, Hkv, D, dtype, ctx, new, where):
+    """Values of up to 6 * 2^125 = 2.6e38, whose weighted sum fits the type though their sum does
+    not: everywhere, at a few positions, and after ordinary ones.  The bounds are those of every
+    other value."""
+    rng = np.random.default_rng(sum(map(ord, name + where)))
+    R, N, L = len(ctx), sum(new), max(c + n for c, n in zip(ctx, new))
+    k = rng.standard_normal((R, Hkv, L, D))
+    v = rng.choice([-6.0, -3, 0, 1, 4, 6], (R, Hkv, L, D), p=[.1, .1, .1, .1, .2, .4])
+    v[..., 0] = 6.0
+    large = {"all": np.ones(L, bool), "some": np.arange(L) % 37 == 5,
+             "late": np.arange(L) >= 0.8 * L}[where]
+    v *= np.where(large, 2.0 ** 125, 1.0)[:, None]
+    cache = mcd.Cache.alloc(R * -(-L // 64) + 1, Hkv, D, R, -(-L // 64) + 1, weights=True)
+    pages, table = fill(cache, k, v)
+    q = rounded(rng.standard_normal((N, Hq, D)) * 2, dtype)
+    rows = make_rows(ctx, new)
+    qt = dev(q).to(dtype)
+    out, wout = torch.zeros_like(qt), torch.zeros_like(cache.weight)
+    lse = torch.zeros((N, Hq), device="cuda")
+    ws = cache.workspace(rows, Hq)
+    print(f"case largest values {name} {where}", flush=True)
+    mcd.mcd_cache_attend(cache, rows, qt, out, ws, scale=0.125, lse=lse, weight_out=wout)
+    got, got_lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    for r in range(R):
+        a, n = starts(new)[r], new[r]
+        kd, vd = slot_kv(pages, table, r, ctx[r] + n, D)
+        o, l, wt, size = ref.attend(kd, vd, q[a:a + n].astype(np.float64), ctx[r], 0.125)
+        to, tw, tl = base.bounds(kd, q[a:a + n], 0.125, dtype, wt, size)
+        assert (np.abs(got[a:a + n] - o) <= to).all(), r
+        w = wout[r, :, :ctx[r] + n].double().cpu().numpy()
+        assert (np.abs(w - wt) <= tw).all()
+        # the logarithm and the reference, both up to 70, cancel: 4 roundings of 2^-18
+        assert (np.abs(got_lse[a:a + n] - l) <= tl + 2.0 ** -22 * np.abs(l) + 2.0 ** -16).all()
