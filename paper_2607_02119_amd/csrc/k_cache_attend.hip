@@ -1094,6 +1094,9 @@ __device__ __forceinline__ void keep_weight(const CacheView &cv, const AttendVie
     av.weight_out[row + pos] = cv.weight ? cv.weight[row + pos] : 0.0f;
 }
 
+// Four of the caller's weights, which may begin at any float (one access all the same).
+typedef float weight4 __attribute__((ext_vector_type(4), aligned(4)));
+
 // Narrow rows, from the scores that narrow_kernel left: 1 KiB of a page of 64
 // tokens and 4 query rows (a quarter of its key codes, or a half for 8 rows).  A
 // wave for four pages, their loads in flight together; bound by HBM: 14 us for 128
@@ -1122,7 +1125,7 @@ __global__ __launch_bounds__(256) void weight_scores_kernel(CacheView cv, RowsVi
       const int p = min(first + k, last);
       s[k][u] = from[(int64_t)p * (256 / PACK) + u * 64];
       const int64_t at = row + p * kPage + 16 * (PACK * u + m / W) + 4 * g;
-      w[k][u] = cv.weight ? *reinterpret_cast<const floatx4 *>(cv.weight + at)
+      w[k][u] = cv.weight ? *reinterpret_cast<const weight4 *>(cv.weight + at)
                           : floatx4{0.0f, 0.0f, 0.0f, 0.0f};
     }
   const float2 st = qr.valid ? av.stats[(int64_t)(sp.t0 + qr.tok) * av.Hq + qr.head]
@@ -1148,7 +1151,7 @@ __global__ __launch_bounds__(256) void weight_scores_kernel(CacheView cv, RowsVi
       }
       if (m % W != 0) continue;
       if (pos + 4 <= sp.len) {
-        *reinterpret_cast<floatx4 *>(av.weight_out + row + pos) = w[k][u];
+        *reinterpret_cast<weight4 *>(av.weight_out + row + pos) = w[k][u];
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)

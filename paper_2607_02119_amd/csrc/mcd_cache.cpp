@@ -44,6 +44,7 @@ mcd_status check_cache(const mcd_cache *c) {
     return bad("cache too large");
   if (!c->pages || !c->table) return bad("null pages or table");
   if (!aligned(c->pages, 16)) return bad("pages must be 16-byte aligned");
+  if (!aligned(c->table, 4) || !aligned(c->weight, 4)) return bad("table or weight not aligned");
   return MCD_OK;
 }
 
@@ -179,6 +180,7 @@ mcd_status mcd_cache_attend(const mcd_cache *c, const mcd_cache_rows *r,
   CHECK(check_dtype(a->dtype));
   if (!heads_ok(a->Hq, c->Hkv)) return bad("Hq=%d is no multiple of Hkv=%d", a->Hq, c->Hkv);
   if (!(a->scale > 0.0f) || !std::isfinite(a->scale)) return bad("scale must be > 0 and finite");
+  if (!aligned(a->weight_out, 4) || !aligned(a->lse, 4)) return bad("weight_out or lse not aligned");
   if (r->n_tokens == 0) {
     if (r->R == 0 || !a->weight_out || a->weight_out == c->weight) return MCD_OK;
     return launched(mcd::launch_cache_keep_weight(view(c), view(r), a->weight_out, stream),

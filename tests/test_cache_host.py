@@ -237,3 +237,12 @@ def test_workspace_of_a_larger_step_serves_smaller_ones():
     # without weights there is no room for scores
     need = size(_cache(weight=None, n_slots=512, max_pages=256), (512, 512, 1, 16384), 8, True)
     assert need < 1 << 24 < size(_cache(n_slots=512, max_pages=256), (512, 512, 1, 16384), 8, True)
+
+
+def test_arrays_that_are_not_aligned_to_their_elements():
+    for b in (dict(weight=FAKE + 2), dict(table=FAKE + 1)):
+        assert _attend(c=_cache(**b)) == mcd.MCD_E_INVALID, b
+        assert _move(mcd._mcd_cache_append, c=_cache(**b)) == mcd.MCD_E_INVALID, b
+        assert _evict(c=_cache(**b)) == mcd.MCD_E_INVALID, b
+    for b in (dict(weight_out=FAKE + 2), dict(lse=FAKE + 3)):
+        assert _attend(**b) == mcd.MCD_E_INVALID, b

@@ -312,3 +312,29 @@ def test_largest_values(name, Hq, Hkv, D, dtype, ctx, new, where):
         assert (np.abs(w - wt) <= tw).all()
         # the logarithm and the reference, both up to 70, cancel: 4 roundings of 2^-18
         assert (np.abs(got_lse[a:a + n] - l) <= tl + 2.0 ** -22 * np.abs(l) + 2.0 ** -16).all()
+
+
+# ---- the caller's buffers ----------------------------------------------------
+
+@pytest.mark.parametrize("Hq", [8, 16, 32])
+def test_weights_that_begin_at_any_float(Hq):
+    """weight and weight_out may be views into larger buffers, at any float."""
+    rng = np.random.default_rng(5)
+    H, D, ctx, new = 2, 64, [300, 64, 5], [1, 1, 1]
+    cache, pages, table, w, _ = make_cache(rng, [c + 1 for c in ctx], H, D, weights=True)
+    rows = make_rows(ctx, new)
+    q = dev(rng.standard_normal((3, Hq, D)).astype(np.float32)).to(BF16)
+    want = None
+    for shift in (0, 1, 2, 3):
+        buf = torch.zeros((2, w.size + 4), device="cuda")
+        win, wout = (b[shift:shift + w.size].view(w.shape) for b in buf)
+        win.copy_(dev(w))
+        here = mcd.Cache(cache.pages, cache.table, D, win)
+        ws = here.workspace(rows, Hq)
+        out = torch.zeros_like(q)
+        print(f"case weights at float {shift} Hq={Hq}", flush=True)
+        mcd.mcd_cache_attend(here, rows, q, out, ws, weight_out=wout)
+        assert mcd.mcd_read_device_status(ws) == 0
+        want = wout.clone() if want is None else want
+        assert torch.equal(wout, want) and torch.equal(win, dev(w))
+        assert bool((buf[:, :shift] == 0).all()) and bool((buf[:, shift + w.size:] == 0).all())
