@@ -468,7 +468,8 @@ typedef struct {
   float scale;               /* > 0, finite: logits are scale * q . k */
   const void *q;             /* [n_tokens][Hq][D], rows q_stride elements apart */
   int64_t q_stride;
-  void *out;                 /* [n_tokens][Hq][D], rows out_stride elements apart */
+  void *out;                 /* [n_tokens][Hq][D], rows out_stride elements apart; q itself, or
+                                apart from it, and apart where there is weight_out */
   int64_t out_stride;
   float *lse;                /* [n_tokens][Hq] or NULL: log of the sum of exp(logits), natural;
                                 -infinity for a token that sees nothing */

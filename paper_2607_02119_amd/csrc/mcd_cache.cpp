@@ -78,6 +78,19 @@ mcd_status check_tokens(const char *name, const void *p, int64_t stride, int64_t
   return MCD_OK;
 }
 
+// Whether n pieces of `bytes` each, a_step apart from a and b_step from b, meet.  (Each
+// array's own pieces lie apart.)
+bool meet(const void *a, int64_t a_step, const void *b, int64_t b_step, int64_t bytes, int64_t n) {
+  uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  if (x + (n - 1) * a_step + bytes <= y || y + (n - 1) * b_step + bytes <= x) return false;
+  for (int64_t i = 0, j = 0; i < n && j < n;) {
+    if (x + bytes <= y) x += a_step, ++i;
+    else if (y + bytes <= x) y += b_step, ++j;
+    else return true;
+  }
+  return false;
+}
+
 mcd_status check_workspace(const void *w, size_t have, size_t need) {
   if (!w || !aligned(w, 256)) return bad("workspace must be 256-byte aligned");
   if (have < need) {
@@ -190,6 +203,13 @@ mcd_status mcd_cache_attend(const mcd_cache *c, const mcd_cache_rows *r,
   if (r->n_tokens * (int64_t)a->Hq > kMost || width > kMost) return bad("too many query rows");
   CHECK(check_tokens("q", a->q, a->q_stride, width, a->dtype));
   CHECK(check_tokens("out", a->out, a->out_stride, width, a->dtype));
+  // a query row is read before its own output is written, and again after it for
+  // the received weight
+  const int64_t eb = a->dtype == MCD_BF16 ? 2 : 4;
+  const bool in_place = a->q == a->out && a->q_stride == a->out_stride && !a->weight_out;
+  if (!in_place && meet(a->q, a->q_stride * eb, a->out, a->out_stride * eb, width * eb,
+                        r->n_tokens))
+    return bad("out must not overlap q%s", a->weight_out ? " with weight_out" : "");
   const mcd::CacheView cv = view(c);
   const mcd::RowsView rv = view(r);
   const mcd::AttendPlan p = mcd::cache_attend_plan(cv, rv, c->D, a->Hq);

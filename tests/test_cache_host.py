@@ -246,3 +246,18 @@ def test_arrays_that_are_not_aligned_to_their_elements():
         assert _evict(c=_cache(**b)) == mcd.MCD_E_INVALID, b
     for b in (dict(weight_out=FAKE + 2), dict(lse=FAKE + 3)):
         assert _attend(**b) == mcd.MCD_E_INVALID, b
+
+
+def test_out_over_the_queries_is_refused():
+    """A query row is read before its own output is written, so out may be q; the received weight
+    is added up from the queries after that."""
+    row = 4 * 128 * 2                                         # bytes of a token
+    for out, stride in ((0, 512), (16, 512), (row - 16, 512), (16 - row, 512), (2 * row, 512),
+                        (2 * row - 16, 1024), (16, 520), (-2 * row + 16, 512)):
+        for q_stride in (512, 520):
+            bad = dict(weight_out=FAKE << 8, q=FAKE << 4, out=(FAKE << 4) + out, out_stride=stride,
+                       q_stride=q_stride)
+            assert _attend(**bad) == mcd.MCD_E_INVALID, (out, stride, q_stride)
+            assert "overlap" in mcd.mcd_last_error()
+            if out or stride != q_stride:
+                assert _attend(**dict(bad, weight_out=None)) == mcd.MCD_E_INVALID

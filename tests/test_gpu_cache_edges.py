@@ -338,3 +338,26 @@ def test_weights_that_begin_at_any_float(Hq):
         want = wout.clone() if want is None else want
         assert torch.equal(wout, want) and torch.equal(win, dev(w))
         assert bool((buf[:, :shift] == 0).all()) and bool((buf[:, shift + w.size:] == 0).all())
+
+
+def test_out_beside_and_in_place_of_the_queries():
+    """q and out may be columns of one buffer; without weight_out they may be the same."""
+    rng = np.random.default_rng(6)
+    H, D, Hq, ctx, new = 2, 64, 8, [300, 0, 5], [1, 40, 1]
+    cache, *_ = make_cache(rng, [c + n for c, n in zip(ctx, new)], H, D, weights=True)
+    rows, N = make_rows(ctx, new), sum(new)
+    buf = torch.zeros((N, 2 * Hq, D), dtype=BF16, device="cuda")
+    q = dev(rng.standard_normal((N, Hq, D)).astype(np.float32)).to(BF16)
+    buf[:, :Hq] = q
+    ws = cache.workspace(rows, Hq)
+    out, wout = torch.zeros_like(q), torch.zeros_like(cache.weight)
+    wout2 = torch.zeros_like(wout)
+    mcd.mcd_cache_attend(cache, rows, q, out, ws, weight_out=wout)
+    mcd.mcd_cache_attend(cache, rows, buf[:, :Hq], buf[:, Hq:], ws, weight_out=wout2)
+    assert torch.equal(buf[:, Hq:], out) and torch.equal(wout, wout2)
+    assert torch.equal(buf[:, :Hq], q)
+    mcd.mcd_cache_attend(cache, rows, buf[:, :Hq], buf[:, :Hq], ws)
+    assert torch.equal(buf[:, :Hq], out)
+    with pytest.raises(mcd.McdError) as e:
+        mcd.mcd_cache_attend(cache, rows, q, q, ws, weight_out=wout)
+    assert e.value.code == mcd.MCD_E_INVALID
