@@ -504,6 +504,8 @@ mcd_status mcd_cache_attend(const mcd_cache *cache, const mcd_cache_rows *rows,
  * so this also gives a Companion a copy of its own.
  *   kept: [R][Hkv][keep] the positions kept, -1 past the row's new length
  *   length_out: [R] min(length[r], keep)
+ * The arrays written must overlap none that the call reads (length_out is not
+ * length; where from and to share weights, no source slot is below R).
  * to->weight may be NULL; from->weight may be NULL when keep >= max_length. */
 typedef struct {
   int32_t R;

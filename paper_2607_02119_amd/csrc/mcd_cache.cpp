@@ -260,6 +260,17 @@ mcd_status mcd_cache_evict(const mcd_cache *from, const mcd_cache *to,
   if (!a->length || !a->kept || !a->length_out) return bad("null array");
   if (!from->weight && a->keep < a->max_length) return bad("eviction needs the cache's weights");
   CHECK(check_workspace(a->workspace, a->workspace_bytes, mcd::kStatusBytes));
+  // every head's workgroup of a row reads its slot and length, one writes length_out
+  const int64_t rows = (int64_t)a->R * 4, most = (int64_t)1 << 60;
+  const int64_t kept = rows * from->Hkv > most / a->keep ? most : rows * from->Hkv * a->keep;
+  const auto apart = [](const int32_t *x, int64_t nx, const int32_t *y, int64_t ny) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(x), q = reinterpret_cast<uintptr_t>(y);
+    return !x || !y || p + nx <= q || q + ny <= p;
+  };
+  if (!apart(a->length_out, rows, a->length, rows) || !apart(a->length_out, rows, a->slot, rows) ||
+      !apart(a->kept, kept, a->length, rows) || !apart(a->kept, kept, a->slot, rows) ||
+      !apart(a->kept, kept, a->length_out, rows))
+    return bad("kept and length_out must overlap neither each other nor length and slot");
   const mcd::EvictView ev{a->R, a->max_length, a->keep, a->recent, a->slot, a->length, a->kept,
                           a->length_out, static_cast<uint32_t *>(a->workspace)};
   return launched(mcd::launch_cache_evict(view(from), view(to), ev, from->D, stream),

@@ -261,3 +261,14 @@ def test_out_over_the_queries_is_refused():
             assert "overlap" in mcd.mcd_last_error()
             if out or stride != q_stride:
                 assert _attend(**dict(bad, weight_out=None)) == mcd.MCD_E_INVALID
+
+
+def test_eviction_in_place_is_refused():
+    """Every head's workgroup reads a row's length and slot, and one of them writes length_out."""
+    at = lambda n: (FAKE << 4) + n  # noqa: E731
+    good = dict(length=at(0), slot=at(12), length_out=at(24), kept=at(36))
+    for b in (dict(length_out=at(0)), dict(length_out=at(-8)), dict(length_out=at(20)),
+              dict(kept=at(8)), dict(kept=at(16)), dict(kept=at(32)), dict(length_out=at(100)),
+              dict(kept=at(40 - 3 * 2 * 64 * 4))):
+        assert _evict(**dict(good, **b)) == mcd.MCD_E_INVALID, b
+        assert "overlap" in mcd.mcd_last_error()
