@@ -81,6 +81,7 @@ class CachedDecode:
         self.next_in = torch.zeros((rows, H), dtype=torch.bfloat16, device=device)   # by slot
         self.null_prompt = null_prompt
         self.workspace = torch.zeros(256, dtype=torch.uint8, device=device)
+        self.reported = 0                      # status bits of workspaces that were replaced
         self.head_workspace = self.head.workspace(rows, device)
         self.frames = 64
         self.grid = torch.full((rows, K, self.frames), -1, dtype=torch.int32, device=device)
@@ -156,6 +157,7 @@ class CachedDecode:
                              max_context=int((context + new).max()))
         need = mcd.mcd_cache_workspace_bytes(self.cache, rows, self.Hq)
         if need > self.workspace.numel():
+            self.reported |= mcd.mcd_read_device_status(self.workspace)
             self.workspace = torch.zeros(2 * need, dtype=torch.uint8, device=self.device)
         mcd.mcd_cache_append(self.cache, rows, k, v, self.workspace)
         mcd.mcd_cache_attend(self.cache, rows, q, out, self.workspace,
@@ -195,7 +197,9 @@ class CachedDecode:
         self.tokens = tokens
 
     def status(self):
-        return mcd.mcd_read_device_status(self.workspace) | \
+        """Device status bits of all steps since the last call."""
+        bits, self.reported = self.reported, 0
+        return bits | mcd.mcd_read_device_status(self.workspace) | \
             mcd.mcd_read_device_status(self.head_workspace)
 
 
