@@ -66,11 +66,11 @@ class CachedDecode:
             return (torch.randn(shape, generator=gen, device=device) * scale).to(torch.bfloat16)
 
         self.W_qkv = normal(H, (Hq + 2 * Hkv) * D, scale=H ** -0.5)
+        self.budget = 8 * rows                 # tokens of a step at most
         self.E, self.E_text = normal(K, V + 1, H, scale=K ** -0.5), normal(V_text, H)
-        self.prompt = normal(4096, H)
+        self.prompt = normal(max(self.budget, 4096), H)
         self.head = mcd.Head(normal(K, V, H, scale=H ** -0.5), np.arange(K), V,
                              W_text=normal(V_text, H, scale=H ** -0.5))
-        self.budget = 8 * rows
         self.sched = mcd.Scheduler(rows, self.budget, null_prompt, K - 1, max_requests=2 * rows)
         # every slot up to its bound and a prompt chunk more, twice over for what moves
         longest = bound + self.budget
