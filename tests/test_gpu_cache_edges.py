@@ -361,3 +361,21 @@ def test_out_beside_and_in_place_of_the_queries():
     with pytest.raises(mcd.McdError) as e:
         mcd.mcd_cache_attend(cache, rows, q, q, ws, weight_out=wout)
     assert e.value.code == mcd.MCD_E_INVALID
+
+
+# ---- every tile of few query rows --------------------------------------------
+
+@pytest.mark.parametrize("weights", [False, True], ids=["plain", "weights"])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("name,Hq,Hkv,ctx,new", [
+    ("three_heads", 3, 1, [2500, 63, 0, 700], [1, 1, 1, 1]),
+    ("five_heads", 10, 2, [2500, 63, 0, 700], [1, 1, 1, 1]),
+    ("eight_heads", 8, 1, [2500, 63, 0, 700], [1, 1, 1, 1]),
+    ("eight_heads_two_tokens", 8, 1, [1300, 62, 0], [2, 2, 1]),
+    ("eleven_heads", 22, 2, [1300, 63, 0], [1, 1, 1]),
+    ("sixteen_heads", 16, 1, [2500, 63, 0, 700], [1, 1, 1, 1]),
+    ("sixteen_heads_beside_a_prompt", 16, 1, [200, 0, 63], [1, 20, 1]),
+])
+def test_narrow_tiles(name, Hq, Hkv, ctx, new, D, dtype, weights):
+    base.test_attend(name, Hq, Hkv, D, dtype, ctx, new, weights)
