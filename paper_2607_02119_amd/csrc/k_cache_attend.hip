@@ -1385,8 +1385,8 @@ void attend_launch(const CacheView &cv, const RowsView &rv, AttendView av, const
     av.part_ml += t.ml_bytes / sizeof(float2);
     av.part_o += t.o_bytes / sizeof(float);
   }
-  if (av.weight_out) {
-    const unsigned pages = (unsigned)plan.score_pages;
+  const unsigned pages = (unsigned)plan.score_pages;
+  if (av.weight_out && pages > 0) {              // (0: no row sees a position)
     if (av.scores) {
       const dim3 grid((pages + 15) / 16, (unsigned)cv.Hkv, (unsigned)rv.R);
       if (plan.pack == 4)

@@ -379,3 +379,20 @@ def test_out_beside_and_in_place_of_the_queries():
 ])
 def test_narrow_tiles(name, Hq, Hkv, ctx, new, D, dtype, weights):
     base.test_attend(name, Hq, Hkv, D, dtype, ctx, new, weights)
+
+
+def test_no_row_sees_a_position():
+    """Rows that see nothing at all: bounds of no position, with every output."""
+    H, D, Hq = 2, 64, 8
+    cache = mcd.Cache.alloc(3, H, D, 2, 2, weights=True)
+    cache.weight.fill_(3.0)
+    for ctx, new in (([-1, -1], [1, 1]), ([-3, -40], [3, 40])):
+        rows, N = make_rows(ctx, new), sum(new)
+        q = torch.ones((N, Hq, D), dtype=BF16, device="cuda")
+        out, lse = torch.full_like(q, 9.0), torch.zeros((N, Hq), device="cuda")
+        wout = torch.full_like(cache.weight, 5.0)
+        ws = cache.workspace(rows, Hq)
+        mcd.mcd_cache_attend(cache, rows, q, out, ws, lse=lse, weight_out=wout)
+        assert mcd.mcd_read_device_status(ws) == 0
+        assert bool((out == 0).all()) and bool(torch.isneginf(lse).all())
+        assert bool((wout == 5.0).all())
