@@ -1245,7 +1245,9 @@ namespace {
 constexpr size_t kMostScores = (size_t)1 << 30;
 
 size_t score_bytes(int64_t R, int64_t Hkv, int64_t pages, int pack) {
-  return (size_t)(R * Hkv * pages) * (64 * 16 / pack) * sizeof(float);
+  // (below 2^56: R, Hkv < 2^16, pages <= 2^24; the bytes may pass 64 bits)
+  const size_t tiles = (size_t)(R * Hkv * pages);
+  return std::min(tiles, kMostScores) * (64 * 16 / pack) * sizeof(float);
 }
 
 // Tiles of `tile` query rows whose pages are split over workgroups until there

@@ -272,3 +272,13 @@ def test_eviction_in_place_is_refused():
               dict(kept=at(40 - 3 * 2 * 64 * 4))):
         assert _evict(**dict(good, **b)) == mcd.MCD_E_INVALID, b
         assert "overlap" in mcd.mcd_last_error()
+
+
+def test_room_for_scores_beyond_64_bits():
+    """65531 rows x 65454 heads x 12599637 pages x 1 KiB wrap to 361 MiB in 64 bits: rows within
+    these bounds keep scores of up to 1 GiB, and more are not kept."""
+    rows = dict(R=65531, n_tokens=1, max_tokens=1, max_context=12599637 * 64, start=FAKE)
+    a, b = (mcd._mcd_cache_workspace_bytes(
+        ctypes.byref(_cache(Hkv=65454, D=64, n_slots=65531, max_pages=12599637, weight=w)),
+        ctypes.byref(_rows(**rows)), 65454) for w in (FAKE, None))
+    assert b > 0 and a - b == 1 << 30
