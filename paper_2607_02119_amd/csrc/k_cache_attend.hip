@@ -820,10 +820,7 @@ __global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, RowsView
   unpack_rows<D, SPL, PACK>(st);
 
   // the waves' sums, to their largest reference
-  if (g == 0 && m < W) {
-    sh_ml[0][wave][m] = st.ref[0];
-    sh_ml[1][wave][m] = st.sum[0];
-  }
+  if (g == 0 && m < W) sh_ml[0][wave][m] = st.ref[0];
   __syncthreads();
   if (m < W) {
     float top = -INFINITY;
@@ -832,6 +829,7 @@ __global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, RowsView
     const float f = st.ref[0] == -INFINITY
                         ? 0.0f
                         : __builtin_amdgcn_exp2f(origin_gap(st.ref[0], top, av.c));
+    if (g == 0) sh_ml[1][wave][m] = st.sum[0] * f;
 #pragma unroll
     for (int c = 0; c < D / 16; ++c)
       *reinterpret_cast<floatx4 *>(sh_o + (wave * W + m) * PITCH + g * (D / 4) + 4 * c) =
@@ -848,9 +846,7 @@ __global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, RowsView
     floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < WAVES; ++k) {
-      const float mk = sh_ml[0][k][row];
-      l += sh_ml[1][k][row] *
-           (mk == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(origin_gap(mk, top, av.c)));
+      l += sh_ml[1][k][row];
       acc += *reinterpret_cast<const floatx4 *>(sh_o + (k * W + row) * PITCH + c4);
     }
     if (used > 1) {
