@@ -531,9 +531,9 @@ __device__ __forceinline__ void add_page(K &&k, V &&v, const uint32_t (&vs)[8], 
 // the end.  (Where the third term of fp32 finds no column it takes an
 // instruction of its own.)  32 matrix instructions for a page of 64 tokens and 128
 // channels, where full tiles take 48, and fewer vector ones.  512 rows of 100 to
-// 1100 positions, 32 query and 8 K/V heads of 128: 65 us for four tiles side by
-// side, 67 for two, 87 for one; 256 rows of 8 query heads a K/V head: 36 for two,
-// 49 for one.
+// 1100 positions, 32 query and 8 K/V heads of 128: 66 us for four tiles side by
+// side, 68 for two, 78 for one; 256 rows of 8 query heads a K/V head: 38.5 for
+// two, 44 for one.
 
 // Value scales of tokens 16 t + 4 g + i as bfloat16 i, t the lane's tile of each
 // of the 4 / PACK registers' worth.
@@ -735,7 +735,7 @@ __device__ __forceinline__ void write_row(const AttendView &av, const Span &sp, 
 // pages dealt out to the waves, whose sums meet in LDS.  HBM bounds it; four
 // waves on a SIMD, each waiting for a page of its own or working on one, keep
 // the loads going (three or two waves that load a page ahead were slower).  512
-// rows of 100 to 1100 positions (8 K/V heads of 128, 341 MB): 61 us, 5.6 TB/s,
+// rows of 100 to 1100 positions (8 K/V heads of 128, 341 MB): 62 us, 5.5 TB/s,
 // where a plain read reaches 6.4.
 template <int D, int SPL, int PACK, int OCC>
 __global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, RowsView rv,
@@ -872,8 +872,10 @@ __global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, RowsView
 // instructions and the softmax's vector work take about as long as each other;
 // two workgroups on a compute unit overlap them (one of eight waves was slower,
 // 785 against 753 us).  Four rows of 2048 new tokens over up to 4096 positions (32
-// query and 8 K/V heads of 128): 719 us, 0.77 PFLOP/s, the matrix units busy half
-// of the time; the values' second term is a third of their work.
+// query and 8 K/V heads of 128): 723 us, 0.77 PFLOP/s (849 in the first passes
+// after a pause; the clock settles in 40), the matrix units busy half of the time;
+// the values' second term is a third of their work.  The look at the scales stands
+// before the barrier: within the page's pass it cost 10 to 20 us more.
 template <int D, int SPL, int NT, int OCC>
 __global__ __launch_bounds__(256, OCC) void wide_kernel(CacheView cv, RowsView rv, AttendView av) {
   constexpr int TQ = 64 * NT, KF = D / 32, VF = D / 16;    // key operands of a tile, value of a half
@@ -1095,7 +1097,7 @@ typedef float weight4 __attribute__((ext_vector_type(4), aligned(4)));
 
 // Narrow rows, from the scores that narrow_kernel left: 1 KiB of a page of 64
 // tokens and 4 query rows (a quarter of its key codes, or a half for 8 rows).  A
-// wave for four pages, their loads in flight together; bound by HBM: 14 us for 128
+// wave for four pages, their loads in flight together; bound by HBM: 15 us for 128
 // rows of 900 to 4500 positions.
 template <int PACK>
 __global__ __launch_bounds__(256) void weight_scores_kernel(CacheView cv, RowsView rv,
@@ -1161,9 +1163,10 @@ __global__ __launch_bounds__(256) void weight_scores_kernel(CacheView cv, RowsVi
 // there are wide rows): the waves of a workgroup take a page's query tiles in
 // turn and their sums meet in LDS, in the same order always; otherwise a wave for
 // each page.  Bound by the chain of its query loads: 21 rows of up to 820
-// positions and 5 prompts with 8 query heads a K/V head of 64 channels took 201 us
-// (the whole call) with a wave for each page, 69 with eight.  (Of the widest rows'
-// operands eight waves spill: four.)
+// positions and 5 prompts with 8 query heads on one K/V head of 64 channels took
+// 145 us (the whole call) with a wave for each page, 52 with eight.  (Of 256
+// channels' fp32 operands eight waves spill: 394 us for 4 chunks of 400 to 512
+// tokens, 424 with eight.)
 constexpr int weight_waves(int D, int SPL) { return D * SPL > 384 ? 4 : 8; }
 
 template <int D, int SPL, bool SHARED>
@@ -1237,7 +1240,7 @@ void weight_kernel(CacheView cv, RowsView rv, AttendView av) {
 namespace {
 
 // Kept scores at most; larger steps compute them again (128 rows of 900 to 4500
-// positions: 104 us with the scores kept, 152 without).
+// positions: 105 us with the scores kept, 152 without).
 constexpr size_t kMostScores = (size_t)1 << 30;
 
 size_t score_bytes(int64_t R, int64_t Hkv, int64_t pages, int pack) {
@@ -1247,12 +1250,20 @@ size_t score_bytes(int64_t R, int64_t Hkv, int64_t pages, int pack) {
 }
 
 // Tiles of `tile` query rows whose pages are split over workgroups until there
-// are `want` of them, in splits of at least `least` pages.  512 workgroups, two on
-// a compute unit, are the best of 256 / 512 / 1024 both for narrow rows (8 of up to
-// 16 k positions: 32.7 / 26.5 / 29.7 us; 64 of up to 3000: 31.5 / 31.7 / 36.7) and
-// for wide ones (2 of 512 tokens over 4 k: 178 / 124 / 143; 9 of 150 to 357 over up
-// to 3 k: 97 / 78 / 77).  Least splits: of narrow rows 8 pages (one row of 4000
-// positions 11.1 us, 16 pages 12.9, 4 pages 11.2), of wide ones 4 (8: no change).
+// are kWantGroups of them, in splits of at least `least` pages.  512 workgroups, two
+// on a compute unit, against 256 and 1024: narrow rows, 8 of up to 16 k positions
+// 28.6 us, 36.7 and 31.6, 64 of up to 3000 32.7, 32.4 and 37.6; wide ones, 2 of 512
+// tokens over 4 k 129, 181 and 147, 9 of 150 to 357 over up to 3 k 79, 99 and 79.
+// Least splits of narrow rows 8 pages: one row of 4000 positions 11.8 us, 16 pages
+// 14.0, 4 pages 10.8.  Rows of up to kWholeNarrow pages are not split, for the
+// join's launch costs more: in us, whole and in splits of 8 pages,
+//   pages              11            16            24            32
+//   1 row          8.3  11.3    10.1  11.9    12.9  12.1    15.2  11.6
+//   8 rows         9.2  12.2    10.4  12.4    13.1  12.6    16.0  12.1
+//   37 rows       11.6  15.8    14.0  16.0    17.9  19.4    21.6  23.4
+// (64 rows alike).  Least splits of wide rows 4 pages: one of 500 tokens over 3.4 k
+// positions 26.3, 8 pages 30.3; but 49 of 2 to 5 tokens over 270 positions, which
+// that makes two splits of, 29 and 15.6.
 constexpr int64_t kWantGroups = 512, kLeastNarrow = 8, kWholeNarrow = 16, kLeastWide = 4;
 
 TilePlan tile_plan(int32_t tile, int64_t tiles, int64_t pages, int Hkv, int D, int64_t least) {
@@ -1288,15 +1299,13 @@ AttendPlan cache_attend_plan(const CacheView &cv, const RowsView &rv, int D, int
   const int64_t rows = wide ? G : (int64_t)rv.max_tokens * G;
   p.pack = rows <= 4 ? 4 : rows <= 8 ? 2 : 1;
   p.narrow_rows = narrow ? 16 / p.pack : 0;
-  // (of up to 16 pages not split: the join's launch costs more, 37 rows of up to
-  // 1003 positions 9.2 us, in two splits 11.2)
   if (narrow)
     p.narrow = tile_plan(16 / p.pack, rv.R, pages, cv.Hkv, D,
                          pages <= kWholeNarrow ? kWholeNarrow : kLeastNarrow);
   if (wide) {
     // steps of short chunks in tiles of 64 rows: 52 rows of 2 to 12 tokens of four
-    // heads (fp32, up to 2221 positions) 208 -> 85 us, 49 of 2 to 5 (bf16, 270)
-    // 38 -> 31
+    // heads (fp32, up to 2221 positions) 34 us, in tiles of 128 43; 49 of 2 to 5
+    // (bf16, 270) 29 and 37
     const int tile = D == 256 || (int64_t)rv.max_tokens * G <= 64 ? 64 : 128;
     p.wide = tile_plan(tile, tile_items(rv.R, rv.N, G, tile, rv.start == nullptr), pages, cv.Hkv, D,
                        kLeastWide);
@@ -1350,7 +1359,9 @@ template <int D, int SPL, int PACK>
 void narrow_launch(const CacheView &cv, const RowsView &rv, const AttendView &av, const dim3 &grid,
                    hipStream_t st) {
   // registers for four waves on a SIMD; a single tile of 128 channels spilled there
-  // (256 rows, 16 query heads a K/V head: 50 us, with three 44)
+  // (256 rows, 16 query heads a K/V head: 53 us, with three 47.5).  256 channels, 128
+  // rows of 100 to 1100 positions, 4 query heads a K/V head: bf16 with two 27 us,
+  // with one 37, with three (spills) 40; fp32 with one 46.5, with two 31.
   constexpr int OCC = D * SPL > 384 ? 1 : D * SPL > 128 ? 2 : PACK == 1 ? 3 : 4;
   hipLaunchKernelGGL((narrow_kernel<D, SPL, PACK, OCC>), grid, dim3(256), 0, st, cv, rv, av);
 }
@@ -1364,6 +1375,9 @@ void attend_launch(const CacheView &cv, const RowsView &rv, AttendView av, const
     av.splits = t.splits;
     av.split_pages = t.split_pages;
     const dim3 grid((unsigned)(t.tiles * t.splits * cv.Hkv));
+    // (workgroups on a compute unit of 256 channels, 4 chunks of 400 to 512 tokens: bf16
+    // two 127 us, one 195; fp32 one 239, two, with 12 registers spilled, 171.  Of 128
+    // channels in fp32: one 146, two 150.)
     if (!narrow && t.tile == 64)
       hipLaunchKernelGGL((wide_kernel<D, SPL, 1, (D * SPL > 384 ? 1 : 2)>), grid, dim3(256), 0, st,
                          cv, rv, av);
