@@ -262,13 +262,17 @@ __device__ __forceinline__ void load_queries(const AttendView &av, const Span &s
 }
 
 // Items of a K/V head: tiles of TQ query rows, at most tokens G / TQ + 1 of a
-// row, so row r's begin at start[r] G / TQ + r.
+// row, so row r's begin at start[r] G / TQ + r.  each: rows of at most a token, and
+// as many tokens: every row's tiles side by side, with no search for the row.
+__host__ __device__ inline bool token_each(const RowsView &rv) {
+  return rv.max_tokens == 1 && rv.N == rv.R;
+}
 __host__ __device__ inline int64_t tile_items(int32_t R, int32_t N, int32_t G, int TQ, bool each) {
   return each ? (int64_t)R * ((G + TQ - 1) / TQ) : (int64_t)N * G / TQ + R;
 }
 
 __device__ __forceinline__ int tile_row(const RowsView &rv, int G, int TQ, int64_t x, int &tile) {
-  if (!rv.start) {
+  if (token_each(rv)) {
     const int per = (G + TQ - 1) / TQ;
     tile = (int)(x % per);
     return (int)(x / per);
@@ -1307,7 +1311,7 @@ AttendPlan cache_attend_plan(const CacheView &cv, const RowsView &rv, int D, int
     // heads (fp32, up to 2221 positions) 34 us, in tiles of 128 43; 49 of 2 to 5
     // (bf16, 270) 29 and 37
     const int tile = D == 256 || (int64_t)rv.max_tokens * G <= 64 ? 64 : 128;
-    p.wide = tile_plan(tile, tile_items(rv.R, rv.N, G, tile, rv.start == nullptr), pages, cv.Hkv, D,
+    p.wide = tile_plan(tile, tile_items(rv.R, rv.N, G, tile, token_each(rv)), pages, cv.Hkv, D,
                        kLeastWide);
   }
   p.stat_bytes = (size_t)rv.N * Hq * sizeof(float2);

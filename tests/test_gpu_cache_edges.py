@@ -95,10 +95,11 @@ def test_large_logits(name, Hq, Hkv, D, dtype, ctx, new):
 
 # ---- start is read when the kernels run --------------------------------------
 
-def test_replay_with_idle_rows():
+@pytest.mark.parametrize("Hq", [8, 80], ids=["narrow", "wide"])
+def test_replay_with_idle_rows(Hq):
     """A decode step (append, read, attention with weights) captured with a token in every row and
     replayed while some rows are idle: equal starts, fewer tokens than the call's bound."""
-    D, Hq, H, R = 64, 8, 2, 4
+    D, H, R = 64, 2, 4
     rng = np.random.default_rng(31)
     ctx0 = [130, 62, 63, 300]
     cache, pages, table, w, _ = make_cache(rng, [c + 3 for c in ctx0], H, D, weights=True)
