@@ -397,3 +397,74 @@ def test_no_row_sees_a_position():
         assert mcd.mcd_read_device_status(ws) == 0
         assert bool((out == 0).all()) and bool(torch.isneginf(lse).all())
         assert bool((wout == 5.0).all())
+
+
+# ---- the types' whole range --------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("n", [1, 90], ids=["one", "chunk"])
+def test_append_over_the_types_range(n, dtype):
+    """Keys and values from the smallest subnormal numbers to the largest, bytes and values."""
+    rng = np.random.default_rng(n)
+    D, H, R = 64, 2, 60 if n == 1 else 2
+    ctx, new = [int(c) for c in rng.integers(0, 70, R)], [n] * R
+    cache, pages, table, _, _ = make_cache(rng, [c + n for c in ctx], H, D)
+    N = R * n
+    with np.errstate(over="ignore"):
+        x = (rng.uniform(1, 2, (N, 2 * H, D)) * rng.choice([-1, 1], (N, 2 * H, D))
+             * np.exp2(rng.integers(-3, 1, (N, 2 * H, D)))).astype(np.float64) \
+            * np.exp2(rng.integers(-149, 128, (N, 2 * H, 1)).astype(np.float64))
+        x = rounded(np.clip(x, -3.38e38, 3.38e38), dtype)
+    x[0] = np.float32(1e-45) if dtype == F32 else rounded(9.2e-41, dtype)
+    t = dev(x).to(dtype)
+    assert torch.equal(t.float().cpu(), torch.from_numpy(x))
+    ws = torch.zeros(256, dtype=torch.uint8, device="cuda")
+    rows = make_rows(ctx, new)
+    print(f"case append range n={n} {dtype}", flush=True)
+    mcd.mcd_cache_append(cache, rows, t[:, :H], t[:, H:], ws)
+    kr, vr = (torch.full((N, H, D), 7.0, device="cuda") for _ in range(2))
+    mcd.mcd_cache_read(cache, rows, kr, vr, ws)
+    got_k, got_v = kr.cpu().numpy(), vr.cpu().numpy()
+    for r in range(R):
+        for i in range(n):
+            pos, tok = ctx[r] + i, starts(new)[r] + i
+            for h in range(H):
+                page = pages[table[r, pos // 64], h]
+                ref.put(page, D, pos % 64, x[tok, h], x[tok, H + h])
+                k, v = ref.get(page, D, pos % 64)
+                assert np.array_equal(got_k[tok, h], k.astype(np.float32)), (tok, h)
+                assert np.array_equal(got_v[tok, h], v.astype(np.float32)), (tok, h)
+    assert np.array_equal(cache.pages.cpu().numpy(), pages)
+
+
+@pytest.mark.parametrize("ks,vs", [(-90, -90), (100, 60), (-60, 63), (90, 64), (-100, 124)])
+@pytest.mark.parametrize("name,Hq,dtype,ctx,new", [
+    ("decode", 8, BF16, [700, 20], [1, 1]), ("decode_fp32", 8, F32, [700, 20], [1, 1]),
+    ("chunk", 4, BF16, [300, 0], [30, 9]), ("chunk_fp32", 4, F32, [300, 0], [30, 9]),
+])
+def test_small_and_large_keys_and_values(name, Hq, dtype, ctx, new, ks, vs):
+    """Keys times 2^ks with queries times 2^-ks, values times 2^vs: powers of two change nothing,
+    so the bounds are those of ordinary numbers, times 2^vs."""
+    rng = np.random.default_rng(sum(map(ord, name)))
+    R, N, L, H, D = len(ctx), sum(new), max(c + n for c, n in zip(ctx, new)), 2, 64
+    k, v = (rng.standard_normal((R, H, L, D)) for _ in range(2))
+    cache = mcd.Cache.alloc(R * -(-L // 64) + 1, H, D, R, -(-L // 64) + 1, weights=True)
+    pages, table = fill(cache, k * 2.0 ** ks, v * 2.0 ** vs)
+    q = rounded(rng.standard_normal((N, Hq, D)) * 2.0, dtype)
+    rows = make_rows(ctx, new)
+    qt = dev(q * np.float32(2.0 ** -ks)).to(dtype)
+    out, wout = torch.zeros_like(qt), torch.zeros_like(cache.weight)
+    ws = cache.workspace(rows, Hq)
+    print(f"case small and large {name} {ks} {vs}", flush=True)
+    mcd.mcd_cache_attend(cache, rows, qt, out, ws, scale=0.125, weight_out=wout)
+    assert mcd.mcd_read_device_status(ws) == 0
+    got = out.double().cpu().numpy()
+    for r in range(R):
+        a, n = starts(new)[r], new[r]
+        kd, vd = slot_kv(pages, table, r, ctx[r] + n, D)
+        kd, vd = kd * 2.0 ** -ks, vd * 2.0 ** -vs
+        o, _, wt, size = ref.attend(kd, vd, q[a:a + n].astype(np.float64), ctx[r], 0.125)
+        to, tw, _ = base.bounds(kd, q[a:a + n], 0.125, dtype, wt, size)
+        assert (np.abs(got[a:a + n] * 2.0 ** -vs - o) <= to).all(), r
+        w = wout[r, :, :ctx[r] + n].double().cpu().numpy()
+        assert (np.abs(w - wt) <= tw).all()
