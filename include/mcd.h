@@ -473,7 +473,7 @@ typedef struct {
   int64_t out_stride;
   float *lse;                /* [n_tokens][Hq] or NULL: log of the sum of exp(logits), natural;
                                 -infinity for a token that sees nothing */
-  float *weight_out;         /* NULL, or laid out as cache->weight (which it may be): receives
+  float *weight_out;         /* NULL, or laid out as cache->weight (it, or apart from it): receives
                                 cache->weight (0 where that is NULL) plus, at every position of
                                 the rows' slots (of rows without a token too), the softmax weight
                                 summed over the row's tokens and the query heads of the K/V head */

@@ -194,6 +194,12 @@ mcd_status mcd_cache_attend(const mcd_cache *c, const mcd_cache_rows *r,
   if (!heads_ok(a->Hq, c->Hkv)) return bad("Hq=%d is no multiple of Hkv=%d", a->Hq, c->Hkv);
   if (!(a->scale > 0.0f) || !std::isfinite(a->scale)) return bad("scale must be > 0 and finite");
   if (!aligned(a->weight_out, 4) || !aligned(a->lse, 4)) return bad("weight_out or lse not aligned");
+  // (at most 2^31 slots x 2^16 heads x 2^30 positions: counted in double)
+  const double weights = 4.0 * c->n_slots * c->Hkv * c->max_pages * MCD_CACHE_PAGE;
+  const double apart = std::fabs((double)reinterpret_cast<uintptr_t>(a->weight_out) -
+                                 (double)reinterpret_cast<uintptr_t>(c->weight));
+  if (a->weight_out && c->weight && apart > 0.0 && apart < weights)
+    return bad("weight_out must be the cache's weight or apart from it");
   if (r->n_tokens == 0) {
     if (r->R == 0 || !a->weight_out || a->weight_out == c->weight) return MCD_OK;
     return launched(mcd::launch_cache_keep_weight(view(c), view(r), a->weight_out, stream),

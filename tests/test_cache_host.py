@@ -282,3 +282,13 @@ def test_room_for_scores_beyond_64_bits():
         ctypes.byref(_cache(Hkv=65454, D=64, n_slots=65531, max_pages=12599637, weight=w)),
         ctypes.byref(_rows(**rows)), 65454) for w in (FAKE, None))
     assert b > 0 and a - b == 1 << 30
+
+
+def test_weight_out_beside_the_weights_is_refused():
+    """In place or apart: shifted, one position's sum would be another's start."""
+    size = 3 * 2 * 4 * 64 * 4
+    for shift in (4, -4, 256, size - 4, 4 - size):
+        at = dict(c=_cache(weight=FAKE << 8), weight_out=(FAKE << 8) + shift, q=FAKE, out=FAKE << 4)
+        assert _attend(**at) == mcd.MCD_E_INVALID, shift
+        assert "apart" in mcd.mcd_last_error()
+        assert _attend(r=_rows(R=3, n_tokens=0, max_tokens=0, start=FAKE), **at) == mcd.MCD_E_INVALID
