@@ -1,0 +1,579 @@
+"""Several continuations of one prompt, and how good each of them is: what a serving program has
+this library do around the decode head when it samples a prompt more than once (the candidates of a
+guided request, the best of n, many questions about one document).
+
+  tables     the page table of the 4-bit key/value cache, kept on the GPU: rows give back the pages
+             past a length, take over the whole pages of another slot's prefix, and get pages for
+             their new tokens, the free pages with the lowest ids in the rows' order; the tokens'
+             packed offsets, rows, positions and places in the pages
+  attend     out = softmax(scale q k^T) v for every new token over its row's cache, causal, where
+             the rows of a group begin with the same pages, read once for all of them
+  logprobs   log softmax of given tokens, the entropy of their distributions and the most likely
+             ids with their log probabilities, over the head's scores or other logits
+
+A page holds 64 tokens' keys and values of every K/V head in 4 bits (e2m1: 0, 1/2, 1, 3/2, 2, 3, 4,
+6 and a sign), keys with a power of two for every token and 32 channels, values with a bfloat16
+for every token.
+
+``own`` says which side runs: the library's kernels, or elementary torch operations in 32 bits.
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import numpy as np
+import torch
+
+own = False
+
+PAGE = 64                      # tokens of a page
+MAX_SEQ = 16384                # longest sequence that the repository's baseline serves
+
+
+# ---- cases -----------------------------------------------------------------
+
+def _tables(name, rows, lo, hi, ctx_lo, ctx_hi, groups=0):
+    """rows get lo to hi tokens after ctx_lo to ctx_hi positions: of their own, or (groups) the
+    whole pages of one of `groups` prompts, as rows that begin anew."""
+    return dict(name=name, kind="tables", rows=rows, lo=lo, hi=hi, ctx_lo=ctx_lo, ctx_hi=ctx_hi,
+                groups=groups)
+
+
+def _attend(name, groups, rows_lo, rows_hi, prefix_lo, prefix_hi, own_lo, own_hi, lo=1, hi=1,
+            Hq=32, Hkv=8, D=128, dtype="bf16"):
+    """groups of rows_lo to rows_hi rows with one prefix; each row has own_lo to own_hi positions
+    more and lo to hi new tokens."""
+    return dict(name=name, kind="attend", groups=groups, rows_lo=rows_lo, rows_hi=rows_hi,
+                prefix_lo=prefix_lo, prefix_hi=prefix_hi, own_lo=own_lo, own_hi=own_hi, lo=lo,
+                hi=hi, Hq=Hq, Hkv=Hkv, D=D, dtype=dtype)
+
+
+def _logprobs(name, n, K, V, top, dtype="fp32", V0=0, masked=0.0, pairs=False):
+    """n rows of K vectors of V logits (the first of V0, where that is not 0), the `top` most
+    likely ids; masked: share of the ids that a vocabulary mask rules out; pairs: the tokens stand
+    in a batch of Main and Companion rows, in the Main rows."""
+    return dict(name=name, kind="logprobs", n=n, K=K, V=V, V0=V0, top=top, dtype=dtype,
+                masked=masked, pairs=pairs)
+
+
+def listed():
+    return [
+        # one more token for every row of the scheduler's 512-row batch
+        _tables("tables_step", 512, 1, 1, 100, 1100),
+        # 32 prompts, 2048 candidates that begin anew on their pages: 1000 slots' worth of pages
+        # given back and taken again
+        _tables("tables_candidates", 2048, 1, 300, 500, 2500, groups=32),
+        # one request's 8 candidates: latency only
+        _attend("attend_candidates", 1, 8, 8, 1000, 1000, 0, 60, Hq=16, Hkv=8),
+        # a batch of 16 prompts with up to 16 candidates each
+        _attend("attend_groups", 16, 4, 16, 500, 4000, 1, 600),
+        # 64 rows on the longest prompt that is served
+        _attend("attend_long", 1, 64, 64, 16000, 16000, 1, 380),
+        # fp32 parity runs: odd head counts, groups of one row, prefixes of less than a page
+        _attend("attend_odd_fp32", 9, 1, 7, 0, 1003, 0, 137, 1, 3, Hq=25, Hkv=5, D=64,
+                dtype="fp32"),
+        # 20 questions about one document, as prompt chunks: matrix products bound it
+        _attend("attend_chunks", 1, 20, 20, 8192, 8192, 0, 0, 100, 400),
+        # a step's scores: 64 guided pairs, 8 codebooks of 4096
+        _logprobs("logprobs_step", 64, 8, 4096, 5, pairs=True),
+        # 512 rows of 16 codebooks of 1024: no alternatives
+        _logprobs("logprobs_wide", 512, 16, 1024, 0),
+        # one row of nine streams, the first twice as large
+        _logprobs("logprobs_one", 1, 9, 1024, 3, V0=2048),
+        # the text rows of a step, an audio region masked, twenty alternatives
+        _logprobs("logprobs_text", 24, 1, 151936, 20, masked=0.03),
+        # a prompt's tokens scored, as bfloat16 logits: many ties
+        _logprobs("logprobs_prompt", 1024, 1, 151936, 1, dtype="bf16"),
+    ]
+
+
+def _log(rng, lo, hi):
+    """A whole number between lo and hi, even over its logarithm."""
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["tables", "attend", "attend", "attend", "logprobs", "logprobs"])
+    if kind == "tables":
+        rows, hi = _log(rng, 1, 2048), _log(rng, 1, 400)
+        ctx = _log(rng, 1, 4000)
+        case = _tables("", rows, rng.randint(0, hi), hi, rng.randint(0, ctx), ctx,
+                       rng.choice([0, 0, 1, rng.randint(1, min(rows, 64))]))
+    elif kind == "attend":
+        form = rng.choice(["step", "step", "chunk"])
+        D, Hkv = rng.choice([64, 128, 128, 256]), rng.choice([1, 2, 5, 8])
+        G = rng.choice([1, 2, 4, 5, 8])
+        dtype = rng.choice(["bf16", "bf16", "fp32"])
+        rows_hi = _log(rng, 1, 64)
+        groups = _log(rng, 1, max(1, min(32, 256 // rows_hi)))
+        if form == "step":
+            prefix = _log(rng, 8, min(MAX_SEQ, 131072 // groups))
+            case = _attend("", groups, rng.randint(1, rows_hi), rows_hi, rng.randint(0, prefix),
+                           prefix, 0, _log(rng, 1, 700), 1, rng.choice([1, 1, 4]),
+                           min(G, 1024 // D) * Hkv, Hkv, D, dtype)
+        else:
+            hi = _log(rng, 2, max(2, min(400, 4000 // (groups * rows_hi))))
+            prefix = _log(rng, 8, 4096)
+            case = _attend("", groups, rng.randint(1, rows_hi), rows_hi, rng.randint(0, prefix),
+                           prefix, 0, _log(rng, 1, 500), rng.randint(1, hi), hi,
+                           min(G, 4) * Hkv, Hkv, min(D, 128), dtype)
+    else:
+        dtype = rng.choice(["fp32", "fp32", "bf16"])
+        top = rng.choice([0, 1, 2, 5, 10, 20, 32])
+        if rng.random() < 0.6:
+            K = rng.choice([1, 4, 8, 9, 16])
+            case = _logprobs("", _log(rng, 1, 512), K, _log(rng, 2, 4096), top, dtype,
+                             rng.choice([0, 0, rng.randint(2, 4096)]), 0.0, rng.random() < 0.5)
+        else:
+            V = _log(rng, 4097, 200000)
+            case = _logprobs("", _log(rng, 1, min(1024, 75000000 // V)), 1, V, top, dtype, 0,
+                             rng.choice([0.0, 0.03, 0.5]))
+    del case["name"]
+    return case
+
+
+def _counts(case):
+    """Host numbers of a case, the same for every seed: for tables contexts and new tokens; for
+    attend the groups' rows and prefixes, contexts and new tokens of the rows."""
+    rng = random.Random(" ".join(str(v) for k, v in sorted(case.items()) if k != "name"))
+    if case["kind"] == "tables":
+        groups = case["groups"]
+        base = [rng.randint(case["ctx_lo"], case["ctx_hi"]) for _ in range(groups or case["rows"])]
+        of = [rng.randrange(groups) for _ in range(case["rows"])] if groups else None
+        ctx = [base[g] // PAGE * PAGE for g in of] if groups else base
+        new = [rng.randint(case["lo"], case["hi"]) for _ in ctx]
+        new[rng.randrange(len(new))] = case["hi"]
+        return np.array(ctx), np.array(new), np.array(base), of and np.array(of)
+    size = [rng.randint(case["rows_lo"], case["rows_hi"]) for _ in range(case["groups"])]
+    size[rng.randrange(len(size))] = case["rows_hi"]
+    prefix = [rng.randint(case["prefix_lo"], case["prefix_hi"]) for _ in size]
+    prefix[rng.randrange(len(size))] = case["prefix_hi"]
+    of = np.repeat(np.arange(len(size)), size)
+    ctx = np.array([prefix[g] + rng.randint(case["own_lo"], case["own_hi"]) for g in of])
+    new = np.array([rng.randint(case["lo"], case["hi"]) for _ in of])
+    return np.array(size), np.array(prefix), of, ctx, new
+
+
+def _streams(case):
+    return [case["V0"] or case["V"]] + [case["V"]] * (case["K"] - 1)
+
+
+def work(case):
+    if case["kind"] == "tables":
+        ctx, new, base, of = _counts(case)
+        # row, position and place of every token out; context, tokens and offset of every row, a
+        # table entry and a count in and out for every page that changes hands
+        pages = np.maximum(-(-(ctx + new) // PAGE) - -(-ctx // PAGE), 0).sum()
+        taken = (ctx // PAGE).sum() if of is not None else 0
+        return {"bytes": int(16 * new.sum() + 12 * len(ctx) + 32 * pages + 24 * taken), "flops": 0}
+    eb = 4 if case["dtype"] == "fp32" else 2
+    if case["kind"] == "attend":
+        size, prefix, of, ctx, new = _counts(case)
+        shared = prefix // PAGE * PAGE
+        N, total = int(new.sum()), int(shared.sum() + (ctx + new - shared[of]).sum())
+        pairs = int((new * ctx + new * (new + 1) // 2).sum())
+        tb = case["D"] + case["D"] // 32 + 2
+        return {"bytes": total * case["Hkv"] * tb + 2 * N * case["Hq"] * case["D"] * eb,
+                "flops": 4 * pairs * case["Hq"] * case["D"]}
+    n, K = case["n"], case["K"]
+    # every logit and token in, log probability, entropy and alternatives out
+    return {"bytes": n * sum(_streams(case)) * eb + n * K * (12 + 8 * case["top"]), "flops": 0}
+
+
+# ---- inputs ----------------------------------------------------------------
+
+def _int32(a):
+    return torch.from_numpy(np.ascontiguousarray(a, np.int32)).to("cuda")
+
+
+def _dtype(case):
+    return torch.float32 if case["dtype"] == "fp32" else torch.bfloat16
+
+
+def _pages_of(n):
+    return -(-np.asarray(n) // PAGE)
+
+
+def prepare(case, seed):
+    mcd = None
+    if own:
+        from paper_2607_02119_amd import mcd
+    gen, rng = torch.Generator("cuda").manual_seed(seed), np.random.default_rng(seed)
+    make = {"tables": _prepare_tables, "attend": _prepare_attend, "logprobs": _prepare_logprobs}
+    s = make[case["kind"]](case, gen, rng, mcd)
+    s.update(case=case, mcd=mcd)
+    return s
+
+
+def _prepare_tables(case, gen, rng, mcd):
+    """A table in use: the rows' slots hold their pages (or an earlier request's), the prompts'
+    slots theirs, other slots some more, and the free pages lie between them."""
+    ctx, new, base, of = _counts(case)
+    R, P = len(ctx), 0 if of is None else len(base)
+    others = max(R // 8, 1)
+    S = R + P + others
+    place, sizes = rng.permutation(S), np.random.default_rng(S)   # as many pages for every seed
+    slot, prompt, other = place[:R], place[R:R + P], place[R + P:]
+    counts = np.zeros(S, int)
+    counts[slot] = _pages_of(ctx) if of is None else sizes.integers(0, _pages_of(ctx + new) + 1)
+    if P:
+        counts[prompt] = _pages_of(base)
+    columns = int(max(_pages_of(ctx + new).max(), counts.max())) + 1
+    counts[other] = sizes.integers(0, columns + 1, others)
+    most = int(counts.sum() + _pages_of(ctx + new).sum())
+    n_pages = most + most // 8 + 5
+    ids, at = rng.permutation(n_pages), 0
+    table = np.full((S, columns), -1, np.int32)
+    for i, c in enumerate(counts):
+        table[i, :c] = ids[at:at + c]
+        at += c
+    N = int(new.sum())
+    s = dict(table=_int32(table), n_pages=n_pages, slot=_int32(slot), context=_int32(ctx),
+             tokens=_int32(new), N=N, keep=_int32(ctx if of is None else np.zeros(R, int)),
+             max_context=int((ctx + new).max()), max_tokens=int(new.max()),
+             source=None if of is None else _int32(prompt[of]),
+             start=torch.zeros(R + 1, dtype=torch.int32, device="cuda"),
+             where=torch.zeros(N, dtype=torch.int64, device="cuda"),
+             row=torch.zeros(N, dtype=torch.int32, device="cuda"),
+             position=torch.zeros(N, dtype=torch.int32, device="cuda"))
+    if mcd:
+        s["pages"] = mcd.CachePages(s["table"], n_pages)
+        s["refs"] = s["pages"].refs
+        s["workspace"] = torch.zeros(s["pages"].workspace_bytes(R), dtype=torch.uint8,
+                                     device="cuda")
+    else:
+        held = torch.from_numpy(table[table >= 0].astype(np.int64)).to("cuda")
+        s["refs"] = torch.bincount(held, minlength=n_pages).int()
+    return s
+
+
+E2M1 = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+def _page_bytes(D):
+    return 66 * D + 128
+
+
+def _nibbles(gen, shape):
+    """Codes of normal numbers quantised to e2m1, largest magnitudes about 3 standard deviations."""
+    x = torch.randn(shape, generator=gen, device="cuda") * 2.0
+    limits = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0], device="cuda")
+    return (torch.bucketize(x.abs(), limits) + 8 * (x < 0)).to(torch.uint8)
+
+
+def _prepare_attend(case, gen, rng, mcd):
+    size, prefix, of, ctx, new = _counts(case)
+    R, N, H, D, dt = len(ctx), int(new.sum()), case["Hkv"], case["D"], _dtype(case)
+    slot = rng.permutation(R)                     # where the scheduler put each row
+    shared = prefix // PAGE
+    mine = _pages_of(ctx + new) - shared[of]
+    n_pages = int(shared.sum() + mine.sum()) + 3
+    columns = int(_pages_of(ctx + new).max()) + 1
+    ids, at = rng.permutation(n_pages), 0
+    table = np.full((R, columns), -1, np.int32)
+    for g, count in enumerate(shared):
+        table[slot[of == g], :count] = ids[at:at + count]
+        at += count
+    for r, count in enumerate(mine):
+        table[slot[r], shared[of[r]]:shared[of[r]] + count] = ids[at:at + count]
+        at += count
+    pages = torch.empty((n_pages, H, _page_bytes(D)), dtype=torch.uint8, device="cuda")
+    step = max(1, (1 << 26) // (H * 128 * D))
+    for i in range(0, n_pages, step):
+        m = min(step, n_pages - i)
+        codes = _nibbles(gen, (m, H, 64 * D, 2))
+        pages[i:i + m, :, :64 * D] = codes[..., 0] | codes[..., 1] << 4
+        # keys of 32 channels: powers of two around a quarter, values of a token: of all sizes
+        pages[i:i + m, :, 64 * D:66 * D] = torch.randint(
+            123, 127, (m, H, 2 * D), generator=gen, device="cuda", dtype=torch.uint8)
+        sizes = (0.05 + torch.rand((m, H, PAGE), generator=gen, device="cuda")) / 4
+        pages[i:i + m, :, 66 * D:] = sizes.to(torch.bfloat16).view(torch.uint8)
+    # past a row's end: what an earlier request left there, numbers that are not finite among it
+    nb, t = D // 32, np.arange(PAGE)
+    key = 64 * D + (t % 16)[:, None] * nb * 4 + np.arange(nb)[None] * 4 + (t // 16)[:, None]
+    val = 66 * D + 2 * (t // 4 % 4 * 16 + t // 16 * 4 + t % 4)
+    for r, length in enumerate(ctx + new):
+        if length % PAGE:
+            past = slice(int(length) % PAGE, None)
+            bad = torch.from_numpy(np.concatenate([key[past].ravel(), val[past], val[past] + 1]))
+            pages[int(table[slot[r], length // PAGE]), :, bad.to("cuda")] = 255
+    # the projection's output: queries beside the new keys and values
+    qkv = torch.zeros((N, case["Hq"] + 2 * H, D), dtype=dt, device="cuda")
+    qkv[:, :case["Hq"]] = torch.randn((N, case["Hq"], D), generator=gen, device="cuda")
+    s = dict(pages=pages, host_table=table, table=_int32(table), slots=slot, ctx=ctx, new=new,
+             q=qkv[:, :case["Hq"]], scale=1.0 / math.sqrt(D),
+             out=torch.zeros((N, case["Hq"], D), dtype=dt, device="cuda"))
+    if mcd:
+        start = np.concatenate([[0], np.cumsum(new)])
+        s["cache"] = mcd.Cache(pages, s["table"], D)
+        s["rows"] = mcd.CacheRows(_int32(ctx), start=_int32(start), slot=_int32(slot),
+                                  n_tokens=N, max_tokens=int(new.max()),
+                                  max_context=int((ctx + new).max()))
+        s["groups"] = mcd.CacheGroups(_int32(np.concatenate([[0], np.cumsum(size)])),
+                                      _int32(prefix), max_rows=int(size.max()),
+                                      max_prefix=int(prefix.max()),
+                                      max_own=int((ctx + new - shared[of] * PAGE).max()))
+        s["workspace"] = s["cache"].workspace(s["rows"], case["Hq"], groups=s["groups"])
+    return s
+
+
+def _prepare_logprobs(case, gen, rng, mcd):
+    n, K, top, streams = case["n"], case["K"], case["top"], _streams(case)
+    off = np.concatenate([[0], np.cumsum(streams)])
+    # rows from nearly even to nearly certain distributions
+    size = torch.exp(torch.rand((n, 1), generator=gen, device="cuda") * 2.5 - 0.5)
+    x = torch.empty((n, int(off[-1])), dtype=_dtype(case), device="cuda")
+    tokens = torch.empty((n, K), dtype=torch.int32, device="cuda")
+    step = max(1, (1 << 24) // int(off[-1]))
+    for i in range(0, n, step):
+        m = min(step, n - i)
+        part = torch.randn((m, int(off[-1])), generator=gen, device="cuda") * size[i:i + m]
+        sure = torch.rand(m, generator=gen, device="cuda") < 0.1
+        for k, V in enumerate(streams):
+            one = part[:, off[k]:off[k + 1]]
+            at = torch.randint(V, (m, 1), generator=gen, device="cuda")
+            one.scatter_add_(1, at, (sure * 30.0).unsqueeze(1))
+            ruled_out = int(V * case["masked"])
+            if ruled_out:
+                one[:, V - ruled_out:] = -float("inf")
+            noise = torch.rand(one.shape, generator=gen, device="cuda").clamp_(1e-7, 1 - 1e-7)
+            tokens[i:i + m, k] = (one - (-noise.log()).log()).argmax(1).int()
+        x[i:i + m] = part
+    # where the delay pattern has no frame: the pad id
+    pad = max(streams)
+    if K > 1:
+        late = torch.rand((n, 1), generator=gen, device="cuda") < 0.1
+        tokens.masked_fill_(late & (torch.arange(K, device="cuda") >= K // 2), pad)
+    row = None
+    if case["pairs"]:
+        order = torch.from_numpy(rng.permutation(2 * n)[:n]).to("cuda")
+        batch = torch.full((2 * n, K), pad, dtype=torch.int32, device="cuda")
+        batch[order] = tokens
+        tokens, row = batch, order.int()
+    f32 = dict(dtype=torch.float32, device="cuda")
+    s = dict(x=x, tokens=tokens, row=row, pad=pad, streams=streams, off=off,
+             logprob=torch.zeros((n, K), **f32), entropy=torch.zeros((n, K), **f32),
+             ids=torch.zeros((n, K, top), dtype=torch.int32, device="cuda"),
+             top=torch.zeros((n, K, top), **f32))
+    if mcd:
+        V = case["V"]
+        s["logits"] = x if case["V0"] else x.view(n, K, V)
+        s["V_stream"] = np.array(streams, np.int32) if case["V0"] else None
+        need = mcd.mcd_logprobs_workspace_bytes(n, K, max(streams), top)
+        s["workspace"] = torch.zeros(need, dtype=torch.uint8, device="cuda")
+    return s
+
+
+# ---- one pass --------------------------------------------------------------
+
+def run(s):
+    kind = s["case"]["kind"]
+    if not own:
+        return {"tables": _plain_tables, "attend": _plain_attend,
+                "logprobs": _plain_logprobs}[kind](s)
+    mcd, ws = s["mcd"], s["workspace"]
+    if kind == "tables":
+        mcd.mcd_cache_release(s["pages"], s["slot"], ws, length=s["keep"])
+        if s["source"] is not None:
+            mcd.mcd_cache_share(s["pages"], s["slot"], s["source"], s["context"], ws)
+        mcd.mcd_cache_reserve(s["pages"], s["context"], s["tokens"], s["start"], ws,
+                              slot=s["slot"], n_tokens=s["N"], max_tokens=s["max_tokens"],
+                              max_context=s["max_context"], where=s["where"], row=s["row"],
+                              position=s["position"])
+        return s["table"], s["refs"], s["start"], s["where"], s["row"], s["position"]
+    if kind == "attend":
+        mcd.mcd_cache_attend_shared(s["cache"], s["rows"], s["groups"], s["q"], s["out"], ws,
+                                    scale=s["scale"])
+        return s["out"]
+    top = s["case"]["top"]
+    mcd.mcd_logprobs(s["logits"], s["tokens"], s["logprob"], ws, entropy=s["entropy"],
+                     top_ids=s["ids"] if top else None, top_logprobs=s["top"] if top else None,
+                     V_stream=s["V_stream"], token_row=s["row"], pad_id=s["pad"])
+    return s["logprob"], s["entropy"], s["ids"], s["top"]
+
+
+def _plain_tables(s):
+    table, refs, slot = s["table"], s["refs"], s["slot"].long()
+    col = torch.arange(table.shape[1], device="cuda")
+
+    def count(pages, change):
+        """Adds change where there is a page."""
+        refs.index_add_(0, pages.clamp(min=0).flatten().long(), change.flatten().int())
+
+    # back to `keep` positions
+    old = table[slot]
+    gone = (col * PAGE >= s["keep"].unsqueeze(1)) & (old >= 0)
+    count(old, -gone.int())
+    table[slot] = torch.where(gone, -1, old)
+    # the whole pages of the prompts
+    context, tokens = s["context"].unsqueeze(1), s["tokens"].unsqueeze(1)
+    if s["source"] is not None:
+        take = (col + 1) * PAGE <= context
+        theirs = table[s["source"].long()]
+        table[slot] = torch.where(take, theirs, table[slot])
+        count(theirs, take)
+    # pages for the new tokens
+    mine = table[slot]
+    want = ((col + 1) * PAGE > context) & (col * PAGE < context + tokens) & (mine < 0)
+    free = (refs == 0).nonzero().squeeze(1)
+    place = want.flatten().cumsum(0) - 1
+    got = free[place.clamp(min=0)].view(want.shape).int()
+    table[slot] = torch.where(want, got, mine)
+    count(got, want)
+    # the tokens' maps
+    start = s["start"]
+    start[1:] = s["tokens"].cumsum(0)
+    row = torch.repeat_interleave(torch.arange(len(slot), device="cuda"), s["tokens"].long(),
+                                  output_size=s["N"])
+    position = s["context"].long()[row] + torch.arange(s["N"], device="cuda") - start.long()[row]
+    s["row"].copy_(row)
+    s["position"].copy_(position)
+    s["where"].copy_(table[slot[row], position // PAGE].long() * PAGE + position % PAGE)
+    return table, refs, start, s["where"], s["row"], s["position"]
+
+
+def _levels(codes):
+    lut = torch.tensor(E2M1 + tuple(-x for x in E2M1), device="cuda")
+    return lut[codes.int()]
+
+
+def _keys_values(pages, D):
+    """Keys and values [Hkv, 64 n, D] in fp32 of pages [n, Hkv, bytes].
+      [0, 32 D)           key codes [token][channel], the lower channel in the low bits
+      [32 D, 64 D)        value codes, eight tokens of a channel to a 32-bit word: token
+                          32 h + 16 j + 4 g + i in bits 4 (4 j + i) of word [h][c / 4][16 g + m]
+                          [c % 4] of channel (m / 4) (D / 4) + 4 c + m % 4
+      [64 D, 66 D)        key scales, token 16 t + m, block b at byte (m D / 32 + b) 4 + t
+      then 128            value scales, token 16 t + 4 g + i at bfloat16 16 g + 4 t + i"""
+    n, H, _ = pages.shape
+    two = lambda x: torch.stack([x & 15, x >> 4], -1).flatten(-2)  # noqa: E731
+    key = _levels(two(pages[..., :32 * D])).view(n, H, PAGE, D // 32, 32)
+    byte = pages[..., 64 * D:66 * D].view(n, H, 16, D // 32, 4).permute(0, 1, 4, 2, 3)
+    scale = torch.where(byte == 255, float("nan"), (byte.int() << 23).view(torch.float32))
+    key = key * scale.reshape(n, H, PAGE, D // 32, 1)
+    # [h][c / 4][g][m / 4][m % 4][c % 4][j][i] -> [h][j][g][i][m / 4][c / 4][c % 4][m % 4]
+    word = two(pages[..., 32 * D:64 * D]).view(n, H, 2, D // 64, 4, 4, 4, 4, 2, 4)
+    value = _levels(word.permute(0, 1, 2, 8, 4, 9, 5, 3, 7, 6).reshape(n, H, PAGE, D))
+    size = pages[..., 66 * D:].contiguous().view(torch.bfloat16).float()
+    value = value * size.view(n, H, 4, 4, 4).transpose(2, 3).reshape(n, H, PAGE, 1)
+    return (x.transpose(0, 1).flatten(1, 2) for x in (key.view(n, H, PAGE, D), value))
+
+
+def _plain_attend(s):
+    D, H, at = s["case"]["D"], s["case"]["Hkv"], 0
+    for r, (ctx, n) in enumerate(zip(s["ctx"].tolist(), s["new"].tolist())):
+        length = ctx + n
+        ids = s["table"][int(s["slots"][r]), :(length + PAGE - 1) // PAGE].long()
+        k, v = (x[:, :length] for x in _keys_values(s["pages"][ids], D))
+        q = s["q"][at:at + n].float().view(n, H, -1, D).permute(1, 2, 0, 3)     # [H, G, n, D]
+        x = q.reshape(H, -1, D) @ k.transpose(1, 2).contiguous() * s["scale"]
+        seen = torch.arange(length, device="cuda") <= \
+            ctx + torch.arange(n, device="cuda").view(-1, 1)
+        x = x.view(H, -1, n, length).masked_fill(~seen, -float("inf"))
+        p = (x - x.amax(-1, keepdim=True)).exp()
+        p = p / p.sum(-1, keepdim=True)
+        y = (p.view(H, -1, length) @ v).view(H, -1, n, D)
+        s["out"][at:at + n] = y.permute(2, 0, 1, 3).reshape(n, -1, D)
+        at += n
+    return s["out"]
+
+
+def _given(s):
+    """The tokens of the logits' rows [n, K]."""
+    return (s["tokens"] if s["row"] is None else s["tokens"][s["row"].long()]).long()
+
+
+def _plain_logprobs(s):
+    top, tokens = s["case"]["top"], _given(s)
+    step = max(1, (1 << 24) // max(s["streams"]))
+    for k, V in enumerate(s["streams"]):
+        for i in range(0, tokens.shape[0], step):
+            rows = slice(i, i + step)
+            x = s["x"][rows, s["off"][k]:s["off"][k + 1]].float()
+            x = x - x.amax(1, keepdim=True)
+            lp = x - x.exp().sum(1, keepdim=True).log()
+            p_lp = torch.where(lp == -float("inf"), 0.0, lp.exp() * lp)
+            s["entropy"][rows, k] = -p_lp.sum(1)
+            t = tokens[rows, k]
+            given = lp.gather(1, t.clamp(0, V - 1).unsqueeze(1)).squeeze(1)
+            # (a pad is no choice: certain)
+            s["logprob"][rows, k] = torch.where(t == s["pad"], 0.0, given)
+            if top:
+                order = lp.sort(dim=1, descending=True, stable=True)
+                val, ids = order.values[:, :top], order.indices[:, :top]
+                s["ids"][rows, k], s["top"][rows, k] = -1, -float("inf")
+                s["ids"][rows, k, :val.shape[1]] = torch.where(val == -float("inf"), -1, ids).int()
+                s["top"][rows, k, :val.shape[1]] = val
+    return s["logprob"], s["entropy"], s["ids"], s["top"]
+
+
+# ---- the same in 64 bits ---------------------------------------------------
+
+def _cached64(pages, D, ids, t):
+    """Keys and values [Hkv, tokens, D] at token t of page ids, in 64 bits, byte by byte."""
+    level = torch.tensor([0, 1, 2, 3, 4, 6, 8, 12], dtype=torch.float64, device="cuda") / 2
+    H, c, t = pages.shape[1], torch.arange(D, device="cuda").unsqueeze(0), t.unsqueeze(1)
+
+    def byte(at):
+        return pages[ids.view(1, -1, 1), torch.arange(H, device="cuda").view(-1, 1, 1),
+                     at.unsqueeze(0)].long()
+
+    def number(at, high):
+        code = byte(at) // torch.where(high, 16, 1) % 16
+        return torch.where(code < 8, level[code % 8], -level[code % 8])
+
+    b = byte(64 * D + (t % 16 * (D // 32) + c // 32) * 4 + t // 16)
+    key = number(t * (D // 2) + c // 2, c % 2 == 1)
+    key = torch.where(b == 255, float("nan"), torch.ldexp(key, b - 127))
+    q = c % (D // 4)
+    lane = t // 4 % 4 * 16 + c // (D // 4) * 4 + q % 4
+    word = ((t // 32 * (D // 64) + q // 16) * 64 + lane) * 4 + q // 4 % 4
+    bits = t // 16 % 2 * 4 + t % 4
+    value = number(32 * D + word * 4 + bits // 2, bits % 2 == 1)
+    at = 66 * D + 2 * (t // 4 % 4 * 16 + t // 16 * 4 + t % 4)
+    size = ((byte(at) + 256 * byte(at + 1)) << 16).int().view(torch.float32).double()
+    return key, value * size
+
+
+def exact(case, seed):
+    if case["kind"] == "tables":
+        return None                               # whole numbers
+    s = prepare(case, seed)
+    if case["kind"] == "logprobs":
+        tokens, n, K, T = _given(s), case["n"], case["K"], case["top"]
+        f64 = dict(dtype=torch.float64, device="cuda")
+        logprob, entropy = torch.zeros((n, K), **f64), torch.zeros((n, K), **f64)
+        top = torch.full((n, K, T), -float("inf"), **f64)
+        for i in range(n):
+            x = s["x"][i].double()
+            for V in sorted(set(s["streams"])):
+                at = [k for k, size in enumerate(s["streams"]) if size == V]
+                y = torch.stack([x[s["off"][k]:s["off"][k] + V] for k in at])
+                lp = y - torch.logsumexp(y, 1, keepdim=True)
+                p = lp.exp()
+                entropy[i, at] = torch.where(p > 0, -p * lp, 0.0).sum(1)
+                t = tokens[i, at]
+                given = lp[torch.arange(len(at), device="cuda"), t.clamp(0, V - 1)]
+                logprob[i, at] = torch.where(t == s["pad"], 0.0, given)
+                m = min(T, V)
+                if m:
+                    best = lp.topk(m, dim=1).values
+                    top[i, at, :m] = best
+        return logprob, entropy, None, top
+    # beyond this the products in 64 bits take longer than they are worth
+    if work(case)["flops"] > 2e12:
+        return None
+    out, at = torch.zeros(s["q"].shape, dtype=torch.float64, device="cuda"), 0
+    H, G = case["Hkv"], case["Hq"] // case["Hkv"]
+    for r, (ctx, n) in enumerate(zip(s["ctx"].tolist(), s["new"].tolist())):
+        position = torch.arange(ctx + n, device="cuda")
+        ids = s["table"][int(s["slots"][r])][position // PAGE].long()
+        k, v = _cached64(s["pages"], case["D"], ids, position % PAGE)
+        hidden = torch.ones((n, ctx + n), dtype=torch.bool, device="cuda").triu(ctx + 1)
+        for h in range(H):
+            for a in range(h * G, h * G + G):
+                x = s["q"][at:at + n, a].double() @ k[h].t().contiguous() * s["scale"]
+                out[at:at + n, a] = torch.softmax(x.masked_fill(hidden, -float("inf")), 1) @ v[h]
+        at += n
+    return out
