@@ -490,8 +490,8 @@ def _plain_logprobs(s):
     for k, V in enumerate(s["streams"]):
         for i in range(0, tokens.shape[0], step):
             rows = slice(i, i + step)
-            x = s["x"][rows, s["off"][k]:s["off"][k + 1]].float()
-            x = x - x.amax(1, keepdim=True)
+            given_x = s["x"][rows, s["off"][k]:s["off"][k + 1]].float()
+            x = given_x - given_x.amax(1, keepdim=True)
             lp = x - x.exp().sum(1, keepdim=True).log()
             p_lp = torch.where(lp == -float("inf"), 0.0, lp.exp() * lp)
             s["entropy"][rows, k] = -p_lp.sum(1)
@@ -500,8 +500,9 @@ def _plain_logprobs(s):
             # (a pad is no choice: certain)
             s["logprob"][rows, k] = torch.where(t == s["pad"], 0.0, given)
             if top:
-                order = lp.sort(dim=1, descending=True, stable=True)
-                val, ids = order.values[:, :top], order.indices[:, :top]
+                # (by the logits: log probabilities that are rounded may meet)
+                ids = given_x.sort(dim=1, descending=True, stable=True).indices[:, :top]
+                val = lp.gather(1, ids)
                 s["ids"][rows, k], s["top"][rows, k] = -1, -float("inf")
                 s["ids"][rows, k, :val.shape[1]] = torch.where(val == -float("inf"), -1, ids).int()
                 s["top"][rows, k, :val.shape[1]] = val
