@@ -125,8 +125,9 @@ __device__ __forceinline__ int row_start(const RowsView &rv, int r) {
 }
 
 // The row that owns work item x, where row r's items begin at base(r), which
-// ascends from base(0) = 0: the last r with base(r) <= x.  The 64 lanes of a
-// wave probe at once: one round of loads for 64 rows, two for 4096.
+// ascends from base(0) = 0: the last r with base(r) <= x (0 if there is none, for
+// arrays that do not begin at 0).  The 64 lanes of a wave probe at once: one round
+// of loads for 64 rows, two for 4096.
 template <class Base>
 __device__ __forceinline__ int find_row(int R, int64_t x, Base &&base) {
   const int lane = threadIdx.x & 63;
@@ -135,7 +136,8 @@ __device__ __forceinline__ int find_row(int R, int64_t x, Base &&base) {
     const int step = (n + 63) >> 6;
     const int at = lane * step;
     const bool below = at < n && base(lo + at) <= x;
-    const int last = max(__popcll(__ballot(below)) - 1, 0);
+    // (the count is unsigned: less one it has to be an int before it meets 0)
+    const int last = max((int)__popcll(__ballot(below)) - 1, 0);
     lo += last * step;
     n = min(step, n - last * step);
   }

@@ -468,3 +468,38 @@ def test_small_and_large_keys_and_values(name, Hq, dtype, ctx, new, ks, vs):
         assert (np.abs(got[a:a + n] * 2.0 ** -vs - o) <= to).all(), r
         w = wout[r, :, :ctx[r] + n].double().cpu().numpy()
         assert (np.abs(w - wt) <= tw).all()
+
+
+def test_starts_that_do_not_begin_at_zero():
+    """Tokens before the first row's belong to no row: no call reads or writes for them, and the
+    rows' own have their results."""
+    rng = np.random.default_rng(31)
+    D, H, Hq, ctx, new, first = 64, 2, 4, [70, 3, 130], [2, 1, 40], 45
+    lengths = [c + n for c, n in zip(ctx, new)]
+    cache, pages, table, _, _ = make_cache(rng, lengths, H, D)
+    N = sum(new)
+    start = first + np.concatenate([[0], np.cumsum(new)])
+    ws = torch.zeros(1 << 24, dtype=torch.uint8, device="cuda")
+    q = dev(rng.standard_normal((first + N, Hq, D)).astype(np.float32))
+    kv = dev(rng.standard_normal((first + N, 2 * H, D)).astype(np.float32))
+
+    def rows(begin):
+        return mcd.CacheRows(i32(ctx), start=i32(start - first + begin), n_tokens=begin + N,
+                             max_tokens=max(new), max_context=max(lengths))
+
+    outs = []
+    for begin in (0, first):
+        cache.pages.copy_(dev(pages))
+        out, ko, vo = (torch.full((begin + N, h, D), 9.0, device="cuda") for h in (Hq, H, H))
+        part = slice(first - begin, None)
+        mcd.mcd_cache_append(cache, rows(begin), kv[part, :H], kv[part, H:], ws)
+        mcd.mcd_cache_read(cache, rows(begin), ko, vo, ws)
+        mcd.mcd_cache_attend(cache, rows(begin), q[part], out, ws)
+        assert mcd.mcd_read_device_status(ws) == 0
+        for x in (out, ko, vo):
+            assert bool((x[:begin] == 9.0).all())
+        outs.append([x[begin:].clone() for x in (out, ko, vo)] + [cache.pages.clone()])
+    for a, b in zip(*outs):
+        # other splits of the pages: exponents of up to 64 are rounded against another reference,
+        # 2^-18 twice, and the sums are added in another order, 16 of 2^-23, of values up to 6
+        assert torch.allclose(a.float(), b.float(), rtol=0, atol=6 * 2.0 ** -16, equal_nan=True)
