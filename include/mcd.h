@@ -71,7 +71,8 @@ enum {
   MCD_DEV_GRID_RANGE = 2u,  /* grid_slot >= n_slots or frame >= F_max: cell not written */
   MCD_DEV_BAD_PLAN = 4u,    /* device plan does not match the counts of the call */
   MCD_DEV_BAD_TOKEN = 8u,   /* mcd_next_input: a token outside its table */
-  MCD_DEV_BAD_PAGE = 16u    /* mcd_cache_*: a slot, length or page id out of range */
+  MCD_DEV_BAD_PAGE = 16u,   /* mcd_cache_*: a slot, length or page id out of range */
+  MCD_DEV_NO_PAGE = 32u     /* mcd_cache_reserve: no free page left for a token */
 };
 
 #define MCD_MAX_K 32         /* codebooks per head */
@@ -298,6 +299,54 @@ typedef struct {
  * MCD_DEV_BAD_TOKEN in the workspace status word (when a workspace is given). */
 mcd_status mcd_next_input(const mcd_next_input_args *args, hipStream_t stream);
 
+/* ---- log probabilities ------------------------------------------------------
+ * How likely the given tokens were, under the softmax of each of K vectors of
+ * logits of n rows: the head's scores (mcd_step_args.scores after a step: fp32,
+ * its sampled rows in plan order, so token_row holds each one's batch row), or any
+ * other logits (K = 1: a text head's).  For vector x of a row and stream, with
+ * p = softmax(x):
+ *   logprob:      log p of its token; 0 for pad_id (no choice)
+ *   entropy:      - sum p log p, natural
+ *   top_ids, top_logprobs: the T largest logits, ties to the lower id, and their
+ *                 log p; -1 and -infinity past the ids that are not -infinity
+ * A logit of -infinity has p = 0.  A vector with a NaN, with +infinity or with
+ * nothing but -infinity has no distribution: NaN for all of it, ids -1 (0 for
+ * pad_id all the same).  A token outside its stream other than pad_id, or a row of
+ * tokens that is not there, gives NaN and sets MCD_DEV_BAD_TOKEN.  Sums and log
+ * probabilities are in fp32; log p near 0 keeps its leading digits (terms of the sum
+ * below 2^-126 are 0). */
+#define MCD_MAX_TOP 32
+
+typedef struct {
+  int32_t n;                 /* rows, >= 0 */
+  int32_t K;                 /* vectors of a row (streams), 1..MCD_MAX_K */
+  int32_t V;                 /* logits of a vector (the largest), 1..2^19 */
+  int32_t T;                 /* alternatives, 0..MCD_MAX_TOP */
+  int32_t pad_id;            /* outside [0, V) */
+  mcd_dtype dtype;           /* of logits */
+  const void *logits;        /* [n][N]: vector k at column off_k, N = K V, or with V_stream
+                                off_k and N its sums (as in mcd_head_desc) */
+  int64_t logits_stride;     /* elements between rows, >= N */
+  const int32_t *V_stream;   /* [host][K] logits of each vector (1..V), or NULL: V */
+  int32_t token_rows;        /* rows of tokens */
+  const int32_t *tokens;     /* [token_rows][K] */
+  const int32_t *token_row;  /* [n] row of tokens of every row, or NULL: its index */
+  float *logprob;            /* [n][K] */
+  float *entropy;            /* [n][K] or NULL */
+  int32_t *top_ids;          /* [n][K][T]; this or top_logprobs may be NULL */
+  float *top_logprobs;       /* [n][K][T] */
+  void *workspace;
+  size_t workspace_bytes;    /* mcd_logprobs_workspace_bytes() */
+} mcd_logprobs_args;
+
+/* Workspace bytes for these sizes and smaller ones, 0 for invalid sizes; 256-byte
+ * aligned, its first 256 bytes (the status word) zeroed once before first use. */
+size_t mcd_logprobs_workspace_bytes(int32_t n, int32_t K, int32_t V, int32_t T);
+
+/* Launches on `stream`; no allocation, no synchronisation.  The arrays written
+ * overlap no other of the call.  The same inputs give the same bits. */
+mcd_status mcd_logprobs(const mcd_logprobs_args *args, hipStream_t stream);
+
 /* ---- paired co-scheduling (Sec. 2.4 input allocation and co-scheduling) ---
  * [host] A continuous-batching scheduler for CFG requests; no HIP calls.
  *   - Auto-allocation: a request with cfg_w > 1 becomes a unit of two rows, its
@@ -494,6 +543,39 @@ typedef struct {
 mcd_status mcd_cache_attend(const mcd_cache *cache, const mcd_cache_rows *rows,
                             const mcd_cache_attend_args *args, hipStream_t stream);
 
+/* Rows that begin with the same pages (several continuations of one prompt, several
+ * questions about one document): groups of consecutive rows of a step.  Rows
+ * start[g] .. start[g + 1] - 1 are group g's, and the table entries of the whole
+ * pages of their first prefix[g] positions (prefix[g] / 64 of them) are the same for
+ * all of them: they are read from the group's first row.  Every row of a group
+ * continues past those pages (context >= prefix[g] / 64 * 64).  The groups hold all
+ * rows (start[0] = 0, start[n] = R); a row that shares nothing is a group of its
+ * own.  The arrays are read when the kernels run, the max_* are bounds as in
+ * mcd_cache_rows; past them, and for a row that breaks the above, MCD_DEV_BAD_PAGE is
+ * set: positions past a bound are not seen, a row outside the groups, short of
+ * its prefix or past max_rows sees nothing. */
+typedef struct {
+  int32_t n;                 /* groups, 0..65535 */
+  int32_t max_rows;          /* no group has more rows */
+  int32_t max_prefix;        /* no prefix is longer */
+  int32_t max_own;           /* no row has more positions past its group's shared pages */
+  const int32_t *start;      /* [n + 1], ascending */
+  const int32_t *prefix;     /* [n] */
+} mcd_cache_groups;
+
+/* Workspace bytes of mcd_cache_attend_shared for these bounds (0 for invalid sizes),
+ * enough for every step of no more rows, tokens, groups and positions too; as
+ * mcd_cache_attend's otherwise, which it also serves when no weight is added up. */
+size_t mcd_cache_shared_workspace_bytes(const mcd_cache *cache, const mcd_cache_rows *rows,
+                                        const mcd_cache_groups *groups, int32_t Hq);
+
+/* mcd_cache_attend of rows in groups, to the same accuracy and with the same refusals,
+ * where a group's shared pages are read once for all of its rows.  weight_out is not
+ * supported (MCD_E_UNSUPPORTED). */
+mcd_status mcd_cache_attend_shared(const mcd_cache *cache, const mcd_cache_rows *rows,
+                                   const mcd_cache_groups *groups,
+                                   const mcd_cache_attend_args *args, hipStream_t stream);
+
 /* Eviction by received weight.  Row r's source slot holds length[r] positions.
  * In every K/V head the `recent` newest stay and, of the others, the keep -
  * recent that received the most weight (from->weight; equal weights: the lower
@@ -521,6 +603,82 @@ typedef struct {
 
 mcd_status mcd_cache_evict(const mcd_cache *from, const mcd_cache *to,
                            const mcd_cache_evict_args *args, hipStream_t stream);
+
+/* ---- page tables on the GPU ---------------------------------------------------
+ * A cache's table (mcd_cache.table), and how many of its entries hold each page.
+ * The table may be one for several layers' caches.  A page that no entry holds is
+ * free.  The calls below keep both, without the host: a captured step can take
+ * pages, give them back, and let rows begin on the pages of another slot's prefix.
+ *   entry:  a page id, or below 0: no page
+ *   refs:   entries that hold the page
+ * Calls on one table must not overlap in time.  Which pages a call hands out
+ * depends on the table alone.  Conditions that only the device sees set bits of
+ * the workspace's status word: a slot or page id out of range, a length below 0
+ * or beyond the table, a page given back more often than counted
+ * (MCD_DEV_BAD_PAGE, what it concerns is skipped); no free page left
+ * (MCD_DEV_NO_PAGE). */
+typedef struct {
+  int32_t n_slots, max_pages;/* rows and columns of table, >= 1 */
+  int32_t n_pages;           /* pages, >= 1 */
+  int32_t *table;            /* [n_slots][max_pages] */
+  int32_t *refs;             /* [n_pages] */
+} mcd_cache_pages;
+
+/* Workspace bytes of mcd_cache_reserve for R rows and fewer (0 for invalid sizes);
+ * the other calls need the 256-byte status word only.  256-byte aligned, the
+ * status word zeroed once before first use. */
+size_t mcd_cache_pages_workspace_bytes(const mcd_cache_pages *pages, int32_t R);
+
+/* refs from the table's entries, for a table that the host has written. */
+mcd_status mcd_cache_count(const mcd_cache_pages *pages, void *workspace, size_t workspace_bytes,
+                           hipStream_t stream);
+
+/* Slot slot[r] (slot NULL: r) keeps the pages of its first length[r] positions
+ * (length NULL: none) and gives back those of the columns past them.  A slot may
+ * be named more than once (the shortest length holds). */
+mcd_status mcd_cache_release(const mcd_cache_pages *pages, int32_t R, const int32_t *slot,
+                             const int32_t *length, void *workspace, size_t workspace_bytes,
+                             hipStream_t stream);
+
+/* The whole pages of source[r]'s first length[r] positions (length[r] / 64 of them)
+ * become slot[r]'s too (slot NULL: r).  Positions past the whole pages are the
+ * caller's to append again, to a page of the slot's own.  An entry of slot[r] that
+ * holds a page already keeps it, and a source without a page gives none
+ * (MCD_DEV_BAD_PAGE): release first.  No source of a call is among its slots, and
+ * no slot is named twice. */
+mcd_status mcd_cache_share(const mcd_cache_pages *pages, int32_t R, const int32_t *slot,
+                           const int32_t *source, const int32_t *length, void *workspace,
+                           size_t workspace_bytes, hipStream_t stream);
+
+/* Pages for the next step's tokens, and the step's rows.  Row r of slot[r] has
+ * tokens[r] new tokens at positions context[r], context[r] + 1, ...: every column
+ * of theirs without a page takes a free one, in the order of the rows and of their
+ * positions the free pages in the order of their ids.  (A page that other entries
+ * hold too is no place for a new token: MCD_DEV_BAD_PAGE, and where is -1.)
+ *   start:    [R + 1] sums of tokens before each row, for mcd_cache_rows
+ *   where:    [n_tokens] page * 64 + position % 64 of each packed token, -1: no page
+ *   row, position: [n_tokens] of each packed token
+ * Entries of where, row and position past start[R] are left as they were, and each
+ * of the three may be NULL.  tokens[r] is taken within 0 .. max_tokens, and tokens past
+ * n_tokens or positions from max_context on get no place (MCD_DEV_BAD_PAGE).  The
+ * arrays written overlap no other of the call. */
+typedef struct {
+  int32_t R;                 /* rows, 0..65535 */
+  int32_t n_tokens;          /* tokens of all rows at most, >= 0 */
+  int32_t max_tokens;        /* of a row at most, 0..n_tokens */
+  int32_t max_context;       /* positions of a row (context + tokens) at most */
+  const int32_t *slot;       /* [R] slot of each row (no two alike), or NULL: its index */
+  const int32_t *context;    /* [R] */
+  const int32_t *tokens;     /* [R] */
+  int32_t *start;
+  int64_t *where;
+  int32_t *row, *position;
+  void *workspace;
+  size_t workspace_bytes;    /* mcd_cache_pages_workspace_bytes() */
+} mcd_cache_reserve_args;
+
+mcd_status mcd_cache_reserve(const mcd_cache_pages *pages, const mcd_cache_reserve_args *args,
+                             hipStream_t stream);
 
 /* ---- device status ----------------------------------------------------------
  * Synchronises `stream`, returns the status word of the workspace in *code

@@ -19,6 +19,7 @@ struct CacheView {
 };
 
 struct RowsView {
+  static constexpr bool kParts = false;
   int32_t R, N, max_tokens, max_context;
   const int32_t *slot, *context, *start;
 };
@@ -41,6 +42,9 @@ struct AttendView {
   float2 *part_ml;
   float *part_o;
   int32_t splits, split_pages; // pages of a split: the workgroups of a tile
+  // of rows whose results are parts (Rows::kParts): parts of a query row, and the first
+  int32_t parts, part0;
+  int32_t wide_tile;           // query rows of the wide rows' tiles
   int32_t narrow;              // query rows of a narrow row at most, 0: no narrow rows
   uint32_t *status;
 };
@@ -72,6 +76,28 @@ hipError_t launch_cache_attend(const CacheView &cv, const RowsView &rv, const At
 // weight_out of a call without a token: what the rows' positions had received.
 hipError_t launch_cache_keep_weight(const CacheView &cv, const RowsView &rv, float *weight_out,
                                     hipStream_t st);
+// Rows that begin with the same pages (k_cache_shared.hip).
+struct GroupsView {
+  int32_t n, max_rows, max_prefix, max_own;
+  const int32_t *start, *prefix;
+};
+// How a call runs: own pages as cache_attend_plan has it, the groups' pages in tiles
+// of all their rows' tokens, and parts of a query row in all.
+struct SharedPlan {
+  bool together;               // false: each row on its own
+  AttendPlan own;
+  TilePlan prefix;
+  int32_t prefix_pack;         // of a narrow prefix tile, 0: wide
+  int32_t parts;
+  size_t ml_bytes, o_bytes;
+};
+SharedPlan cache_shared_plan(const CacheView &cv, const RowsView &rv, const GroupsView &gv, int D,
+                             int32_t Hq);
+// Parts of all query rows that no plan within the bounds of rv and gv passes.
+int64_t cache_shared_room(const RowsView &rv, const GroupsView &gv, int32_t Hq);
+hipError_t launch_cache_shared(const CacheView &cv, const RowsView &rv, const GroupsView &gv,
+                               const AttendView &av, const SharedPlan &plan, int D, bool bf16,
+                               hipStream_t st);
 struct EvictView {
   int32_t R, max_length, keep, recent;
   const int32_t *slot, *length;
@@ -81,6 +107,42 @@ struct EvictView {
 hipError_t launch_cache_evict(const CacheView &from, const CacheView &to, const EvictView &ev,
                               int D, hipStream_t st);
 
+// Page tables (k_cache_pages.hip).
+struct PagesView {
+  int32_t n_slots, max_pages, n_pages;
+  int32_t *table, *refs;
+};
+constexpr int kMostChunks = 1024;
+struct RowSum {
+  long long need, tokens;      // columns without a page; tokens
+};
+struct ReserveView {
+  int32_t R, N, max_tokens, max_context;
+  const int32_t *slot, *context, *tokens;
+  int32_t *start;
+  int64_t *where;              // this and the next two: or null
+  int32_t *row, *position;
+  // workspace: [R] sums of the rows before within a block, [row_blocks], free pages
+  // of a chunk, and a bit for every page
+  RowSum *row_sum, *block_sum;
+  int32_t *chunk_free;
+  uint64_t *free_bits;
+  int32_t row_blocks, chunks, chunk_words;
+  uint32_t *status;
+};
+struct ReserveRoom {
+  int32_t row_blocks, chunks, chunk_words;
+  size_t row_bytes, block_bytes, chunk_bytes, bit_bytes;
+};
+ReserveRoom reserve_room(int32_t R, int32_t n_pages);
+hipError_t launch_cache_count(const PagesView &pv, uint32_t *status, hipStream_t st);
+hipError_t launch_cache_release(const PagesView &pv, int32_t R, const int32_t *slot,
+                                const int32_t *length, uint32_t *status, hipStream_t st);
+hipError_t launch_cache_share(const PagesView &pv, int32_t R, const int32_t *slot,
+                              const int32_t *source, const int32_t *length, uint32_t *status,
+                              hipStream_t st);
+hipError_t launch_cache_reserve(const PagesView &pv, const ReserveView &rv, hipStream_t st);
+
 namespace {
 
 // A row's slot and its tokens; positions and tokens past a bound are cut off
@@ -89,11 +151,13 @@ namespace {
 struct Span {
   int slot, ctx, t0, n;        // positions before the tokens; first token; tokens
   int len;                     // positions up to and with the last token, clamped to >= 0
+  int page0;                   // first page that attention reads
   bool bad;
 };
 
 __device__ __forceinline__ Span row_span(const CacheView &cv, const RowsView &rv, int r) {
   Span s;
+  s.page0 = 0;
   s.slot = rv.slot ? ld_const(rv.slot, r) : r;
   // (far beyond every bound below, and sums with it stay in 32 bits)
   s.ctx = min(max(ld_const(rv.context, r), -(1 << 30)), 1 << 30);

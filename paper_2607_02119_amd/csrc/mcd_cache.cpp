@@ -6,6 +6,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <initializer_list>
 
 #include "cache_common.h"
 
@@ -128,11 +129,128 @@ size_t workspace_need(const mcd::AttendPlan &p, const mcd::CacheView &cv, const 
   return std::max(attend_bytes(p), attend_bytes(mcd::cache_attend_room(cv, rv, D, Hq)));
 }
 
+mcd_status check_pages(const mcd_cache_pages *p) {
+  if (!p) return bad("null pages");
+  if (p->n_slots < 1 || p->max_pages < 1 || p->n_pages < 1)
+    return bad("bad page sizes (n_slots=%d max_pages=%d n_pages=%d)", p->n_slots, p->max_pages,
+               p->n_pages);
+  if ((int64_t)p->max_pages * MCD_CACHE_PAGE > kMost) return bad("page table too wide");
+  if ((int64_t)p->n_slots * p->max_pages > ((int64_t)1 << 36)) return bad("page table too large");
+  if (!p->table || !p->refs) return bad("null table or refs");
+  if (!aligned(p->table, 4) || !aligned(p->refs, 4)) return bad("table or refs not aligned");
+  return MCD_OK;
+}
+
+mcd::PagesView view(const mcd_cache_pages *p) {
+  return mcd::PagesView{p->n_slots, p->max_pages, p->n_pages, p->table, p->refs};
+}
+
+size_t reserve_bytes(const mcd::ReserveRoom &p) {
+  return mcd::kStatusBytes + p.row_bytes + p.block_bytes + p.chunk_bytes + p.bit_bytes;
+}
+
+// Arrays that a call reads and writes; nothing where there is no array.
+struct Bytes {
+  const void *p;
+  int64_t n;
+};
+bool overlap(const Bytes &a, const Bytes &b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return x && y && a.n > 0 && b.n > 0 && x < y + b.n && y < x + a.n;
+}
+Bytes table_of(const mcd_cache_pages *p) {
+  return Bytes{p->table, (int64_t)p->n_slots * p->max_pages * 4};
+}
+Bytes refs_of(const mcd_cache_pages *p) { return Bytes{p->refs, (int64_t)p->n_pages * 4}; }
+
+// Rows' arrays of whole numbers that a call on page tables reads.
+mcd_status check_page_rows(const mcd_cache_pages *p, int32_t R,
+                           std::initializer_list<const int32_t *> rows) {
+  if (R < 0 || R > 65535) return bad("bad row sizes (R=%d)", R);
+  if (overlap(table_of(p), refs_of(p))) return bad("table and refs overlap");
+  for (const int32_t *x : rows) {
+    if (!aligned(x, 4)) return bad("array not aligned");
+    if (overlap(table_of(p), Bytes{x, (int64_t)R * 4}) ||
+        overlap(refs_of(p), Bytes{x, (int64_t)R * 4}))
+      return bad("table and refs must not overlap the rows' arrays");
+  }
+  return MCD_OK;
+}
+
+mcd_status check_groups(const mcd_cache_groups *g, const mcd_cache_rows *r) {
+  if (!g) return bad("null groups");
+  if (g->n < 0 || g->n > 65535 || g->max_rows < 0 || g->max_prefix < 0 || g->max_own < 0 ||
+      g->max_prefix > kMost || g->max_own > kMost)
+    return bad("bad group sizes (n=%d max_rows=%d max_prefix=%d max_own=%d)", g->n, g->max_rows,
+               g->max_prefix, g->max_own);
+  if (r->n_tokens == 0) return MCD_OK;
+  if ((int64_t)std::min(g->max_rows, r->R) * r->max_tokens * g->n < r->n_tokens)
+    return bad("%d groups of %d rows do not hold %d tokens", g->n, g->max_rows, r->n_tokens);
+  if (!g->start || !g->prefix) return bad("null array");
+  if (!aligned(g->start, 4) || !aligned(g->prefix, 4)) return bad("array not aligned");
+  return MCD_OK;
+}
+
+mcd::GroupsView view(const mcd_cache_groups *g) {
+  return mcd::GroupsView{g->n, g->max_rows, g->max_prefix, g->max_own, g->start, g->prefix};
+}
+
+size_t shared_bytes(int64_t parts, int D) {
+  return mcd::kStatusBytes + round_up((size_t)parts * sizeof(float2)) +
+         round_up((size_t)parts * D * sizeof(float));
+}
+
+// Enough for every step within the bounds, together or each row on its own.
+size_t shared_need(const mcd::CacheView &cv, const mcd::RowsView &rv, const mcd::GroupsView &gv,
+                   const mcd::SharedPlan &p, int D, int32_t Hq) {
+  const size_t alone = workspace_need(mcd::cache_attend_plan(cv, rv, D, Hq), cv, rv, D, Hq);
+  const int64_t parts =
+      std::max((int64_t)rv.N * Hq * p.parts, mcd::cache_shared_room(rv, gv, Hq));
+  return std::max(alone, shared_bytes(parts, D));
+}
+
 #define CHECK(x)                        \
   do {                                  \
     const mcd_status s_ = (x);          \
     if (s_ != MCD_OK) return s_;        \
   } while (0)
+
+mcd_status check_attend(const mcd_cache *c, const mcd_cache_attend_args *a) {
+  CHECK(check_dtype(a->dtype));
+  if (!heads_ok(a->Hq, c->Hkv)) return bad("Hq=%d is no multiple of Hkv=%d", a->Hq, c->Hkv);
+  if (!(a->scale > 0.0f) || !std::isfinite(a->scale)) return bad("scale must be > 0 and finite");
+  if (!aligned(a->weight_out, 4) || !aligned(a->lse, 4)) return bad("weight_out or lse not aligned");
+  return MCD_OK;
+}
+
+mcd_status check_query(const mcd_cache *c, const mcd_cache_rows *r, const mcd_cache_attend_args *a) {
+  const int64_t width = (int64_t)a->Hq * c->D;
+  if (r->n_tokens * (int64_t)a->Hq > kMost || width > kMost) return bad("too many query rows");
+  CHECK(check_tokens("q", a->q, a->q_stride, width, a->dtype));
+  CHECK(check_tokens("out", a->out, a->out_stride, width, a->dtype));
+  // a query row is read before its own output is written, and again after it for
+  // the received weight
+  const int64_t eb = a->dtype == MCD_BF16 ? 2 : 4;
+  const bool in_place = a->q == a->out && a->q_stride == a->out_stride && !a->weight_out;
+  if (!in_place && meet(a->q, a->q_stride * eb, a->out, a->out_stride * eb, width * eb,
+                        r->n_tokens))
+    return bad("out must not overlap q%s", a->weight_out ? " with weight_out" : "");
+  return MCD_OK;
+}
+
+// The queries, without the workspace and what each launch sets.
+mcd::AttendView query_view(const mcd_cache *c, const mcd_cache_attend_args *a) {
+  mcd::AttendView av = {};
+  av.Hq = a->Hq;
+  av.G = a->Hq / c->Hkv;
+  av.q = a->q;
+  av.out = a->out;
+  av.q_stride = a->q_stride;
+  av.out_stride = a->out_stride;
+  av.c = a->scale * 1.4426950408889634f;
+  av.lse = a->lse;
+  return av;
+}
 
 mcd_status move_tokens(const mcd_cache *c, const mcd_cache_rows *r, mcd_dtype d, const void *k,
                        int64_t ks, const void *v, int64_t vs, void *ws, size_t wb) {
@@ -190,10 +308,7 @@ mcd_status mcd_cache_attend(const mcd_cache *c, const mcd_cache_rows *r,
   CHECK(check_cache(c));
   CHECK(check_rows(r));
   if (!a) return bad("null args");
-  CHECK(check_dtype(a->dtype));
-  if (!heads_ok(a->Hq, c->Hkv)) return bad("Hq=%d is no multiple of Hkv=%d", a->Hq, c->Hkv);
-  if (!(a->scale > 0.0f) || !std::isfinite(a->scale)) return bad("scale must be > 0 and finite");
-  if (!aligned(a->weight_out, 4) || !aligned(a->lse, 4)) return bad("weight_out or lse not aligned");
+  CHECK(check_attend(c, a));
   // (at most 2^31 slots x 2^16 heads x 2^30 positions: counted in double)
   const double weights = 4.0 * c->n_slots * c->Hkv * c->max_pages * MCD_CACHE_PAGE;
   const double apart = std::fabs((double)reinterpret_cast<uintptr_t>(a->weight_out) -
@@ -205,17 +320,7 @@ mcd_status mcd_cache_attend(const mcd_cache *c, const mcd_cache_rows *r,
     return launched(mcd::launch_cache_keep_weight(view(c), view(r), a->weight_out, stream),
                     "cache weight launch");
   }
-  const int64_t width = (int64_t)a->Hq * c->D;
-  if (r->n_tokens * (int64_t)a->Hq > kMost || width > kMost) return bad("too many query rows");
-  CHECK(check_tokens("q", a->q, a->q_stride, width, a->dtype));
-  CHECK(check_tokens("out", a->out, a->out_stride, width, a->dtype));
-  // a query row is read before its own output is written, and again after it for
-  // the received weight
-  const int64_t eb = a->dtype == MCD_BF16 ? 2 : 4;
-  const bool in_place = a->q == a->out && a->q_stride == a->out_stride && !a->weight_out;
-  if (!in_place && meet(a->q, a->q_stride * eb, a->out, a->out_stride * eb, width * eb,
-                        r->n_tokens))
-    return bad("out must not overlap q%s", a->weight_out ? " with weight_out" : "");
+  CHECK(check_query(c, r, a));
   const mcd::CacheView cv = view(c);
   const mcd::RowsView rv = view(r);
   const mcd::AttendPlan p = mcd::cache_attend_plan(cv, rv, c->D, a->Hq);
@@ -224,15 +329,7 @@ mcd_status mcd_cache_attend(const mcd_cache *c, const mcd_cache_rows *r,
   CHECK(check_workspace(a->workspace, a->workspace_bytes,
                         workspace_need(p, cv, rv, c->D, a->Hq)));
   char *w = static_cast<char *>(a->workspace);
-  mcd::AttendView av;
-  av.Hq = a->Hq;
-  av.G = a->Hq / c->Hkv;
-  av.q = a->q;
-  av.out = a->out;
-  av.q_stride = a->q_stride;
-  av.out_stride = a->out_stride;
-  av.c = a->scale * 1.4426950408889634f;
-  av.lse = a->lse;
+  mcd::AttendView av = query_view(c, a);
   av.weight_out = a->weight_out;
   av.status = reinterpret_cast<uint32_t *>(w);
   w += mcd::kStatusBytes;
@@ -245,7 +342,6 @@ mcd_status mcd_cache_attend(const mcd_cache *c, const mcd_cache_rows *r,
   av.scores = a->weight_out && p.score_bytes ? reinterpret_cast<mcd::floatx4 *>(w) : nullptr;
   av.score_pages = p.score_pages;
   av.narrow = p.narrow_rows;
-  av.splits = av.split_pages = 0;              // of each part's launch
   return launched(mcd::launch_cache_attend(cv, rv, av, p, c->D, a->dtype == MCD_BF16, stream),
                   "cache attention launch");
 }
@@ -281,6 +377,151 @@ mcd_status mcd_cache_evict(const mcd_cache *from, const mcd_cache *to,
                           a->length_out, static_cast<uint32_t *>(a->workspace)};
   return launched(mcd::launch_cache_evict(view(from), view(to), ev, from->D, stream),
                   "cache eviction launch");
+}
+
+size_t mcd_cache_shared_workspace_bytes(const mcd_cache *c, const mcd_cache_rows *r,
+                                        const mcd_cache_groups *g, int32_t Hq) {
+  if (check_cache(c) != MCD_OK || check_rows(r) != MCD_OK || check_groups(g, r) != MCD_OK) return 0;
+  if (!heads_ok(Hq, c->Hkv)) {
+    bad("Hq=%d is no multiple of Hkv=%d", Hq, c->Hkv);
+    return 0;
+  }
+  if (r->n_tokens * (int64_t)Hq > kMost) {
+    bad("too many query rows");
+    return 0;
+  }
+  mcd::CacheView cv = view(c);
+  cv.weight = nullptr;                           // (nothing is added up)
+  const mcd::RowsView rv = view(r);
+  const mcd::GroupsView gv = view(g);
+  return shared_need(cv, rv, gv, mcd::cache_shared_plan(cv, rv, gv, c->D, Hq), c->D, Hq);
+}
+
+mcd_status mcd_cache_attend_shared(const mcd_cache *c, const mcd_cache_rows *r,
+                                   const mcd_cache_groups *g, const mcd_cache_attend_args *a,
+                                   hipStream_t stream) {
+  CHECK(check_cache(c));
+  CHECK(check_rows(r));
+  CHECK(check_groups(g, r));
+  if (!a) return bad("null args");
+  if (a->weight_out)
+    return mcd::record_error(MCD_E_UNSUPPORTED, "no weight_out for rows that share pages");
+  mcd_cache alone = *c;
+  alone.weight = nullptr;
+  CHECK(check_attend(c, a));
+  if (r->n_tokens == 0) return MCD_OK;
+  CHECK(check_query(c, r, a));
+  const mcd::CacheView cv = view(&alone);
+  const mcd::RowsView rv = view(r);
+  const mcd::GroupsView gv = view(g);
+  const mcd::SharedPlan p = mcd::cache_shared_plan(cv, rv, gv, c->D, a->Hq);
+  CHECK(check_workspace(a->workspace, a->workspace_bytes,
+                        shared_need(cv, rv, gv, p, c->D, a->Hq)));
+  if (!p.together) return mcd_cache_attend(&alone, r, a, stream);
+  if ((p.prefix.tiles * p.prefix.splits + p.own.narrow.tiles * p.own.narrow.splits +
+       p.own.wide.tiles * p.own.wide.splits) * c->Hkv > kMost)
+    return bad("too many query rows");
+  char *w = static_cast<char *>(a->workspace);
+  mcd::AttendView av = query_view(c, a);
+  av.status = reinterpret_cast<uint32_t *>(w);
+  w += mcd::kStatusBytes;
+  av.part_ml = reinterpret_cast<float2 *>(w);
+  w += round_up((size_t)rv.N * a->Hq * p.parts * sizeof(float2));
+  av.part_o = reinterpret_cast<float *>(w);
+  return launched(mcd::launch_cache_shared(cv, rv, gv, av, p, c->D, a->dtype == MCD_BF16, stream),
+                  "shared cache attention launch");
+}
+
+size_t mcd_cache_pages_workspace_bytes(const mcd_cache_pages *p, int32_t R) {
+  if (check_pages(p) != MCD_OK || check_page_rows(p, R, {}) != MCD_OK) return 0;
+  return reserve_bytes(mcd::reserve_room(R, p->n_pages));
+}
+
+mcd_status mcd_cache_count(const mcd_cache_pages *p, void *ws, size_t wb, hipStream_t stream) {
+  CHECK(check_pages(p));
+  CHECK(check_page_rows(p, 0, {}));
+  CHECK(check_workspace(ws, wb, mcd::kStatusBytes));
+  return launched(mcd::launch_cache_count(view(p), static_cast<uint32_t *>(ws), stream),
+                  "page count launch");
+}
+
+mcd_status mcd_cache_release(const mcd_cache_pages *p, int32_t R, const int32_t *slot,
+                             const int32_t *length, void *ws, size_t wb, hipStream_t stream) {
+  CHECK(check_pages(p));
+  CHECK(check_page_rows(p, R, {slot, length}));
+  if (R == 0) return MCD_OK;
+  CHECK(check_workspace(ws, wb, mcd::kStatusBytes));
+  return launched(mcd::launch_cache_release(view(p), R, slot, length, static_cast<uint32_t *>(ws),
+                                            stream),
+                  "page release launch");
+}
+
+mcd_status mcd_cache_share(const mcd_cache_pages *p, int32_t R, const int32_t *slot,
+                           const int32_t *source, const int32_t *length, void *ws, size_t wb,
+                           hipStream_t stream) {
+  CHECK(check_pages(p));
+  CHECK(check_page_rows(p, R, {slot, source, length}));
+  if (R == 0) return MCD_OK;
+  if (!source || !length) return bad("null array");
+  CHECK(check_workspace(ws, wb, mcd::kStatusBytes));
+  return launched(mcd::launch_cache_share(view(p), R, slot, source, length,
+                                          static_cast<uint32_t *>(ws), stream),
+                  "page share launch");
+}
+
+mcd_status mcd_cache_reserve(const mcd_cache_pages *p, const mcd_cache_reserve_args *a,
+                             hipStream_t stream) {
+  CHECK(check_pages(p));
+  if (!a) return bad("null args");
+  CHECK(check_page_rows(p, a->R, {a->slot, a->context, a->tokens}));
+  if (a->n_tokens < 0 || a->max_tokens < 0 || a->max_context < 0 || a->n_tokens > kMost ||
+      a->max_tokens > a->n_tokens || a->max_context > kMost)
+    return bad("bad row sizes (R=%d n_tokens=%d max_tokens=%d max_context=%d)", a->R, a->n_tokens,
+               a->max_tokens, a->max_context);
+  if (a->R == 0) return a->n_tokens ? bad("%d tokens but R=0", a->n_tokens) : MCD_OK;
+  if (!a->context || !a->tokens || !a->start) return bad("null array");
+  if (!aligned(a->start, 4) || !aligned(a->where, 8) || !aligned(a->row, 4) ||
+      !aligned(a->position, 4))
+    return bad("array not aligned");
+  const mcd::ReserveRoom room = mcd::reserve_room(a->R, p->n_pages);
+  CHECK(check_workspace(a->workspace, a->workspace_bytes, reserve_bytes(room)));
+  const int64_t rows = (int64_t)a->R * 4, N = a->n_tokens;
+  const Bytes out[] = {{a->start, rows + 4}, {a->where, 8 * N}, {a->row, 4 * N},
+                       {a->position, 4 * N}};
+  const Bytes in[] = {{a->slot, rows}, {a->context, rows}, {a->tokens, rows}, table_of(p),
+                      refs_of(p)};
+  for (int i = 0; i < 4; ++i) {
+    for (const Bytes &x : in)
+      if (overlap(out[i], x)) return bad("the arrays written must not overlap those read");
+    for (int k = 0; k < i; ++k)
+      if (overlap(out[i], out[k])) return bad("the arrays written must not overlap each other");
+  }
+  char *w = static_cast<char *>(a->workspace);
+  mcd::ReserveView rv = {};
+  rv.R = a->R;
+  rv.N = a->n_tokens;
+  rv.max_tokens = a->max_tokens;
+  rv.max_context = a->max_context;
+  rv.slot = a->slot;
+  rv.context = a->context;
+  rv.tokens = a->tokens;
+  rv.start = a->start;
+  rv.where = a->where;
+  rv.row = a->row;
+  rv.position = a->position;
+  rv.status = reinterpret_cast<uint32_t *>(w);
+  w += mcd::kStatusBytes;
+  rv.row_sum = reinterpret_cast<mcd::RowSum *>(w);
+  w += room.row_bytes;
+  rv.block_sum = reinterpret_cast<mcd::RowSum *>(w);
+  w += room.block_bytes;
+  rv.chunk_free = reinterpret_cast<int32_t *>(w);
+  w += room.chunk_bytes;
+  rv.free_bits = reinterpret_cast<uint64_t *>(w);
+  rv.row_blocks = room.row_blocks;
+  rv.chunks = room.chunks;
+  rv.chunk_words = room.chunk_words;
+  return launched(mcd::launch_cache_reserve(view(p), rv, stream), "page reserve launch");
 }
 
 }  // extern "C"

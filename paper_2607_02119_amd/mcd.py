@@ -25,9 +25,9 @@ MCD_OK, MCD_E_INVALID, MCD_E_UNSUPPORTED, MCD_E_WORKSPACE, MCD_E_HIP = range(5)
 MCD_F32, MCD_BF16 = 0, 1
 MCD_ROW_COND, MCD_ROW_UNCOND, MCD_ROW_SOLO, MCD_ROW_TEXT = 0, 1, 2, 3
 MCD_DEV_BAD_PARAM, MCD_DEV_GRID_RANGE, MCD_DEV_BAD_PLAN, MCD_DEV_BAD_TOKEN = 1, 2, 4, 8
-MCD_DEV_BAD_PAGE = 16
+MCD_DEV_BAD_PAGE, MCD_DEV_NO_PAGE = 16, 32
 MCD_CACHE_PAGE = 64
-MCD_MAX_K, MCD_MAX_V = 32, 4096
+MCD_MAX_K, MCD_MAX_V, MCD_MAX_TOP = 32, 4096, 32
 
 _vp = ctypes.c_void_p
 _i32 = ctypes.c_int32
@@ -96,10 +96,35 @@ class mcd_cache_attend_args(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_size_t)]
 
 
+class mcd_cache_groups(ctypes.Structure):
+    _fields_ = [("n", _i32), ("max_rows", _i32), ("max_prefix", _i32), ("max_own", _i32),
+                ("start", _vp), ("prefix", _vp)]
+
+
 class mcd_cache_evict_args(ctypes.Structure):
     _fields_ = [("R", _i32), ("max_length", _i32), ("keep", _i32), ("recent", _i32),
                 ("slot", _vp), ("length", _vp), ("kept", _vp), ("length_out", _vp),
                 ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class mcd_logprobs_args(ctypes.Structure):
+    _fields_ = [("n", _i32), ("K", _i32), ("V", _i32), ("T", _i32), ("pad_id", _i32),
+                ("dtype", ctypes.c_int), ("logits", _vp), ("logits_stride", ctypes.c_int64),
+                ("V_stream", _vp), ("token_rows", _i32), ("tokens", _vp), ("token_row", _vp),
+                ("logprob", _vp), ("entropy", _vp), ("top_ids", _vp), ("top_logprobs", _vp),
+                ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class mcd_cache_pages(ctypes.Structure):
+    _fields_ = [("n_slots", _i32), ("max_pages", _i32), ("n_pages", _i32), ("table", _vp),
+                ("refs", _vp)]
+
+
+class mcd_cache_reserve_args(ctypes.Structure):
+    _fields_ = [("R", _i32), ("n_tokens", _i32), ("max_tokens", _i32), ("max_context", _i32),
+                ("slot", _vp), ("context", _vp), ("tokens", _vp), ("start", _vp), ("where", _vp),
+                ("row", _vp), ("position", _vp), ("workspace", _vp),
+                ("workspace_bytes", ctypes.c_size_t)]
 
 
 def _sig(name, res, *args):
@@ -149,8 +174,24 @@ _mcd_cache_read = _sig("mcd_cache_read", ctypes.c_int, _cache_p, _rows_p, ctypes
                        _i64, _vp, _i64, _vp, _size, _vp)
 _mcd_cache_attend = _sig("mcd_cache_attend", ctypes.c_int, _cache_p, _rows_p,
                          ctypes.POINTER(mcd_cache_attend_args), _vp)
+_groups_p = ctypes.POINTER(mcd_cache_groups)
+_mcd_cache_shared_workspace_bytes = _sig("mcd_cache_shared_workspace_bytes", _size, _cache_p,
+                                         _rows_p, _groups_p, _i32)
+_mcd_cache_attend_shared = _sig("mcd_cache_attend_shared", ctypes.c_int, _cache_p, _rows_p,
+                                _groups_p, ctypes.POINTER(mcd_cache_attend_args), _vp)
 _mcd_cache_evict = _sig("mcd_cache_evict", ctypes.c_int, _cache_p, _cache_p,
                         ctypes.POINTER(mcd_cache_evict_args), _vp)
+_pages_p = ctypes.POINTER(mcd_cache_pages)
+_mcd_cache_pages_workspace_bytes = _sig("mcd_cache_pages_workspace_bytes", _size, _pages_p, _i32)
+_mcd_cache_count = _sig("mcd_cache_count", ctypes.c_int, _pages_p, _vp, _size, _vp)
+_mcd_cache_release = _sig("mcd_cache_release", ctypes.c_int, _pages_p, _i32, _vp, _vp, _vp, _size,
+                          _vp)
+_mcd_cache_share = _sig("mcd_cache_share", ctypes.c_int, _pages_p, _i32, _vp, _vp, _vp, _vp, _size,
+                        _vp)
+_mcd_cache_reserve = _sig("mcd_cache_reserve", ctypes.c_int, _pages_p,
+                          ctypes.POINTER(mcd_cache_reserve_args), _vp)
+_mcd_logprobs_workspace_bytes = _sig("mcd_logprobs_workspace_bytes", _size, _i32, _i32, _i32, _i32)
+_mcd_logprobs = _sig("mcd_logprobs", ctypes.c_int, ctypes.POINTER(mcd_logprobs_args), _vp)
 _mcd_status_string = _sig("mcd_status_string", ctypes.c_char_p, ctypes.c_int)
 _mcd_last_error = _sig("mcd_last_error", ctypes.c_char_p)
 
@@ -164,6 +205,9 @@ EXPORTED = ["mcd_head_create", "mcd_head_destroy", "mcd_plan_words", "mcd_batch_
             "mcd_sched_commit", "mcd_sched_counts",
             "mcd_cache_page_bytes", "mcd_cache_workspace_bytes", "mcd_cache_append",
             "mcd_cache_read", "mcd_cache_attend", "mcd_cache_evict",
+            "mcd_cache_shared_workspace_bytes", "mcd_cache_attend_shared",
+            "mcd_logprobs_workspace_bytes", "mcd_logprobs", "mcd_cache_pages_workspace_bytes", "mcd_cache_count", "mcd_cache_release",
+            "mcd_cache_share", "mcd_cache_reserve",
             "mcd_status_string", "mcd_last_error"]
 
 
@@ -425,6 +469,13 @@ def mcd_cache_workspace_bytes(cache, rows, Hq):
     return n
 
 
+def mcd_cache_shared_workspace_bytes(cache, rows, groups, Hq):
+    n = int(_mcd_cache_shared_workspace_bytes(cache.ref, rows.ref, groups.ref, Hq))
+    if n == 0:
+        raise McdError(MCD_E_INVALID, "mcd_cache_shared_workspace_bytes")
+    return n
+
+
 _DTYPES = {torch.bfloat16: MCD_BF16, torch.float32: MCD_F32}
 
 
@@ -478,10 +529,11 @@ class Cache:
             if weights else None
         return cls(pages, table, D, weight)
 
-    def workspace(self, rows, Hq):
-        """A zeroed workspace for these rows' bounds and every smaller step."""
-        return torch.zeros(mcd_cache_workspace_bytes(self, rows, Hq), dtype=torch.uint8,
-                           device=self.pages.device)
+    def workspace(self, rows, Hq, groups=None):
+        """A zeroed workspace for these rows' (and groups') bounds and every smaller step."""
+        need = mcd_cache_workspace_bytes(self, rows, Hq) if groups is None else \
+            mcd_cache_shared_workspace_bytes(self, rows, groups, Hq)
+        return torch.zeros(need, dtype=torch.uint8, device=self.pages.device)
 
 
 class CacheRows:
@@ -505,6 +557,22 @@ class CacheRows:
                                      _ptr(slot), _ptr(context), _ptr(start))
         self.ref = ctypes.byref(self.struct)
         self.on_gpu = all(t is None or t.is_cuda for t in (context, start, slot))
+
+
+class CacheGroups:
+    """Groups of consecutive rows whose first prefix positions' whole pages are the same (int32
+    device tensors, borrowed): start [n + 1], prefix [n].  max_rows, max_prefix and max_own bound
+    every group's rows, its prefix and its rows' positions past the shared pages."""
+
+    def __init__(self, start, prefix, max_rows, max_prefix, max_own):
+        self.start, self.prefix, self.n = start, prefix, prefix.shape[0]
+        for name, t, n in (("start", start, self.n + 1), ("prefix", prefix, self.n)):
+            if t.dtype != torch.int32 or tuple(t.shape) != (n,) or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous int32 [{n}]")
+        self.struct = mcd_cache_groups(self.n, int(max_rows), int(max_prefix), int(max_own),
+                                       _ptr(start), _ptr(prefix))
+        self.ref = ctypes.byref(self.struct)
+        self.on_gpu = start.is_cuda and prefix.is_cuda
 
 
 def _on_gpu(*parts):
@@ -532,10 +600,7 @@ def mcd_cache_read(cache, rows, k, v, workspace, stream=None):
            "mcd_cache_read")
 
 
-def mcd_cache_attend(cache, rows, q, out, workspace, scale=None, lse=None, weight_out=None,
-                     stream=None):
-    """out = softmax(scale q k^T) v for q, out [n_tokens][Hq][D] (bf16 or fp32); scale: default
-    1 / sqrt(D).  weight_out: laid out as cache.weight (which it may be)."""
+def _attend_args(cache, rows, q, out, workspace, scale, lse, weight_out):
     Hq = q.shape[1]
     dt, qs = _tokens("q", q, rows, Hq, cache.D)
     _, os_ = _tokens("out", out, rows, Hq, cache.D, q)
@@ -547,11 +612,28 @@ def mcd_cache_attend(cache, rows, q, out, workspace, scale=None, lse=None, weigh
             or weight_out.numel() != cache.n_slots * cache.Hkv * cache.max_pages * MCD_CACHE_PAGE):
         raise ValueError("weight_out must be laid out as the cache's weight")
     _on_gpu(cache, rows, lse, weight_out, workspace)
-    a = mcd_cache_attend_args(Hq, dt, cache.D ** -0.5 if scale is None else scale, q.data_ptr(),
-                              qs, out.data_ptr(), os_, _ptr(lse), _ptr(weight_out),
-                              workspace.data_ptr(), workspace.nbytes)
+    return mcd_cache_attend_args(Hq, dt, cache.D ** -0.5 if scale is None else scale,
+                                 q.data_ptr(), qs, out.data_ptr(), os_, _ptr(lse),
+                                 _ptr(weight_out), workspace.data_ptr(), workspace.nbytes)
+
+
+def mcd_cache_attend(cache, rows, q, out, workspace, scale=None, lse=None, weight_out=None,
+                     stream=None):
+    """out = softmax(scale q k^T) v for q, out [n_tokens][Hq][D] (bf16 or fp32); scale: default
+    1 / sqrt(D).  weight_out: laid out as cache.weight (which it may be)."""
+    a = _attend_args(cache, rows, q, out, workspace, scale, lse, weight_out)
     _check(_mcd_cache_attend(cache.ref, rows.ref, ctypes.byref(a), _stream(stream)),
            "mcd_cache_attend")
+
+
+def mcd_cache_attend_shared(cache, rows, groups, q, out, workspace, scale=None, lse=None,
+                            stream=None):
+    """mcd_cache_attend of rows in groups (CacheGroups), a group's shared pages read once for all of
+    its rows; workspace: cache.workspace(rows, Hq, groups=groups)."""
+    a = _attend_args(cache, rows, q, out, workspace, scale, lse, None)
+    _on_gpu(groups)
+    _check(_mcd_cache_attend_shared(cache.ref, rows.ref, groups.ref, ctypes.byref(a),
+                                    _stream(stream)), "mcd_cache_attend_shared")
 
 
 def mcd_cache_evict(src, dst, length, keep, recent, kept, length_out, workspace, max_length,
@@ -568,6 +650,143 @@ def mcd_cache_evict(src, dst, length, keep, recent, kept, length_out, workspace,
                              _ptr(kept), _ptr(length_out), workspace.data_ptr(), workspace.nbytes)
     _check(_mcd_cache_evict(src.ref, dst.ref, ctypes.byref(a), _stream(stream)),
            "mcd_cache_evict")
+
+
+# ---------------------------------------------------------------------------
+# page tables on the GPU
+
+class CachePages:
+    """A cache's page table (int32 [n_slots][max_pages], borrowed; below 0: no page) and how many
+    of its entries hold each of n_pages pages (refs, counted here)."""
+
+    def __init__(self, table, n_pages):
+        if table.dtype != torch.int32 or table.dim() != 2 or not table.is_contiguous():
+            raise ValueError("table must be contiguous int32 [n_slots][max_pages]")
+        self.table, self.n_pages = table, int(n_pages)
+        self.n_slots, self.max_pages = table.shape
+        self.refs = torch.zeros(max(self.n_pages, 0), dtype=torch.int32, device=table.device)
+        self.struct = mcd_cache_pages(self.n_slots, self.max_pages, self.n_pages, _ptr(table),
+                                      _ptr(self.refs))
+        self.ref = ctypes.byref(self.struct)
+        self.on_gpu = table.is_cuda
+        if self.on_gpu:
+            mcd_cache_count(self, torch.zeros(256, dtype=torch.uint8, device=table.device))
+
+    def workspace_bytes(self, R):
+        n = int(_mcd_cache_pages_workspace_bytes(self.ref, int(R)))
+        if n == 0:
+            raise McdError(MCD_E_INVALID, "mcd_cache_pages_workspace_bytes")
+        return n
+
+    def workspace(self, R):
+        """A zeroed workspace of the calls on R rows and fewer."""
+        return torch.zeros(self.workspace_bytes(R), dtype=torch.uint8, device=self.table.device)
+
+
+def _whole(name, t, n, dtype=torch.int32):
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous {dtype} [{n}]")
+
+
+def mcd_cache_count(pages, workspace, stream=None):
+    """pages.refs from the table, after the host has written it."""
+    _on_gpu(pages, workspace)
+    _check(_mcd_cache_count(pages.ref, workspace.data_ptr(), workspace.nbytes, _stream(stream)),
+           "mcd_cache_count")
+
+
+def mcd_cache_release(pages, slot, workspace, length=None, stream=None):
+    """The slots keep the pages of their first length positions (None: no page); slot, length:
+    int32 [R]."""
+    R = slot.shape[0]
+    _whole("slot", slot, R)
+    _whole("length", length, R)
+    _on_gpu(pages, slot, length, workspace)
+    _check(_mcd_cache_release(pages.ref, R, slot.data_ptr(), _ptr(length), workspace.data_ptr(),
+                              workspace.nbytes, _stream(stream)), "mcd_cache_release")
+
+
+def mcd_cache_share(pages, slot, source, length, workspace, stream=None):
+    """The whole pages of the sources' first length positions become the slots' too; slot, source,
+    length: int32 [R]."""
+    R = slot.shape[0]
+    for name, t in (("slot", slot), ("source", source), ("length", length)):
+        _whole(name, t, R)
+    _on_gpu(pages, slot, source, length, workspace)
+    _check(_mcd_cache_share(pages.ref, R, slot.data_ptr(), source.data_ptr(), length.data_ptr(),
+                            workspace.data_ptr(), workspace.nbytes, _stream(stream)),
+           "mcd_cache_share")
+
+
+def mcd_cache_reserve(pages, context, tokens, start, workspace, slot=None, n_tokens=0,
+                      max_tokens=0, max_context=0, where=None, row=None, position=None,
+                      stream=None):
+    """Pages for tokens[r] new tokens of every row after context[r] positions (int32 [R]); start:
+    int32 [R + 1], where: int64, row, position: int32 [n_tokens] receive the tokens' places."""
+    R = context.shape[0]
+    for name, t, n in (("context", context, R), ("tokens", tokens, R), ("slot", slot, R),
+                       ("start", start, R + 1), ("row", row, n_tokens),
+                       ("position", position, n_tokens)):
+        _whole(name, t, n)
+    _whole("where", where, n_tokens, torch.int64)
+    _on_gpu(pages, context, tokens, slot, start, where, row, position, workspace)
+    a = mcd_cache_reserve_args(R, int(n_tokens), int(max_tokens), int(max_context), _ptr(slot),
+                               _ptr(context), _ptr(tokens), _ptr(start), _ptr(where), _ptr(row),
+                               _ptr(position), workspace.data_ptr(), workspace.nbytes)
+    _check(_mcd_cache_reserve(pages.ref, ctypes.byref(a), _stream(stream)), "mcd_cache_reserve")
+
+
+# ---------------------------------------------------------------------------
+# log probabilities
+
+def mcd_logprobs_workspace_bytes(n, K, V, T):
+    b = int(_mcd_logprobs_workspace_bytes(int(n), int(K), int(V), int(T)))
+    if b == 0:
+        raise McdError(MCD_E_INVALID, "mcd_logprobs_workspace_bytes")
+    return b
+
+
+def mcd_logprobs(logits, tokens, logprob, workspace, entropy=None, top_ids=None,
+                 top_logprobs=None, V_stream=None, token_row=None, pad_id=-1, stream=None):
+    """Log probabilities of tokens (int32 [rows][K]) under logits (bf16 or fp32 [n][K][V], or [n][N]
+    with V_stream), entropies [n][K] (float32) and the T most likely ids [n][K][T] (int32) with
+    theirs.  token_row: int32 [n], the row of tokens of each row of logits, or None: its index."""
+    if logits.dtype not in _DTYPES:
+        raise ValueError(f"logits: dtype {logits.dtype}")
+    if V_stream is None:
+        if logits.dim() != 3 or logits.stride(2) != 1 or (
+                logits.shape[1] > 1 and logits.stride(1) != logits.shape[2]):
+            raise ValueError("logits must be [n][K][V], a row's logits contiguous")
+        n, K, V = logits.shape
+    else:
+        V_stream = np.ascontiguousarray(V_stream, dtype=np.int32)
+        K, V = V_stream.shape[0], int(V_stream.max())
+        n = logits.shape[0]
+        if logits.dim() != 2 or logits.stride(1) != 1 or logits.shape[1] != int(V_stream.sum()):
+            raise ValueError("logits must be [n][sum of V_stream], a row's logits contiguous")
+    for name, t, dt, shape in (
+            ("tokens", tokens, torch.int32, (tokens.shape[0], K)),
+            ("token_row", token_row, torch.int32, (n,)), ("logprob", logprob, torch.float32, (n, K)),
+            ("entropy", entropy, torch.float32, (n, K))):
+        if t is not None and (t.dtype != dt or tuple(t.shape) != shape or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous {dt} {list(shape)}")
+    T = 0
+    for name, t, dt in (("top_ids", top_ids, torch.int32),
+                        ("top_logprobs", top_logprobs, torch.float32)):
+        if t is None:
+            continue
+        if t.dtype != dt or t.dim() != 3 or t.shape[:2] != (n, K) or not t.is_contiguous() \
+                or t.shape[2] < 1 or (T and t.shape[2] != T):
+            raise ValueError(f"{name} must be contiguous {dt} [{n}][{K}][T]")
+        T = t.shape[2]
+    _on_gpu(logits, tokens, token_row, logprob, entropy, top_ids, top_logprobs, workspace)
+    width = logits[0].numel() if n else 0
+    a = mcd_logprobs_args(
+        n, K, V, T, int(pad_id), _DTYPES[logits.dtype], _ptr(logits),
+        logits.stride(0) if n > 1 else width, _ptr(V_stream), tokens.shape[0], _ptr(tokens),
+        _ptr(token_row), _ptr(logprob), _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs),
+        workspace.data_ptr(), workspace.nbytes)
+    _check(_mcd_logprobs(ctypes.byref(a), _stream(stream)), "mcd_logprobs")
 
 
 # ---------------------------------------------------------------------------

@@ -1,0 +1,244 @@
+"""Attention of rows that share pages, against its description in 64 bits (tests/_cache_ref.py) and
+against each row on its own."""
+import numpy as np
+import pytest
+
+import _cache_ref as ref
+
+torch = pytest.importorskip("torch")
+mcd = pytest.importorskip("paper_2607_02119_amd.mcd", reason="libmcd.so not built")
+
+from test_gpu_cache import bounds, dev, i32, make_cache, make_rows, rounded, slot_kv, starts  # noqa: E402
+
+pytestmark = [pytest.mark.gpu,
+              pytest.mark.skipif(not torch.cuda.is_available(), reason="no GPU")]
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+class Step:
+    """Rows in groups: groups is a list of (prefix, [(positions past its whole pages, new tokens)]).
+    The first row of a group holds the pages that the others' tables name too."""
+
+    def __init__(self, rng, groups, Hq, Hkv, D, dtype, spare_rows=0, slack=0):
+        self.prefix = np.array([p for p, _ in groups])
+        self.sizes = np.array([len(rows) for _, rows in groups])
+        self.of = np.repeat(np.arange(len(groups)), self.sizes)
+        own = [x for _, rows in groups for x in rows]
+        self.shared = self.prefix // 64
+        self.ctx = np.array([self.shared[g] * 64 + c for g, (c, _) in zip(self.of, own)], int)
+        self.new = np.array([n for _, n in own], int)
+        R = len(own)
+        self.slot = rng.permutation(R)
+        lengths = np.zeros(R, int)
+        lengths[self.slot] = self.ctx + self.new
+        self.cache, self.pages, self.table, _, _ = make_cache(rng, lengths, Hkv, D)
+        first = np.concatenate([[0], np.cumsum(self.sizes)])
+        for r, g in enumerate(self.of):
+            n = self.shared[g]
+            self.table[self.slot[r], :n] = self.table[self.slot[first[g]], :n]
+        self.cache.table.copy_(i32(self.table))
+        self.rows = make_rows(self.ctx, self.new, self.slot,
+                              max_context=int((self.ctx + self.new).max()) + slack)
+        self.groups = mcd.CacheGroups(
+            i32(first), i32(self.prefix), int(self.sizes.max()) + slack,
+            int(self.prefix.max()) + slack,
+            int((self.ctx + self.new - 64 * self.shared[self.of]).max()) + slack)
+        self.Hq, self.D, self.dtype, self.N = Hq, D, dtype, int(self.new.sum())
+        self.q = rounded(rng.standard_normal((self.N, Hq, D)) * 2, dtype)
+
+    def run(self, shared=True, scale=0.07):
+        wide = torch.zeros((self.N, self.Hq + 3, self.D), dtype=self.dtype, device="cuda")
+        wide[:, :self.Hq] = dev(self.q).to(self.dtype)
+        out = torch.full((self.N, self.Hq + 1, self.D), 9.0, dtype=self.dtype, device="cuda")
+        lse = torch.full((self.N, self.Hq), 9.0, device="cuda")
+        ws = self.cache.workspace(self.rows, self.Hq, groups=self.groups)
+        ws[256:] = 255
+        if shared:
+            mcd.mcd_cache_attend_shared(self.cache, self.rows, self.groups, wide[:, :self.Hq],
+                                        out[:, :self.Hq], ws, scale=scale, lse=lse)
+        else:
+            mcd.mcd_cache_attend(self.cache, self.rows, wide[:, :self.Hq], out[:, :self.Hq], ws,
+                                 scale=scale, lse=lse)
+        status = mcd.mcd_read_device_status(ws)
+        assert bool((out[:, self.Hq] == 9.0).all())
+        return out[:, :self.Hq], lse, status
+
+    def check(self, got, lse, rows=None, scale=0.07):
+        got, lse = got.double().cpu().numpy(), lse.double().cpu().numpy()
+        scale = float(np.float32(scale))
+        for r in range(len(self.ctx)) if rows is None else rows:
+            a, n = starts(self.new)[r], self.new[r]
+            if n == 0:
+                continue
+            k, v = slot_kv(self.pages, self.table, self.slot[r], self.ctx[r] + n, self.D)
+            q = self.q[a:a + n]
+            o, l, wt, size = ref.attend(k, v, q.astype(np.float64), self.ctx[r], scale)
+            to, _, tl = bounds(k, q, scale, self.dtype, wt, size)
+            assert (np.abs(got[a:a + n] - o) <= to).all(), (r, np.abs(got[a:a + n] - o).max())
+            assert (np.abs(lse[a:a + n] - l) <= tl + 2.0 ** -22 * np.abs(l)).all()
+
+
+def _same(prefix, rows, own=3, new=1):
+    return (prefix, [(own + 7 * i % 60, new) for i in range(rows)])
+
+
+CASES = [
+    # name, Hq, Hkv, D, dtype, groups
+    ("two_rows", 2, 2, 64, BF16, [_same(64, 2)]),
+    ("two_rows_fp32", 2, 2, 64, F32, [_same(130, 2)]),
+    ("a_row_alone", 4, 1, 128, BF16, [(200, [(9, 1)])]),
+    ("nothing_of_their_own_yet", 4, 2, 128, BF16, [(256, [(0, 1), (0, 1), (0, 1)])]),
+    ("four_columns", 4, 4, 128, BF16, [_same(700, 4), _same(100, 3)]),
+    ("eight_columns", 8, 2, 128, BF16, [_same(700, 2), _same(90, 1)]),
+    ("eight_columns_fp32", 4, 2, 128, F32, [_same(700, 4), _same(90, 1)]),
+    ("sixteen_columns", 16, 8, 128, BF16, [_same(1000, 8)]),
+    ("sixteen_columns_fp32", 8, 4, 256, F32, [_same(500, 8)]),
+    ("tile_of_64", 8, 2, 128, BF16, [_same(300, 16), _same(640, 5), _same(20, 3)]),
+    ("tile_of_64_fp32", 10, 2, 64, F32, [_same(300, 12), _same(640, 5)]),
+    ("tile_of_128", 8, 2, 128, BF16, [_same(300, 50), _same(500, 33), _same(64, 1)]),
+    ("tile_of_128_fp32", 4, 1, 128, F32, [_same(300, 50), _same(640, 33)]),
+    ("wide_heads", 8, 2, 256, BF16, [_same(300, 30), _same(640, 5)]),
+    ("wide_heads_fp32", 4, 1, 256, F32, [_same(129, 20), _same(640, 5)]),
+    ("group_of_17_heads", 17, 1, 64, BF16, [_same(200, 3), _same(64, 2)]),
+    ("no_prefix_in_some", 8, 2, 64, BF16, [(0, [(100, 1)]), _same(200, 4), (63, [(5, 1), (64, 1)])]),
+    ("drafts", 8, 2, 128, BF16, [_same(300, 6, 10, 4), _same(90, 3, 60, 3)]),
+    ("drafts_fp32", 25, 5, 64, F32, [_same(300, 6, 10, 3), (0, [(3, 2)]), _same(1003, 7, 0, 1)]),
+    ("rows_without_tokens", 8, 2, 128, BF16, [(300, [(10, 0), (5, 1), (0, 0)]), (100, [(3, 0)]),
+                                              (70, [(1, 2), (0, 0)])]),
+    ("long_prefix", 8, 2, 128, BF16, [_same(9000, 9), _same(5, 2)]),
+    ("long_prefix_fp32", 4, 2, 64, F32, [_same(7000, 20)]),
+    ("long_own_rows", 4, 1, 128, BF16, [(128, [(3000, 1), (5, 1), (1100, 1)])]),
+    ("long_own_rows_and_drafts", 8, 1, 64, BF16, [(128, [(3000, 5), (5, 1), (1100, 3), (700, 1)])]),
+    ("chunks_beside_single_tokens", 8, 4, 64, BF16, [(500, [(0, 40)] + [(9 * i, 1) for i in range(20)]),
+                                                     (64, [(1, 70), (2, 1)])]),
+    ("chunks", 8, 4, 64, BF16, [(500, [(0, 70), (30, 90)]), (100, [(0, 33)])]),
+    ("many_groups", 6, 3, 64, BF16, [_same(64 + 13 * i, 1 + i % 4, i) for i in range(70)]),
+    ("empty_groups", 8, 2, 64, BF16, [(100, []), _same(200, 3), (50, []), _same(64, 2), (9, [])]),
+]
+
+
+@pytest.mark.parametrize("slack", [0, 700], ids=["", "loose"])
+@pytest.mark.parametrize("name,Hq,Hkv,D,dtype,groups", CASES, ids=[c[0] for c in CASES])
+def test_attend(name, Hq, Hkv, D, dtype, groups, slack):
+    rng = np.random.default_rng(sum(map(ord, name)))
+    s = Step(rng, groups, Hq, Hkv, D, dtype, slack=slack)
+    print(f"case shared {name} slack={slack}", flush=True)
+    out, lse, status = s.run()
+    assert status == 0
+    s.check(out, lse)
+    again, lse2, _ = s.run()
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+def test_one_token_each_without_start():
+    """Rows of one token each: start may be NULL; q is out; scale is 1 / sqrt(D)."""
+    rng = np.random.default_rng(2)
+    s = Step(rng, [_same(300, 20), _same(64, 3)], 8, 2, 128, BF16)
+    rows = mcd.CacheRows(i32(s.ctx), slot=i32(s.slot), max_context=int(s.ctx.max()) + 1)
+    ws = s.cache.workspace(rows, 8, groups=s.groups)
+    q = dev(s.q).to(BF16)
+    lse = torch.zeros((s.N, 8), device="cuda")
+    mcd.mcd_cache_attend_shared(s.cache, rows, s.groups, q, q, ws, lse=lse)
+    s.check(q, lse, scale=128 ** -0.5)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+def test_values_and_keys_that_are_not_finite(dtype):
+    """In a shared page: NaN for all rows of the group and its head, and no other group's."""
+    rng = np.random.default_rng(4)
+    D = 128
+    for part in ("key", "value"):
+        s = Step(rng, [_same(200, 20), _same(128, 5)], 8, 2, D, dtype)
+        page, t = s.table[s.slot[0], 1], 37
+        if part == "key":
+            s.pages[page, 1, 64 * D + ((t % 16) * 4 + 2) * 4 + t // 16] = 255
+        else:
+            at = 66 * D + 2 * (t // 4 % 4 * 16 + t // 16 * 4 + t % 4)
+            s.pages[page, 1, at:at + 2] = [0xC0, 0x7F]
+        s.cache.pages.copy_(dev(s.pages))
+        out, lse, status = s.run()
+        nan = torch.isnan(out).all(-1).cpu().numpy()
+        assert status == 0 and nan[:20, 4:].all()
+        assert not torch.isnan(out[20:]).any() and not torch.isnan(out[:, :4]).any()
+        s.check(out[:, :], lse, rows=range(20, 25))
+
+
+def test_extreme_logits_meet_in_the_join():
+    """Prefix and own scores far beyond what exp holds, of both signs."""
+    D, H = 64, 2
+    for sign in (1.0, -1.0):
+        cache = mcd.Cache.alloc(8, H, D, 3, 3)
+        cache.table.copy_(i32([[1, 0, 2], [1, 3, 7], [1, 4, 6]]))
+        ws = torch.zeros(1 << 22, dtype=torch.uint8, device="cuda")
+        L = 100
+        for slot in (0, 1, 2):
+            k = torch.zeros((L, H, D), device="cuda")
+            k[:, :, 0] = torch.linspace(-6, 6, L, device="cuda").view(L, 1)
+            v = torch.arange(L, device="cuda").float().view(L, 1, 1).expand(L, H, D).contiguous()
+            mcd.mcd_cache_append(cache, make_rows([0], [L], [slot]), k, v, ws)
+        rows = make_rows([L - 1] * 3, [1] * 3, [0, 1, 2])
+        groups = mcd.CacheGroups(i32([0, 3]), i32([64]), 3, 64, 64)
+        q = torch.zeros((3, 4, D), device="cuda")
+        q[:, :, 0] = sign * 1e30
+        alone, out = torch.zeros_like(q), torch.zeros_like(q)
+        mcd.mcd_cache_attend(cache, rows, q, alone, ws, scale=1.0)
+        mcd.mcd_cache_attend_shared(cache, rows, groups, q, out, ws, scale=1.0)
+        # (which parts are added first differs: a few roundings of fp32)
+        assert torch.allclose(out, alone, rtol=2.0 ** -18, atol=0) and out.isfinite().all()
+
+
+def test_bad_groups_are_reported():
+    """Rows outside every group, short of the prefix or past max_rows see nothing; lengths past a
+    bound are cut; other rows keep their results."""
+    rng = np.random.default_rng(6)
+    s = Step(rng, [_same(200, 20), _same(128, 5)], 8, 2, 64, BF16)
+    good, lse, _ = s.run()
+
+    def run(start=(0, 20, 25), prefix=(200, 128), max_rows=20, max_prefix=200, max_own=None,
+            ctx=None):
+        s.groups = mcd.CacheGroups(i32(start), i32(prefix), max_rows, max_prefix,
+                                   int((s.ctx + 1 - 64 * s.shared[s.of]).max())
+                                   if max_own is None else max_own)
+        s.rows = make_rows(s.ctx if ctx is None else ctx, s.new, s.slot, max_context=400)
+        out, _, status = s.run()
+        return out, status
+
+    for kw, zero in ((dict(start=(0, 20, 23)), range(23, 25)),
+                     (dict(start=(2, 20, 25)), range(0, 2)),
+                     (dict(start=(0, 20, 90)), []),
+                     (dict(max_rows=17), range(17, 20)),
+                     (dict(ctx=np.where(np.arange(25) == 3, 100, s.ctx)), [3])):
+        out, status = run(**kw)
+        assert status == mcd.MCD_DEV_BAD_PAGE, kw
+        for r in range(25):
+            if r in zero:
+                assert not out[r].any(), (kw, r)
+            else:
+                assert torch.equal(out[r], good[r]), (kw, r)
+    for kw in (dict(prefix=(200, -1)), dict(max_prefix=150), dict(max_own=8),
+               dict(start=(0, 30, 25)), dict(start=(0, -4, 25)), dict(start=(20, 0, 25))):
+        out, status = run(**kw)
+        assert status == mcd.MCD_DEV_BAD_PAGE, kw
+    # a page id out of range in a shared page: its positions are not seen
+    s.cache.table[int(s.slot[0]), 1] = 1 << 20
+    out, status = run()
+    assert status == mcd.MCD_DEV_BAD_PAGE and out.isfinite().all()
+    assert torch.equal(out[20:], good[20:])
+
+
+def test_a_workspace_serves_smaller_steps():
+    rng = np.random.default_rng(7)
+    big = Step(rng, [_same(3000, 64, 100), _same(200, 3)], 8, 2, 128, BF16)
+    ws = big.cache.workspace(big.rows, 8, groups=big.groups)
+    for groups in ([_same(3000, 64, 100)], [_same(3000, 1)], [_same(64, 2)], [_same(1000, 9)] * 2):
+        s = Step(rng, groups, 8, 2, 128, BF16)
+        assert s.cache.workspace(s.rows, 8, groups=s.groups).numel() <= ws.numel()
+        q = dev(s.q).to(BF16)
+        out, lse = torch.zeros_like(q), torch.zeros((s.N, 8), device="cuda")
+        mcd.mcd_cache_attend_shared(s.cache, s.rows, s.groups, q, out, ws, scale=0.07, lse=lse)
+        s.check(out, lse)
+    with pytest.raises(mcd.McdError, match="needed"):
+        mcd.mcd_cache_attend_shared(big.cache, big.rows, big.groups, dev(big.q).to(BF16),
+                                    torch.zeros((big.N, 8, 128), dtype=BF16, device="cuda"),
+                                    ws[:ws.numel() - 256])
