@@ -39,15 +39,39 @@ __device__ __forceinline__ bool before(const Entry &a, const Entry &b) {
   return a.order > b.order || (a.order == b.order && a.id < b.id);
 }
 
+// Over the 64 lanes, on the vector units: within rows of 16 lanes by rotation, across them
+// by swaps.
+template <int CTRL>
+__device__ __forceinline__ uint32_t row_move(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false);
+}
+template <class F>
+__device__ __forceinline__ uint32_t wave_reduce(uint32_t x, F &&f) {
+  x = f(x, row_move<0x128>(x));                      // row_ror 8, 4, 2, 1
+  x = f(x, row_move<0x124>(x));
+  x = f(x, row_move<0x122>(x));
+  x = f(x, row_move<0x121>(x));
+  const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = f(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return f(b[0], b[1]);
+}
 __device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
-  return x;
+  return __uint_as_float(wave_reduce(__float_as_uint(x), [](uint32_t a, uint32_t b)
+                                         __attribute__((always_inline)) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  }));
 }
 __device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
-  return x;
+  return __uint_as_float(wave_reduce(__float_as_uint(x), [](uint32_t a, uint32_t b)
+                                         __attribute__((always_inline)) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
+}
+__device__ __forceinline__ uint32_t wave_min(uint32_t x) {
+  return wave_reduce(x, [](uint32_t a, uint32_t b) __attribute__((always_inline)) {
+    return min(a, b);
+  });
 }
 
 // The wave's LDS accesses so far are done before those that follow (of the same wave).
@@ -58,52 +82,66 @@ __device__ __forceinline__ void wave_lds_sync() {
 
 constexpr int kRoom = 128;                           // candidates that a wave sorts
 
-// The T (1..kMostTop) first of the wave's entries order[i], id(i) (i < E, every lane's
-// own) into list[0..T), {0, ~0} past the last; orders up to kMaskedOrder are no
-// entries.  room: kRoom entries of LDS of the wave's own.
+// The first T of `count` (at most kRoom) entries of LDS into list, in order: each is compared
+// with all.
+__device__ __forceinline__ void rank_entries(const Entry *room, int count, int T, Entry *list) {
+  for (int c = threadIdx.x & 63; c < count; c += 64) {
+    const Entry e = room[c];
+    int rank = 0;
+    for (int k = 0; k < count; ++k) rank += before(room[k], e);
+    if (rank < T) list[rank] = e;
+  }
+}
+
+// The T (2..kMostTop) first of the wave's logits x[i] with ids id(i) (i < E, every lane's own)
+// into list[0..T), {0, ~0} past the last; -infinity and NaN are none.  room: kRoom entries of
+// LDS of the wave's own.
 //
-// T lanes hold a largest entry of at least `least`, so the T first are among the entries
-// from `least` on: usually little more than T of them, which are compared each with all.
-// Where ties make them more than kRoom, they are taken one by one.
+// T lanes hold a largest logit of at least `least`, so the T first are among the logits
+// from `least` on.  It is found bit by bit from the lanes' largest; its upper 16 bits do unless
+// more than kRoom logits lie there, which takes the others too, and where ties leave more
+// even so, the first are taken one by one.
 template <int E, class Id>
-__device__ __forceinline__ void wave_top(const uint32_t (&order)[E], Id &&id, int T, Entry *room,
+__device__ __forceinline__ void wave_top(const float (&x)[E], Id &&id, int T, Entry *room,
                                          Entry *list) {
   const int lane = threadIdx.x & 63;
-  uint32_t mine = order[0];
+  float most = x[0];
 #pragma unroll
-  for (int i = 1; i < E; ++i) mine = max(mine, order[i]);
+  for (int i = 1; i < E; ++i) most = fmaxf(most, x[i]);
+  const uint32_t mine = order_of(most);
   uint32_t least = 0;
-#pragma unroll 1
-  for (uint32_t bit = 1u << 31; bit; bit >>= 1)
-    if (__popcll(__ballot(mine >= (least | bit))) >= T) least |= bit;
-  least = max(least, kMaskedOrder + 1);
   int count = 0;
+#pragma unroll 1
+  for (int half = 0; half < 2; ++half) {
+#pragma unroll 4
+    for (uint32_t bit = half ? 1u << 15 : 1u << 31; bit >= (half ? 1u : 1u << 16); bit >>= 1)
+      if ((int)__popcll(__ballot(mine >= (least | bit))) >= T) least |= bit;
+    const float from = logit_of(max(least, kMaskedOrder + 1));
+    count = 0;
 #pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const bool in = order[i] >= least;
-    const uint64_t all = __ballot(in);
-    const int at = count + __popcll(all & ((1ull << lane) - 1));
-    if (in && at < kRoom) room[at] = Entry{order[i], id(i)};
-    count += __popcll(all);
+    for (int i = 0; i < E; ++i) {
+      const bool in = x[i] >= from;
+      const uint64_t all = __ballot(in);
+      if (!all) continue;
+      const int at = count + (int)__popcll(all & ((1ull << lane) - 1));
+      if (in && at < kRoom) room[at] = Entry{order_of(x[i]), id(i)};
+      count += (int)__popcll(all);
+    }
+    if (count <= kRoom) break;
   }
   if (lane < T) list[lane] = Entry{0u, ~0u};
   wave_lds_sync();
   if (count <= kRoom) {
-    for (int c = lane; c < count; c += 64) {
-      const Entry e = room[c];
-      int rank = 0;
-      for (int k = 0; k < count; ++k) rank += before(room[k], e);
-      if (rank < T) list[rank] = e;
-    }
+    rank_entries(room, count, T, list);
   } else {
     Entry last = {~0u, 0u};
     for (int n = 0; n < T; ++n) {
       Entry best = {0u, ~0u};
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        const Entry e = {order[i], id(i)};
+        const Entry e = {order_of(x[i]), id(i)};
         // (count > kRoom >= T: there is one every time)
-        if (e.order >= least && (n == 0 || before(last, e)) && before(e, best)) best = e;
+        if (e.order > kMaskedOrder && (n == 0 || before(last, e)) && before(e, best)) best = e;
       }
 #pragma unroll
       for (int d = 32; d > 0; d >>= 1) {
@@ -163,27 +201,38 @@ __device__ __forceinline__ Vector vector_of(const LogprobView &lv, uint32_t v) {
   return x;
 }
 
-// A vector's results, by a wave: from m, S, U and its first T entries (order of each).
+// A vector's token and its logit, loaded before the sums are known.
+struct Given {
+  int token;
+  float logit;
+  bool has;                    // a row of tokens that is there
+};
 template <bool BF16>
-__device__ __forceinline__ void write_vector(const LogprobView &lv, const Vector &x, float m,
-                                             float S, float U, const Entry *list) {
+__device__ __forceinline__ Given given_of(const LogprobView &lv, const Vector &x) {
+  Given g;
+  const int row = lv.token_row ? lv.token_row[x.row] : x.row;
+  g.has = row >= 0 && row < lv.token_rows;
+  g.token = g.has ? lv.tokens[(int64_t)row * lv.K + x.k] : 0;
+  g.logit = Group<BF16>::one(lv.logits, x.at + min(max(g.token, 0), x.V - 1));
+  return g;
+}
+
+// A vector's results, by a wave: from m, S, U and its first T entries.
+__device__ __forceinline__ void write_vector(const LogprobView &lv, const Vector &x,
+                                             const Given &g, float m, float S, float U,
+                                             const Entry *list) {
   const int lane = threadIdx.x & 63;
   const int64_t out = (int64_t)x.row * lv.K + x.k;
   // no distribution: a NaN, infinity or nothing but -infinity among the logits
   const bool none = S != S || m == INFINITY || m == -INFINITY;
   const float nan = __builtin_nanf(""), log_sum = log1pf(S);
   if (lane == 0) {
-    const int row = lv.token_row ? lv.token_row[x.row] : x.row;
-    const bool has = row >= 0 && row < lv.token_rows;
-    const int t = has ? lv.tokens[(int64_t)row * lv.K + x.k] : 0;
-    float lp;
-    if (has && t == lv.pad_id) {
+    float lp = none ? nan : (g.logit - m) - log_sum;
+    if (g.has && g.token == lv.pad_id) {
       lp = 0.0f;                                     // no choice: certain
-    } else if (!has || t < 0 || t >= x.V) {
+    } else if (!g.has || g.token < 0 || g.token >= x.V) {
       lp = nan;
       atomicOr(lv.status, (uint32_t)MCD_DEV_BAD_TOKEN);
-    } else {
-      lp = none ? nan : (Group<BF16>::one(lv.logits, x.at + t) - m) - log_sum;
     }
     lv.logprob[out] = lp;
     if (lv.entropy) lv.entropy[out] = none ? nan : log_sum + U / (1.0f + S);
@@ -198,12 +247,18 @@ __device__ __forceinline__ void write_vector(const LogprobView &lv, const Vector
   }
 }
 
+enum { kNoTop, kFirst, kTop };   // alternatives: none, the first alone, more
+
 // WAVES waves to a part of E * 64 WAVES logits of a vector.
-template <bool BF16, int WAVES, int E, bool TOP>
+//
+// Exponents are y = x log2 e - m', m' = m log2 e rounded to fp32: one operation for a logit,
+// whose error is y's own rounding and a shift that all share.  The shift, m' less what it
+// stands for, is known (fma), and taken out of S and U at the end.
+template <bool BF16, int WAVES, int E, int TOP>
 __global__ __launch_bounds__(256) void part_kernel(LogprobView lv) {
   typedef Group<BF16> G;
   constexpr int PART = 64 * WAVES * E;
-  __shared__ Entry room[TOP ? 4 * kRoom : 1], list[TOP ? 4 * kMostTop : 1];
+  __shared__ Entry room[TOP == kTop ? 4 * kRoom : 1], list[TOP ? 4 * kMostTop : 1];
   __shared__ float sh_m[4], sh_s[4], sh_u[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // (below 2^31)
@@ -228,6 +283,8 @@ __global__ __launch_bounds__(256) void part_kernel(LogprobView lv) {
     if (at + G::N <= v.V)
       raw[i] = *reinterpret_cast<const typename G::raw *>(base + (int64_t)at * (BF16 ? 2 : 4));
   }
+  Given given = {};
+  if (lv.parts == 1 && (WAVES == 1 || wave == 0)) given = given_of<BF16>(lv, v);
 #pragma unroll
   for (int i = 0; i < E / G::N; ++i) {
     const int at = (int)id(i * G::N);
@@ -256,35 +313,54 @@ __global__ __launch_bounds__(256) void part_kernel(LogprobView lv) {
     for (int i = 0; i < E; ++i) S += x[i] != x[i] ? x[i] : 0.0f;
     S = wave_sum(S);
   } else {
+    // (a maximum beyond what the product holds: differences first)
+    const bool large = fabsf(m) > 0x1p100f;
+    const float top = large ? 0.0f : __fmul_rn(m, kLog2e), shift = large ? m : 0.0f;
+    const float gap = large ? 0.0f : fmaf(m, kLog2e, -top);   // what top falls short of m log2 e by
     int ones = 0;
-    const bool at_m = wave_m == m;                   // (uniform)
+    auto sums = [&](auto at_m) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const float d = x[i] - m;
-      float e = __builtin_amdgcn_exp2f(d * kLog2e);
-      if (at_m) {                                    // 1 for every logit of m's size, counted
-        ones += __popcll(__ballot(d == 0.0f));
-        e = d == 0.0f ? 0.0f : e;
+      for (int i = 0; i < E; ++i) {
+        const float z = large ? x[i] - shift : x[i];
+        const float y = fmaf(z, kLog2e, -top);
+        float e = __builtin_amdgcn_exp2f(y);
+        if constexpr (decltype(at_m)::value) {       // 1 for every logit of m's size, counted
+          const bool is = x[i] == m;
+          ones += (int)__popcll(__ballot(is));
+          e = is ? 0.0f : e;
+        }
+        S += e;
+        // (e is 0 from there on, and 0 times infinity is not)
+        U = fmaf(e, fmaxf(y, -300.0f), U);
       }
-      S += e;
-      // (e is 0 from there on, and 0 times infinity is not)
-      U = fmaf(e, fmaxf(d, -256.0f), U);
-    }
-    S = wave_sum(S) + (float)max(ones - 1, 0);
-    U = wave_sum(-U);
+    };
+    if (wave_m == m) sums(std::true_type{});
+    else sums(std::false_type{});
+    S = wave_sum(S);
+    U = wave_sum(U);
+    // 2^y = 2^(true exponent + gap): both sums carry 2^gap
+    const float f = __builtin_amdgcn_exp2f(-gap);
+    U = (gap * S - U) * f * 0.6931471805599453f;
+    S = S * f + (float)max(ones - 1, 0);
     // m of other waves too: their ones are not the vector's first
     if constexpr (WAVES > 1) {
       bool earlier = false;
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) earlier |= w < wave && sh_m[w] == m;
-      if (at_m && earlier && ones) S += 1.0f;
+      if (ones && earlier) S += 1.0f;
     }
   }
-  if constexpr (TOP) {
-    uint32_t order[E];
+  if constexpr (TOP == kTop)
+    wave_top<E>(x, id, lv.T, room + wave * kRoom, list + wave * kMostTop);
+  if constexpr (TOP == kFirst) {
+    uint32_t at = ~0u;
+    if (wave_m == m && m > -INFINITY) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) order[i] = order_of(x[i]);
-    wave_top<E>(order, id, lv.T, room + wave * kRoom, list + wave * kMostTop);
+      for (int i = E - 1; i >= 0; --i) at = x[i] == m ? id(i) : at;
+      at = wave_min(at);
+    }
+    if (lane == 0) list[wave * kMostTop] = Entry{at == ~0u ? 0u : order_of(m), at};
+    if constexpr (WAVES == 1) wave_lds_sync();
   }
   if constexpr (WAVES > 1) {
     if (lane == 0) {
@@ -299,30 +375,37 @@ __global__ __launch_bounds__(256) void part_kernel(LogprobView lv) {
       S += sh_s[w];
       U += sh_u[w];
     }
-    if constexpr (TOP) {
-      // the waves' lists: two entries a lane
-      uint32_t order[2], ids[2];
+    if constexpr (TOP == kFirst) {
+      Entry best = list[0];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int at = i * 64 + lane;
-        const bool in = at % kMostTop < lv.T;
-        order[i] = in ? list[at].order : 0u;
-        ids[i] = in ? list[at].id : ~0u;
-      }
+      for (int w = 1; w < WAVES; ++w)
+        if (before(list[w * kMostTop], best)) best = list[w * kMostTop];
       wave_lds_sync();
-      wave_top<2>(order, [&](int i) __attribute__((always_inline)) { return ids[i]; }, lv.T, room,
-                  list);
+      if (lane == 0) list[0] = best;
+      wave_lds_sync();
+    }
+    if constexpr (TOP == kTop) {
+      // the waves' lists, T of each: WAVES T entries, which room holds
+      static_assert(WAVES * kMostTop <= kRoom, "room for the waves' lists");
+      for (int i = lane; i < WAVES * lv.T; i += 64)
+        room[i] = list[i / lv.T * kMostTop + i % lv.T];
+      wave_lds_sync();
+      if (lane < lv.T) list[lane] = Entry{0u, ~0u};
+      wave_lds_sync();
+      rank_entries(room, WAVES * lv.T, lv.T, list);
+      wave_lds_sync();
     }
   }
   const Entry *mine_list = list + (TOP && WAVES == 1 ? wave * kMostTop : 0);
   if (lv.parts == 1) {
-    write_vector<BF16>(lv, v, m, S, U, mine_list);
+    write_vector(lv, v, given, m, S, U, mine_list);
     return;
   }
   if (lane == 0) lv.part_sums[item] = make_float4(m, S, U, 0.0f);
   if constexpr (TOP) {
     if (lane < lv.T)
-      lv.part_top[(int64_t)item * lv.T + lane] = make_uint2(mine_list[lane].order, mine_list[lane].id);
+      lv.part_top[(int64_t)item * lv.T + lane] =
+          make_uint2(mine_list[lane].order, mine_list[lane].id);
   }
 }
 
@@ -336,6 +419,29 @@ __global__ __launch_bounds__(256) void join_kernel(LogprobView lv) {
   const Vector v = vector_of(lv, (uint32_t)vec);
   const float4 p = lane < lv.parts ? lv.part_sums[vec * lv.parts + lane]
                                    : make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
+  Entry *mine_list = list + wave * kMostTop;
+  constexpr int E = kMostTop;                        // entries a lane, of 64 parts
+  const uint2 *top = lv.part_top + vec * lv.parts * lv.T;
+  const Given given = given_of<BF16>(lv, v);
+  if (lv.T == 1) {
+    const uint2 e = lane < lv.parts ? top[lane] : make_uint2(0u, ~0u);
+    const uint32_t most = ~wave_min(~e.x), id = wave_min(e.x == most ? e.y : ~0u);
+    if (lane == 0) *mine_list = Entry{most, id};
+    wave_lds_sync();
+  } else if (lv.T) {
+    float x[E];
+    uint32_t ids[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int at = i * 64 + lane;
+      uint2 e = make_uint2(0u, ~0u);
+      if (i * 64 < lv.parts * lv.T && at < lv.parts * lv.T) e = top[at];
+      x[i] = e.x > kMaskedOrder ? logit_of(e.x) : -INFINITY;
+      ids[i] = e.y;
+    }
+    wave_top<E>(x, [&](int i) __attribute__((always_inline)) { return ids[i]; }, lv.T,
+                room + wave * kRoom, mine_list);
+  }
   const float m = wave_max(p.x);
   float S, U = 0.0f;
   if (p.x == m) {                                    // (also where all are -infinity)
@@ -351,32 +457,19 @@ __global__ __launch_bounds__(256) void join_kernel(LogprobView lv) {
   const int ones = __popcll(__ballot(p.x == m && lane < lv.parts));
   S = wave_sum(S) + (float)max(ones - 1, 0);
   U = wave_sum(U);
-  Entry *mine_list = list + wave * kMostTop;
-  if (lv.T) {
-    constexpr int E = 64 * kMostTop / 64;
-    uint32_t order[E], ids[E];
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const int at = i * 64 + lane;
-      uint2 e = make_uint2(0u, ~0u);
-      if (at < lv.parts * lv.T) e = lv.part_top[vec * lv.parts * lv.T + at];
-      order[i] = e.x;
-      ids[i] = e.y;
-    }
-    wave_top<E>(order, [&](int i) __attribute__((always_inline)) { return ids[i]; }, lv.T,
-                room + wave * kRoom, mine_list);
-  }
-  write_vector<BF16>(lv, v, m, S, U, mine_list);
+  write_vector(lv, v, given, m, S, U, mine_list);
 }
 
 template <bool BF16, int WAVES, int E>
 void part_launch(const LogprobView &lv, hipStream_t st) {
   const int64_t items = lv.vectors * lv.parts;
   const dim3 grid((unsigned)(WAVES == 1 ? (items + 3) / 4 : items));
-  if (lv.T)
-    hipLaunchKernelGGL((part_kernel<BF16, WAVES, E, true>), grid, dim3(256), 0, st, lv);
+  if (lv.T > 1)
+    hipLaunchKernelGGL((part_kernel<BF16, WAVES, E, kTop>), grid, dim3(256), 0, st, lv);
+  else if (lv.T)
+    hipLaunchKernelGGL((part_kernel<BF16, WAVES, E, kFirst>), grid, dim3(256), 0, st, lv);
   else
-    hipLaunchKernelGGL((part_kernel<BF16, WAVES, E, false>), grid, dim3(256), 0, st, lv);
+    hipLaunchKernelGGL((part_kernel<BF16, WAVES, E, kNoTop>), grid, dim3(256), 0, st, lv);
 }
 
 template <bool BF16>

@@ -16,11 +16,12 @@ NAN, INF = float("nan"), float("inf")
 def reference(x, T):
     """Of one vector in float64: log p of every id, entropy, the T first ids, and for a fp32 sum of
     e^d the bounds on log p and on the entropy in units of 2^-24.
-      d = x - m and its product with log2 e are rounded once each, and so is log2 e itself: an
+      d = x - m and its product with log2 e are rounded once each at most, and so is log2 e itself: an
       exponent is off by 5/2 |d| units, which changes S = sum e^d by 5/2 U, U = sum e^d |d|, and U by
       5/2 W, W = sum e^d d^2.  exp2 is good to one ulp (2 units).  A sum goes through at most 32
-      additions of a lane, 6 of lanes, 4 of waves and 6 of parts, and one product for each of the
-      two joins: with the exponential's 2 and the product e d below 54 units of it.
+      additions of a lane, 6 of lanes, 4 of waves and 6 of parts: with the exponential's 2, the product
+      e d, and an exponential and a product for the shared shift and for the join below 60 units of
+      it.
     Exponentials below the smallest normal number of fp32 are 0: V 2^-126 of S at most, and 88 times
     that of U, e d being largest there at d = -126 log 2."""
     V = len(x)
@@ -34,10 +35,10 @@ def reference(x, T):
     fin = np.where(np.isfinite(d), d, 0.0)
     U, W = -(e * fin).sum(), (e * fin * fin).sum()
     lp = d - np.log1p(S)
-    log_units = (2.5 * U + 54 * S) / (1 + S) + 2 * np.log1p(S)
+    log_units = (2.5 * U + 60 * S) / (1 + S) + 2 * np.log1p(S)
     order = np.lexsort((np.arange(V), -x))[:T]
     H = np.log1p(S) + U / (1 + S)
-    H_units = log_units + (2.5 * W + 54 * U) / (1 + S) + U / (1 + S) * (54 * S / (1 + S) + 4) + H
+    H_units = log_units + (2.5 * W + 60 * U) / (1 + S) + U / (1 + S) * (60 * S / (1 + S) + 4) + H
     return lp, H, order[x[order] > -INF], np.abs(fin) + log_units + np.abs(fin - np.log1p(S)), H_units
 
 
@@ -250,5 +251,5 @@ def test_another_stream():
     mcd.mcd_logprobs(x, tok, lp, ws, stream=side.cuda_stream)
     side.synchronize()
     want = torch.log_softmax(x.double(), 2)[:, :, 1]
-    # |log p| below 16 here: its own rounding and 54 units of the sum (see reference)
+    # |log p| below 16 here: its own rounding and 60 units of the sum (see reference)
     assert (lp - want).abs().max() <= 2.0 ** -24 * (16 + 60 + 2.5 * 16)
