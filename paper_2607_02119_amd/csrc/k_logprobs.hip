@@ -83,14 +83,35 @@ __device__ __forceinline__ void wave_lds_sync() {
 constexpr int kRoom = 128;                           // candidates that a wave sorts
 
 // The first T of `count` (at most kRoom) entries of LDS into list, in order: each is compared
-// with all.
+// with all.  The entries are held by the lanes, two each, and go round through scalar
+// registers (from LDS, one read for each, the four waves' lists of 20 took 5 us).
 __device__ __forceinline__ void rank_entries(const Entry *room, int count, int T, Entry *list) {
-  for (int c = threadIdx.x & 63; c < count; c += 64) {
-    const Entry e = room[c];
-    int rank = 0;
-    for (int k = 0; k < count; ++k) rank += before(room[k], e);
-    if (rank < T) list[rank] = e;
+  const int lane = threadIdx.x & 63;
+  static_assert(kRoom == 128, "two entries a lane");
+  uint64_t key[2];
+  int rank[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int at = i * 64 + lane;
+    const Entry e = room[min(at, count - 1)];
+    key[i] = at < count ? (uint64_t)e.order << 32 | ~e.id : 0;
   }
+  const bool two = count > 64;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t hi = (uint32_t)(key[i] >> 32), lo = (uint32_t)key[i];
+#pragma unroll 4
+    for (int k = 0; k < min(count - 64 * i, 64); ++k) {
+      const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, k) << 32 |
+                             (uint32_t)__builtin_amdgcn_readlane((int)lo, k);
+      rank[0] += other > key[0];
+      if (two) rank[1] += other > key[1];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (i * 64 + lane < count && rank[i] < T)
+      list[rank[i]] = Entry{(uint32_t)(key[i] >> 32), ~(uint32_t)key[i]};
 }
 
 // The T (2..kMostTop) first of the wave's logits x[i] with ids id(i) (i < E, every lane's own)
@@ -131,7 +152,8 @@ __device__ __forceinline__ void wave_top(const float (&x)[E], Id &&id, int T, En
   }
   if (lane < T) list[lane] = Entry{0u, ~0u};
   wave_lds_sync();
-  if (count <= kRoom) {
+  if (count == 0) {
+  } else if (count <= kRoom) {
     rank_entries(room, count, T, list);
   } else {
     Entry last = {~0u, 0u};
@@ -318,10 +340,10 @@ __global__ __launch_bounds__(256) void part_kernel(LogprobView lv) {
     const float top = large ? 0.0f : __fmul_rn(m, kLog2e), shift = large ? m : 0.0f;
     const float gap = large ? 0.0f : fmaf(m, kLog2e, -top);   // what top falls short of m log2 e by
     int ones = 0;
-    auto sums = [&](auto at_m) __attribute__((always_inline)) {
+    auto sums = [&](auto at_m, auto far) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        const float z = large ? x[i] - shift : x[i];
+        const float z = decltype(far)::value ? x[i] - shift : x[i];
         const float y = fmaf(z, kLog2e, -top);
         float e = __builtin_amdgcn_exp2f(y);
         if constexpr (decltype(at_m)::value) {       // 1 for every logit of m's size, counted
@@ -334,8 +356,11 @@ __global__ __launch_bounds__(256) void part_kernel(LogprobView lv) {
         U = fmaf(e, fmaxf(y, -300.0f), U);
       }
     };
-    if (wave_m == m) sums(std::true_type{});
-    else sums(std::false_type{});
+    const std::integral_constant<bool, true> yes{};
+    const std::integral_constant<bool, false> no{};
+    if (large) sums(yes, yes);
+    else if (wave_m == m) sums(yes, no);
+    else sums(no, no);
     S = wave_sum(S);
     U = wave_sum(U);
     // 2^y = 2^(true exponent + gap): both sums carry 2^gap

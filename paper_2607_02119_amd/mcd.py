@@ -751,41 +751,41 @@ def mcd_logprobs(logits, tokens, logprob, workspace, entropy=None, top_ids=None,
     """Log probabilities of tokens (int32 [rows][K]) under logits (bf16 or fp32 [n][K][V], or [n][N]
     with V_stream), entropies [n][K] (float32) and the T most likely ids [n][K][T] (int32) with
     theirs.  token_row: int32 [n], the row of tokens of each row of logits, or None: its index."""
-    if logits.dtype not in _DTYPES:
+    dt, shape, stride = _DTYPES.get(logits.dtype), logits.shape, logits.stride()
+    if dt is None:
         raise ValueError(f"logits: dtype {logits.dtype}")
     if V_stream is None:
-        if logits.dim() != 3 or logits.stride(2) != 1 or (
-                logits.shape[1] > 1 and logits.stride(1) != logits.shape[2]):
+        if len(shape) != 3 or stride[2] != 1 or (shape[1] > 1 and stride[1] != shape[2]):
             raise ValueError("logits must be [n][K][V], a row's logits contiguous")
-        n, K, V = logits.shape
+        n, K, V = shape
+        width = K * V
     else:
         V_stream = np.ascontiguousarray(V_stream, dtype=np.int32)
-        K, V = V_stream.shape[0], int(V_stream.max())
-        n = logits.shape[0]
-        if logits.dim() != 2 or logits.stride(1) != 1 or logits.shape[1] != int(V_stream.sum()):
+        K, V, width = V_stream.shape[0], int(V_stream.max()), int(V_stream.sum())
+        n = shape[0]
+        if len(shape) != 2 or stride[1] != 1 or shape[1] != width:
             raise ValueError("logits must be [n][sum of V_stream], a row's logits contiguous")
-    for name, t, dt, shape in (
-            ("tokens", tokens, torch.int32, (tokens.shape[0], K)),
-            ("token_row", token_row, torch.int32, (n,)), ("logprob", logprob, torch.float32, (n, K)),
-            ("entropy", entropy, torch.float32, (n, K))):
-        if t is not None and (t.dtype != dt or tuple(t.shape) != shape or not t.is_contiguous()):
-            raise ValueError(f"{name} must be contiguous {dt} {list(shape)}")
-    T = 0
-    for name, t, dt in (("top_ids", top_ids, torch.int32),
-                        ("top_logprobs", top_logprobs, torch.float32)):
+    rows, T = tokens.shape[0], 0
+    if top_ids is not None:
+        T = top_ids.shape[-1]
+    elif top_logprobs is not None:
+        T = top_logprobs.shape[-1]
+    f32, i32 = torch.float32, torch.int32
+    for name, t, dtype, want in (("tokens", tokens, i32, (rows, K)), ("logprob", logprob, f32, (n, K)),
+                                 ("token_row", token_row, i32, (n,)), ("entropy", entropy, f32, (n, K)),
+                                 ("top_ids", top_ids, i32, (n, K, T)),
+                                 ("top_logprobs", top_logprobs, f32, (n, K, T))):
         if t is None:
             continue
-        if t.dtype != dt or t.dim() != 3 or t.shape[:2] != (n, K) or not t.is_contiguous() \
-                or t.shape[2] < 1 or (T and t.shape[2] != T):
-            raise ValueError(f"{name} must be contiguous {dt} [{n}][{K}][T]")
-        T = t.shape[2]
-    _on_gpu(logits, tokens, token_row, logprob, entropy, top_ids, top_logprobs, workspace)
-    width = logits[0].numel() if n else 0
+        if t.dtype != dtype or t.shape != want or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous {dtype} {list(want)}")
+        if not t.is_cuda:
+            raise ValueError("a tensor of the call is not on the GPU")
+    _on_gpu(logits, workspace)
     a = mcd_logprobs_args(
-        n, K, V, T, int(pad_id), _DTYPES[logits.dtype], _ptr(logits),
-        logits.stride(0) if n > 1 else width, _ptr(V_stream), tokens.shape[0], _ptr(tokens),
-        _ptr(token_row), _ptr(logprob), _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs),
-        workspace.data_ptr(), workspace.nbytes)
+        n, K, V, T, int(pad_id), dt, logits.data_ptr(), stride[0] if n > 1 else width,
+        _ptr(V_stream), rows, tokens.data_ptr(), _ptr(token_row), logprob.data_ptr(), _ptr(entropy),
+        _ptr(top_ids), _ptr(top_logprobs), workspace.data_ptr(), workspace.nbytes)
     _check(_mcd_logprobs(ctypes.byref(a), _stream(stream)), "mcd_logprobs")
 
 
