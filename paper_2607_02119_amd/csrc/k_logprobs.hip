@@ -82,36 +82,70 @@ __device__ __forceinline__ void wave_lds_sync() {
 
 constexpr int kRoom = 128;                           // candidates that a wave sorts
 
-// The first T of `count` (at most kRoom) entries of LDS into list, in order: each is compared
-// with all.  The entries are held by the lanes, two each, and go round through scalar
-// registers (from LDS, one read for each, the four waves' lists of 20 took 5 us).
-__device__ __forceinline__ void rank_entries(const Entry *room, int count, int T, Entry *list) {
+__device__ __forceinline__ uint64_t key_of(const Entry &e) {
+  return (uint64_t)e.order << 32 | ~e.id;            // larger: before
+}
+__device__ __forceinline__ Entry entry_of(uint64_t key) {
+  return Entry{(uint32_t)(key >> 32), ~(uint32_t)key};
+}
+
+// The lanes' keys in descending order, in blocks of N lanes (the first of them: other blocks the
+// other way in turn).
+template <int N>
+__device__ __forceinline__ uint64_t sort_lanes(uint64_t key) {
   const int lane = threadIdx.x & 63;
-  static_assert(kRoom == 128, "two entries a lane");
-  uint64_t key[2];
-  int rank[2] = {0, 0};
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int at = i * 64 + lane;
-    const Entry e = room[min(at, count - 1)];
-    key[i] = at < count ? (uint64_t)e.order << 32 | ~e.id : 0;
-  }
-  const bool two = count > 64;
+  for (int size = 2; size <= N; size *= 2)
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint32_t hi = (uint32_t)(key[i] >> 32), lo = (uint32_t)key[i];
-#pragma unroll 4
-    for (int k = 0; k < min(count - 64 * i, 64); ++k) {
-      const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, k) << 32 |
-                             (uint32_t)__builtin_amdgcn_readlane((int)lo, k);
-      rank[0] += other > key[0];
-      if (two) rank[1] += other > key[1];
+    for (int d = size / 2; d > 0; d /= 2) {
+      const uint64_t other = __shfl_xor((unsigned long long)key, d);
+      // the larger to the lower lane, the other way in every second block
+      const bool larger = ((lane & d) == 0) == ((lane & size) == 0);
+      key = (other > key) == larger ? other : key;
     }
+  return key;
+}
+
+// The first T of `count` (at most kRoom) entries of LDS into list, in order.  Up to 64 of them
+// (nearly always) are sorted by the lanes, in 10 or 21 exchanges; more are compared each with
+// all.  (Comparing 24 to 44 entries each with all took 1.5 to 3 us.)
+__device__ __forceinline__ void sort_entries(const Entry *room, int count, int T, Entry *list) {
+  const int lane = threadIdx.x & 63;
+  if (count <= 64) {
+    uint64_t key = lane < count ? key_of(room[lane]) : 0;
+    if (count <= 16) key = sort_lanes<16>(key);
+    else key = sort_lanes<64>(key);
+    if (lane < T && lane < count) list[lane] = entry_of(key);
+    return;
   }
+  for (int c = lane; c < count; c += 64) {
+    const Entry e = room[c];
+    int rank = 0;
+    for (int k = 0; k < count; ++k) rank += before(room[k], e);
+    if (rank < T) list[rank] = e;
+  }
+}
+
+// The first T of four sorted lists of T entries, kMostTop apart, into `to` (apart from them), by
+// a wave: an entry's place is its own in its list and, for each other list, how many there
+// come before it.
+__device__ __forceinline__ void merge_lists(const Entry *lists, int T, Entry *to) {
+  const int step = 1 << (31 - __clz(T));
+  for (int i = threadIdx.x & 63; i < 4 * T; i += 64) {
+    const int mine = i / T;
+    const Entry e = lists[mine * kMostTop + i % T];
+    int n[3] = {0, 0, 0};                            // of the others', before e
+    for (int d = step; d > 0; d >>= 1) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-    if (i * 64 + lane < count && rank[i] < T)
-      list[rank[i]] = Entry{(uint32_t)(key[i] >> 32), ~(uint32_t)key[i]};
+      for (int w = 0; w < 3; ++w) {
+        const Entry o = lists[((mine + 1 + w) & 3) * kMostTop + min(n[w] + d, T) - 1];
+        if ((n[w] + d <= T) & before(o, e)) n[w] += d;
+      }
+    }
+    const int rank = i % T + n[0] + n[1] + n[2];
+    // (entries that are none are before no other, and equal: any of them may stay)
+    if (rank < T) to[rank] = e;
+  }
 }
 
 // The T (2..kMostTop) first of the wave's logits x[i] with ids id(i) (i < E, every lane's own)
@@ -119,9 +153,9 @@ __device__ __forceinline__ void rank_entries(const Entry *room, int count, int T
 // LDS of the wave's own.
 //
 // T lanes hold a largest logit of at least `least`, so the T first are among the logits
-// from `least` on.  It is found bit by bit from the lanes' largest; its upper 16 bits do unless
-// more than kRoom logits lie there, which takes the others too, and where ties leave more
-// even so, the first are taken one by one.
+// from `least` on.  It is found bit by bit from the lanes' largest, until little more than T
+// lanes are left or 16 bits are known; where more than kRoom logits lie there the other
+// bits follow, and where ties leave more even so, the first are taken one by one.
 template <int E, class Id>
 __device__ __forceinline__ void wave_top(const float (&x)[E], Id &&id, int T, Entry *room,
                                          Entry *list) {
@@ -130,13 +164,21 @@ __device__ __forceinline__ void wave_top(const float (&x)[E], Id &&id, int T, En
 #pragma unroll
   for (int i = 1; i < E; ++i) most = fmaxf(most, x[i]);
   const uint32_t mine = order_of(most);
-  uint32_t least = 0;
-  int count = 0;
+  // the bits that all of the lanes' largest have in common are its too
+  const uint32_t low = wave_min(mine), differ = low ^ ~wave_min(~mine);
+  const int bits = 32 - __clz((int)differ);
+  uint32_t least = differ ? low >> (bits - 1) >> 1 << (bits - 1) << 1 : low;
+  // (of more lanes there would soon be more than the 64 candidates that are sorted at once)
+  const int enough = T + (T < 8 ? 2 : 0);
+  int count = 0, next = bits - 1;
 #pragma unroll 1
   for (int half = 0; half < 2; ++half) {
-#pragma unroll 4
-    for (uint32_t bit = half ? 1u << 15 : 1u << 31; bit >= (half ? 1u : 1u << 16); bit >>= 1)
-      if ((int)__popcll(__ballot(mine >= (least | bit))) >= T) least |= bit;
+    for (const int end = half ? 0 : max(bits - 16, 0); next >= end; --next) {
+      const uint32_t more = least | 1u << next;
+      const int lanes = __popcll(__ballot(mine >= more));
+      if (lanes >= T) least = more;
+      if (lanes >= T && lanes <= enough && !half) break;
+    }
     const float from = logit_of(max(least, kMaskedOrder + 1));
     count = 0;
 #pragma unroll
@@ -154,7 +196,7 @@ __device__ __forceinline__ void wave_top(const float (&x)[E], Id &&id, int T, En
   wave_lds_sync();
   if (count == 0) {
   } else if (count <= kRoom) {
-    rank_entries(room, count, T, list);
+    sort_entries(room, count, T, list);
   } else {
     Entry last = {~0u, 0u};
     for (int n = 0; n < T; ++n) {
@@ -410,18 +452,14 @@ __global__ __launch_bounds__(256) void part_kernel(LogprobView lv) {
       wave_lds_sync();
     }
     if constexpr (TOP == kTop) {
-      // the waves' lists, T of each: WAVES T entries, which room holds
-      static_assert(WAVES * kMostTop <= kRoom, "room for the waves' lists");
-      for (int i = lane; i < WAVES * lv.T; i += 64)
-        room[i] = list[i / lv.T * kMostTop + i % lv.T];
+      if (lane < lv.T) room[lane] = Entry{0u, ~0u};
       wave_lds_sync();
-      if (lane < lv.T) list[lane] = Entry{0u, ~0u};
-      wave_lds_sync();
-      rank_entries(room, WAVES * lv.T, lv.T, list);
+      merge_lists(list, lv.T, room);
       wave_lds_sync();
     }
   }
-  const Entry *mine_list = list + (TOP && WAVES == 1 ? wave * kMostTop : 0);
+  const Entry *mine_list = TOP == kTop && WAVES > 1 ? room
+                                                    : list + (TOP && WAVES == 1 ? wave * kMostTop : 0);
   if (lv.parts == 1) {
     write_vector(lv, v, given, m, S, U, mine_list);
     return;
@@ -458,9 +496,11 @@ __global__ __launch_bounds__(256) void join_kernel(LogprobView lv) {
     uint32_t ids[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      const int at = i * 64 + lane;
+      // (the parts' first entries, then their second, ...: spread over the lanes)
+      const int at = i * 64 + lane, rank = at / lv.parts;
       uint2 e = make_uint2(0u, ~0u);
-      if (i * 64 < lv.parts * lv.T && at < lv.parts * lv.T) e = top[at];
+      if (i * 64 < lv.parts * lv.T && at < lv.parts * lv.T)
+        e = top[(at - rank * lv.parts) * lv.T + rank];
       x[i] = e.x > kMaskedOrder ? logit_of(e.x) : -INFINITY;
       ids[i] = e.y;
     }

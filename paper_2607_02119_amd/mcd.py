@@ -761,8 +761,8 @@ def mcd_logprobs(logits, tokens, logprob, workspace, entropy=None, top_ids=None,
         width = K * V
     else:
         V_stream = np.ascontiguousarray(V_stream, dtype=np.int32)
-        K, V, width = V_stream.shape[0], int(V_stream.max()), int(V_stream.sum())
-        n = shape[0]
+        sizes = V_stream.tolist()
+        n, K, V, width = shape[0], len(sizes), max(sizes), sum(sizes)
         if len(shape) != 2 or stride[1] != 1 or shape[1] != width:
             raise ValueError("logits must be [n][sum of V_stream], a row's logits contiguous")
     rows, T = tokens.shape[0], 0
