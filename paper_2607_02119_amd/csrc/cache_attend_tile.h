@@ -458,15 +458,20 @@ __device__ __forceinline__ float special_page(const uint32_t (&vs)[8], int g,
 // One page into the running state.  edge (uniform): some of its positions may be
 // hidden from some rows (limit: each row's last visible position less the page's
 // first).  lift: special_page's; CHECK: looked for here.
-template <int D, int SPL, int NT, bool CHECK, class K, class V, class Q>
+// scored(): called when the keys are done with.
+struct Nothing {
+  __device__ __forceinline__ void operator()() const {}
+};
+template <int D, int SPL, int NT, bool CHECK, class K, class V, class Q, class F = Nothing>
 __device__ __forceinline__ void add_page(K &&k, V &&v, const uint32_t (&vs)[8], Q &&q, int g,
                                          bool edge, const int (&limit)[NT], float c, float lift,
-                                         Running<D, NT> &st) {
+                                         Running<D, NT> &st, F &&scored = F()) {
   // terms of a softmax weight: 16 bits, so that a bf16 output is off by its own
   // rounding alone; 24 for fp32
   constexpr int PTERMS = SPL == 1 ? 2 : 3;
   floatx4 s[NT][4];
   scores<D, SPL, NT>(k, q, s);
+  scored();
   if (edge) {
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -753,22 +758,31 @@ __device__ __forceinline__ void write_row(const AttendView &av, const Span &sp, 
 // the loads going (three or two waves that load a page ahead were slower).  512
 // rows of 100 to 1100 positions (8 K/V heads of 128, 341 MB): 62 us, 5.5 TB/s,
 // where a plain read reaches 6.4.
-template <int D, int SPL, int PACK, int OCC, class Rows>
-__global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, Rows rv,
-                                                         AttendView av) {
+template <int D, int SPL, int PACK>
+struct NarrowLds {
+  static constexpr int W = 16 / PACK, WAVES = 4, PITCH = D + 4;
+  float ml[2][WAVES][W];
+  alignas(16) float o[WAVES * W * PITCH];
+  // the queries' operands: in LDS they leave registers for the fourth wave
+  bf16x8 q[SPL * (D / 32) * 64];
+};
+
+template <int D, int SPL, int PACK, class Rows>
+__device__ __forceinline__ void narrow_rows(const CacheView &cv, const Rows &rv,
+                                            const AttendView &av, uint32_t block,
+                                            NarrowLds<D, SPL, PACK> &sh) {
   constexpr int W = 16 / PACK, WAVES = 4;
   constexpr bool BF16 = SPL == 1;
   constexpr int PITCH = D + 4;
-  __shared__ float sh_ml[2][WAVES][W];
-  __shared__ __align__(16) float sh_o[WAVES * W * PITCH];
-  // the queries' operands: in LDS they leave registers for the fourth wave
-  __shared__ bf16x8 sh_q[SPL * (D / 32) * 64];
+  auto &sh_ml = sh.ml;
+  auto &sh_o = sh.o;
+  auto &sh_q = sh.q;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, m = lane & 15;
   // (heads fastest: a page's heads lie side by side)
-  const int h = blockIdx.x % cv.Hkv;
-  const int r = blockIdx.x / cv.Hkv / av.splits;
-  const int split = blockIdx.x / cv.Hkv - r * av.splits;
+  const int h = block % cv.Hkv;
+  const int r = block / cv.Hkv / av.splits;
+  const int split = block / cv.Hkv - r * av.splits;
   const Span sp = row_span(cv, rv, r);
   if (sp.bad && h == 0 && threadIdx.x == 0) set_bad(av.status);
   if (!is_narrow(sp, av)) return;
@@ -881,6 +895,12 @@ __global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, Rows rv,
     store4<BF16>(av.out, tok * av.out_stride + qy.head * D + c4, y);
     if (c4 == 0) finish_row(av, tok * av.Hq + qy.head, top, l);
   }
+}
+
+template <int D, int SPL, int PACK, int OCC, class Rows>
+__global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, Rows rv, AttendView av) {
+  __shared__ NarrowLds<D, SPL, PACK> sh;
+  narrow_rows<D, SPL, PACK>(cv, rv, av, blockIdx.x, sh);
 }
 
 // Wide rows: a workgroup of four waves for 64 NT query rows of a K/V head and a
@@ -1051,8 +1071,8 @@ void narrow_launch(const CacheView &cv, const Rows &rv, const AttendView &av, co
                      av);
 }
 
-// The narrow or the wide rows' tiles and splits.
-template <int D, int SPL, class Rows>
+// The narrow or the wide rows' tiles and splits (NARROW: there may be narrow ones).
+template <int D, int SPL, class Rows, bool NARROW = true>
 void tiles_launch(const CacheView &cv, const Rows &rv, const AttendView &av, int pack,
                   const TilePlan &t, bool narrow, hipStream_t st) {
   const dim3 grid((unsigned)(t.tiles * t.splits * cv.Hkv));
@@ -1066,12 +1086,11 @@ void tiles_launch(const CacheView &cv, const Rows &rv, const AttendView &av, int
     if constexpr (D < 256)
       hipLaunchKernelGGL((wide_kernel<D, SPL, 2, (D * SPL > 256 ? 1 : 2), Rows>), grid, dim3(256),
                          0, st, cv, rv, av);
-  } else if (pack == 4) {
-    narrow_launch<D, SPL, 4>(cv, rv, av, grid, st);
-  } else if (pack == 2) {
-    narrow_launch<D, SPL, 2>(cv, rv, av, grid, st);
-  } else {
-    narrow_launch<D, SPL, 1>(cv, rv, av, grid, st);
+  }
+  if constexpr (NARROW) {
+    if (narrow && pack == 4) narrow_launch<D, SPL, 4>(cv, rv, av, grid, st);
+    else if (narrow && pack == 2) narrow_launch<D, SPL, 2>(cv, rv, av, grid, st);
+    else if (narrow) narrow_launch<D, SPL, 1>(cv, rv, av, grid, st);
   }
 }
 
@@ -1094,6 +1113,7 @@ void tiles_launch(const CacheView &cv, const Rows &rv, const AttendView &av, int
 // that makes two splits of, 29 and 15.6.
 constexpr int64_t kWantGroups = 512, kLeastNarrow = 8, kWholeNarrow = 16, kLeastWide = 4;
 
-TilePlan tile_plan(int32_t tile, int64_t tiles, int64_t pages, int Hkv, int D, int64_t least);
+TilePlan tile_plan(int32_t tile, int64_t tiles, int64_t pages, int Hkv, int D, int64_t least,
+                   int64_t want = kWantGroups);
 
 }  // namespace mcd

@@ -87,7 +87,6 @@ struct SharedPlan {
   bool together;               // false: each row on its own
   AttendPlan own;
   TilePlan prefix;
-  int32_t prefix_pack;         // of a narrow prefix tile, 0: wide
   int32_t parts;
   size_t ml_bytes, o_bytes;
 };

@@ -236,8 +236,8 @@ size_t score_bytes(int64_t R, int64_t Hkv, int64_t pages, int pack) {
 
 }  // namespace
 
-TilePlan tile_plan(int32_t tile, int64_t tiles, int64_t pages, int Hkv, int D, int64_t least) {
-  constexpr int64_t want = kWantGroups;
+TilePlan tile_plan(int32_t tile, int64_t tiles, int64_t pages, int Hkv, int D, int64_t least,
+                   int64_t want) {
   TilePlan p = {};
   if (tiles == 0) return p;
   p.tile = tile;

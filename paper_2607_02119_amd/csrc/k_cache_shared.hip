@@ -89,7 +89,6 @@ __device__ __forceinline__ Span own_span(const CacheView &cv, const RowsView &rv
 
 // The two kinds of rows for the tiles' kernels.
 struct PrefixRows {
-  static constexpr bool kParts = true;
   RowsView rv;
   GroupsView gv;
 };
@@ -120,6 +119,157 @@ __device__ __forceinline__ Span row_span(const CacheView &cv, const OwnRows &p, 
 }
 __device__ __forceinline__ int tile_row(const OwnRows &p, int G, int TQ, int64_t x, int &tile) {
   return tile_row(p.rv, G, TQ, x, tile);
+}
+
+// ---- prefixes of few query rows -------------------------------------------------
+//
+// A workgroup of four waves for 16 NT query rows of a group and K/V head and a split of the
+// prefix, the pages dealt out to the waves: each turns the codes of its page into
+// operands in registers, for all of its NT tiles, with no barrier until the end, and has
+// the next page's codes in flight.
+template <int D, int SPL, int NT>
+struct PrefixLds {
+  float ml[2][4][16 * NT];
+  alignas(16) float o[4 * 16 * (D + 4)];
+  bf16x8 q[NT * SPL * (D / 32) * 64];
+};
+
+template <int D, int SPL, int NT>
+__device__ __forceinline__ void prefix_rows(const CacheView &cv, const PrefixRows &rv,
+                                            const AttendView &av, uint32_t block,
+                                            PrefixLds<D, SPL, NT> &sh) {
+  constexpr int TQ = 16 * NT, WAVES = 4, PITCH = D + 4;
+  auto &sh_ml = sh.ml;
+  auto &sh_o = sh.o;
+  auto &sh_q = sh.q;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, m = lane & 15;
+  const int h = block % cv.Hkv;
+  const int item = block / cv.Hkv / av.splits;
+  const int split = block / cv.Hkv - item * av.splits;
+  int tile;
+  const int r = tile_row(rv, av.G, TQ, item, tile);
+  const Span sp = row_span(cv, rv, r);
+  if (sp.bad && h == 0 && threadIdx.x == 0) set_bad(av.status);
+  const int rows = sp.n * av.G, rho0 = tile * TQ;
+  const int pages = sp.len / kPage;
+  const int p0 = split * av.split_pages, p1 = min(pages, p0 + av.split_pages);
+  if (rho0 >= rows || p0 >= p1) return;
+
+  Query qr[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) qr[n] = query_of(sp, av, h, rho0 + 16 * n + m);
+  Running<D, NT> st;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    st.ref[n] = st.top[n] = -INFINITY;
+    st.sum[n] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) st.o[n][c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  PageRegs<D> x;
+  const int32_t *table = cv.table + (int64_t)sp.slot * cv.max_pages;
+  // a page id out of range is replaced by page 0 with every position hidden
+  auto page_at = [&](int id) __attribute__((always_inline)) {
+    const bool ok = id >= 0 && id < cv.n_pages;
+    return cv.pages + ((int64_t)(ok ? id : 0) * cv.Hkv + h) * cache_page_bytes(D);
+  };
+  int p = p0 + wave;
+  int id = p < p1 ? ld_const(table, p) : 0, id_next = 0;
+  if (p < p1) {
+    load_keys<D>(page_at(id), g, m, x);
+    load_values<D>(page_at(id), lane, x);
+    if (p + WAVES < p1) id_next = ld_const(table, p + WAVES);
+  }
+  for (int n = wave; n < NT; n += WAVES) {
+    const Query one[1] = {query_of(sp, av, h, rho0 + 16 * n + m)};
+    bf16x8 w[1][SPL][D / 32];
+    load_queries<D, SPL, 1>(av, sp, one, g, w);
+#pragma unroll
+    for (int i = 0; i < SPL; ++i)
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) sh_q[((n * SPL + i) * (D / 32) + e) * 64 + lane] = w[0][i][e];
+  }
+  __syncthreads();
+  auto q = [&](int n, int i, int e) __attribute__((always_inline)) {
+    return sh_q[((n * SPL + i) * (D / 32) + e) * 64 + lane];
+  };
+  while (p < p1) {
+    const bool ok = id >= 0 && id < cv.n_pages;
+    if (!ok && lane == 0) set_bad(av.status);
+    int limit[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) limit[n] = ok ? kPage - 1 : -1;
+    const bool more = p + WAVES < p1;
+    // the next keys into the registers of these once the scores are there, the next values
+    // once these are added
+    auto scored = [&]() __attribute__((always_inline)) {
+      if (more) load_keys<D>(page_at(id_next), g, m, x);
+    };
+    add_page<D, SPL, NT, true>(keys_of(x), values_of(x), x.vs, q, g, !ok, limit, av.c, 0.0f, st,
+                               scored);
+    p += WAVES;
+    id = id_next;
+    if (more) load_values<D>(page_at(id), lane, x);
+    id_next = p + WAVES < p1 ? ld_const(table, p + WAVES) : 0;
+  }
+
+  // the waves' sums, to their largest reference, a tile at a time
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    st.sum[n] = across_groups_sum(st.sum[n]);
+    if (g == 0) sh_ml[0][wave][16 * n + m] = st.ref[n];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) top = fmaxf(top, sh_ml[0][i][16 * n + m]);
+    const float f = st.ref[n] == -INFINITY
+                        ? 0.0f
+                        : __builtin_amdgcn_exp2f(origin_gap(st.ref[n], top, av.c));
+    if (g == 0) sh_ml[1][wave][16 * n + m] = st.sum[n] * f;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c)
+      *reinterpret_cast<floatx4 *>(sh_o + (wave * 16 + m) * PITCH + g * (D / 4) + 4 * c) =
+          st.o[n][c] * f;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * (D / 4); i += 256) {
+      const int row = i / (D / 4), c4 = i % (D / 4) * 4;
+      const Query qy = query_of(sp, av, h, rho0 + 16 * n + row);
+      if (!qy.valid) continue;
+      floatx4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+      float best = -INFINITY, l = 0.0f;
+#pragma unroll
+      for (int k = 0; k < WAVES; ++k) {
+        best = fmaxf(best, sh_ml[0][k][16 * n + row]);
+        l += sh_ml[1][k][16 * n + row];
+        acc += *reinterpret_cast<const floatx4 *>(sh_o + (k * 16 + row) * PITCH + c4);
+      }
+      const int64_t part = part_of(av, sp.t0 + qy.tok, qy.head) + split;
+      *reinterpret_cast<floatx4 *>(av.part_o + part * D + c4) = acc;
+      if (c4 == 0) av.part_ml[part] = make_float2(best, l);
+    }
+    if (n + 1 < NT) __syncthreads();
+  }
+}
+
+// Prefixes and narrow rows' own pages in one launch, so that the long chains of loads
+// of the rows, which leave the compute units mostly idle, run beside the prefixes' matrix
+// products.  prefix: the workgroups of the prefixes, in front.
+template <int D, int SPL, int NT, int PACK, int OCC>
+__global__ __launch_bounds__(256, OCC) void together_kernel(CacheView cv, RowsView rv,
+                                                           GroupsView gv, AttendView av,
+                                                           AttendView own, uint32_t prefix) {
+  __shared__ union {
+    PrefixLds<D, SPL, NT> prefix;
+    NarrowLds<D, SPL, PACK> own;
+  } sh;
+  if (blockIdx.x < prefix)
+    prefix_rows<D, SPL, NT>(cv, PrefixRows{rv, gv}, av, blockIdx.x, sh.prefix);
+  else
+    narrow_rows<D, SPL, PACK>(cv, OwnRows{rv, gv}, own, blockIdx.x - prefix, sh.own);
 }
 
 // A workgroup for 1024 / D query heads of a token, a thread for four channels of one.
@@ -213,14 +363,10 @@ SharedPlan cache_shared_plan(const CacheView &cv, const RowsView &rv, const Grou
   }
   const int64_t pages = std::min<int64_t>(gv.max_prefix / kPage, cv.max_pages);
   const int64_t most = std::min<int64_t>(rv.N, (int64_t)gv.max_rows * rv.max_tokens) * G;
-  p.prefix_pack = most <= 4 ? 4 : most <= 8 ? 2 : most <= 16 ? 1 : 0;
-  if (p.prefix_pack) {
-    p.prefix = tile_plan(16 / p.prefix_pack, gv.n, pages, cv.Hkv, D, kLeastNarrow);
-  } else {
-    const int tile = D == 256 || most <= 64 ? 64 : 128;
-    p.prefix = tile_plan(tile, tile_items(gv.n, rv.N, G, tile, false), pages, cv.Hkv, D,
-                         kLeastWide);
-  }
+  // (with 16 query rows of a group or fewer, in tiles of 16)
+  const int tile = most <= 16 ? 16 : 32;
+  p.prefix = tile_plan(tile, tile_items(gv.n, rv.N, G, tile, false), pages, cv.Hkv, D,
+                       kLeastNarrow);
   p.parts = p.prefix.splits + std::max(p.own.narrow.splits, p.own.wide.splits);
   p.ml_bytes = (size_t)rv.N * Hq * p.parts * sizeof(float2);
   p.o_bytes = (size_t)rv.N * Hq * p.parts * D * sizeof(float);
@@ -240,30 +386,51 @@ int64_t cache_shared_room(const RowsView &rv, const GroupsView &gv, int32_t Hq) 
 
 namespace {
 
+template <int D, int SPL, int NT>
+void together_launch(const CacheView &cv, const RowsView &rv, const GroupsView &gv,
+                     const AttendView &av, const AttendView &own, int pack, unsigned prefix,
+                     unsigned all, hipStream_t st) {
+  constexpr int OCC = NT == 1 ? (D * SPL > 384 ? 1 : D * SPL > 128 ? 2 : 3) : D < 256 ? 2 : 1;
+  auto go = [&](auto p) {
+    hipLaunchKernelGGL((together_kernel<D, SPL, NT, decltype(p)::value, OCC>), dim3(all), dim3(256),
+                       0, st, cv, rv, gv, av, own, prefix);
+  };
+  if (pack == 4) go(std::integral_constant<int, 4>{});
+  else if (pack == 2) go(std::integral_constant<int, 2>{});
+  else go(std::integral_constant<int, 1>{});
+}
+
 template <int D, int SPL>
 void shared_launch(const CacheView &cv, const RowsView &rv, const GroupsView &gv, AttendView av,
                    const SharedPlan &plan, hipStream_t st) {
   av.parts = plan.parts;
   av.part0 = 0;
-  av.narrow = plan.prefix_pack ? 16 / plan.prefix_pack : 0;
+  av.narrow = 0;
   av.splits = plan.prefix.splits;
   av.split_pages = plan.prefix.split_pages;
-  tiles_launch<D, SPL>(cv, PrefixRows{rv, gv}, av, plan.prefix_pack, plan.prefix,
-                       plan.prefix_pack != 0, st);
-  av.part0 = plan.prefix.splits;
-  av.narrow = plan.own.narrow_rows;
-  for (const bool narrow : {true, false}) {
-    const TilePlan &t = narrow ? plan.own.narrow : plan.own.wide;
-    if (t.tiles == 0) continue;
-    av.splits = t.splits;
-    av.split_pages = t.split_pages;
-    tiles_launch<D, SPL>(cv, OwnRows{rv, gv}, av, plan.own.pack, t, narrow, st);
+  AttendView own = av;
+  own.part0 = plan.prefix.splits;
+  own.narrow = plan.own.narrow_rows;
+  const TilePlan &n = plan.own.narrow, &w = plan.own.wide;
+  own.splits = std::max(n.splits, 1);
+  own.split_pages = std::max(n.split_pages, 1);
+  const unsigned prefix = (unsigned)(plan.prefix.tiles * plan.prefix.splits * cv.Hkv);
+  const unsigned all = prefix + (unsigned)(n.tiles * n.splits * cv.Hkv);
+  if (plan.prefix.tile == 16)
+    together_launch<D, SPL, 1>(cv, rv, gv, av, own, plan.own.pack, prefix, all, st);
+  else
+    together_launch<D, SPL, 2>(cv, rv, gv, av, own, plan.own.pack, prefix, all, st);
+  if (w.tiles) {
+    AttendView wide = own;
+    wide.splits = w.splits;
+    wide.split_pages = w.split_pages;
+    tiles_launch<D, SPL, OwnRows, false>(cv, OwnRows{rv, gv}, wide, 1, w, false, st);
   }
-  av.wide_tile = plan.own.wide.tile;
+  own.wide_tile = w.tile;
   hipLaunchKernelGGL((join_parts_kernel<D, SPL == 1>),
                      dim3((unsigned)rv.N, (unsigned)(((int64_t)av.Hq * (D / 4) + 255) / 256)),
-                     dim3(256), 0, st, cv, rv, gv, av, plan.prefix.split_pages,
-                     std::max(plan.own.narrow.split_pages, 1), std::max(plan.own.wide.split_pages, 1));
+                     dim3(256), 0, st, cv, rv, gv, own, plan.prefix.split_pages,
+                     std::max(n.split_pages, 1), std::max(w.split_pages, 1));
 }
 
 }  // namespace
