@@ -551,9 +551,12 @@ mcd_status mcd_cache_attend(const mcd_cache *cache, const mcd_cache_rows *rows,
  * continues past those pages (context >= prefix[g] / 64 * 64).  The groups hold all
  * rows (start[0] = 0, start[n] = R); a row that shares nothing is a group of its
  * own.  The arrays are read when the kernels run, the max_* are bounds as in
- * mcd_cache_rows; past them, and for a row that breaks the above, MCD_DEV_BAD_PAGE is
- * set: positions past a bound are not seen, a row outside the groups, short of
- * its prefix or past max_rows sees nothing. */
+ * mcd_cache_rows (n groups of max_rows rows of max_tokens hold n_tokens).  Where the
+ * rows are few or the prefixes short, every row is read by itself, from its own
+ * table entries, and the groups are not looked at.  Otherwise MCD_DEV_BAD_PAGE is
+ * set past a bound, and for a row that breaks the above: positions past a bound are
+ * not seen, a row outside the groups, short of its prefix or past max_rows sees
+ * nothing. */
 typedef struct {
   int32_t n;                 /* groups, 0..65535 */
   int32_t max_rows;          /* no group has more rows */

@@ -570,14 +570,15 @@ __device__ __forceinline__ void load_packed_scales(const uint8_t *page, uint32_t
   }
 }
 
-template <int D, int SPL, int PACK, class Q>
+template <int D, int SPL, int PACK, class Q, class F = Nothing>
 __device__ __forceinline__ void add_page_packed(const PageRegs<D> &x, Q &&q, int g, int m, bool edge,
                                                 int limit, float c, floatx4 *keep_scores,
-                                                Running<D, 1> &st) {
+                                                Running<D, 1> &st, F &&scored = F()) {
   constexpr int PTERMS = SPL == 1 ? 2 : 3;
   constexpr int W = 16 / PACK, U = 4 / PACK;     // columns of a tile; registers of scores x 4
   floatx4 s[1][4];
   scores<D, SPL, 1>(keys_of(x), q, s);
+  scored();
   // p[u][i]: lane 16 g + m has token 16 (PACK u + m / W) + 4 g + i, query row m % W
   float p[U][4];
 #pragma unroll

@@ -81,15 +81,16 @@ struct GroupsView {
   int32_t n, max_rows, max_prefix, max_own;
   const int32_t *start, *prefix;
 };
-// How a call runs: own pages as cache_attend_plan has it, the groups' pages in tiles
-// of all their rows' tokens, and parts of a query row in all.
+// Rows together: own pages as cache_attend_plan has it, the groups' pages in tiles of all
+// their rows' tokens, and parts of a query row in all.
 struct SharedPlan {
-  bool together;               // false: each row on its own
   AttendPlan own;
   TilePlan prefix;
   int32_t parts;
-  size_t ml_bytes, o_bytes;
 };
+// Whether rows that share pages run together.
+bool cache_shared_worth(const CacheView &cv, const RowsView &rv, const GroupsView &gv, int D,
+                        int32_t Hq);
 SharedPlan cache_shared_plan(const CacheView &cv, const RowsView &rv, const GroupsView &gv, int D,
                              int32_t Hq);
 // Parts of all query rows that no plan within the bounds of rv and gv passes.

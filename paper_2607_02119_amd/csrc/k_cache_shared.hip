@@ -255,6 +255,79 @@ __device__ __forceinline__ void prefix_rows(const CacheView &cv, const PrefixRow
   }
 }
 
+// ---- the rows' own pages ---------------------------------------------------------
+//
+// A wave for each narrow row, K/V head and split of the row's own pages: few pages mostly,
+// whose cost is a chain of loads, so that waves that work alone finish sooner in all
+// than four that share a row's pages and meet in LDS.
+template <int D, int SPL, int PACK>
+__device__ __forceinline__ void own_rows(const CacheView &cv, const OwnRows &rv,
+                                         const AttendView &av, uint32_t unit) {
+  constexpr int W = 16 / PACK;
+  const int lane = threadIdx.x & 63, g = lane >> 4, m = lane & 15;
+  const int h = unit % cv.Hkv;
+  const int r = unit / cv.Hkv / av.splits;
+  const int split = unit / cv.Hkv - r * av.splits;
+  if (r >= rv.rv.R) return;
+  const Span sp = row_span(cv, rv, r);
+  if (sp.bad && h == 0 && lane == 0) set_bad(av.status);
+  if (!is_narrow(sp, av)) return;
+  const int rows = sp.n * av.G;
+  const int pages = tile_pages(sp, av.G, rows), used = splits_used(sp, av, pages);
+  if (split > 0 && split >= used) return;
+  const int p0 = sp.page0 + split * av.split_pages, p1 = min(pages, p0 + av.split_pages);
+  const Query qr = query_of(sp, av, h, m % W);
+  const int all = min(sp.len - 1, sp.ctx);       // positions that every row sees
+  Running<D, 1> st;
+  st.ref[0] = st.top[0] = -INFINITY;
+  st.sum[0] = 0.0f;
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) st.o[0][c] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  PageRegs<D> x;
+  const int32_t *table = cv.table + (int64_t)sp.slot * cv.max_pages;
+  // a page id out of range is replaced by page 0 with every position hidden
+  auto page_at = [&](int id) __attribute__((always_inline)) {
+    const bool ok = id >= 0 && id < cv.n_pages;
+    return cv.pages + ((int64_t)(ok ? id : 0) * cv.Hkv + h) * cache_page_bytes(D);
+  };
+  auto get_values = [&](int id) __attribute__((always_inline)) {
+    load_values<D, PACK == 1, true>(page_at(id), lane, x);
+    if constexpr (PACK > 1) load_packed_scales<D, PACK>(page_at(id), g, m, x);
+  };
+  int p = p0, id = p < p1 ? ld_const(table, p) : 0, id_next = 0;
+  if (p < p1) {
+    load_keys<D, true>(page_at(id), g, m, x);
+    get_values(id);
+    if (p + 1 < p1) id_next = ld_const(table, p + 1);
+  }
+  const Query one[1] = {qr};
+  bf16x8 w[1][SPL][D / 32];
+  load_queries<D, SPL, 1>(av, sp, one, g, w, m < W);
+  auto q = [&](int, int i, int e) __attribute__((always_inline)) { return w[0][i][e]; };
+  while (p < p1) {
+    const bool ok = id >= 0 && id < cv.n_pages, more = p + 1 < p1;
+    if (!ok && lane == 0) set_bad(av.status);
+    const int limit[1] = {ok ? qr.limit - p * kPage : -1};
+    const bool edge = !ok || p * kPage + kPage - 1 > all;
+    auto scored = [&]() __attribute__((always_inline)) {
+      if (more) load_keys<D, true>(page_at(id_next), g, m, x);
+    };
+    if constexpr (PACK == 1)
+      add_page<D, SPL, 1, true>(keys_of(x), values_of(x), x.vs, q, g, edge, limit, av.c, 0.0f, st,
+                                scored);
+    else
+      add_page_packed<D, SPL, PACK>(x, q, g, m, edge, limit[0], av.c, nullptr, st, scored);
+    ++p;
+    id = id_next;
+    if (more) get_values(id);
+    id_next = p + 1 < p1 ? ld_const(table, p + 1) : 0;
+  }
+  unpack_rows<D, SPL, PACK>(st);
+  if (m < W && qr.valid)
+    write_row<D, SPL == 1>(av, sp, qr, part_of(av, sp.t0 + qr.tok, qr.head) + split, true, g,
+                           st.ref[0], st.sum[0], st.o[0]);
+}
+
 // Prefixes and narrow rows' own pages in one launch, so that the long chains of loads
 // of the rows, which leave the compute units mostly idle, run beside the prefixes' matrix
 // products.  prefix: the workgroups of the prefixes, in front.
@@ -262,14 +335,13 @@ template <int D, int SPL, int NT, int PACK, int OCC>
 __global__ __launch_bounds__(256, OCC) void together_kernel(CacheView cv, RowsView rv,
                                                            GroupsView gv, AttendView av,
                                                            AttendView own, uint32_t prefix) {
-  __shared__ union {
-    PrefixLds<D, SPL, NT> prefix;
-    NarrowLds<D, SPL, PACK> own;
-  } sh;
+  __shared__ PrefixLds<D, SPL, NT> sh;
   if (blockIdx.x < prefix)
-    prefix_rows<D, SPL, NT>(cv, PrefixRows{rv, gv}, av, blockIdx.x, sh.prefix);
+    prefix_rows<D, SPL, NT>(cv, PrefixRows{rv, gv}, av, blockIdx.x, sh);
   else
-    narrow_rows<D, SPL, PACK>(cv, OwnRows{rv, gv}, own, blockIdx.x - prefix, sh.own);
+    own_rows<D, SPL, PACK>(cv, OwnRows{rv, gv}, own,
+                           __builtin_amdgcn_readfirstlane((blockIdx.x - prefix) * 4 +
+                                                          (threadIdx.x >> 6)));
 }
 
 // A workgroup for 1024 / D query heads of a token, a thread for four channels of one.
@@ -339,23 +411,50 @@ __global__ __launch_bounds__(256) void join_parts_kernel(CacheView cv, RowsView 
   if (c4 == 0) finish_row(av, (int64_t)tok * av.Hq + head, top, l);
 }
 
-// Splits at most of pages that are read in splits of `per` and more.
+// Waves that are to work on the rows' own pages.
+constexpr int64_t kWantWaves = 4096;
+static_assert(16 * kWantWaves <= 128 * kWantGroups, "the room for parts");
+
+// Splits at most: of four pages and more.
 int64_t most_splits(int64_t pages) { return std::max<int64_t>((pages + 3) / 4, 1); }
 
 }  // namespace
+
+// Alone each row reads its prefix through the
+// caches, at about 8 (units of 0.1 ns over the chip, 128 channels) for a page and K/V head
+// of a row of up to 16 query rows and 46 in a tile of 64; together a page costs 23 for each tile
+// of 32 query rows of its group, and 7 us for the join and the rows' longer chain.  Rows
+// of 64 query rows fill tiles by themselves.  In us, alone and together (32 query and 8 K/V
+// heads of 128, bf16):
+//   groups x rows, prefix          1 x 8, 500     7.5  13.5     1 x 64, 16000   110  49
+//                                  1 x 8, 8000     16  17.6     1 x 256, 4000   100  59
+//                                  32 x 8, 1000    41  44       8 x 32, 2000     60  46
+//                                  64 x 2, 1000  24.5  27       4 x 16, 3000     35  45
+//                                                               (4 tokens a row)
+// Bounded from the call's bounds: groups of shorter prefixes than max_prefix gain less.
+bool cache_shared_worth(const CacheView &cv, const RowsView &rv, const GroupsView &gv, int D,
+                        int32_t Hq) {
+  const double rows = (double)rv.N * (Hq / cv.Hkv);
+  if (gv.max_prefix < kPage || rows >= 64.0 * rv.R) return false;
+  const double alone = (rows > 16.0 * rv.R ? 46.0 : 8.0) * rv.R;
+  const double together = 23.0 * (rows / 32 + 0.5 * gv.n);
+  return (alone - together) * cv.Hkv * (gv.max_prefix / kPage) * (D / 128.0) > 150e3;
+}
 
 SharedPlan cache_shared_plan(const CacheView &cv, const RowsView &rv, const GroupsView &gv, int D,
                              int32_t Hq) {
   SharedPlan p = {};
   const int32_t G = Hq / cv.Hkv;
-  // rows that fill tiles by themselves gain nothing
-  p.together = gv.max_prefix >= kPage && (int64_t)rv.N * G < (int64_t)64 * rv.R;
-  if (!p.together) return p;
   CacheView c = cv;
   c.weight = nullptr;
   RowsView own = rv;
   own.max_context = std::min(rv.max_context, gv.max_own);
   p.own = cache_attend_plan(c, own, D, Hq);
+  const int64_t own_pages =
+      std::min<int64_t>(((int64_t)own.max_context + kPage - 1) / kPage, cv.max_pages);
+  if (p.own.narrow.tiles)
+    p.own.narrow = tile_plan(16 / p.own.pack, rv.R, own_pages, cv.Hkv, D, kLeastNarrow,
+                             kWantWaves);
   if (p.own.narrow.tiles && p.own.wide.tiles) {
     // (one number of parts for all rows: the wide rows', which is bounded by the tokens)
     p.own.narrow.splits = p.own.wide.splits;
@@ -368,13 +467,12 @@ SharedPlan cache_shared_plan(const CacheView &cv, const RowsView &rv, const Grou
   p.prefix = tile_plan(tile, tile_items(gv.n, rv.N, G, tile, false), pages, cv.Hkv, D,
                        kLeastNarrow);
   p.parts = p.prefix.splits + std::max(p.own.narrow.splits, p.own.wide.splits);
-  p.ml_bytes = (size_t)rv.N * Hq * p.parts * sizeof(float2);
-  p.o_bytes = (size_t)rv.N * Hq * p.parts * D * sizeof(float);
   return p;
 }
 
-// Splits are made until there are kWantGroups workgroups, whose tiles hold at most 128 query
-// rows, so N Hq s <= N Hq + 128 kWantGroups for s splits of N tokens.
+// Splits are made until there are kWantGroups workgroups (kWantWaves waves of rows that work
+// alone), whose tiles hold at most 128 query rows (16), so N Hq s <= N Hq + 128
+// kWantGroups for s splits of N tokens.
 int64_t cache_shared_room(const RowsView &rv, const GroupsView &gv, int32_t Hq) {
   const int64_t rows = (int64_t)rv.N * Hq, more = rows + 128 * kWantGroups;
   const int64_t own = std::min(rv.max_context, gv.max_own);
@@ -415,7 +513,7 @@ void shared_launch(const CacheView &cv, const RowsView &rv, const GroupsView &gv
   own.splits = std::max(n.splits, 1);
   own.split_pages = std::max(n.split_pages, 1);
   const unsigned prefix = (unsigned)(plan.prefix.tiles * plan.prefix.splits * cv.Hkv);
-  const unsigned all = prefix + (unsigned)(n.tiles * n.splits * cv.Hkv);
+  const unsigned all = prefix + (unsigned)((n.tiles * n.splits * cv.Hkv + 3) / 4);
   if (plan.prefix.tile == 16)
     together_launch<D, SPL, 1>(cv, rv, gv, av, own, plan.own.pack, prefix, all, st);
   else

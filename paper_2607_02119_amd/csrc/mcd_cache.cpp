@@ -184,8 +184,10 @@ mcd_status check_groups(const mcd_cache_groups *g, const mcd_cache_rows *r) {
     return bad("bad group sizes (n=%d max_rows=%d max_prefix=%d max_own=%d)", g->n, g->max_rows,
                g->max_prefix, g->max_own);
   if (r->n_tokens == 0) return MCD_OK;
-  if ((int64_t)std::min(g->max_rows, r->R) * r->max_tokens * g->n < r->n_tokens)
-    return bad("%d groups of %d rows do not hold %d tokens", g->n, g->max_rows, r->n_tokens);
+  if ((int64_t)std::min(g->max_rows, r->R) * r->max_tokens * g->n < r->n_tokens ||
+      (int64_t)r->R * r->max_tokens < r->n_tokens)
+    return bad("%d groups of %d rows, %d in all, of %d tokens do not hold %d", g->n, g->max_rows,
+               r->R, r->max_tokens, r->n_tokens);
   if (!g->start || !g->prefix) return bad("null array");
   if (!aligned(g->start, 4) || !aligned(g->prefix, 4)) return bad("array not aligned");
   return MCD_OK;
@@ -202,11 +204,9 @@ size_t shared_bytes(int64_t parts, int D) {
 
 // Enough for every step within the bounds, together or each row on its own.
 size_t shared_need(const mcd::CacheView &cv, const mcd::RowsView &rv, const mcd::GroupsView &gv,
-                   const mcd::SharedPlan &p, int D, int32_t Hq) {
-  const size_t alone = workspace_need(mcd::cache_attend_plan(cv, rv, D, Hq), cv, rv, D, Hq);
-  const int64_t parts =
-      std::max((int64_t)rv.N * Hq * p.parts, mcd::cache_shared_room(rv, gv, Hq));
-  return std::max(alone, shared_bytes(parts, D));
+                   int D, int32_t Hq) {
+  return std::max(workspace_need(mcd::cache_attend_plan(cv, rv, D, Hq), cv, rv, D, Hq),
+                  shared_bytes(mcd::cache_shared_room(rv, gv, Hq), D));
 }
 
 #define CHECK(x)                        \
@@ -394,12 +394,18 @@ size_t mcd_cache_shared_workspace_bytes(const mcd_cache *c, const mcd_cache_rows
   cv.weight = nullptr;                           // (nothing is added up)
   const mcd::RowsView rv = view(r);
   const mcd::GroupsView gv = view(g);
-  return shared_need(cv, rv, gv, mcd::cache_shared_plan(cv, rv, gv, c->D, Hq), c->D, Hq);
+  return shared_need(cv, rv, gv, c->D, Hq);
 }
 
 mcd_status mcd_cache_attend_shared(const mcd_cache *c, const mcd_cache_rows *r,
                                    const mcd_cache_groups *g, const mcd_cache_attend_args *a,
                                    hipStream_t stream) {
+  return mcd_cache_attend_route(c, r, g, a, -1, stream);
+}
+
+mcd_status mcd_cache_attend_route(const mcd_cache *c, const mcd_cache_rows *r,
+                                  const mcd_cache_groups *g, const mcd_cache_attend_args *a,
+                                  int32_t way, hipStream_t stream) {
   CHECK(check_cache(c));
   CHECK(check_rows(r));
   CHECK(check_groups(g, r));
@@ -407,17 +413,17 @@ mcd_status mcd_cache_attend_shared(const mcd_cache *c, const mcd_cache_rows *r,
   if (a->weight_out)
     return mcd::record_error(MCD_E_UNSUPPORTED, "no weight_out for rows that share pages");
   mcd_cache alone = *c;
-  alone.weight = nullptr;
+  alone.weight = nullptr;                        // (nothing is added up)
   CHECK(check_attend(c, a));
   if (r->n_tokens == 0) return MCD_OK;
   CHECK(check_query(c, r, a));
   const mcd::CacheView cv = view(&alone);
   const mcd::RowsView rv = view(r);
   const mcd::GroupsView gv = view(g);
+  CHECK(check_workspace(a->workspace, a->workspace_bytes, shared_need(cv, rv, gv, c->D, a->Hq)));
+  if (way < 0) way = mcd::cache_shared_worth(cv, rv, gv, c->D, a->Hq) ? 1 : 0;
+  if (!way) return mcd_cache_attend(&alone, r, a, stream);
   const mcd::SharedPlan p = mcd::cache_shared_plan(cv, rv, gv, c->D, a->Hq);
-  CHECK(check_workspace(a->workspace, a->workspace_bytes,
-                        shared_need(cv, rv, gv, p, c->D, a->Hq)));
-  if (!p.together) return mcd_cache_attend(&alone, r, a, stream);
   if ((p.prefix.tiles * p.prefix.splits + p.own.narrow.tiles * p.own.narrow.splits +
        p.own.wide.tiles * p.own.wide.splits) * c->Hkv > kMost)
     return bad("too many query rows");

@@ -137,3 +137,10 @@ hipError_t launch_interleave(const int32_t *grid, int32_t n_req, int32_t F, int3
 // (0: no such part, or no streaming tile): for the tests, which have to reach every tile.
 extern "C" void mcd_projection_route(int32_t Mg, int32_t N, int32_t n_text, int32_t V_text,
                                      int32_t H, int32_t out[7]);
+
+// mcd_cache_attend_shared with its rows together (way 1), each on its own (0) or as the call
+// chooses (-1): for the tests, which have to reach both at every size.
+extern "C" mcd_status mcd_cache_attend_route(const mcd_cache *cache, const mcd_cache_rows *rows,
+                                             const mcd_cache_groups *groups,
+                                             const mcd_cache_attend_args *args, int32_t way,
+                                             hipStream_t stream);

@@ -1,5 +1,7 @@
 """Attention of rows that share pages, against its description in 64 bits (tests/_cache_ref.py) and
 against each row on its own."""
+import ctypes
+
 import numpy as np
 import pytest
 
@@ -14,6 +16,22 @@ pytestmark = [pytest.mark.gpu,
               pytest.mark.skipif(not torch.cuda.is_available(), reason="no GPU")]
 
 BF16, F32 = torch.bfloat16, torch.float32
+route = mcd._lib.mcd_cache_attend_route             # one way or the other, whatever the sizes
+route.restype = ctypes.c_int
+route.argtypes = [mcd._cache_p, mcd._rows_p, mcd._groups_p, ctypes.POINTER(mcd.mcd_cache_attend_args),
+                  ctypes.c_int32, ctypes.c_void_p]
+
+
+def attend(way, cache, rows, groups, q, out, ws, scale=None, lse=None):
+    """mcd_cache_attend_shared with the rows together ("together"), or as it chooses ("call")."""
+    if way == "call":
+        mcd.mcd_cache_attend_shared(cache, rows, groups, q, out, ws, scale=scale, lse=lse)
+        return
+    a = mcd._attend_args(cache, rows, q, out, ws, scale, lse, None)
+    mcd._check(route(cache.ref, rows.ref, groups.ref, ctypes.byref(a), 1, mcd._stream(None)), "route")
+
+
+WAYS = pytest.mark.parametrize("way", ["together", "call"])
 
 
 class Step:
@@ -47,19 +65,15 @@ class Step:
         self.Hq, self.D, self.dtype, self.N = Hq, D, dtype, int(self.new.sum())
         self.q = rounded(rng.standard_normal((self.N, Hq, D)) * 2, dtype)
 
-    def run(self, shared=True, scale=0.07):
+    def run(self, way="together", scale=0.07):
         wide = torch.zeros((self.N, self.Hq + 3, self.D), dtype=self.dtype, device="cuda")
         wide[:, :self.Hq] = dev(self.q).to(self.dtype)
         out = torch.full((self.N, self.Hq + 1, self.D), 9.0, dtype=self.dtype, device="cuda")
         lse = torch.full((self.N, self.Hq), 9.0, device="cuda")
         ws = self.cache.workspace(self.rows, self.Hq, groups=self.groups)
         ws[256:] = 255
-        if shared:
-            mcd.mcd_cache_attend_shared(self.cache, self.rows, self.groups, wide[:, :self.Hq],
-                                        out[:, :self.Hq], ws, scale=scale, lse=lse)
-        else:
-            mcd.mcd_cache_attend(self.cache, self.rows, wide[:, :self.Hq], out[:, :self.Hq], ws,
-                                 scale=scale, lse=lse)
+        attend(way, self.cache, self.rows, self.groups, wide[:, :self.Hq], out[:, :self.Hq], ws,
+               scale=scale, lse=lse)
         status = mcd.mcd_read_device_status(ws)
         assert bool((out[:, self.Hq] == 9.0).all())
         return out[:, :self.Hq], lse, status
@@ -118,20 +132,22 @@ CASES = [
 ]
 
 
+@WAYS
 @pytest.mark.parametrize("slack", [0, 700], ids=["", "loose"])
 @pytest.mark.parametrize("name,Hq,Hkv,D,dtype,groups", CASES, ids=[c[0] for c in CASES])
-def test_attend(name, Hq, Hkv, D, dtype, groups, slack):
+def test_attend(name, Hq, Hkv, D, dtype, groups, slack, way):
     rng = np.random.default_rng(sum(map(ord, name)))
     s = Step(rng, groups, Hq, Hkv, D, dtype, slack=slack)
-    print(f"case shared {name} slack={slack}", flush=True)
-    out, lse, status = s.run()
+    print(f"case shared {name} slack={slack} {way}", flush=True)
+    out, lse, status = s.run(way)
     assert status == 0
     s.check(out, lse)
-    again, lse2, _ = s.run()
+    again, lse2, _ = s.run(way)
     assert torch.equal(out, again) and torch.equal(lse, lse2)
 
 
-def test_one_token_each_without_start():
+@WAYS
+def test_one_token_each_without_start(way):
     """Rows of one token each: start may be NULL; q is out; scale is 1 / sqrt(D)."""
     rng = np.random.default_rng(2)
     s = Step(rng, [_same(300, 20), _same(64, 3)], 8, 2, 128, BF16)
@@ -139,12 +155,13 @@ def test_one_token_each_without_start():
     ws = s.cache.workspace(rows, 8, groups=s.groups)
     q = dev(s.q).to(BF16)
     lse = torch.zeros((s.N, 8), device="cuda")
-    mcd.mcd_cache_attend_shared(s.cache, rows, s.groups, q, q, ws, lse=lse)
+    attend(way, s.cache, rows, s.groups, q, q, ws, lse=lse)
     s.check(q, lse, scale=128 ** -0.5)
 
 
+@WAYS
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
-def test_values_and_keys_that_are_not_finite(dtype):
+def test_values_and_keys_that_are_not_finite(dtype, way):
     """In a shared page: NaN for all rows of the group and its head, and no other group's."""
     rng = np.random.default_rng(4)
     D = 128
@@ -157,7 +174,7 @@ def test_values_and_keys_that_are_not_finite(dtype):
             at = 66 * D + 2 * (t // 4 % 4 * 16 + t // 16 * 4 + t % 4)
             s.pages[page, 1, at:at + 2] = [0xC0, 0x7F]
         s.cache.pages.copy_(dev(s.pages))
-        out, lse, status = s.run()
+        out, lse, status = s.run(way)
         nan = torch.isnan(out).all(-1).cpu().numpy()
         assert status == 0 and nan[:20, 4:].all()
         assert not torch.isnan(out[20:]).any() and not torch.isnan(out[:, :4]).any()
@@ -183,7 +200,7 @@ def test_extreme_logits_meet_in_the_join():
         q[:, :, 0] = sign * 1e30
         alone, out = torch.zeros_like(q), torch.zeros_like(q)
         mcd.mcd_cache_attend(cache, rows, q, alone, ws, scale=1.0)
-        mcd.mcd_cache_attend_shared(cache, rows, groups, q, out, ws, scale=1.0)
+        attend("together", cache, rows, groups, q, out, ws, scale=1.0)
         # (which parts are added first differs: a few roundings of fp32)
         assert torch.allclose(out, alone, rtol=2.0 ** -18, atol=0) and out.isfinite().all()
 
@@ -236,9 +253,27 @@ def test_a_workspace_serves_smaller_steps():
         assert s.cache.workspace(s.rows, 8, groups=s.groups).numel() <= ws.numel()
         q = dev(s.q).to(BF16)
         out, lse = torch.zeros_like(q), torch.zeros((s.N, 8), device="cuda")
-        mcd.mcd_cache_attend_shared(s.cache, s.rows, s.groups, q, out, ws, scale=0.07, lse=lse)
-        s.check(out, lse)
+        for way in ("together", "call"):
+            attend(way, s.cache, s.rows, s.groups, q, out, ws, scale=0.07, lse=lse)
+            s.check(out, lse)
     with pytest.raises(mcd.McdError, match="needed"):
         mcd.mcd_cache_attend_shared(big.cache, big.rows, big.groups, dev(big.q).to(BF16),
                                     torch.zeros((big.N, 8, 128), dtype=BF16, device="cuda"),
                                     ws[:ws.numel() - 256])
+
+
+def test_the_call_takes_many_rows_of_a_long_prefix_together():
+    """Sizes from which the rows run together by themselves: the same bits as that way, and those
+    below as each row on its own."""
+    rng = np.random.default_rng(12)
+    for rows, prefix, same in ((100, 4000, "together"), (2, 4000, None)):
+        s = Step(rng, [_same(prefix, rows)], 16, 8, 128, BF16)
+        out, lse, _ = s.run("call")
+        s.check(out, lse, rows=[0, rows - 1])
+        other = s.run("together")[0]
+        if same:
+            assert torch.equal(out, other)
+        else:
+            ws = s.cache.workspace(s.rows, 16)
+            mcd.mcd_cache_attend(s.cache, s.rows, dev(s.q).to(BF16), other, ws, scale=0.07)
+            assert torch.equal(out, other)
