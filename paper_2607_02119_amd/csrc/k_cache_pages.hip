@@ -204,40 +204,42 @@ __device__ __forceinline__ int select_bit(uint64_t x, int k) {
 
 // The free pages of ranks first, first + 1, ..., one for every lane whose `rank` is
 // among the `count` of them (a wave together; lanes without one: rank < 0); -1 from
-// the rank of the last free page on.  before[c]: free pages of the chunks before c.
-__device__ __forceinline__ int free_pages(const ReserveView &rv, const int *before, int64_t first,
-                                          int count, int64_t rank) {
+// the rank of the last free page on.
+__device__ __forceinline__ int free_pages(const ReserveView &rv, int64_t first, int count,
+                                          int64_t rank) {
   const int lane = threadIdx.x & 63;
+  const int64_t end = first + count;
   int page = -1;
-  int64_t at = first;
-  const int64_t end = min(first + count, (int64_t)before[rv.chunks]);
-  while (at < end) {
-    const int chunk = find_row(rv.chunks, at, [&](int c) __attribute__((always_inline)) {
-      return before[c];
-    });
-    int64_t base = before[chunk];
-    const int64_t stop = min(end, (int64_t)before[chunk + 1]);
-    for (int w0 = 0; w0 < rv.chunk_words && at < stop; w0 += 64) {
-      const int64_t word = (int64_t)chunk * rv.chunk_words + w0 + lane;
-      const uint64_t bits = rv.free_bits[word];        // (chunks are whole rounds of 64 words)
-      const int n = __popcll(bits), upto = wave_scan(n);
-      const int total = __shfl(upto, 63);
-      const bool mine = rank >= base && rank < base + total;
-      const int k = mine ? (int)(rank - base) : 0;
-      // the first lane with upto > k
-      int from = 0;
+  int64_t before = 0;                            // free pages of the chunks so far
+  for (int c0 = 0; c0 < rv.chunks && before < end; c0 += 64) {
+    const int free = c0 + lane < rv.chunks ? rv.chunk_free[c0 + lane] : 0;
+    const int upto = wave_scan(free), all = __shfl(upto, 63);
+    // the chunks of these 64 that hold one of the ranks
+    uint64_t holds = __ballot(free > 0 && before + upto > first && before + upto - free < end);
+    while (holds) {
+      const int k = __builtin_ctzll(holds);
+      holds &= holds - 1;
+      int64_t base = before + __shfl(upto - free, k);
+      const int64_t chunk = c0 + k;
+      for (int w0 = 0; w0 < rv.chunk_words; w0 += 64) {
+        const int64_t word = chunk * rv.chunk_words + w0 + lane;
+        const uint64_t bits = w0 + lane < rv.chunk_words ? rv.free_bits[word] : 0;
+        const int n = __popcll(bits), so_far = wave_scan(n), total = __shfl(so_far, 63);
+        const bool mine = rank >= base && rank < base + total;
+        const int nth = mine ? (int)(rank - base) : 0;
+        // the first lane with so_far > nth
+        int from = 0;
 #pragma unroll
-      for (int d = 32; d > 0; d >>= 1)
-        if (__shfl(upto, from + d - 1) <= k) from += d;
-      const uint64_t found = __shfl((unsigned long long)bits, from & 63);
-      const int skipped = __shfl(upto - n, from & 63);
-      if (mine && rank < stop)
-        page = (int)(((int64_t)chunk * rv.chunk_words + w0 + from) * 64 +
-                     select_bit(found, k - skipped));
-      base += total;
-      at = max(at, min(base, stop));
+        for (int d = 32; d > 0; d >>= 1)
+          if (__shfl(so_far, from + d - 1) <= nth) from += d;
+        const uint64_t found = __shfl((unsigned long long)bits, from & 63);
+        const int skipped = __shfl(so_far - n, from & 63);
+        if (mine)
+          page = (int)((chunk * rv.chunk_words + w0 + from) * 64 + select_bit(found, nth - skipped));
+        base += total;
+      }
     }
-    at = max(at, stop);
+    before += all;
   }
   return page;
 }
@@ -246,32 +248,8 @@ __device__ __forceinline__ int free_pages(const ReserveView &rv, const int *befo
 // (WIDE, rows of many tokens) a workgroup whose first wave sees to the pages.
 template <bool WIDE>
 __global__ __launch_bounds__(256) void reserve_kernel(PagesView pv, ReserveView rv) {
-  __shared__ int before[kMostChunks + 1];
-  __shared__ int sums[4], column[WIDE ? 64 : 1];
+  __shared__ int column[WIDE ? 64 : 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  {                                              // free pages before every chunk
-    constexpr int PER = kMostChunks / 256;
-    int n[PER], all = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int c = threadIdx.x * PER + i;
-      n[i] = c < rv.chunks ? rv.chunk_free[c] : 0;
-      all += n[i];
-    }
-    const int upto = wave_scan(all);
-    if (lane == 63) sums[wave] = upto;
-    __syncthreads();
-    int base = upto - all;
-    for (int w = 0; w < wave; ++w) base += sums[w];
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int c = threadIdx.x * PER + i;
-      if (c <= rv.chunks) before[c] = base;
-      base += n[i];
-    }
-    if (threadIdx.x == 255 && rv.chunks == kMostChunks) before[kMostChunks] = base;
-    __syncthreads();
-  }
   const int r = WIDE ? blockIdx.x
                      : __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (int)(threadIdx.x >> 6));
   if (r >= rv.R) return;
@@ -304,7 +282,7 @@ __global__ __launch_bounds__(256) void reserve_kernel(PagesView pv, ReserveView 
       if (lacking) {
         const int count = __popcll(lacking);
         const int64_t rank = need + __popcll(lacking & ((1ull << lane) - 1));
-        const int page = free_pages(rv, before, need, count, lacks ? rank : -1);
+        const int page = free_pages(rv, need, count, lacks ? rank : -1);
         need += count;
         if (lacks) {
           id = page;
@@ -343,6 +321,116 @@ __global__ __launch_bounds__(256) void reserve_kernel(PagesView pv, ReserveView 
   }
 }
 
+// A decode step in one launch: rows of at most kFewTokens tokens, so of one column or two,
+// a thread for each, and the free pages' bits in LDS.  512 rows of one token and 10 thousand
+// pages: two launches took 10.6 us.
+constexpr int kSmallRows = 1024, kSmallPages = 32768, kFewTokens = 8;
+
+__global__ __launch_bounds__(1024) void reserve_small_kernel(PagesView pv, ReserveView rv) {
+  constexpr int WORDS = kSmallPages / 64;
+  __shared__ uint64_t bits[WORDS];
+  __shared__ int upto[WORDS];                    // free pages up to and with a word
+  __shared__ int2 sums[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = threadIdx.x;
+  Want w = {};
+  int32_t *row = pv.table;
+  int id[2] = {-1, -1}, need = 0, tokens = 0;
+  if (r < rv.R) {
+    w = want_of(pv, rv, r);
+    row += (int64_t)max(w.slot, 0) * pv.max_pages + w.p0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (w.p0 + i < w.p1) {
+        id[i] = row[i];
+        need += id[i] < 0;
+      }
+    tokens = (int)(w.end - w.ctx);
+  }
+  const int need_to = wave_scan(need), tokens_to = wave_scan(tokens);
+  if (lane == 63) sums[wave] = make_int2(need_to, tokens_to);
+  __syncthreads();
+  int rank = need_to - need, first = tokens_to - tokens, wanted = 0, all = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int2 x = sums[i];
+    if (i < wave) {
+      rank += x.x;
+      first += x.y;
+    }
+    wanted += x.x;
+    all += x.y;
+  }
+  const int words = (pv.n_pages + 63) / 64;
+  int free = 0;
+  if (wanted) {                                  // (uniform)
+#pragma unroll 8
+    for (int i = wave; i < words; i += 16) {
+      const int page = i * 64 + lane;
+      const uint64_t b = __ballot(page < pv.n_pages && pv.refs[min(page, pv.n_pages - 1)] <= 0);
+      if (lane == 0) bits[i] = b;
+    }
+    __syncthreads();
+    if (wave == 0) {                             // words in order: WORDS / 64 a lane
+      constexpr int PER = WORDS / 64;
+      int n = 0;
+      for (int i = 0; i < PER; ++i)
+        if (lane * PER + i < words) n += __popcll(bits[lane * PER + i]);
+      int so_far = wave_scan(n) - n;
+      for (int i = 0; i < PER; ++i) {
+        if (lane * PER + i < words) so_far += __popcll(bits[lane * PER + i]);
+        upto[lane * PER + i] = so_far;
+      }
+    }
+    __syncthreads();
+    free = upto[WORDS - 1];
+  }
+  if (r < rv.R) {
+    if (w.bad) set_bad(rv.status);
+    rv.start[r] = min(first, rv.N);
+    if (r == rv.R - 1) {
+      rv.start[rv.R] = min(all, rv.N);
+      if (all > rv.N) set_bad(rv.status);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (w.p0 + i >= w.p1) continue;
+      if (id[i] < 0) {
+        const int old = id[i], k = rank++;
+        id[i] = -1;
+        if (k >= free) {
+          atomicOr(rv.status, (uint32_t)MCD_DEV_NO_PAGE);
+          continue;
+        }
+        int at = 0;                              // the first word with upto > k
+#pragma unroll
+        for (int d = WORDS / 2; d > 0; d >>= 1)
+          if (upto[at + d - 1] <= k) at += d;
+        const uint64_t b = bits[at];
+        const int page = at * 64 + select_bit(b, k - (upto[at] - (int)__popcll(b)));
+        // (a slot named twice: the page stays free)
+        const int seen = atomicCAS(row + i, old, page);
+        id[i] = seen == old ? page : seen;
+        if (seen == old) pv.refs[page] = 1;
+        else set_bad(rv.status);
+      } else if (id[i] >= pv.n_pages || pv.refs[id[i]] > 1) {
+        id[i] = -1;
+        set_bad(rv.status);
+      }
+      if (id[i] >= pv.n_pages) id[i] = -1;
+    }
+    for (int t = 0; t < tokens; ++t) {
+      const int tok = first + t;
+      const int64_t pos = w.ctx + t;
+      if (tok >= rv.N) break;
+      const int page = (pos >> 6) == w.p0 ? id[0] : id[1];
+      const bool ok = page >= 0 && pos >= 0 && pos < w.cap && w.p1 > w.p0;
+      if (rv.where) rv.where[tok] = ok ? (int64_t)page * kPage + (pos & (kPage - 1)) : -1;
+      if (rv.row) rv.row[tok] = r;
+      if (rv.position) rv.position[tok] = (int)pos;
+    }
+  }
+}
+
 size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
 
 }  // namespace
@@ -350,8 +438,8 @@ size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
 ReserveRoom reserve_room(int32_t R, int32_t n_pages) {
   ReserveRoom p;
   p.row_blocks = (R + kRowBlock - 1) / kRowBlock;
-  // chunks of 4096 pages, more where that makes more than kMostChunks of them
-  int64_t pages = 4096;
+  // chunks of 1024 pages, more where that makes more than kMostChunks of them
+  int64_t pages = 1024;
   while ((n_pages + pages - 1) / pages > kMostChunks) pages *= 2;
   p.chunks = (int32_t)((n_pages + pages - 1) / pages);
   p.chunk_words = (int32_t)(pages / 64);
@@ -387,6 +475,10 @@ hipError_t launch_cache_share(const PagesView &pv, int32_t R, const int32_t *slo
 }
 
 hipError_t launch_cache_reserve(const PagesView &pv, const ReserveView &rv, hipStream_t st) {
+  if (rv.R <= kSmallRows && rv.max_tokens <= kFewTokens && pv.n_pages <= kSmallPages) {
+    hipLaunchKernelGGL(reserve_small_kernel, dim3(1), dim3(1024), 0, st, pv, rv);
+    return hipGetLastError();
+  }
   const dim3 grid((unsigned)(rv.row_blocks + rv.chunks));
   if (rv.max_tokens > 4096)
     hipLaunchKernelGGL(count_kernel<16>, grid, dim3(256), 0, st, pv, rv);

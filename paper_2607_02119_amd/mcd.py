@@ -684,7 +684,7 @@ class CachePages:
 
 
 def _whole(name, t, n, dtype=torch.int32):
-    if t is not None and (t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_contiguous()):
+    if t is not None and (t.dtype != dtype or t.shape != (n,) or not t.is_contiguous()):
         raise ValueError(f"{name} must be contiguous {dtype} [{n}]")
 
 

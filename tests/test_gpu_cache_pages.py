@@ -114,7 +114,8 @@ def random_table(rng, slots, columns, n_pages, counts):
 
 
 @pytest.mark.parametrize("R,columns,n_pages", [(1, 1, 1), (3, 4, 13), (65, 9, 700), (200, 20, 5001),
-                                               (513, 5, 4096), (1000, 30, 9000)])
+                                               (513, 5, 4096), (1000, 30, 9000),
+                                               (1500, 6, 9000), (700, 60, 40000)])
 def test_steps(R, columns, n_pages):
     rng = np.random.default_rng(R)
     most = max(n_pages // R - 1, 0)
@@ -171,7 +172,7 @@ def test_out_of_pages():
 
 
 def test_many_pages():
-    """More pages than 1024 chunks of 4096, the free ones far apart."""
+    """More pages than 1024 chunks of the smallest size, the free ones far apart."""
     n_pages = (1 << 22) + 4097
     rng = np.random.default_rng(1)
     held = rng.permutation(n_pages)[:n_pages - 60]
