@@ -179,7 +179,7 @@ __device__ __forceinline__ void prefix_rows(const CacheView &cv, const PrefixRow
   if (p < p1) {
     load_keys<D>(page_at(id), g, m, x);
     load_values<D>(page_at(id), lane, x);
-    if (p + WAVES < p1) id_next = ld_const(table, p + WAVES);
+    id_next = ld_const(table, min(p + WAVES, p1 - 1));
   }
   for (int n = wave; n < NT; n += WAVES) {
     const Query one[1] = {query_of(sp, av, h, rho0 + 16 * n + m)};
@@ -200,18 +200,18 @@ __device__ __forceinline__ void prefix_rows(const CacheView &cv, const PrefixRow
     int limit[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) limit[n] = ok ? kPage - 1 : -1;
-    const bool more = p + WAVES < p1;
     // the next keys into the registers of these once the scores are there, the next values
-    // once these are added
+    // once these are added; after the last page that page again, for loads on a condition
+    // would have the values waited for together with the keys behind them
     auto scored = [&]() __attribute__((always_inline)) {
-      if (more) load_keys<D>(page_at(id_next), g, m, x);
+      load_keys<D>(page_at(id_next), g, m, x);
     };
     add_page<D, SPL, NT, true>(keys_of(x), values_of(x), x.vs, q, g, !ok, limit, av.c, 0.0f, st,
                                scored);
     p += WAVES;
     id = id_next;
-    if (more) load_values<D>(page_at(id), lane, x);
-    id_next = p + WAVES < p1 ? ld_const(table, p + WAVES) : 0;
+    load_values<D>(page_at(id), lane, x);
+    id_next = ld_const(table, min(p + WAVES, p1 - 1));
   }
 
   // the waves' sums, to their largest reference, a tile at a time
@@ -298,19 +298,19 @@ __device__ __forceinline__ void own_rows(const CacheView &cv, const OwnRows &rv,
   if (p < p1) {
     load_keys<D, true>(page_at(id), g, m, x);
     get_values(id);
-    if (p + 1 < p1) id_next = ld_const(table, p + 1);
+    id_next = ld_const(table, min(p + 1, p1 - 1));
   }
   const Query one[1] = {qr};
   bf16x8 w[1][SPL][D / 32];
   load_queries<D, SPL, 1>(av, sp, one, g, w, m < W);
   auto q = [&](int, int i, int e) __attribute__((always_inline)) { return w[0][i][e]; };
   while (p < p1) {
-    const bool ok = id >= 0 && id < cv.n_pages, more = p + 1 < p1;
+    const bool ok = id >= 0 && id < cv.n_pages;
     if (!ok && lane == 0) set_bad(av.status);
     const int limit[1] = {ok ? qr.limit - p * kPage : -1};
     const bool edge = !ok || p * kPage + kPage - 1 > all;
     auto scored = [&]() __attribute__((always_inline)) {
-      if (more) load_keys<D, true>(page_at(id_next), g, m, x);
+      load_keys<D, true>(page_at(id_next), g, m, x);
     };
     if constexpr (PACK == 1)
       add_page<D, SPL, 1, true>(keys_of(x), values_of(x), x.vs, q, g, edge, limit, av.c, 0.0f, st,
@@ -319,8 +319,8 @@ __device__ __forceinline__ void own_rows(const CacheView &cv, const OwnRows &rv,
       add_page_packed<D, SPL, PACK>(x, q, g, m, edge, limit[0], av.c, nullptr, st, scored);
     ++p;
     id = id_next;
-    if (more) get_values(id);
-    id_next = p + 1 < p1 ? ld_const(table, p + 1) : 0;
+    get_values(id);
+    id_next = ld_const(table, min(p + 1, p1 - 1));
   }
   unpack_rows<D, SPL, PACK>(st);
   if (m < W && qr.valid)
