@@ -420,25 +420,30 @@ int64_t most_splits(int64_t pages) { return std::max<int64_t>((pages + 3) / 4, 1
 
 }  // namespace
 
-// Alone each row reads its prefix through the
-// caches, at about 8 (units of 0.1 ns over the chip, 128 channels) for a page and K/V head
-// of a row of up to 16 query rows and 46 in a tile of 64; together a page costs 23 for each tile
-// of 32 query rows of its group, and 7 us for the join and the rows' longer chain.  Rows
-// of 64 query rows fill tiles by themselves.  In us, alone and together (32 query and 8 K/V
-// heads of 128, bf16):
-//   groups x rows, prefix          1 x 8, 500     7.5  13.5     1 x 64, 16000   110  49
-//                                  1 x 8, 8000     16  17.6     1 x 256, 4000   100  59
-//                                  32 x 8, 1000    41  44       8 x 32, 2000     60  46
-//                                  64 x 2, 1000  24.5  27       4 x 16, 3000     35  45
-//                                                               (4 tokens a row)
-// Bounded from the call's bounds: groups of shorter prefixes than max_prefix gain less.
+// Alone each row reads its prefix through the caches, at about 8 (units of 0.1 ns over the
+// chip, 128 channels) for a page and K/V head of a row of up to 4 query rows, 10 of up to 16,
+// and 46 in a tile of 64; together a page costs 23 for each tile of 32 query rows of its group,
+// and some 8 us for the join and the rows' longer chain.  Rows of 64 query rows
+// fill tiles by themselves.  In us, alone and together (32 query and 8 K/V heads of 128,
+// bf16, one token a row if not said):
+//   groups x rows, prefix        1 x 8, 1000     10  12      1 x 64, 16000          110  47
+//                                1 x 8, 16000    23  26      1 x 256, 4000          100  59
+//                                1 x 16, 16000   33  27      8 x 32, 2000            61  46
+//                                32 x 8, 1000    41  44      16 x 4 to 16, 500-4000   75  55
+//                                64 x 2, 1000    25  27      4 x 16, 3000, 4 tokens  35  45
+//   1 to 6 tokens a row: 1 x 64, 16000 790 and 133, 8 x 32, 2000 246 and 108
+//   8 query heads a K/V head: 4 x 32, 4000 60 and 52; fp32: 81 and 47; 256 channels 66 and 51
+// From the call's bounds: groups of shorter prefixes than max_prefix gain less.
 bool cache_shared_worth(const CacheView &cv, const RowsView &rv, const GroupsView &gv, int D,
                         int32_t Hq) {
-  const double rows = (double)rv.N * (Hq / cv.Hkv);
-  if (gv.max_prefix < kPage || rows >= 64.0 * rv.R) return false;
-  const double alone = (rows > 16.0 * rv.R ? 46.0 : 8.0) * rv.R;
+  const int32_t G = Hq / cv.Hkv;
+  const double rows = (double)rv.N * G, each = rows / std::max(rv.R, 1);
+  if (gv.max_prefix < kPage || each >= 64.0) return false;
+  // (rows of several tokens beside single ones go through tiles of 64)
+  const bool wide = (int64_t)rv.max_tokens * G > 16 && (G > 16 || each > 1.5 * G);
+  const double alone = (wide ? 46.0 : each > 4.0 ? 10.0 : 8.0) * rv.R;
   const double together = 23.0 * (rows / 32 + 0.5 * gv.n);
-  return (alone - together) * cv.Hkv * (gv.max_prefix / kPage) * (D / 128.0) > 150e3;
+  return (alone - together) * cv.Hkv * (gv.max_prefix / kPage) * (D / 128.0) > 120e3;
 }
 
 SharedPlan cache_shared_plan(const CacheView &cv, const RowsView &rv, const GroupsView &gv, int D,
@@ -453,10 +458,13 @@ SharedPlan cache_shared_plan(const CacheView &cv, const RowsView &rv, const Grou
   const int64_t own_pages =
       std::min<int64_t>(((int64_t)own.max_context + kPage - 1) / kPage, cv.max_pages);
   if (p.own.narrow.tiles)
-    p.own.narrow = tile_plan(16 / p.own.pack, rv.R, own_pages, cv.Hkv, D, kLeastNarrow,
+    // (up to 8 pages whole: 256 rows of 5 pages 46 us, in splits of 4 53; but 183 rows of up
+    // to 11 in splits of 4 54, of 8 60)
+    p.own.narrow = tile_plan(16 / p.own.pack, rv.R, own_pages, cv.Hkv, D, own_pages <= 8 ? 8 : 4,
                              kWantWaves);
-  if (p.own.narrow.tiles && p.own.wide.tiles) {
-    // (one number of parts for all rows: the wide rows', which is bounded by the tokens)
+  if (p.own.narrow.tiles && p.own.wide.tiles &&
+      (int64_t)rv.N * Hq * (p.own.narrow.splits - 1) > 128 * kWantGroups) {
+    // (as many parts for every token, those of the wide rows too: past the room for them)
     p.own.narrow.splits = p.own.wide.splits;
     p.own.narrow.split_pages = p.own.wide.split_pages;
   }
