@@ -422,6 +422,7 @@ mcd_status mcd_cache_attend_route(const mcd_cache *c, const mcd_cache_rows *r,
   const mcd::GroupsView gv = view(g);
   CHECK(check_workspace(a->workspace, a->workspace_bytes, shared_need(cv, rv, gv, c->D, a->Hq)));
   if (way < 0) way = mcd::cache_shared_worth(cv, rv, gv, c->D, a->Hq) ? 1 : 0;
+  if ((int64_t)a->Hq * c->D > (int64_t)65535 * 1024) way = 0;   // (the join's grid)
   if (!way) return mcd_cache_attend(&alone, r, a, stream);
   const mcd::SharedPlan p = mcd::cache_shared_plan(cv, rv, gv, c->D, a->Hq);
   if ((p.prefix.tiles * p.prefix.splits + p.own.narrow.tiles * p.own.narrow.splits +

@@ -80,8 +80,8 @@ mcd_status mcd_logprobs(const mcd_logprobs_args *a, hipStream_t stream) {
   if (a->n == 0) return MCD_OK;
   if (!a->logits || !a->tokens || !a->logprob) return bad("null array");
   const int64_t eb = a->dtype == MCD_BF16 ? 2 : 4, n = a->n, vectors = n * a->K;
-  if (a->logits_stride < width || a->logits_stride > ((int64_t)1 << 40))
-    return bad("logits: bad row stride");
+  if (a->logits_stride < width || a->logits_stride > ((int64_t)1 << 30))
+    return bad("logits: bad row stride");                // (n - 1 of them: below 2^61)
   if (a->token_rows < 1 || (!a->token_row && a->token_rows < a->n))
     return bad("tokens of %d rows", a->token_rows);
   if (a->T == 0 ? a->top_ids || a->top_logprobs : !a->top_ids && !a->top_logprobs)
@@ -95,7 +95,9 @@ mcd_status mcd_logprobs(const mcd_logprobs_args *a, hipStream_t stream) {
                        {a->entropy, vectors * 4},
                        {a->top_ids, vectors * a->T * 4},
                        {a->top_logprobs, vectors * a->T * 4}};
-  const Bytes in[] = {{a->logits, ((n - 1) * a->logits_stride + width) * eb},
+  const int64_t span = (n - 1) * a->logits_stride + width;
+  if (span > ((int64_t)1 << 58)) return bad("logits: bad row stride");
+  const Bytes in[] = {{a->logits, span * eb},
                       {a->tokens, (int64_t)a->token_rows * a->K * 4},
                       {a->token_row, n * 4}};
   for (int i = 0; i < 4; ++i) {

@@ -242,6 +242,15 @@ def test_a_slot_named_twice_loses_no_page():
     held = b.pages.table[b.pages.table >= 0]
     assert len(held) == 2 and torch.equal(
         b.pages.refs, torch.bincount(held, minlength=9).int())
+    # more tokens than one launch takes, and shares into one slot and from a slot of the call
+    mcd.mcd_cache_release(b.pages, i32([1]), b.ws)
+    mcd.mcd_cache_reserve(b.pages, i32([0, 0]), i32([5, 8]), start, b.ws, slot=i32([1, 1]),
+                          n_tokens=20, max_tokens=8, max_context=100)
+    for slot, source in (([0, 0, 0], [1, 1, 1]), ([1, 0], [0, 1])):
+        mcd.mcd_cache_share(b.pages, i32(slot), i32(source), i32([64] * len(slot)), b.ws)
+        held = b.pages.table[b.pages.table >= 0]
+        assert torch.equal(b.pages.refs, torch.bincount(held, minlength=9).int())
+    mcd.mcd_read_device_status(b.ws)
 
 
 def test_captured_and_replayed():
