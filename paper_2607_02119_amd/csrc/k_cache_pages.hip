@@ -3,8 +3,9 @@
 // taken, and where the new tokens of a step lie.
 //
 // Everything here is bound by the latency of a few dependent loads and of the
-// launches themselves: a step of 512 rows moves some 40 KB, one of 2048 rows with
-// 300 thousand tokens 5 MB.  Counts change by atomic additions of whole numbers, and
+// launches themselves: a step of 512 rows moves some 40 KB (release 2.8 us, reserve 7.6),
+// one of 2048 rows with 300 thousand tokens 5 MB (release 3.8 to 7, share 7.4, reserve
+// 3.7 and 8.0).  Counts change by atomic additions of whole numbers, and
 // which page a row gets follows from ranks alone, so the same table gives the same
 // pages whatever order the workgroups run in.
 #include "cache_common.h"
@@ -322,8 +323,8 @@ __global__ __launch_bounds__(256) void reserve_kernel(PagesView pv, ReserveView 
 }
 
 // A decode step in one launch: rows of at most kFewTokens tokens, so of one column or two,
-// a thread for each, and the free pages' bits in LDS.  512 rows of one token and 10 thousand
-// pages: two launches took 10.6 us.
+// a thread for each, and the free pages' bits in LDS.  512 rows of one token and 3200 pages:
+// 7.6 us; the two launches below take 10.6.
 constexpr int kSmallRows = 1024, kSmallPages = 32768, kFewTokens = 8;
 
 __global__ __launch_bounds__(1024) void reserve_small_kernel(PagesView pv, ReserveView rv) {

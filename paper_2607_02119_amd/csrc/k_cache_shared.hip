@@ -126,7 +126,12 @@ __device__ __forceinline__ int tile_row(const OwnRows &p, int G, int TQ, int64_t
 // A workgroup of four waves for 16 NT query rows of a group and K/V head and a split of the
 // prefix, the pages dealt out to the waves: each turns the codes of its page into
 // operands in registers, for all of its NT tiles, with no barrier until the end, and has
-// the next page's codes in flight.
+// the next page's codes in flight.  Issuing vector instructions bounds it (560 a page of 128
+// channels for two tiles, 128 of them conversions), at two waves on a SIMD, which hardly
+// overlap them with the matrix units.  The prefix of 64 rows on 16000 positions (32 query
+// and 8 K/V heads of 128): two tiles 36 us, one 41 (the conversions for half the
+// rows), four 60 (one wave on a SIMD), the tiles of 128 rows of wide_kernel, whose
+// waves share the conversions but wait for each other, 49.
 template <int D, int SPL, int NT>
 struct PrefixLds {
   float ml[2][4][16 * NT];
@@ -258,8 +263,9 @@ __device__ __forceinline__ void prefix_rows(const CacheView &cv, const PrefixRow
 // ---- the rows' own pages ---------------------------------------------------------
 //
 // A wave for each narrow row, K/V head and split of the row's own pages: few pages mostly,
-// whose cost is a chain of loads, so that waves that work alone finish sooner in all
-// than four that share a row's pages and meet in LDS.
+// whose cost is a chain of loads.  Beside the prefixes there is room for two workgroups on a
+// compute unit, where waves that work alone are sooner through many rows than four that
+// share a row's pages and meet in LDS (256 rows of 5 pages, whole call: 46 and 55 us).
 template <int D, int SPL, int PACK>
 __device__ __forceinline__ void own_rows(const CacheView &cv, const OwnRows &rv,
                                          const AttendView &av, uint32_t unit) {
@@ -330,7 +336,8 @@ __device__ __forceinline__ void own_rows(const CacheView &cv, const OwnRows &rv,
 
 // Prefixes and narrow rows' own pages in one launch, so that the long chains of loads
 // of the rows, which leave the compute units mostly idle, run beside the prefixes' matrix
-// products.  prefix: the workgroups of the prefixes, in front.
+// products.  prefix: the workgroups of the prefixes, in front.  64 rows on 16000 positions:
+// 41 us, in launches of their own 36 and 10; 256 rows in 8 groups on 2000: 38, 24 and 21.
 template <int D, int SPL, int NT, int PACK, int OCC>
 __global__ __launch_bounds__(256, OCC) void together_kernel(CacheView cv, RowsView rv,
                                                            GroupsView gv, AttendView av,
@@ -344,7 +351,8 @@ __global__ __launch_bounds__(256, OCC) void together_kernel(CacheView cv, RowsVi
                                                           (threadIdx.x >> 6)));
 }
 
-// A workgroup for 1024 / D query heads of a token, a thread for four channels of one.
+// A workgroup for 1024 / D query heads of a token, a thread for four channels of one: a
+// search for the token's row and group, then its parts, 6 us for 183 tokens.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void join_parts_kernel(CacheView cv, RowsView rv, GroupsView gv,
                                                          AttendView av, int prefix_pages,

@@ -11,6 +11,11 @@
 // the part's maximum first, then its sums against it, so nothing is scaled again.
 // Sums and log probabilities are in fp32.  Parts meet in a second launch, in their
 // order: the same inputs give the same bits.
+//
+// 1024 vectors of 151936 bf16 logits with the first alternative: 63 us, 4.9 TB/s; the vector
+// units are busy all the time, at 13 instructions a logit.  Parts of 4096 logits took 78.
+// Small calls are a launch and one chain of loads: 64 rows of 8 x 4096 fp32 logits 4.0 us,
+// with the first alternative 4.4, with 5 7.4, with 32 10.1.
 #include "gemm_common.h"
 
 #include "logprobs.h"
@@ -340,24 +345,33 @@ __global__ __launch_bounds__(256) void part_kernel(LogprobView lv) {
   auto id = [&](int i) __attribute__((always_inline)) {
     return (uint32_t)(first + (i / G::N * 64 * WAVES + tid) * G::N + i % G::N);
   };
-  typename G::raw raw[E / G::N];
-#pragma unroll
-  for (int i = 0; i < E / G::N; ++i) {
-    const int at = (int)id(i * G::N);
-    if (at + G::N <= v.V)
-      raw[i] = *reinterpret_cast<const typename G::raw *>(base + (int64_t)at * (BF16 ? 2 : 4));
-  }
   Given given = {};
-  if (lv.parts == 1 && (WAVES == 1 || wave == 0)) given = given_of<BF16>(lv, v);
+  if (first + PART <= v.V) {                         // (uniform) all there
+    typename G::raw raw[E / G::N];
 #pragma unroll
-  for (int i = 0; i < E / G::N; ++i) {
-    const int at = (int)id(i * G::N);
-    if (at + G::N <= v.V) {
-      G::get(raw[i], x + i * G::N);
-    } else {
+    for (int i = 0; i < E / G::N; ++i)
+      raw[i] = *reinterpret_cast<const typename G::raw *>(base +
+                                                          (int64_t)id(i * G::N) * (BF16 ? 2 : 4));
+    if (lv.parts == 1 && (WAVES == 1 || wave == 0)) given = given_of<BF16>(lv, v);
 #pragma unroll
-      for (int j = 0; j < G::N; ++j)
-        x[i * G::N + j] = at + j < v.V ? G::one(base, at + j) : -INFINITY;
+    for (int i = 0; i < E / G::N; ++i) G::get(raw[i], x + i * G::N);
+  } else {
+    if (lv.parts == 1 && (WAVES == 1 || wave == 0)) given = given_of<BF16>(lv, v);
+    // the group across the end, the same for all lanes
+    const int end = v.V / G::N * G::N;
+    float rest[G::N];
+#pragma unroll
+    for (int j = 0; j < G::N; ++j) rest[j] = end + j < v.V ? G::one(base, end + j) : -INFINITY;
+#pragma unroll
+    for (int i = 0; i < E / G::N; ++i) {
+      const int at = (int)id(i * G::N);
+      float y[G::N];
+#pragma unroll
+      for (int j = 0; j < G::N; ++j) y[j] = at == end ? rest[j] : -INFINITY;
+      if (at < end)
+        G::get(*reinterpret_cast<const typename G::raw *>(base + (int64_t)at * (BF16 ? 2 : 4)), y);
+#pragma unroll
+      for (int j = 0; j < G::N; ++j) x[i * G::N + j] = y[j];
     }
   }
   float mine = x[0];
