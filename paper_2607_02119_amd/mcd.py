@@ -576,8 +576,9 @@ class CacheGroups:
 
 
 def _on_gpu(*parts):
-    if not all(p.on_gpu if hasattr(p, "on_gpu") else p is None or p.is_cuda for p in parts):
-        raise ValueError("a tensor of the call is not on the GPU")
+    for p in parts:
+        if p is not None and not (p.is_cuda if isinstance(p, torch.Tensor) else p.on_gpu):
+            raise ValueError("a tensor of the call is not on the GPU")
 
 
 def mcd_cache_append(cache, rows, k, v, workspace, stream=None):
@@ -684,8 +685,14 @@ class CachePages:
 
 
 def _whole(name, t, n, dtype=torch.int32):
-    if t is not None and (t.dtype != dtype or t.shape != (n,) or not t.is_contiguous()):
+    """Pointer of an optional array of n whole numbers on the GPU."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous {dtype} [{n}]")
+    if not t.is_cuda:
+        raise ValueError(f"{name} is not on the GPU")
+    return t.data_ptr()
 
 
 def mcd_cache_count(pages, workspace, stream=None):
@@ -699,23 +706,21 @@ def mcd_cache_release(pages, slot, workspace, length=None, stream=None):
     """The slots keep the pages of their first length positions (None: no page); slot, length:
     int32 [R]."""
     R = slot.shape[0]
-    _whole("slot", slot, R)
-    _whole("length", length, R)
-    _on_gpu(pages, slot, length, workspace)
-    _check(_mcd_cache_release(pages.ref, R, slot.data_ptr(), _ptr(length), workspace.data_ptr(),
-                              workspace.nbytes, _stream(stream)), "mcd_cache_release")
+    slot, length = _whole("slot", slot, R), _whole("length", length, R)
+    _on_gpu(pages, workspace)
+    _check(_mcd_cache_release(pages.ref, R, slot, length, workspace.data_ptr(), workspace.nbytes,
+                              _stream(stream)), "mcd_cache_release")
 
 
 def mcd_cache_share(pages, slot, source, length, workspace, stream=None):
     """The whole pages of the sources' first length positions become the slots' too; slot, source,
     length: int32 [R]."""
     R = slot.shape[0]
-    for name, t in (("slot", slot), ("source", source), ("length", length)):
-        _whole(name, t, R)
-    _on_gpu(pages, slot, source, length, workspace)
-    _check(_mcd_cache_share(pages.ref, R, slot.data_ptr(), source.data_ptr(), length.data_ptr(),
-                            workspace.data_ptr(), workspace.nbytes, _stream(stream)),
-           "mcd_cache_share")
+    slot, source, length = (_whole(name, t, R) for name, t in
+                            (("slot", slot), ("source", source), ("length", length)))
+    _on_gpu(pages, workspace)
+    _check(_mcd_cache_share(pages.ref, R, slot, source, length, workspace.data_ptr(),
+                            workspace.nbytes, _stream(stream)), "mcd_cache_share")
 
 
 def mcd_cache_reserve(pages, context, tokens, start, workspace, slot=None, n_tokens=0,
@@ -724,15 +729,12 @@ def mcd_cache_reserve(pages, context, tokens, start, workspace, slot=None, n_tok
     """Pages for tokens[r] new tokens of every row after context[r] positions (int32 [R]); start:
     int32 [R + 1], where: int64, row, position: int32 [n_tokens] receive the tokens' places."""
     R = context.shape[0]
-    for name, t, n in (("context", context, R), ("tokens", tokens, R), ("slot", slot, R),
-                       ("start", start, R + 1), ("row", row, n_tokens),
-                       ("position", position, n_tokens)):
-        _whole(name, t, n)
-    _whole("where", where, n_tokens, torch.int64)
-    _on_gpu(pages, context, tokens, slot, start, where, row, position, workspace)
-    a = mcd_cache_reserve_args(R, int(n_tokens), int(max_tokens), int(max_context), _ptr(slot),
-                               _ptr(context), _ptr(tokens), _ptr(start), _ptr(where), _ptr(row),
-                               _ptr(position), workspace.data_ptr(), workspace.nbytes)
+    a = mcd_cache_reserve_args(
+        R, n_tokens, max_tokens, max_context, _whole("slot", slot, R),
+        _whole("context", context, R), _whole("tokens", tokens, R), _whole("start", start, R + 1),
+        _whole("where", where, n_tokens, torch.int64), _whole("row", row, n_tokens),
+        _whole("position", position, n_tokens), workspace.data_ptr(), workspace.nbytes)
+    _on_gpu(pages, workspace)
     _check(_mcd_cache_reserve(pages.ref, ctypes.byref(a), _stream(stream)), "mcd_cache_reserve")
 
 
