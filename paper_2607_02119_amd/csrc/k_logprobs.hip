@@ -486,26 +486,29 @@ __global__ __launch_bounds__(256) void part_kernel(LogprobView lv) {
   }
 }
 
-// A wave for each vector joins its parts (at most 64, one a lane).
-template <bool BF16>
+// A wave for each vector joins its parts (at most 64, one a lane).  (Joined by the last of the
+// vector's workgroups in the first launch, 24 vectors took 20 us without alternatives
+// instead of 6.3: the fences between the parts and their count write the caches back.)
+template <bool BF16, int TOP>
 __global__ __launch_bounds__(256) void join_kernel(LogprobView lv) {
-  __shared__ Entry room[4 * kRoom], list[4 * kMostTop];
+  __shared__ Entry rooms[TOP == kTop ? 4 * kRoom : 1], lists[4 * kMostTop];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t vec = (int64_t)blockIdx.x * 4 + wave;
   if (vec >= lv.vectors) return;
+  Entry *list = lists + wave * kMostTop;
   const Vector v = vector_of(lv, (uint32_t)vec);
-  const float4 p = lane < lv.parts ? lv.part_sums[vec * lv.parts + lane]
+  const int64_t first = vec * lv.parts;
+  const float4 p = lane < lv.parts ? lv.part_sums[first + lane]
                                    : make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
-  Entry *mine_list = list + wave * kMostTop;
-  constexpr int E = kMostTop;                        // entries a lane, of 64 parts
-  const uint2 *top = lv.part_top + vec * lv.parts * lv.T;
+  const uint2 *top = lv.part_top + first * lv.T;
   const Given given = given_of<BF16>(lv, v);
-  if (lv.T == 1) {
+  if constexpr (TOP == kFirst) {
     const uint2 e = lane < lv.parts ? top[lane] : make_uint2(0u, ~0u);
     const uint32_t most = ~wave_min(~e.x), id = wave_min(e.x == most ? e.y : ~0u);
-    if (lane == 0) *mine_list = Entry{most, id};
+    if (lane == 0) *list = Entry{most, id};
     wave_lds_sync();
-  } else if (lv.T) {
+  } else if constexpr (TOP == kTop) {
+    constexpr int E = kMostTop;                      // entries a lane, of 64 parts
     float x[E];
     uint32_t ids[E];
 #pragma unroll
@@ -519,7 +522,7 @@ __global__ __launch_bounds__(256) void join_kernel(LogprobView lv) {
       ids[i] = e.y;
     }
     wave_top<E>(x, [&](int i) __attribute__((always_inline)) { return ids[i]; }, lv.T,
-                room + wave * kRoom, mine_list);
+                rooms + wave * kRoom, list);
   }
   const float m = wave_max(p.x);
   float S, U = 0.0f;
@@ -536,7 +539,7 @@ __global__ __launch_bounds__(256) void join_kernel(LogprobView lv) {
   const int ones = __popcll(__ballot(p.x == m && lane < lv.parts));
   S = wave_sum(S) + (float)max(ones - 1, 0);
   U = wave_sum(U);
-  write_vector(lv, v, given, m, S, U, mine_list);
+  write_vector(lv, v, given, m, S, U, list);
 }
 
 template <bool BF16, int WAVES, int E>
@@ -556,9 +559,11 @@ void logprobs_launch(const LogprobView &lv, const LogprobPlan &p, hipStream_t st
   if (p.part == 1024) part_launch<BF16, 1, 16>(lv, st);
   else if (p.part == 4096) part_launch<BF16, 4, 16>(lv, st);
   else part_launch<BF16, 4, 32>(lv, st);
-  if (p.parts > 1)
-    hipLaunchKernelGGL(join_kernel<BF16>, dim3((unsigned)((lv.vectors + 3) / 4)), dim3(256), 0, st,
-                       lv);
+  if (p.parts == 1) return;
+  const dim3 grid((unsigned)((lv.vectors + 3) / 4));
+  if (lv.T > 1) hipLaunchKernelGGL((join_kernel<BF16, kTop>), grid, dim3(256), 0, st, lv);
+  else if (lv.T) hipLaunchKernelGGL((join_kernel<BF16, kFirst>), grid, dim3(256), 0, st, lv);
+  else hipLaunchKernelGGL((join_kernel<BF16, kNoTop>), grid, dim3(256), 0, st, lv);
 }
 
 }  // namespace
