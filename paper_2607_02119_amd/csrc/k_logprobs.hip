@@ -79,6 +79,27 @@ __device__ __forceinline__ uint32_t wave_min(uint32_t x) {
   });
 }
 
+// x of the lane whose number differs in bit D alone, on the vector units.
+template <int D>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t x) {
+  const bool upper = threadIdx.x & D;
+  if constexpr (D == 1) return row_move<0xB1>(x);    // quad_perm 1 0 3 2
+  if constexpr (D == 2) return row_move<0x4E>(x);    // quad_perm 2 3 0 1
+  if constexpr (D == 4) {                            // row_shl 4 and row_shr 4, by fours of lanes
+    const int down = __builtin_amdgcn_update_dpp((int)x, (int)x, 0x104, 0xF, 0x5, false);
+    return (uint32_t)__builtin_amdgcn_update_dpp(down, (int)x, 0x114, 0xF, 0xA, false);
+  }
+  if constexpr (D == 8) return row_move<0x128>(x);   // row_ror 8
+  if constexpr (D == 16) {
+    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return upper ? a[0] : a[1];
+  }
+  if constexpr (D == 32) {
+    const auto a = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return upper ? a[0] : a[1];
+  }
+}
+
 // The wave's LDS accesses so far are done before those that follow (of the same wave).
 __device__ __forceinline__ void wave_lds_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -96,18 +117,20 @@ __device__ __forceinline__ Entry entry_of(uint64_t key) {
 
 // The lanes' keys in descending order, in blocks of N lanes (the first of them: other blocks the
 // other way in turn).
-template <int N>
-__device__ __forceinline__ uint64_t sort_lanes(uint64_t key) {
+template <int SIZE, int D>
+__device__ __forceinline__ void exchange(uint64_t &key) {
   const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int size = 2; size <= N; size *= 2)
-#pragma unroll
-    for (int d = size / 2; d > 0; d /= 2) {
-      const uint64_t other = __shfl_xor((unsigned long long)key, d);
-      // the larger to the lower lane, the other way in every second block
-      const bool larger = ((lane & d) == 0) == ((lane & size) == 0);
-      key = (other > key) == larger ? other : key;
-    }
+  const uint64_t other = (uint64_t)lane_xor<D>((uint32_t)(key >> 32)) << 32 |
+                         lane_xor<D>((uint32_t)key);
+  // the larger to the lower lane, the other way in every second block
+  const bool larger = ((lane & D) == 0) == ((lane & SIZE) == 0);
+  key = (other > key) == larger ? other : key;
+  if constexpr (D > 1) exchange<SIZE, D / 2>(key);
+}
+template <int N, int SIZE = 2>
+__device__ __forceinline__ uint64_t sort_lanes(uint64_t key) {
+  exchange<SIZE, SIZE / 2>(key);
+  if constexpr (SIZE < N) return sort_lanes<N, 2 * SIZE>(key);
   return key;
 }
 
@@ -489,7 +512,8 @@ __global__ __launch_bounds__(256) void part_kernel(LogprobView lv) {
 // A wave for each vector joins its parts (at most 64, one a lane).  (Joined by the last of the
 // vector's workgroups in the first launch, 24 vectors took 20 us without alternatives
 // instead of 6.3: the fences between the parts and their count write the caches back.)
-template <bool BF16, int TOP>
+// E: entries of the alternatives a lane.
+template <bool BF16, int TOP, int E = 1>
 __global__ __launch_bounds__(256) void join_kernel(LogprobView lv) {
   __shared__ Entry rooms[TOP == kTop ? 4 * kRoom : 1], lists[4 * kMostTop];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -508,18 +532,23 @@ __global__ __launch_bounds__(256) void join_kernel(LogprobView lv) {
     if (lane == 0) *list = Entry{most, id};
     wave_lds_sync();
   } else if constexpr (TOP == kTop) {
-    constexpr int E = kMostTop;                      // entries a lane, of 64 parts
     float x[E];
     uint32_t ids[E];
+    // (the parts' first entries, then their second, ...: spread over the lanes)
+    const int parts = lv.parts, skip = 64 / parts, rest = 64 % parts;
+    int rank = lane / parts, part = lane - rank * parts;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      // (the parts' first entries, then their second, ...: spread over the lanes)
-      const int at = i * 64 + lane, rank = at / lv.parts;
       uint2 e = make_uint2(0u, ~0u);
-      if (i * 64 < lv.parts * lv.T && at < lv.parts * lv.T)
-        e = top[(at - rank * lv.parts) * lv.T + rank];
+      if (rank < lv.T) e = top[part * lv.T + rank];
       x[i] = e.x > kMaskedOrder ? logit_of(e.x) : -INFINITY;
       ids[i] = e.y;
+      rank += skip;
+      part += rest;
+      if (part >= parts) {
+        part -= parts;
+        ++rank;
+      }
     }
     wave_top<E>(x, [&](int i) __attribute__((always_inline)) { return ids[i]; }, lv.T,
                 rooms + wave * kRoom, list);
@@ -561,7 +590,13 @@ void logprobs_launch(const LogprobView &lv, const LogprobPlan &p, hipStream_t st
   else part_launch<BF16, 4, 32>(lv, st);
   if (p.parts == 1) return;
   const dim3 grid((unsigned)((lv.vectors + 3) / 4));
-  if (lv.T > 1) hipLaunchKernelGGL((join_kernel<BF16, kTop>), grid, dim3(256), 0, st, lv);
+  const int entries = (lv.parts * lv.T + 63) / 64;   // (at most kMostTop: 64 parts)
+  if (lv.T > 1 && entries <= 4)
+    hipLaunchKernelGGL((join_kernel<BF16, kTop, 4>), grid, dim3(256), 0, st, lv);
+  else if (lv.T > 1 && entries <= 16)
+    hipLaunchKernelGGL((join_kernel<BF16, kTop, 16>), grid, dim3(256), 0, st, lv);
+  else if (lv.T > 1)
+    hipLaunchKernelGGL((join_kernel<BF16, kTop, kMostTop>), grid, dim3(256), 0, st, lv);
   else if (lv.T) hipLaunchKernelGGL((join_kernel<BF16, kFirst>), grid, dim3(256), 0, st, lv);
   else hipLaunchKernelGGL((join_kernel<BF16, kNoTop>), grid, dim3(256), 0, st, lv);
 }
