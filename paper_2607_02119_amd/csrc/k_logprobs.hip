@@ -134,24 +134,23 @@ __device__ __forceinline__ uint64_t sort_lanes(uint64_t key) {
   return key;
 }
 
-// The first T of `count` (at most kRoom) entries of LDS into list, in order.  Up to 64 of them
-// (nearly always) are sorted by the lanes, in 10 or 21 exchanges; more are compared each with
-// all.  (Comparing 24 to 44 entries each with all took 1.5 to 3 us.)
+// The first T of `count` (at most kRoom) entries of LDS into list, in order: sorted by the lanes,
+// in 10 or 21 exchanges; of more than 64 the first 32 of each half are merged in 6 more.
+// (Comparing 24 to 44 entries each with all took 1.5 to 3 us.)
 __device__ __forceinline__ void sort_entries(const Entry *room, int count, int T, Entry *list) {
+  static_assert(kRoom == 128 && kMostTop <= 32, "two halves");
   const int lane = threadIdx.x & 63;
-  if (count <= 64) {
-    uint64_t key = lane < count ? key_of(room[lane]) : 0;
-    if (count <= 16) key = sort_lanes<16>(key);
-    else key = sort_lanes<64>(key);
-    if (lane < T && lane < count) list[lane] = entry_of(key);
-    return;
+  uint64_t key = lane < count ? key_of(room[lane]) : 0;
+  if (count <= 16) key = sort_lanes<16>(key);
+  else key = sort_lanes<64>(key);
+  if (count > 64) {
+    const uint64_t more =
+        sort_lanes<64>(64 + lane < count ? key_of(room[64 + lane]) : 0);
+    const uint64_t turned = __shfl((unsigned long long)more, 63 - lane);
+    key = lane < 32 ? key : turned;                  // down, then up
+    exchange<64, 32>(key);
   }
-  for (int c = lane; c < count; c += 64) {
-    const Entry e = room[c];
-    int rank = 0;
-    for (int k = 0; k < count; ++k) rank += before(room[k], e);
-    if (rank < T) list[rank] = e;
-  }
+  if (lane < T && lane < count) list[lane] = entry_of(key);
 }
 
 // The first T of four sorted lists of T entries, kMostTop apart, into `to` (apart from them), by

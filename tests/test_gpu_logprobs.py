@@ -147,6 +147,19 @@ def test_ties(V):
             check(x, [V], rng.integers(0, V, (5, 1)), T, V, dtype)
 
 
+@pytest.mark.parametrize("lanes,each", [(32, 2), (32, 3), (33, 3), (40, 2), (32, 4)])
+def test_more_candidates_than_lanes(lanes, each):
+    """Neighbouring logits in twos to fours, so that the lanes' largest leave 64 to 128 candidates."""
+    rng = np.random.default_rng(lanes * each)
+    x = (rng.standard_normal((6, 1024)) * 0.5).astype(np.float32)
+    for i in range(6):
+        for group in rng.permutation(64)[:lanes]:
+            x[i, 4 * group:4 * group + each] = 10 + rng.random(each)
+        x[i, 4 * group:4 * group + 4] = 9.5          # one lane's largest below all others
+    for T in (16, 31, 32):
+        check(x, [1024], rng.integers(0, 1024, (6, 1)), T, -1, F32)
+
+
 @pytest.mark.parametrize("V", [6, 900, 5000, 9000])
 def test_masked_and_not_finite(V):
     rng = np.random.default_rng(V)
