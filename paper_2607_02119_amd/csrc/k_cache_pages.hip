@@ -206,14 +206,15 @@ __device__ __forceinline__ int select_bit(uint64_t x, int k) {
 // The free pages of ranks first, first + 1, ..., one for every lane whose `rank` is
 // among the `count` of them (a wave together; lanes without one: rank < 0); -1 from
 // the rank of the last free page on.
-__device__ __forceinline__ int free_pages(const ReserveView &rv, int64_t first, int count,
-                                          int64_t rank) {
+// counts: the first 64 chunks'.
+__device__ __forceinline__ int free_pages(const ReserveView &rv, int counts, int64_t first,
+                                          int count, int64_t rank) {
   const int lane = threadIdx.x & 63;
   const int64_t end = first + count;
   int page = -1;
   int64_t before = 0;                            // free pages of the chunks so far
   for (int c0 = 0; c0 < rv.chunks && before < end; c0 += 64) {
-    const int free = c0 + lane < rv.chunks ? rv.chunk_free[c0 + lane] : 0;
+    const int free = c0 == 0 ? counts : c0 + lane < rv.chunks ? rv.chunk_free[c0 + lane] : 0;
     const int upto = wave_scan(free), all = __shfl(upto, 63);
     // the chunks of these 64 that hold one of the ranks
     uint64_t holds = __ballot(free > 0 && before + upto > first && before + upto - free < end);
@@ -255,6 +256,14 @@ __global__ __launch_bounds__(256) void reserve_kernel(PagesView pv, ReserveView 
                      : __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (int)(threadIdx.x >> 6));
   if (r >= rv.R) return;
   const Want w = want_of(pv, rv, r);
+  int32_t *row = pv.table + (int64_t)max(w.slot, 0) * pv.max_pages;
+  // loads that wait for no sum go out first: the first columns' entries, the chunks' counts
+  const int64_t c0 = w.ctx >> 6;
+  auto entry = [&](int64_t c) __attribute__((always_inline)) {
+    return c >= w.p0 && c < w.p1 ? row[c] : 0;
+  };
+  int old = entry(c0 + lane);
+  const int chunks = lane < rv.chunks ? rv.chunk_free[lane] : 0;
   int64_t need = 0, first = 0;                   // ranks and tokens before the row's
   for (int b = lane; b < r / kRowBlock; b += 64) {
     need += rv.block_sum[b].need;
@@ -268,22 +277,20 @@ __global__ __launch_bounds__(256) void reserve_kernel(PagesView pv, ReserveView 
     if (r == rv.R - 1) rv.start[rv.R] = (int)min(last, (int64_t)rv.N);
     if (last > rv.N) set_bad(rv.status);
   }
-  int32_t *row = pv.table + (int64_t)max(w.slot, 0) * pv.max_pages;
   // 64 columns at a time
-  const int64_t c0 = w.ctx >> 6;
   for (int64_t c = c0; c * kPage < w.end; c += 64) {
     int id = -1;
     if (!WIDE || wave == 0) {
       const int64_t mine = c + lane;
       const bool in = mine >= w.p0 && mine < w.p1;
-      const int old = in ? row[mine] : 0;
+      if (c != c0) old = entry(mine);
       const bool lacks = in && old < 0;
       const uint64_t lacking = __ballot(lacks);
       id = in ? old : -1;
       if (lacking) {
         const int count = __popcll(lacking);
         const int64_t rank = need + __popcll(lacking & ((1ull << lane) - 1));
-        const int page = free_pages(rv, need, count, lacks ? rank : -1);
+        const int page = free_pages(rv, chunks, need, count, lacks ? rank : -1);
         need += count;
         if (lacks) {
           id = page;
