@@ -15,7 +15,7 @@
 // 1024 vectors of 151936 bf16 logits with the first alternative: 63 us, 4.9 TB/s; the vector
 // units are busy all the time, at 13 instructions a logit.  Parts of 4096 logits took 78.
 // Small calls are a launch and one chain of loads: 64 rows of 8 x 4096 fp32 logits 4.0 us,
-// with the first alternative 4.4, with 5 7.4, with 32 10.1.
+// with the first alternative 4.4, with 5 7.2, with 32 9.7.
 #include "gemm_common.h"
 
 #include "logprobs.h"
