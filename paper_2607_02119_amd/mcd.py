@@ -730,7 +730,7 @@ def mcd_cache_reserve(pages, context, tokens, start, workspace, slot=None, n_tok
     int32 [R + 1], where: int64, row, position: int32 [n_tokens] receive the tokens' places."""
     R = context.shape[0]
     a = mcd_cache_reserve_args(
-        R, n_tokens, max_tokens, max_context, _whole("slot", slot, R),
+        R, int(n_tokens), int(max_tokens), int(max_context), _whole("slot", slot, R),
         _whole("context", context, R), _whole("tokens", tokens, R), _whole("start", start, R + 1),
         _whole("where", where, n_tokens, torch.int64), _whole("row", row, n_tokens),
         _whole("position", position, n_tokens), workspace.data_ptr(), workspace.nbytes)

@@ -181,6 +181,28 @@ def test_values_and_keys_that_are_not_finite(dtype, way):
         s.check(out[:, :], lse, rows=range(20, 25))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("where", ["shared", "own", "both"])
+def test_values_up_to_the_types_range(where, dtype):
+    """Value scales of 2^60 to 2^123 and of 2^-100 beside ordinary ones: parts of references that
+    are lifted meet parts that are not."""
+    rng = np.random.default_rng(11)
+    D = 64
+    s = Step(rng, [_same(300, 20, 20), _same(128, 5, 70)], 8, 2, D, dtype)
+    slots = s.slot[[0, 20]] if where == "shared" else s.slot[[3, 7, 22]]
+    for n, slot in enumerate(list(slots) + ([s.slot[0]] if where == "both" else [])):
+        first = n < len(slots) and where != "shared"
+        pages = s.table[slot][4 if first and n < 2 else 2 if first else 0:]
+        page = pages[pages >= 0][0]
+        for t, bits in ((0, 0x7D00), (1, 0x5D80), (2, 0x0D80)):
+            at = 66 * D + 2 * (t // 4 % 4 * 16 + t // 16 * 4 + t % 4)
+            s.pages[page, n % 2, at:at + 2] = [bits & 255, bits >> 8]
+    s.cache.pages.copy_(dev(s.pages))
+    out, lse, status = s.run()
+    assert status == 0 and out.isfinite().all()
+    s.check(out, lse)
+
+
 def test_extreme_logits_meet_in_the_join():
     """Prefix and own scores far beyond what exp holds, of both signs."""
     D, H = 64, 2
