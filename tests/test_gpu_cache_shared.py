@@ -175,10 +175,29 @@ def test_values_and_keys_that_are_not_finite(dtype, way):
             s.pages[page, 1, at:at + 2] = [0xC0, 0x7F]
         s.cache.pages.copy_(dev(s.pages))
         out, lse, status = s.run(way)
+        assert bool(torch.isnan(lse[:20, 4:]).all()) or part == "value"
         nan = torch.isnan(out).all(-1).cpu().numpy()
         assert status == 0 and nan[:20, 4:].all()
         assert not torch.isnan(out[20:]).any() and not torch.isnan(out[:, :4]).any()
         s.check(out[:, :], lse, rows=range(20, 25))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+def test_parts_of_nothing_but_keys_that_are_not_finite(dtype):
+    """Whole shared and whole own parts without a single score: NaN all the same."""
+    rng = np.random.default_rng(14)
+    D = 64
+    for pages in (slice(0, 2), slice(2, None)):
+        s = Step(rng, [_same(128, 9), _same(128, 2)], 4, 2, D, dtype)
+        for r in range(9):
+            ids = s.table[s.slot[r]][pages]
+            s.pages[ids[ids >= 0], 1, 64 * D:66 * D] = 255
+        s.cache.pages.copy_(dev(s.pages))
+        out, lse, status = s.run()
+        assert status == 0
+        assert torch.isnan(out[:9, 2:]).all() and out[:9, :2].isfinite().all()
+        assert out[9:].isfinite().all()
+        s.check(out, lse, rows=[9, 10])
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
