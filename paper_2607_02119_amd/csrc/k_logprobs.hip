@@ -24,6 +24,10 @@ namespace mcd {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+// The maximum from which differences are taken first.  Up to here its product with log2 e is
+// rounded by 2^-8 at most; the rounding grows with the product, 128 powers of two (more than
+// fp32 holds, to be taken out again) from 2^31 on.
+constexpr float kLargeLogit = 0x1p16f;
 
 // Logits as whole numbers in the same order, -0 and 0 alike; NaN: 0, below all.
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -344,7 +348,8 @@ enum { kNoTop, kFirst, kTop };   // alternatives: none, the first alone, more
 //
 // Exponents are y = x log2 e - m', m' = m log2 e rounded to fp32: one operation for a logit,
 // whose error is y's own rounding and a shift that all share.  The shift, m' less what it
-// stands for, is known (fma), and taken out of S and U at the end.
+// stands for, is known (fma), and taken out of S and U at the end.  Of maxima beyond kLargeLogit
+// y = (x - m) log2 e, an operation more.
 template <bool BF16, int WAVES, int E, int TOP>
 __global__ __launch_bounds__(256) void part_kernel(LogprobView lv) {
   typedef Group<BF16> G;
@@ -413,8 +418,7 @@ __global__ __launch_bounds__(256) void part_kernel(LogprobView lv) {
     for (int i = 0; i < E; ++i) S += x[i] != x[i] ? x[i] : 0.0f;
     S = wave_sum(S);
   } else {
-    // (a maximum beyond what the product holds: differences first)
-    const bool large = fabsf(m) > 0x1p100f;
+    const bool large = fabsf(m) > kLargeLogit;
     const float top = large ? 0.0f : __fmul_rn(m, kLog2e), shift = large ? m : 0.0f;
     const float gap = large ? 0.0f : fmaf(m, kLog2e, -top);   // what top falls short of m log2 e by
     int ones = 0;

@@ -266,3 +266,55 @@ def test_another_stream():
     want = torch.log_softmax(x.double(), 2)[:, :, 1]
     # |log p| below 16 here: its own rounding and 60 units of the sum (see reference)
     assert (lp - want).abs().max() <= 2.0 ** -24 * (16 + 60 + 2.5 * 16)
+
+
+def heads_of_any_size(rng, V, dtype):
+    """Vectors whose largest logit is every power of two from 2^10 on, times three mantissas and of
+    both signs, with logits close below it and far from it."""
+    rows = []
+    for e in range(10, 128):
+        for mantissa in (1.0, 1.372, 1.9):
+            for sign in (1.0, -1.0):
+                m = sign * mantissa * 2.0 ** e
+                if sign > 0:
+                    x = rng.standard_normal(V) * 4
+                else:
+                    x = np.maximum(m * (1 + rng.random(V)), torch.finfo(F32).min)
+                near = rng.permutation(V)[:min(V, 9)]
+                x[near] = m - abs(m) * 2.0 ** -rng.integers(4, 25, len(near))
+                x[near[0]] = m
+                rows.append(x)
+    lowest = torch.finfo(dtype).min
+    return np.stack([rounded(np.maximum(x, lowest), dtype) for x in rows])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("V", [1, 2, 900, 3000, 9000])
+def test_largest_logits_of_any_size(V, dtype):
+    """Logits in the thousands (drawn at a small temperature) up to the types' largest: a
+    distribution all the same, in one wave, in four and in parts that are joined."""
+    rng = np.random.default_rng(V)
+    x = heads_of_any_size(rng, V, dtype)
+    tokens = np.where(rng.random(len(x)) < 0.5, x.argmax(1), rng.integers(0, V, len(x)))[:, None]
+    for T in (0, 1, 5):
+        check(x, [V], tokens, T, -1, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("V,n", [(9000, 1), (20000, 500)])
+def test_parts_of_masked_logits(V, n, dtype):
+    """A mask of a finite value that covers whole parts of a vector beside ordinary logits, in parts of
+    4096 and (more than 2048 of those) of 8192 logits."""
+    rng = np.random.default_rng(n)
+    fills = [-1e4, -1e9, -1e10, -1e12, -1e15, -1e20, -1e25, -1e30, -1e36, torch.finfo(dtype).min]
+    x = rng.standard_normal((max(n, len(fills)), V)) * 2
+    for i in range(len(x)):
+        part = 8192 if n > 1 else 4096
+        kept = slice(0, part) if i % 2 else slice(part, 2 * part)
+        masked = np.ones(V, bool)
+        masked[kept] = False
+        x[i, masked] = fills[i % len(fills)]
+    x = rounded(x, dtype)
+    tokens = rng.integers(0, V, (len(x), 1))
+    for T in (0, 1, 5):
+        check(x, [V], tokens, T, -1, dtype)
