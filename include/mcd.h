@@ -638,7 +638,8 @@ mcd_status mcd_cache_count(const mcd_cache_pages *pages, void *workspace, size_t
 
 /* Slot slot[r] (slot NULL: r) keeps the pages of its first length[r] positions
  * (length NULL: none) and gives back those of the columns past them.  A slot may
- * be named more than once (the shortest length holds). */
+ * be named more than once (the shortest length holds).  A length below 0 or beyond
+ * the table gives nothing back (MCD_DEV_BAD_PAGE). */
 mcd_status mcd_cache_release(const mcd_cache_pages *pages, int32_t R, const int32_t *slot,
                              const int32_t *length, void *workspace, size_t workspace_bytes,
                              hipStream_t stream);

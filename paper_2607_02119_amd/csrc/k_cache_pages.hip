@@ -70,9 +70,12 @@ __global__ __launch_bounds__(256) void release_kernel(PagesView pv, int R, const
   const int s = slot_of(pv, slot, r, status);
   if (s < 0) return;
   const int keep = length ? ld_const(length, r) : 0;
-  if (keep < 0 && (threadIdx.x & 63) == 0) set_bad(status);
+  const int first = (int)(((int64_t)keep + kPage - 1) / kPage);
+  if (keep < 0 || first > pv.max_pages) {
+    if ((threadIdx.x & 63) == 0) set_bad(status);
+    return;
+  }
   int32_t *row = pv.table + (int64_t)s * pv.max_pages;
-  const int first = keep <= 0 ? 0 : (int)(((int64_t)keep + kPage - 1) / kPage);
   for (int64_t c = (int64_t)first + (threadIdx.x & 63); c < pv.max_pages; c += 64) {
     if (row[c] < 0) continue;
     const int id = atomicExch(row + c, -1);

@@ -284,3 +284,21 @@ def test_captured_and_replayed():
         N = int(new.sum())
         assert np.array_equal(where.cpu().numpy()[:N], want[0])
         b.check(want[3])
+
+
+def test_release_of_lengths_out_of_range_gives_nothing_back():
+    """A length below 0 or beyond the table is reported and its row keeps every page; the other
+    rows of the call give theirs back."""
+    b = Both(4, 3, 12)
+    b.reserve(None, [0, 0, 0, 0], [192, 130, 64, 192])
+    for lengths in ([-1, 65, 64, 193], [-2 ** 31, 65, 0, 2 ** 31 - 1], [-64, 1, 0, 256]):
+        mcd.mcd_cache_release(b.pages, i32([0, 1, 2, 3]), b.ws, length=i32(lengths))
+        b.mirror.release([1, 2], lengths[1:3])
+        b.check(mcd.MCD_DEV_BAD_PAGE)
+        assert (b.mirror.table[[0, 3]] >= 0).all()
+    b.release([0, 3], [192, 129])                    # the table's whole length, and into its last page
+    assert (b.mirror.table[[0, 3]] >= 0).all()
+    # named twice, once out of range: the other length holds
+    mcd.mcd_cache_release(b.pages, i32([0, 0]), b.ws, length=i32([-5, 64]))
+    b.mirror.release([0], [64])
+    b.check(mcd.MCD_DEV_BAD_PAGE)
