@@ -340,7 +340,9 @@ typedef struct {
 } mcd_logprobs_args;
 
 /* Workspace bytes for these sizes and smaller ones, 0 for invalid sizes; 256-byte
- * aligned, its first 256 bytes (the status word) zeroed once before first use. */
+ * aligned, its first 256 bytes (the status word) zeroed once before first use.  A call
+ * takes fewer than 2^26 - 3 vectors (n K) for V <= 1024, and fewer than 2^24 pieces
+ * of 8192 logits otherwise (MCD_E_UNSUPPORTED). */
 size_t mcd_logprobs_workspace_bytes(int32_t n, int32_t K, int32_t V, int32_t T);
 
 /* Launches on `stream`; no allocation, no synchronisation.  The arrays written

@@ -614,6 +614,12 @@ LogprobPlan logprob_plan(int64_t vectors, int32_t V) {
   return p;
 }
 
+int64_t logprob_groups(int64_t vectors, int32_t V) {
+  const LogprobPlan p = logprob_plan(vectors, V);
+  const int64_t items = vectors * p.parts;
+  return p.part == 1024 ? (items + 3) / 4 : items;   // (as part_launch)
+}
+
 hipError_t launch_logprobs(const LogprobView &lv, const LogprobPlan &p, bool bf16,
                            hipStream_t st) {
   if (bf16) logprobs_launch<true>(lv, p, st);

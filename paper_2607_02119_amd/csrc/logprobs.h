@@ -27,6 +27,8 @@ struct LogprobPlan {
   int32_t part, parts;
 };
 LogprobPlan logprob_plan(int64_t vectors, int32_t V);
+// Workgroups of the largest launch.
+int64_t logprob_groups(int64_t vectors, int32_t V);
 hipError_t launch_logprobs(const LogprobView &lv, const LogprobPlan &p, bool bf16, hipStream_t st);
 
 }  // namespace mcd

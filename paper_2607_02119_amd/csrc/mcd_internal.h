@@ -15,6 +15,8 @@ constexpr int kPlanHeader = 8;
 enum { kPlanMagicWord = 0, kPlanR = 1, kPlanPairs = 2, kPlanSolo = 3, kPlanText = 4 };
 
 constexpr int kStatusBytes = 256;  // status word region at the start of the workspace
+// Workgroups of 256 threads in a launch: HIP takes fewer than 2^32 threads.
+constexpr int64_t kMostGroups = ((int64_t)1 << 24) - 1;
 
 // The text GEMM writes one (max, lowest argmax) partial per row for every
 // kTextPartCols columns of the text vocabulary.

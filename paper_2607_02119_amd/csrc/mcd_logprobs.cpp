@@ -32,6 +32,8 @@ mcd_status check_sizes(int32_t n, int32_t K, int32_t V, int32_t T) {
   }
   // (items of a launch: a part of a vector each)
   if ((int64_t)n * K * ((V + 4095) / 4096) >= (int64_t)1 << 31) return bad("too many vectors");
+  if (mcd::logprob_groups((int64_t)n * K, V) > mcd::kMostGroups)
+    return mcd::record_error(MCD_E_UNSUPPORTED, "more vectors than a launch takes");
   return MCD_OK;
 }
 

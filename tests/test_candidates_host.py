@@ -144,3 +144,19 @@ def test_logprob_tensors_are_checked():
                   ((x.flatten(1), i, f), dict(V_stream=[10, 11]))):
         with pytest.raises(ValueError):
             mcd.mcd_logprobs(*a, ws, **kw)
+
+
+def test_logprobs_of_more_vectors_than_a_launch_takes():
+    """A launch has fewer than 2^32 threads: 2^24 workgroups of 256, each for a vector's part of up to
+    8192 logits or for four vectors of up to 1024."""
+    f = mcd._mcd_logprobs_workspace_bytes
+    for V, most in ((1, (1 << 26) - 4), (1024, (1 << 26) - 4), (1025, (1 << 24) - 1),
+                    (4096, (1 << 24) - 1), (8192, (1 << 24) - 1), (8193, (1 << 23) - 1),
+                    (151936, ((1 << 24) - 1) // 19), (1 << 19, ((1 << 24) - 1) // 64)):
+        for T in (0, 1, 5):
+            assert f(most, 1, V, T) > 0 and f(most // 16, 16, V, T) > 0
+            assert f(most + 1, 1, V, T) == 0 and f(most // 16 + 1, 16, V, T) == 0
+        b = dict(n=most + 1, K=1, V=V, T=0, pad_id=-1, logits=1 << 60, logits_stride=V,
+                 token_rows=most + 1, token_row=None, entropy=None, top_ids=None,
+                 top_logprobs=None, workspace_bytes=1 << 50)
+        assert _logprobs(**b) == mcd.MCD_E_UNSUPPORTED, V

@@ -318,3 +318,19 @@ def test_parts_of_masked_logits(V, n, dtype):
     tokens = rng.integers(0, V, (len(x), 1))
     for T in (0, 1, 5):
         check(x, [V], tokens, T, -1, dtype)
+
+
+def test_as_many_vectors_as_a_launch_takes():
+    """2^26 - 4 vectors: 2^24 - 1 workgroups."""
+    n = (1 << 26) - 4
+    x = torch.randn((n, 1, 2), dtype=BF16, device="cuda")
+    tokens = torch.randint(0, 2, (n, 1), dtype=torch.int32, device="cuda")
+    lp = torch.full((n, 1), 7.0, device="cuda")
+    ws = torch.zeros(mcd.mcd_logprobs_workspace_bytes(n, 1, 2, 0), dtype=torch.uint8, device="cuda")
+    mcd.mcd_logprobs(x, tokens, lp, ws)
+    assert mcd.mcd_read_device_status(ws) == 0
+    for part in (slice(0, 1 << 20), slice(n // 2, n // 2 + (1 << 20)), slice(n - (1 << 20), n)):
+        want = torch.log_softmax(x[part].double(), 2).gather(2, tokens[part, :, None].long())[..., 0]
+        # |log p| below 16 and 60 units of the sum (see reference)
+        assert (lp[part] - want).abs().max() <= 2.0 ** -24 * (16 + 60 + 2.5 * 16)
+    assert bool((lp <= 0).all())
