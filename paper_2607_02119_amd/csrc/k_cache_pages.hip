@@ -44,12 +44,15 @@ __global__ __launch_bounds__(256) void clear_kernel(int32_t *refs, int32_t n) {
   if (i < n) refs[i] = 0;
 }
 
+// (in turns, where the table has more entries than a launch has threads)
 __global__ __launch_bounds__(256) void refs_kernel(PagesView pv, uint32_t *status) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (int64_t)pv.n_slots * pv.max_pages) return;
-  const int id = pv.table[i];
-  if (id >= pv.n_pages) set_bad(status);
-  else if (id >= 0) atomicAdd(pv.refs + id, 1);
+  const int64_t entries = (int64_t)pv.n_slots * pv.max_pages;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < entries;
+       i += (int64_t)gridDim.x * 256) {
+    const int id = pv.table[i];
+    if (id >= pv.n_pages) set_bad(status);
+    else if (id >= 0) atomicAdd(pv.refs + id, 1);
+  }
 }
 
 // A row's slot, or -1 (reported).
@@ -465,8 +468,8 @@ hipError_t launch_cache_count(const PagesView &pv, uint32_t *status, hipStream_t
   hipLaunchKernelGGL(clear_kernel, dim3((unsigned)(((int64_t)pv.n_pages + 255) / 256)), dim3(256),
                      0, st, pv.refs, pv.n_pages);
   const int64_t entries = (int64_t)pv.n_slots * pv.max_pages;
-  hipLaunchKernelGGL(refs_kernel, dim3((unsigned)((entries + 255) / 256)), dim3(256), 0, st, pv,
-                     status);
+  const int64_t groups = std::min<int64_t>((entries + 255) / 256, kMostGroups);
+  hipLaunchKernelGGL(refs_kernel, dim3((unsigned)groups), dim3(256), 0, st, pv, status);
   return hipGetLastError();
 }
 

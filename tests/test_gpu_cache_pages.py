@@ -302,3 +302,24 @@ def test_release_of_lengths_out_of_range_gives_nothing_back():
     mcd.mcd_cache_release(b.pages, i32([0, 0]), b.ws, length=i32([-5, 64]))
     b.mirror.release([0], [64])
     b.check(mcd.MCD_DEV_BAD_PAGE)
+
+
+def test_count_of_more_entries_than_a_launch_has_threads():
+    slots, columns, n_pages = (1 << 18) + 1, 1 << 14, 1000         # 2^32 + 2^14 entries
+    table = torch.full((slots, columns), -1, dtype=torch.int32, device="cuda")
+    flat, rng = table.view(-1), np.random.default_rng(0)
+    at = np.unique(np.concatenate([rng.integers(0, slots * columns, 5000), [0, (1 << 32) - 257,
+                                   (1 << 32) - 256, (1 << 32) - 1, 1 << 32, slots * columns - 1]]))
+    ids = rng.integers(0, n_pages, len(at))
+    flat[torch.from_numpy(at).cuda()] = i32(ids)
+    pages = mcd.CachePages(table, n_pages)
+    assert np.array_equal(pages.refs.cpu().numpy(), np.bincount(ids, minlength=n_pages))
+    # release and share of the last slot
+    ws, last = pages.workspace(1), i32([slots - 1])
+    mcd.mcd_cache_share(pages, i32([slots - 2]), last, i32([columns * 64]), ws)
+    mcd.mcd_read_device_status(ws)
+    mcd.mcd_cache_release(pages, last, ws)
+    mcd.mcd_cache_release(pages, i32([slots - 2]), ws)
+    assert mcd.mcd_read_device_status(ws) == 0 and bool((table[-2:] == -1).all())
+    want = np.bincount(ids[at < (slots - 2) * columns], minlength=n_pages)
+    assert np.array_equal(pages.refs.cpu().numpy(), want)
