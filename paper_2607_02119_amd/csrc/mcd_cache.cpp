@@ -324,7 +324,8 @@ mcd_status mcd_cache_attend(const mcd_cache *c, const mcd_cache_rows *r,
   const mcd::CacheView cv = view(c);
   const mcd::RowsView rv = view(r);
   const mcd::AttendPlan p = mcd::cache_attend_plan(cv, rv, c->D, a->Hq);
-  if ((p.narrow.tiles * p.narrow.splits + p.wide.tiles * p.wide.splits) * c->Hkv > kMost)
+  if (std::max(p.narrow.tiles * p.narrow.splits, p.wide.tiles * p.wide.splits) * c->Hkv >
+      mcd::kMostGroups)
     return bad("too many query rows");
   CHECK(check_workspace(a->workspace, a->workspace_bytes,
                         workspace_need(p, cv, rv, c->D, a->Hq)));
@@ -422,12 +423,17 @@ mcd_status mcd_cache_attend_route(const mcd_cache *c, const mcd_cache_rows *r,
   const mcd::GroupsView gv = view(g);
   CHECK(check_workspace(a->workspace, a->workspace_bytes, shared_need(cv, rv, gv, c->D, a->Hq)));
   if (way < 0) way = mcd::cache_shared_worth(cv, rv, gv, c->D, a->Hq) ? 1 : 0;
-  if ((int64_t)a->Hq * c->D > (int64_t)65535 * 1024) way = 0;   // (the join's grid)
+  mcd::SharedPlan p = {};
+  if (way) {
+    p = mcd::cache_shared_plan(cv, rv, gv, c->D, a->Hq);
+    const int64_t both = p.prefix.tiles * p.prefix.splits +
+                         (p.own.narrow.tiles * p.own.narrow.splits + 3) / 4;
+    // (the launches' grids, the join's with them)
+    if (std::max(both, p.own.wide.tiles * p.own.wide.splits) * c->Hkv > mcd::kMostGroups ||
+        rv.N > mcd::kMostGroups || (int64_t)a->Hq * c->D > (int64_t)65535 * 1024)
+      way = 0;
+  }
   if (!way) return mcd_cache_attend(&alone, r, a, stream);
-  const mcd::SharedPlan p = mcd::cache_shared_plan(cv, rv, gv, c->D, a->Hq);
-  if ((p.prefix.tiles * p.prefix.splits + p.own.narrow.tiles * p.own.narrow.splits +
-       p.own.wide.tiles * p.own.wide.splits) * c->Hkv > kMost)
-    return bad("too many query rows");
   char *w = static_cast<char *>(a->workspace);
   mcd::AttendView av = query_view(c, a);
   av.status = reinterpret_cast<uint32_t *>(w);

@@ -160,3 +160,27 @@ def test_logprobs_of_more_vectors_than_a_launch_takes():
                  token_rows=most + 1, token_row=None, entropy=None, top_ids=None,
                  top_logprobs=None, workspace_bytes=1 << 50)
         assert _logprobs(**b) == mcd.MCD_E_UNSUPPORTED, V
+
+
+def test_attention_of_more_tiles_than_a_launch_takes():
+    """65535 rows of 257 heads and prompts of 2^26 tokens: more than 2^24 - 1 workgroups.  Together
+    four single rows are a workgroup's, so of rows that share pages only the prompts are refused."""
+    route = mcd._lib.mcd_cache_attend_route
+    route.restype = ctypes.c_int
+    for Hkv, D, rows in ((257, 64, dict(R=65535, n_tokens=65535, max_tokens=1, max_context=5000)),
+                         (16, 256, dict(R=1, n_tokens=1 << 26, max_tokens=1 << 26,
+                                        max_context=1 << 26, start=FAKE))):
+        cache = mcd.mcd_cache(Hkv=Hkv, D=D, n_slots=70000, max_pages=1 << 20, n_pages=9, pages=FAKE,
+                              table=FAKE)
+        r = mcd.mcd_cache_rows(slot=None, context=FAKE, **rows)
+        a = mcd.mcd_cache_attend_args(Hq=Hkv, dtype=mcd.MCD_BF16, scale=0.1, q=FAKE,
+                                      q_stride=Hkv * D, out=1 << 60, out_stride=Hkv * D,
+                                      workspace=FAKE, workspace_bytes=1 << 50)
+        ref = [ctypes.byref(x) for x in (cache, r, a)]
+        assert mcd._mcd_cache_attend(*ref, None) == mcd.MCD_E_INVALID
+        assert "too many query rows" in mcd.mcd_last_error()
+    g = mcd.mcd_cache_groups(n=1, max_rows=65535, max_prefix=4096, max_own=1 << 26, start=FAKE,
+                             prefix=FAKE)
+    for way in (-1, 0, 1):
+        assert route(*ref[:2], ctypes.byref(g), ref[2], way, None) == mcd.MCD_E_INVALID
+        assert "too many query rows" in mcd.mcd_last_error()
