@@ -570,7 +570,8 @@ typedef struct {
 
 /* Workspace bytes of mcd_cache_attend_shared for these bounds (0 for invalid sizes),
  * enough for every step of no more rows, tokens, groups and positions too; as
- * mcd_cache_attend's otherwise, which it also serves when no weight is added up. */
+ * mcd_cache_attend's otherwise, which it also serves for a cache with weight NULL
+ * (with weights that call asks for more, whether any are added up or not). */
 size_t mcd_cache_shared_workspace_bytes(const mcd_cache *cache, const mcd_cache_rows *rows,
                                         const mcd_cache_groups *groups, int32_t Hq);
 

@@ -318,3 +318,27 @@ def test_the_call_takes_many_rows_of_a_long_prefix_together():
             ws = s.cache.workspace(s.rows, 16)
             mcd.mcd_cache_attend(s.cache, s.rows, dev(s.q).to(BF16), other, ws, scale=0.07)
             assert torch.equal(out, other)
+
+
+def test_the_workspace_serves_rows_alone():
+    """The groups' workspace has no room for the scores that received weight is added up from: it
+    serves mcd_cache_attend of the cache without weights, and is refused for one that has them."""
+    rng = np.random.default_rng(77)
+    s = Step(rng, [_same(640, 4), _same(1100, 3)], 4, 2, 64, BF16)
+    plain, lse, status = s.run("call")
+    assert status == 0
+    weight = torch.zeros((s.cache.n_slots, 2, s.cache.max_pages * 64), device="cuda")
+    weighted = mcd.Cache(s.cache.pages, s.cache.table, s.D, weight)
+    ws = weighted.workspace(s.rows, s.Hq, groups=s.groups)
+    out, l2 = torch.full_like(plain, 9.0).contiguous(), torch.zeros_like(lse)
+    q = dev(s.q).to(BF16)
+    mcd.mcd_cache_attend(s.cache, s.rows, q, out, ws, scale=0.07, lse=l2)
+    s.check(out, l2)
+    attend("call", weighted, s.rows, s.groups, q, out, ws, scale=0.07, lse=l2)
+    assert mcd.mcd_read_device_status(ws) == 0
+    s.check(out, l2)
+    assert torch.equal(out, plain) and torch.equal(l2, lse) and not weight.any()
+    for w in (None, weight):
+        with pytest.raises(mcd.McdError) as e:
+            mcd.mcd_cache_attend(weighted, s.rows, q, out, ws, scale=0.07, weight_out=w)
+        assert e.value.code == mcd.MCD_E_WORKSPACE
