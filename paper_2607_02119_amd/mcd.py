@@ -658,9 +658,11 @@ def mcd_cache_evict(src, dst, length, keep, recent, kept, length_out, workspace,
 
 class CachePages:
     """A cache's page table (int32 [n_slots][max_pages], borrowed; below 0: no page) and how many
-    of its entries hold each of n_pages pages (refs, counted here)."""
+    of its entries hold each of n_pages pages (refs, counted here).  A table that names other
+    pages is refused, which waits for the count; with a workspace, its status word says so
+    (MCD_DEV_BAD_PAGE) and nothing waits."""
 
-    def __init__(self, table, n_pages):
+    def __init__(self, table, n_pages, workspace=None):
         if table.dtype != torch.int32 or table.dim() != 2 or not table.is_contiguous():
             raise ValueError("table must be contiguous int32 [n_slots][max_pages]")
         self.table, self.n_pages = table, int(n_pages)
@@ -671,7 +673,12 @@ class CachePages:
         self.ref = ctypes.byref(self.struct)
         self.on_gpu = table.is_cuda
         if self.on_gpu:
-            mcd_cache_count(self, torch.zeros(256, dtype=torch.uint8, device=table.device))
+            ws = torch.zeros(256, dtype=torch.uint8, device=table.device) if workspace is None \
+                else workspace
+            mcd_cache_count(self, ws)
+            if workspace is None and not torch.cuda.is_current_stream_capturing() \
+                    and mcd_read_device_status(ws):
+                raise ValueError(f"table names pages from n_pages ({self.n_pages}) on")
 
     def workspace_bytes(self, R):
         n = int(_mcd_cache_pages_workspace_bytes(self.ref, int(R)))

@@ -323,3 +323,26 @@ def test_count_of_more_entries_than_a_launch_has_threads():
     assert mcd.mcd_read_device_status(ws) == 0 and bool((table[-2:] == -1).all())
     want = np.bincount(ids[at < (slots - 2) * columns], minlength=n_pages)
     assert np.array_equal(pages.refs.cpu().numpy(), want)
+
+
+def test_a_table_that_names_other_pages():
+    """Refused where the pages are counted, or reported in the workspace that the count is given;
+    the entries within are counted."""
+    table = i32([[0, 4, -1], [4, 5, 2 ** 31 - 1], [-7, 2, 0]])
+    with pytest.raises(ValueError, match="from n_pages"):
+        mcd.CachePages(table, 5)
+    ws = torch.zeros(256, dtype=torch.uint8, device="cuda")
+    pages = mcd.CachePages(table, 5, workspace=ws)
+    assert mcd.mcd_read_device_status(ws) == mcd.MCD_DEV_BAD_PAGE
+    assert pages.refs.tolist() == [2, 0, 1, 0, 2]
+    table[1, 1:] = -1
+    assert mcd.CachePages(table, 5).refs.tolist() == [2, 0, 1, 0, 2]
+    mcd.CachePages(table, 5, workspace=ws)
+    assert mcd.mcd_read_device_status(ws) == 0
+    # within a capture nothing waits
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = mcd.CachePages(table, 5)
+    graph.replay()
+    assert captured.refs.tolist() == [2, 0, 1, 0, 2]
