@@ -431,7 +431,8 @@ mcd_status mcd_sched_counts(const mcd_sched *s, int32_t *waiting, int32_t *runni
  * A slot is a sequence of positions 0, 1, ... in pages of MCD_CACHE_PAGE tokens:
  * position t lies in page table[slot][t / 64] at token t % 64.  Slots may share
  * pages (a Companion that joins with a copy of its Main row's prefix) as long as
- * no call appends to a shared page.  Keys are cached as attention multiplies
+ * no call writes to a shared page: with refs, such pages are left alone and
+ * MCD_DEV_BAD_PAGE is set.  Keys are cached as attention multiplies
  * them (after any rotary embedding), so positions may later be dropped.
  *
  * A page holds, for each K/V head, mcd_cache_page_bytes(D) bytes (66 D + 128):
@@ -468,6 +469,9 @@ typedef struct {
   const int32_t *table;      /* [n_slots][max_pages] page ids; read up to a slot's length only */
   float *weight;             /* [n_slots][Hkv][max_pages * 64] attention weight every position
                                 has received, or NULL */
+  const int32_t *refs;       /* [n_pages] how many table entries hold each page
+                                (mcd_cache_pages.refs): append, and evict into this cache,
+                                write to no page that more than one holds; or NULL */
 } mcd_cache;
 
 /* The rows of a step and their new tokens; tokens of row r are start[r] ..
@@ -661,7 +665,9 @@ mcd_status mcd_cache_share(const mcd_cache_pages *pages, int32_t R, const int32_
  * tokens[r] new tokens at positions context[r], context[r] + 1, ...: every column
  * of theirs without a page takes a free one, in the order of the rows and of their
  * positions the free pages in the order of their ids.  (A page that other entries
- * hold too is no place for a new token: MCD_DEV_BAD_PAGE, and where is -1.)
+ * hold too is no place for a new token, as after a release to a length within it:
+ * MCD_DEV_BAD_PAGE, and where is -1.  mcd_cache_append goes by the table, not by where:
+ * give its cache the refs, or it writes there all the same.)
  *   start:    [R + 1] sums of tokens before each row, for mcd_cache_rows
  *   where:    [n_tokens] page * 64 + position % 64 of each packed token, -1: no page
  *   row, position: [n_tokens] of each packed token

@@ -16,6 +16,7 @@ struct CacheView {
   uint8_t *pages;
   const int32_t *table;
   float *weight;
+  const int32_t *refs;
 };
 
 struct RowsView {
@@ -209,11 +210,12 @@ __device__ __forceinline__ int find_row(int R, int64_t x, Base &&base) {
 }
 
 // First byte of page `at` of a slot for head h, or null for a page id out of
-// range.  at is below max_pages.
-template <int D>
+// range and (WRITE) for a page that other entries hold too.  at is below max_pages.
+template <int D, bool WRITE = false>
 __device__ __forceinline__ uint8_t *page_of(const CacheView &cv, int slot, int at, int h) {
   const int id = ld_const(cv.table + (int64_t)slot * cv.max_pages, at);
   if (id < 0 || id >= cv.n_pages) return nullptr;
+  if (WRITE && cv.refs && ld_const(cv.refs, id) > 1) return nullptr;
   return cv.pages + ((int64_t)id * cv.Hkv + h) * cache_page_bytes(D);
 }
 

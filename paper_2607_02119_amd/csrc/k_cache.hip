@@ -143,7 +143,7 @@ __global__ __launch_bounds__(256) void append_one_kernel(CacheView cv, RowsView 
     return;
   }
   const int id = cv.table[(int64_t)slot * cv.max_pages + pos / kPage];
-  if (id < 0 || id >= cv.n_pages) {
+  if (id < 0 || id >= cv.n_pages || (cv.refs && cv.refs[id] > 1)) {
     if (chunk == 0) set_bad(status);
     return;
   }
@@ -187,7 +187,7 @@ struct StretchItem {
   uint8_t *page;             // of head 0
 };
 
-template <int D, int TOK>
+template <int D, int TOK, bool WRITE>
 __device__ __forceinline__ StretchItem stretch_item(const CacheView &cv, const RowsView &rv,
                                                     uint32_t *status) {
   StretchItem it;
@@ -209,7 +209,7 @@ __device__ __forceinline__ StretchItem stretch_item(const CacheView &cv, const R
   it.pos0 = (int)at * TOK;
   it.lo = max(first - it.pos0, 0);
   it.hi = min(s.len - it.pos0, TOK);
-  it.page = page_of<D>(cv, s.slot, it.pos0 / kPage, 0);
+  it.page = page_of<D, WRITE>(cv, s.slot, it.pos0 / kPage, 0);
   if (!it.page) {
     it.hi = it.lo;
     if (threadIdx.x == 0) set_bad(status);
@@ -238,7 +238,7 @@ __global__ __launch_bounds__(256) void append_kernel(CacheView cv, RowsView rv, 
                                                      uint32_t *status) {
   constexpr int L = D / 8, E = kHalf * L / 256;
   __shared__ uint32_t codes[2][kHalf][L + 1];
-  const StretchItem it = stretch_item<D, kHalf>(cv, rv, status);
+  const StretchItem it = stretch_item<D, kHalf, true>(cv, rv, status);
   if (it.lo >= it.hi) return;
   const int t0 = it.pos0 % kPage;                // the half's first token in the page
   int b = 0;
@@ -346,7 +346,7 @@ __global__ __launch_bounds__(256) void read_kernel(CacheView cv, RowsView rv, vo
                                                    void *v, int64_t vs, uint32_t *status) {
   constexpr int L = D / 8, E = kPage * L / 256, V = (2 * D + 255) / 256;
   __shared__ u32x4 words[2][2 * D];
-  const StretchItem it = stretch_item<D, kPage>(cv, rv, status);
+  const StretchItem it = stretch_item<D, kPage, false>(cv, rv, status);
   if (it.lo >= it.hi) return;
   u32x4 vw[V];
   uint32_t kc[E];
@@ -572,7 +572,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(CacheView from, CacheVi
   if (pos0 >= len) return;
   const int count = min(len - pos0, kPage);
   uint8_t *dst = nullptr;
-  if (r < to.n_slots && at < to.max_pages) dst = page_of<D>(to, r, at, h);
+  if (r < to.n_slots && at < to.max_pages) dst = page_of<D, true>(to, r, at, h);
   if (!dst) {
     if (tid == 0) set_bad(ev.status);
     return;

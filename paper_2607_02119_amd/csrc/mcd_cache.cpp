@@ -45,7 +45,8 @@ mcd_status check_cache(const mcd_cache *c) {
     return bad("cache too large");
   if (!c->pages || !c->table) return bad("null pages or table");
   if (!aligned(c->pages, 16)) return bad("pages must be 16-byte aligned");
-  if (!aligned(c->table, 4) || !aligned(c->weight, 4)) return bad("table or weight not aligned");
+  if (!aligned(c->table, 4) || !aligned(c->weight, 4) || !aligned(c->refs, 4))
+    return bad("table, weight or refs not aligned");
   return MCD_OK;
 }
 
@@ -104,7 +105,7 @@ mcd_status check_workspace(const void *w, size_t have, size_t need) {
 
 mcd::CacheView view(const mcd_cache *c) {
   return mcd::CacheView{c->Hkv, c->n_slots, c->max_pages, c->n_pages,
-                        static_cast<uint8_t *>(c->pages), c->table, c->weight};
+                        static_cast<uint8_t *>(c->pages), c->table, c->weight, c->refs};
 }
 
 mcd::RowsView view(const mcd_cache_rows *r) {

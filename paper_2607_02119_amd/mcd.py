@@ -81,7 +81,7 @@ class mcd_sched_batch(ctypes.Structure):
 
 class mcd_cache(ctypes.Structure):
     _fields_ = [("Hkv", _i32), ("D", _i32), ("n_slots", _i32), ("max_pages", _i32),
-                ("n_pages", _i32), ("pages", _vp), ("table", _vp), ("weight", _vp)]
+                ("n_pages", _i32), ("pages", _vp), ("table", _vp), ("weight", _vp), ("refs", _vp)]
 
 
 class mcd_cache_rows(ctypes.Structure):
@@ -498,10 +498,12 @@ class Cache:
     """A layer's 4-bit key/value cache and the device tensors it borrows.
 
     pages: uint8 [n_pages][Hkv][mcd_cache_page_bytes(D)]; table: int32 [n_slots][max_pages];
-    weight: float32 [n_slots][Hkv][max_pages * 64] or None.  Cache.alloc makes the pages."""
+    weight: float32 [n_slots][Hkv][max_pages * 64] or None; refs: int32 [n_pages], how many table
+    entries hold each page (CachePages.refs): no call writes to a page that more than one holds; or
+    None.  Cache.alloc makes the pages."""
 
-    def __init__(self, pages, table, D, weight=None):
-        self.pages, self.table, self.weight, self.D = pages, table, weight, int(D)
+    def __init__(self, pages, table, D, weight=None, refs=None):
+        self.pages, self.table, self.weight, self.D, self.refs = pages, table, weight, int(D), refs
         n_pages, self.Hkv, page_bytes = pages.shape
         self.n_slots, self.max_pages = table.shape
         if page_bytes != mcd_cache_page_bytes(D):
@@ -509,15 +511,17 @@ class Cache:
                              f"{mcd_cache_page_bytes(D)}")
         shape = (self.n_slots, self.Hkv, self.max_pages * MCD_CACHE_PAGE)
         for name, t, dt in (("pages", pages, torch.uint8), ("table", table, torch.int32),
-                            ("weight", weight, torch.float32)):
+                            ("weight", weight, torch.float32), ("refs", refs, torch.int32)):
             if t is not None and (t.dtype != dt or not t.is_contiguous()):
                 raise ValueError(f"{name} must be contiguous {dt}")
         if weight is not None and tuple(weight.shape) != shape:
             raise ValueError(f"weight: shape {tuple(weight.shape)}, expected {shape}")
+        if refs is not None and tuple(refs.shape) != (n_pages,):
+            raise ValueError(f"refs: shape {tuple(refs.shape)}, expected {(n_pages,)}")
         self.struct = mcd_cache(self.Hkv, self.D, self.n_slots, self.max_pages, n_pages,
-                                _ptr(pages), _ptr(table), _ptr(weight))
+                                _ptr(pages), _ptr(table), _ptr(weight), _ptr(refs))
         self.ref = ctypes.byref(self.struct)
-        self.on_gpu = all(t is None or t.is_cuda for t in (pages, table, weight))
+        self.on_gpu = all(t is None or t.is_cuda for t in (pages, table, weight, refs))
 
     @classmethod
     def alloc(cls, n_pages, Hkv, D, n_slots, max_pages, weights=False, device="cuda"):

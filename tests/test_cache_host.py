@@ -292,3 +292,16 @@ def test_weight_out_beside_the_weights_is_refused():
         assert _attend(**at) == mcd.MCD_E_INVALID, shift
         assert "apart" in mcd.mcd_last_error()
         assert _attend(r=_rows(R=3, n_tokens=0, max_tokens=0, start=FAKE), **at) == mcd.MCD_E_INVALID
+
+
+def test_refs_are_checked():
+    """How many entries hold each page: int32, one for every page, where the pages are."""
+    for f in (mcd._mcd_cache_append, mcd._mcd_cache_read):
+        assert _move(f, c=_cache(refs=FAKE + 2)) == mcd.MCD_E_INVALID
+    cache = mcd.Cache.alloc(3, 2, 64, 2, 2, device="cpu")
+    refs = torch.zeros(3, dtype=torch.int32)
+    assert mcd.Cache(cache.pages, cache.table, 64, refs=refs).struct.refs == refs.data_ptr()
+    assert cache.struct.refs is None
+    for bad in (refs[:2], refs.long(), torch.zeros((3, 1), dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            mcd.Cache(cache.pages, cache.table, 64, refs=bad)

@@ -346,3 +346,86 @@ def test_a_table_that_names_other_pages():
         captured = mcd.CachePages(table, 5)
     graph.replay()
     assert captured.refs.tolist() == [2, 0, 1, 0, 2]
+
+
+@pytest.mark.parametrize("captured", [False, True], ids=["eager", "captured"])
+@pytest.mark.parametrize("tokens", [[1, 1, 1], [40, 2, 1], [70, 100, 0]], ids=str)
+def test_no_call_writes_to_a_shared_page(tokens, captured):
+    """A row that was cut off within a page that others hold: its new tokens there have no place, and
+    an append of the cache with refs leaves the page alone; every other token is written."""
+    rng = np.random.default_rng(sum(tokens))
+    H, D, n_pages = 2, 64, 30
+    b = Both(4, 6, n_pages)
+    pages = torch.from_numpy(rng.integers(0, 256, (n_pages, H, mcd.mcd_cache_page_bytes(D)),
+                                          dtype=np.uint8)).cuda()
+    cache = mcd.Cache(pages, b.pages.table, D, refs=b.pages.refs)
+    plain = mcd.Cache(pages, b.pages.table, D)
+    b.reserve([0], [0], [150])
+    b.share([1, 2, 3], [0, 0, 0], [150] * 3)             # two pages each, by all
+    b.reserve([1, 2, 3], [128] * 3, [9, 20, 9])
+    b.release([1, 3], [100, 60])                         # within their second and first pages
+    slot, context = [1, 2, 3], [100, 148, 60]
+    N, most = sum(tokens), max(tokens)
+    kv = torch.randn((N, 2, H, D), device="cuda")
+    start = torch.zeros(4, dtype=torch.int32, device="cuda")
+    where = torch.zeros(N, dtype=torch.int64, device="cuda")
+    before, ctx, new, at = pages.clone(), i32(context), i32(tokens), i32(slot)
+    rows = mcd.CacheRows(ctx, start=start, slot=at, n_tokens=N, max_tokens=most, max_context=384)
+    kr, vr = (torch.full((N, H, D), 9.0, device="cuda") for _ in range(2))
+
+    def calls():
+        mcd.mcd_cache_reserve(b.pages, ctx, new, start, b.ws, slot=at, n_tokens=N, max_tokens=most,
+                              max_context=384, where=where)
+        mcd.mcd_cache_append(cache, rows, kv[:, 0], kv[:, 1], b.ws)
+
+    if captured:
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            calls()
+        graph.replay()
+    else:
+        calls()
+    want = b.mirror.reserve(slot, context, tokens)
+    assert np.array_equal(where.cpu().numpy(), want[0]) and (want[0] == -1).any()
+    b.check(mcd.MCD_DEV_BAD_PAGE)                        # reserve's and append's
+    mcd.mcd_cache_append(cache, rows, kv[:, 0], kv[:, 1], b.ws)
+    assert mcd.mcd_read_device_status(b.ws) == mcd.MCD_DEV_BAD_PAGE
+    # the pages of other slots, and those that nothing was appended to, as they were
+    touched = np.unique(want[0][want[0] >= 0] // 64)
+    others = np.setdiff1d(np.arange(n_pages), touched)
+    assert torch.equal(pages[others], before[others])
+    assert set(b.mirror.table[0, :3]) <= set(others)
+    # what has a place was written: as an append of those tokens alone, to a copy of the pages
+    mcd.mcd_cache_read(plain, rows, kr, vr, b.ws)
+    assert mcd.mcd_read_device_status(b.ws) == 0
+    copy = mcd.Cache(before.clone(), i32(np.arange(n_pages)[:, None]), D)
+    for t in np.flatnonzero(want[0] >= 0):
+        page, pos = divmod(int(want[0][t]), 64)
+        one = mcd.CacheRows(i32([pos]), slot=i32([page]), n_tokens=1, max_tokens=1, max_context=64)
+        mcd.mcd_cache_append(copy, one, kv[t:t + 1, 0], kv[t:t + 1, 1], b.ws)
+        k1, v1 = (torch.zeros((1, H, D), device="cuda") for _ in range(2))
+        mcd.mcd_cache_read(copy, one, k1, v1, b.ws)
+        assert torch.equal(k1[0], kr[t]) and torch.equal(v1[0], vr[t])
+    assert mcd.mcd_read_device_status(b.ws) == 0
+    if most == 1:
+        assert torch.equal(copy.pages, pages)
+
+
+def test_no_eviction_writes_to_a_shared_page():
+    rng = np.random.default_rng(5)
+    H, D, n_pages = 2, 64, 12
+    pages = torch.from_numpy(rng.integers(0, 256, (n_pages, H, mcd.mcd_cache_page_bytes(D)),
+                                          dtype=np.uint8)).cuda()
+    src = mcd.Cache(pages, i32([[0, 1, 2]]), D)
+    refs = i32([1] * n_pages)
+    refs[5] = 2
+    to = mcd.Cache(pages, i32([[4, 5, 6]]), D, refs=refs)
+    ws = torch.zeros(256, dtype=torch.uint8, device="cuda")
+    kept = torch.zeros((1, H, 192), dtype=torch.int32, device="cuda")
+    out, before = torch.zeros(1, dtype=torch.int32, device="cuda"), pages.clone()
+    mcd.mcd_cache_evict(src, to, i32([192]), 192, 192, kept, out, ws, 192)
+    assert mcd.mcd_read_device_status(ws) == mcd.MCD_DEV_BAD_PAGE
+    assert torch.equal(pages[4], before[0]) and torch.equal(pages[6], before[2])
+    rest = [0, 1, 2, 3, 5, 7, 8, 9, 10, 11]
+    assert torch.equal(pages[rest], before[rest])
