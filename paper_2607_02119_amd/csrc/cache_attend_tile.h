@@ -1,5 +1,5 @@
 // Attention over the 4-bit key/value cache: a page of keys and values against tiles of
-// query rows, and the kernels of few and of many query rows, for any rows that have
+// query rows, the kernel of few query rows, and that of many for any rows that have
 //   row_span(cv, rows, r)   a row's tokens and positions, and its first page to read
 //   tile_row(rows, G, TQ, x, tile)  the row and tile of work item x
 //   Rows::kParts            results as parts of every query row, for another kernel to join
@@ -768,22 +768,21 @@ struct NarrowLds {
   bf16x8 q[SPL * (D / 32) * 64];
 };
 
-template <int D, int SPL, int PACK, class Rows>
-__device__ __forceinline__ void narrow_rows(const CacheView &cv, const Rows &rv,
-                                            const AttendView &av, uint32_t block,
-                                            NarrowLds<D, SPL, PACK> &sh) {
+template <int D, int SPL, int PACK, int OCC>
+__global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, RowsView rv, AttendView av) {
   constexpr int W = 16 / PACK, WAVES = 4;
   constexpr bool BF16 = SPL == 1;
   constexpr int PITCH = D + 4;
+  __shared__ NarrowLds<D, SPL, PACK> sh;
   auto &sh_ml = sh.ml;
   auto &sh_o = sh.o;
   auto &sh_q = sh.q;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, m = lane & 15;
   // (heads fastest: a page's heads lie side by side)
-  const int h = block % cv.Hkv;
-  const int r = block / cv.Hkv / av.splits;
-  const int split = block / cv.Hkv - r * av.splits;
+  const int h = blockIdx.x % cv.Hkv;
+  const int r = blockIdx.x / cv.Hkv / av.splits;
+  const int split = blockIdx.x / cv.Hkv - r * av.splits;
   const Span sp = row_span(cv, rv, r);
   if (sp.bad && h == 0 && threadIdx.x == 0) set_bad(av.status);
   if (!is_narrow(sp, av)) return;
@@ -791,7 +790,7 @@ __device__ __forceinline__ void narrow_rows(const CacheView &cv, const Rows &rv,
   const int pages = tile_pages(sp, av.G, rows);
   const int used = splits_used(sp, av, pages);
   if (split > 0 && split >= used) return;
-  const int p0 = sp.page0 + split * av.split_pages, p1 = min(pages, p0 + av.split_pages);
+  const int p0 = split * av.split_pages, p1 = min(pages, p0 + av.split_pages);
 
   const Query qr = query_of(sp, av, h, m % W);
   const int all = min(sp.len - 1, sp.ctx);       // positions that every row sees
@@ -880,10 +879,8 @@ __device__ __forceinline__ void narrow_rows(const CacheView &cv, const Rows &rv,
       l += sh_ml[1][k][row];
       acc += *reinterpret_cast<const floatx4 *>(sh_o + (k * W + row) * PITCH + c4);
     }
-    if (Rows::kParts || used > 1) {
-      const int64_t part = Rows::kParts
-                               ? part_of(av, sp.t0 + qy.tok, qy.head) + split
-                               : (((int64_t)r * cv.Hkv + h) * av.splits + split) * W + row;
+    if (used > 1) {
+      const int64_t part = (((int64_t)r * cv.Hkv + h) * av.splits + split) * W + row;
       *reinterpret_cast<floatx4 *>(av.part_o + part * D + c4) = acc;
       if (c4 == 0) av.part_ml[part] = make_float2(top, l);
       continue;
@@ -896,12 +893,6 @@ __device__ __forceinline__ void narrow_rows(const CacheView &cv, const Rows &rv,
     store4<BF16>(av.out, tok * av.out_stride + qy.head * D + c4, y);
     if (c4 == 0) finish_row(av, tok * av.Hq + qy.head, top, l);
   }
-}
-
-template <int D, int SPL, int PACK, int OCC, class Rows>
-__global__ __launch_bounds__(256, OCC) void narrow_kernel(CacheView cv, Rows rv, AttendView av) {
-  __shared__ NarrowLds<D, SPL, PACK> sh;
-  narrow_rows<D, SPL, PACK>(cv, rv, av, blockIdx.x, sh);
 }
 
 // Wide rows: a workgroup of four waves for 64 NT query rows of a K/V head and a
@@ -1060,38 +1051,32 @@ __global__ __launch_bounds__(256, OCC) void wide_kernel(CacheView cv, Rows rv, A
   }
 }
 
-template <int D, int SPL, int PACK, class Rows>
-void narrow_launch(const CacheView &cv, const Rows &rv, const AttendView &av, const dim3 &grid,
+template <int D, int SPL, int PACK>
+void narrow_launch(const CacheView &cv, const RowsView &rv, const AttendView &av, const TilePlan &t,
                    hipStream_t st) {
   // registers for four waves on a SIMD; a single tile of 128 channels spilled there
   // (256 rows, 16 query heads a K/V head: 53 us, with three 47.5).  256 channels, 128
   // rows of 100 to 1100 positions, 4 query heads a K/V head: bf16 with two 27 us,
   // with one 37, with three (spills) 40; fp32 with one 46.5, with two 31.
   constexpr int OCC = D * SPL > 384 ? 1 : D * SPL > 128 ? 2 : PACK == 1 ? 3 : 4;
-  hipLaunchKernelGGL((narrow_kernel<D, SPL, PACK, OCC, Rows>), grid, dim3(256), 0, st, cv, rv,
-                     av);
+  hipLaunchKernelGGL((narrow_kernel<D, SPL, PACK, OCC>),
+                     dim3((unsigned)(t.tiles * t.splits * cv.Hkv)), dim3(256), 0, st, cv, rv, av);
 }
 
-// The narrow or the wide rows' tiles and splits (NARROW: there may be narrow ones).
-template <int D, int SPL, class Rows, bool NARROW = true>
-void tiles_launch(const CacheView &cv, const Rows &rv, const AttendView &av, int pack,
-                  const TilePlan &t, bool narrow, hipStream_t st) {
+template <int D, int SPL, class Rows>
+void wide_launch(const CacheView &cv, const Rows &rv, const AttendView &av, const TilePlan &t,
+                 hipStream_t st) {
   const dim3 grid((unsigned)(t.tiles * t.splits * cv.Hkv));
   // (workgroups on a compute unit of 256 channels, 4 chunks of 400 to 512 tokens: bf16
   // two 127 us, one 195; fp32 one 239, two, with 12 registers spilled, 171.  Of 128
   // channels in fp32: one 146, two 150.)
-  if (!narrow && t.tile == 64)
+  if (t.tile == 64) {
     hipLaunchKernelGGL((wide_kernel<D, SPL, 1, (D * SPL > 384 ? 1 : 2), Rows>), grid, dim3(256), 0,
                        st, cv, rv, av);
-  else if (!narrow) {
+  } else {
     if constexpr (D < 256)
       hipLaunchKernelGGL((wide_kernel<D, SPL, 2, (D * SPL > 256 ? 1 : 2), Rows>), grid, dim3(256),
                          0, st, cv, rv, av);
-  }
-  if constexpr (NARROW) {
-    if (narrow && pack == 4) narrow_launch<D, SPL, 4>(cv, rv, av, grid, st);
-    else if (narrow && pack == 2) narrow_launch<D, SPL, 2>(cv, rv, av, grid, st);
-    else if (narrow) narrow_launch<D, SPL, 1>(cv, rv, av, grid, st);
   }
 }
 

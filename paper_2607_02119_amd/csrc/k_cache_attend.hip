@@ -331,7 +331,10 @@ void attend_launch(const CacheView &cv, const RowsView &rv, AttendView av, const
     if (t.tiles == 0) continue;
     av.splits = t.splits;
     av.split_pages = t.split_pages;
-    tiles_launch<D, SPL>(cv, rv, av, plan.pack, t, narrow, st);
+    if (!narrow) wide_launch<D, SPL>(cv, rv, av, t, st);
+    else if (plan.pack == 4) narrow_launch<D, SPL, 4>(cv, rv, av, t, st);
+    else if (plan.pack == 2) narrow_launch<D, SPL, 2>(cv, rv, av, t, st);
+    else narrow_launch<D, SPL, 1>(cv, rv, av, t, st);
     if (t.splits > 1)
       hipLaunchKernelGGL((join_kernel<D, SPL == 1>),
                          dim3((unsigned)t.tiles, (unsigned)cv.Hkv,

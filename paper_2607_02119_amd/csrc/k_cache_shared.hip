@@ -562,7 +562,7 @@ void shared_launch(const CacheView &cv, const RowsView &rv, const GroupsView &gv
     AttendView wide = own;
     wide.splits = w.splits;
     wide.split_pages = w.split_pages;
-    tiles_launch<D, SPL, OwnRows, false>(cv, OwnRows{rv, gv}, wide, 1, w, false, st);
+    wide_launch<D, SPL>(cv, OwnRows{rv, gv}, wide, w, st);
   }
   own.wide_tile = w.tile;
   hipLaunchKernelGGL((join_parts_kernel<D, SPL == 1>),
