@@ -31,6 +31,7 @@ __device__ __forceinline__ Group group_at(const CacheView &cv, const RowsView &r
   x.pages = min(min(max(n, 0), gv.max_prefix) / kPage, cv.max_pages);
   x.bad = x.a != a || x.b != b || x.b - x.a > gv.max_rows || n < 0 || n > gv.max_prefix ||
           n / kPage > cv.max_pages;
+  x.b = min(x.b, x.a + min(gv.max_rows, rv.R));  // (rows past max_rows are in no group)
   return x;
 }
 

@@ -342,3 +342,24 @@ def test_the_workspace_serves_rows_alone():
         with pytest.raises(mcd.McdError) as e:
             mcd.mcd_cache_attend(weighted, s.rows, q, out, ws, scale=0.07, weight_out=w)
         assert e.value.code == mcd.MCD_E_WORKSPACE
+
+
+@pytest.mark.parametrize("Hq,tokens", [(4, 4), (4, 30), (10, 3)])
+def test_rows_past_max_rows_of_several_tokens(Hq, tokens):
+    """A group's rows past max_rows see nothing, also where max_rows rows of max_tokens tokens would
+    be more than all of them have."""
+    rng = np.random.default_rng(tokens)
+    rows = [(3 + 9 * i, 1) for i in range(7)]
+    rows[2] = (11, tokens)
+    s = Step(rng, [(330, rows), _same(130, 3)], Hq, 2, 64, BF16)
+    good, lse, status = s.run()
+    assert status == 0
+    s.check(good, lse)
+    s.groups = mcd.CacheGroups(i32([0, 7, 10]), i32([330, 130]), 4, 330, 200)
+    out, lse, status = s.run()
+    assert status == mcd.MCD_DEV_BAD_PAGE
+    first = starts(s.new)
+    unseen = slice(first[4], first[7])
+    assert not out[unseen].any() and bool((lse[unseen] == float("-inf")).all())
+    assert torch.equal(out[:first[4]], good[:first[4]])
+    assert torch.equal(out[first[7]:], good[first[7]:])
