@@ -463,7 +463,9 @@ int64_t most_splits(int64_t pages) { return std::max<int64_t>((pages + 3) / 4, 1
 //   1 to 6 tokens a row: 1 x 64, 16000 790 and 133, 8 x 32, 2000 246 and 108
 //   8 query heads a K/V head: 4 x 32, 4000 60 and 52; fp32: 81 and 47; 256 channels 66 and 51
 // From the call's bounds: groups of shorter prefixes than max_prefix gain less (prefixes of 29
-// to 380, 4 x 30 to 53 rows of 1 to 4 tokens: 63 us alone, 81 as taken).  Of 90 shapes drawn
+// to 380, 4 x 30 to 53 rows of 1 to 4 tokens: 63 us alone, 81 as taken), and bounds far above
+// what is there cost splits too (64 rows on 16000 positions with up to 380 of their own 46 us;
+// with max_own 16768 60).  Of 90 shapes drawn
 // over all of these 83 take the quicker way or one within 12 %; the worst take rows alone with
 // two K/V heads on long prefixes, where they do not fill the chip and wait for loads instead
 // (4 x 7 to 48 rows, 482-8901, 8 query heads of 64: 35.7 us, 18.4 together).

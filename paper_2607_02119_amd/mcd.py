@@ -206,7 +206,8 @@ EXPORTED = ["mcd_head_create", "mcd_head_destroy", "mcd_plan_words", "mcd_batch_
             "mcd_cache_page_bytes", "mcd_cache_workspace_bytes", "mcd_cache_append",
             "mcd_cache_read", "mcd_cache_attend", "mcd_cache_evict",
             "mcd_cache_shared_workspace_bytes", "mcd_cache_attend_shared",
-            "mcd_logprobs_workspace_bytes", "mcd_logprobs", "mcd_cache_pages_workspace_bytes", "mcd_cache_count", "mcd_cache_release",
+            "mcd_logprobs_workspace_bytes", "mcd_logprobs",
+            "mcd_cache_pages_workspace_bytes", "mcd_cache_count", "mcd_cache_release",
             "mcd_cache_share", "mcd_cache_reserve",
             "mcd_status_string", "mcd_last_error"]
 
