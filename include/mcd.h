@@ -553,7 +553,8 @@ mcd_status mcd_cache_attend(const mcd_cache *cache, const mcd_cache_rows *rows,
  * questions about one document): groups of consecutive rows of a step.  Rows
  * start[g] .. start[g + 1] - 1 are group g's, and the table entries of the whole
  * pages of their first prefix[g] positions (prefix[g] / 64 of them) are the same for
- * all of them: they are read from the group's first row.  Every row of a group
+ * all of them, rows without a token too: they are read from the group's first row.
+ * Every row of a group with tokens
  * continues past those pages (context >= prefix[g] / 64 * 64).  The groups hold all
  * rows (start[0] = 0, start[n] = R); a row that shares nothing is a group of its
  * own.  The arrays are read when the kernels run, the max_* are bounds as in

@@ -360,7 +360,10 @@ __global__ __launch_bounds__(256) void join_parts_kernel(CacheView cv, RowsView 
                                                          AttendView av, int prefix_pages,
                                                          int narrow_pages, int wide_pages) {
   const int tok = blockIdx.x;
-  const int r = token_each(rv) ? tok : find_row(rv.R, tok, [&](int i) __attribute__((always_inline)) {
+  // (a step of a token for every row may have idle rows, whose tokens the others' follow)
+  const bool same = token_each(rv) && row_start(rv, tok) == tok &&
+                    (tok + 1 == rv.R || row_start(rv, tok + 1) > tok);
+  const int r = same ? tok : find_row(rv.R, tok, [&](int i) __attribute__((always_inline)) {
     return row_start(rv, i);
   });
   Group x;

@@ -363,3 +363,34 @@ def test_rows_past_max_rows_of_several_tokens(Hq, tokens):
     assert not out[unseen].any() and bool((lse[unseen] == float("-inf")).all())
     assert torch.equal(out[:first[4]], good[:first[4]])
     assert torch.equal(out[first[7]:], good[first[7]:])
+
+
+@WAYS
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("most", [1, 3])
+def test_idle_rows_within_the_bounds(most, dtype, way):
+    """A step whose bounds hold a token (or three) of every row, as a captured one has, with rows that
+    have none: the others' results, and no other token's."""
+    rng = np.random.default_rng(most)
+    D, Hq = 64, 8
+    for idle in ([], [0], [3, 4, 5], [0, 1, 2, 3], [24], [6, 13, 14, 20, 23], list(range(1, 25))):
+        new = rng.integers(1, most + 1, 25)
+        new[idle] = 0
+        own = rng.integers(0, 100, 25)
+        groups = [(330, list(zip(own[:6], new[:6]))), (128, list(zip(own[6:14], new[6:14]))),
+                  (700, list(zip(own[14:], new[14:])))]
+        s = Step(rng, groups, Hq, 2, D, dtype)
+        N = 25 * most
+        s.rows = mcd.CacheRows(i32(s.ctx), start=i32(np.concatenate([[0], np.cumsum(new)])),
+                               slot=i32(s.slot), n_tokens=N, max_tokens=most,
+                               max_context=int(s.ctx.max()) + most)
+        q = torch.zeros((N, Hq, D), dtype=dtype, device="cuda")
+        q[:s.N] = dev(s.q).to(dtype)
+        out = torch.full((N, Hq, D), 9.0, dtype=dtype, device="cuda")
+        lse = torch.full((N, Hq), 9.0, device="cuda")
+        ws = s.cache.workspace(s.rows, Hq, groups=s.groups)
+        ws[256:] = 255
+        attend(way, s.cache, s.rows, s.groups, q, out, ws, scale=0.07, lse=lse)
+        assert mcd.mcd_read_device_status(ws) == 0
+        s.check(out[:s.N], lse[:s.N])
+        assert bool((out[s.N:] == 9.0).all()) and bool((lse[s.N:] == 9.0).all())
