@@ -554,10 +554,9 @@ mcd_status mcd_cache_attend(const mcd_cache *cache, const mcd_cache_rows *rows,
  * start[g] .. start[g + 1] - 1 are group g's, and the table entries of the whole
  * pages of their first prefix[g] positions (prefix[g] / 64 of them) are the same for
  * all of them, rows without a token too: they are read from the group's first row.
- * Every row of a group with tokens
- * continues past those pages (context >= prefix[g] / 64 * 64).  The groups hold all
- * rows (start[0] = 0, start[n] = R); a row that shares nothing is a group of its
- * own.  The arrays are read when the kernels run, the max_* are bounds as in
+ * Every row of a group that has tokens continues past those pages (context >=
+ * prefix[g] / 64 * 64).  The groups hold all rows (start[0] = 0, start[n] = R); a
+ * row that shares nothing is a group of its own.  The arrays are read when the kernels run, the max_* are bounds as in
  * mcd_cache_rows (n groups of max_rows rows of max_tokens hold n_tokens).  Where the
  * rows are few or the prefixes short, every row is read by itself, from its own
  * table entries, and the groups are not looked at.  Otherwise MCD_DEV_BAD_PAGE is
